@@ -120,6 +120,7 @@ typedef struct ihip_cache ihip_cache;
 #define IHIP_OP_PRUNE_ALL     3
 #define IHIP_OP_DECODE_LAYER  4
 #define IHIP_OP_PREFILL_LAYER 5
+#define IHIP_OP_ATTN_DECODE_MX4 6
 
 /* ==========================================================================
  * Variants of the storage and of the scores, used by the calls below
@@ -449,6 +450,94 @@ int32_t ihip_decode_layer_static(const ihip_shape *shape, ihip_tensor q, ihip_te
                                  int32_t n_stages, const int32_t *chunk_sizes, const int32_t *keeps,
                                  float sm_scale, void *out, float *out_lse, int32_t *out_block_starts,
                                  void *stream);
+
+/* ==========================================================================
+ * Filling a KV cache, reading it back, and the dense attention of whole prompts
+ * ========================================================================== */
+
+/*
+ * A KV cache of one layer as the calls below write and read it: the caches (or
+ * page pools) of the calls above, and one more storage.
+ *   format     IHIP_KV_BF16: 256-byte rows, strides of k and v in elements.
+ *              IHIP_KV_E4M3: 128-byte rows, strides in bytes; element = scale * decoded
+ *              byte, the scales k_scale and v_scale ("FP8 KV cache" above).
+ *              IHIP_KV_MX4: 4-bit rows (OCP Microscaling, MXFP4).  A row is 64 bytes,
+ *              element 2i in the low and 2i+1 in the high half of byte i, E2M1 codes
+ *              (sign, then 0, 1/2, 1, 3/2, 2, 3, 4, 6), strides in bytes, multiples of 64,
+ *              the same for k and v.  Every 32 elements share a scale 2^(s-127), s in
+ *              1..252 (6 * 2^125 is still a bf16 number; 255: the 32 elements are NaN); the 4 scale bytes of the row at
+ *              byte o of k stand at byte o/16 of k_scales (4-byte aligned), those of v
+ *              in v_scales: 4.25 bits an element.
+ *   k, v       stride_b is that between sequences, or between pages.
+ *   paged      the block table, if k and v are page pools, or NULL.  A negative page id
+ *              stands for no page: ihip_kv_append drops what belongs there.
+ * The memory is the caller's; ihip_kv_append writes to it.
+ */
+#define IHIP_KV_BF16 0
+#define IHIP_KV_E4M3 1
+#define IHIP_KV_MX4  2
+typedef struct ihip_kv_store {
+    int32_t format;
+    ihip_tensor k, v;
+    void *k_scales, *v_scales;   /* IHIP_KV_MX4 */
+    float k_scale, v_scale;      /* IHIP_KV_E4M3 */
+    const ihip_paged_kv *paged;
+} ihip_kv_store;
+
+/*
+ * Sequences of different lengths one behind the other ("packed"): the new
+ * tokens of sequence b are rows cu_q[b] .. cu_q[b+1]-1 of tensors of `rows`
+ * rows.  cu_q is device int32 [B+1], ascending from 0 (two equal entries: a
+ * sequence without new tokens); rows from cu_q[B] on belong to no sequence:
+ * none is used, and what stands there in an output is left as it was.  Packed
+ * tensors are ihip_tensors whose stride_t goes from row to row; stride_b is
+ * not used.  Hq and Hkv as in ihip_shape, but any whole Hq/Hkv will do.
+ */
+typedef struct ihip_packed {
+    int32_t B, Hq, Hkv, d;       /* d must be 128 */
+    const int32_t *cu_q;
+    int32_t rows;
+    int32_t max_q;               /* host-side upper bound of a sequence's new tokens (sizes the launch) */
+} ihip_packed;
+
+/*
+ * Appends new tokens to a cache.  Token i of the n that sequence b brings
+ * stands at position seq_lens[b] - n + i (seq_lens as in ihip_shape: the new
+ * tokens are counted), where its K and V rows are written in the store's
+ * format.  With rope, K is rotated to its position first, and so are the
+ * queries: dims (2j, 2j+1) by the angle of table row `position`, column j, as
+ * the dynamic RoPE above does (the styles are not looked at; keys that dynamic
+ * RoPE is to rotate later are stored without).
+ *   k, v       packed, bf16 [rows, Hkv, d]
+ *   q, q_out   packed, bf16 [rows, Hq, d]: the queries, and where to write them rotated
+ *              (without rope: copied); q_out.ptr == NULL: q is not looked at
+ *   k_out      packed, bf16 [rows, Hkv, d]: where to write the rotated K as well, for
+ *              ihip_prompt_attn; ptr == NULL: nowhere
+ *              (q_out may be q and k_out may be k: in place)
+ *   rope       needs n_pos >= max_seq_len; or NULL
+ * The rotation is done in fp32, each product and sum rounded on its own, and
+ * its result rounded once to what is stored, to nearest, ties to even.  E4M3:
+ * value / scale, beyond +-448 becomes +-448 (NaN stays NaN).  MX4: the scale of 32
+ * elements is the smallest power of two, from 2^-100 to 2^125, with which their largest
+ * magnitude is at most 7 (which rounds to 6; above 7 * 2^125 everything does); with a NaN or infinity among them it is 255.
+ * A token whose position is outside [0, max_seq_len) is dropped: nothing is written
+ * for it.  Two tokens must not share a row of the cache.
+ */
+int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v,
+                       const int32_t *seq_lens, int32_t max_seq_len, const ihip_rope *rope,
+                       const ihip_kv_store *store, ihip_tensor q_out, ihip_tensor k_out, void *stream);
+
+/*
+ * Reads a cache back: rows 0 .. seq_lens[b]-1 (at most max_seq_len) of every sequence and KV head,
+ * widened to bf16 (exact for bf16 and MX4 rows whose scale is not 255, and for E4M3 rows
+ * whose scale is a power of two; rounded to nearest otherwise).  k_out and v_out
+ * are bf16 [B, Hkv, max_seq_len, d] through their strides, either may have ptr ==
+ * NULL.  Rows behind a sequence, and rows of a page with a negative id, are
+ * left as they were.  What the pruning and prefill calls read where the cache
+ * itself is kept in 4 bits, or in pages of E4M3.
+ */
+int32_t ihip_kv_gather(const ihip_kv_store *store, int32_t B, int32_t Hkv, int32_t d, const int32_t *seq_lens,
+                       int32_t max_seq_len, ihip_tensor k_out, ihip_tensor v_out, void *stream);
 
 /* ==========================================================================
  * Host-memory KV tier with the on-GPU hot-block cache

@@ -16,7 +16,8 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libihip.so")
 
-OP_ATTN_DECODE, OP_ATTN_PREFILL, OP_PRUNE_ALL, OP_DECODE_LAYER, OP_PREFILL_LAYER = 1, 2, 3, 4, 5
+OP_ATTN_DECODE, OP_ATTN_PREFILL, OP_PRUNE_ALL, OP_DECODE_LAYER, OP_PREFILL_LAYER, OP_ATTN_DECODE_MX4 = 1, 2, 3, 4, 5, 6
+KV_BF16, KV_E4M3, KV_MX4 = 0, 1, 2
 
 c_i32, c_i64, c_f, vp, c_sz = (ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p,
                                ctypes.c_size_t)
@@ -93,6 +94,8 @@ EXPORTS = {
                                          c_f, vp, vp, vp, c_sz, vp]),
     "ihip_prefill_layer": (c_i32, [ctypes.POINTER(Shape), Tensor, Tensor, Tensor, c_i32, vp, vp, c_f,
                                    vp, vp, vp, vp, c_sz, vp]),
+    "ihip_kv_append": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, vp, vp, Tensor, Tensor, vp]),
+    "ihip_kv_gather": (c_i32, [vp, c_i32, c_i32, c_i32, vp, c_i32, Tensor, Tensor, vp]),
     "ihip_cache_device_bytes": (c_sz, [c_i32, c_i32, c_i64, c_i32, c_i32, c_i32]),
     "ihip_cache_device_bytes_fp8": (c_sz, [c_i32, c_i32, c_i64, c_i32, c_i32, c_i32]),
     "ihip_cache_create_fp8": (c_i32, [ctypes.POINTER(vp), vp, c_sz, Tensor, Tensor, c_i32, c_i32, c_i64, c_i32,
@@ -726,3 +729,143 @@ def decode_layer_cached(layer: "Layer", q, cache: HostKVCache, chunk_sizes, keep
                                           len(chunk_sizes), _i32(chunk_sizes), _i32(keeps), sm_scale, _ptr(out),
                                           _ptr(lse), _ptr(out_blocks), _ptr(ws), ws.numel(), _stream()))
     return out
+
+
+# ---- filling a KV cache, reading it back ----------------------------------------------
+NO_TENSOR = Tensor(None, 0, 0, 0)
+
+
+class StoreStruct(ctypes.Structure):
+    _fields_ = [("format", c_i32), ("k", Tensor), ("v", Tensor), ("k_scales", vp), ("v_scales", vp),
+                ("k_scale", c_f), ("v_scale", c_f), ("paged", vp)]
+
+
+class PackedStruct(ctypes.Structure):
+    _fields_ = [("B", c_i32), ("Hq", c_i32), ("Hkv", c_i32), ("d", c_i32), ("cu_q", vp), ("rows", c_i32), ("max_q", c_i32)]
+
+
+class KVStore:
+    """ihip_kv_store: one layer's K and V caches, [B, Hkv, T, width], or page pools [n_pages, Hkv, page_tokens, width]
+    with block_table int32 [B, pages].  Made by KVStore.bf16 (bf16, width 128), .e4m3 (uint8, 128, one scale a tensor)
+    or .mx4 (uint8 codes, 64, and uint8 scales [..., 4]).  The tensors stay the caller's."""
+
+    def __init__(self, fmt: int, k: torch.Tensor, v: torch.Tensor, k_scales: Optional[torch.Tensor] = None,
+                 v_scales: Optional[torch.Tensor] = None, scales: Sequence[float] = (1.0, 1.0),
+                 block_table: Optional[torch.Tensor] = None):
+        width = {KV_BF16: 128, KV_E4M3: 128, KV_MX4: 64}[fmt]
+        conv = _tensor if fmt == KV_BF16 else _tensor8
+        if k.shape != v.shape or k.shape[-1] != width:
+            raise IhipError(f"k, v: need the same shape [.., Hkv, tokens, {width}]")
+        used = [k, v]
+        if fmt == KV_MX4:
+            for codes, sc, name in ((k, k_scales, "k_scales"), (v, v_scales, "v_scales")):
+                if sc is None or sc.dtype != torch.uint8 or sc.shape != (*codes.shape[:3], 4) or not sc.is_cuda or \
+                        [16 * x for x in sc.stride()[:3]] != list(codes.stride()[:3]) or sc.stride(3) != 1:
+                    raise IhipError(f"{name}: need a uint8 device tensor [.., Hkv, tokens, 4] laid out like the codes")
+                used.append(sc)
+        self.paged = None
+        if block_table is not None:
+            self.paged = PagedKV(k, v, block_table)
+            used.append(block_table)
+        if any(t.device != k.device for t in used):
+            raise IhipError("the tensors of a store must be on one device")
+        self.format, self.k, self.v, self.k_scales, self.v_scales = fmt, k, v, k_scales, v_scales
+        self.block_table, self.device, self.Hkv = block_table, k.device, k.shape[1]
+        #: sequences (None: as many as the block table's rows) and the tokens that each can hold
+        self.B = k.shape[0] if block_table is None else block_table.shape[0]
+        self.tokens = k.shape[2] if block_table is None else block_table.shape[1] * k.shape[2]
+        self.c = StoreStruct(fmt, conv(k, "k"), conv(v, "v"), _ptr(k_scales), _ptr(v_scales), scales[0], scales[1],
+                             ctypes.cast(self.paged.ref(), vp) if self.paged is not None else None)
+
+    @classmethod
+    def bf16(cls, k, v, block_table=None):
+        return cls(KV_BF16, k, v, block_table=block_table)
+
+    @classmethod
+    def e4m3(cls, k, v, scales: Sequence[float], block_table=None):
+        return cls(KV_E4M3, k, v, scales=scales, block_table=block_table)
+
+    @classmethod
+    def mx4(cls, k, v, k_scales, v_scales, block_table=None):
+        return cls(KV_MX4, k, v, k_scales, v_scales, block_table=block_table)
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def _packed_tensor(t: torch.Tensor, name: str, rows: Optional[int] = None, heads: Optional[int] = None) -> Tensor:
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.stride(2) != 1 or not t.is_cuda:
+        raise IhipError(f"{name}: need a 3-d bf16 device tensor [rows, heads, d] with contiguous last dim")
+    if (rows is not None and t.shape[0] != rows) or (heads is not None and t.shape[1] != heads):
+        raise IhipError(f"{name}: need {rows} rows of {heads} heads, got {tuple(t.shape[:2])}")
+    return Tensor(t.data_ptr(), 0, t.stride(1), t.stride(0))
+
+
+def _lengths(t: torch.Tensor, n: int, name: str, device) -> int:
+    if t.dtype != torch.int32 or t.device != device or t.numel() != n or not t.is_contiguous():
+        raise IhipError(f"{name}: need a contiguous int32 tensor of {n} on {device}")
+    return t.data_ptr()
+
+
+def _same_device(device, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise IhipError(f"{name} is on {t.device}, not on {device}")
+
+
+def _stream_of(device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def kv_append(store: KVStore, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int,
+              q: Optional[torch.Tensor] = None, rope: Optional[Sequence[torch.Tensor]] = None,
+              q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """ihip_kv_append: packed new tokens k, v [rows, Hkv, d] (bf16) of sequences cu_q int32 [B+1] into the store, at the
+    end of sequences that are seq_lens [B] long with them (at most max_seq_len).  rope: (cos, sin) fp32 [n_pos, d/2]:
+    keys are rotated to their positions, and the queries q [rows, Hq, d] into q_out (may be q; made if not given).
+    k_out: where the rotated keys go as well.  -> (q_out or None, k_out or None)."""
+    rows, Hkv, d = k.shape
+    B = cu_q.numel() - 1
+    _same_device(store.device, k=k, v=v, q=q, q_out=q_out, k_out=k_out)
+    if Hkv != store.Hkv or B > store.B or max_seq_len > store.tokens:
+        raise IhipError(f"the store holds {store.B} sequences of {store.Hkv} heads and {store.tokens} tokens")
+    cos_sin = None
+    if rope is not None:
+        _same_device(store.device, cos=rope[0], sin=rope[1])
+        cos_sin = Rope(rope[0], rope[1])
+        if rope[0].shape[1] * 2 != d:
+            raise IhipError("rope tables: need d / 2 columns")
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if q is None and q_out is not None:
+        raise IhipError("q_out without q")
+    Hq = Hkv if q is None else q.shape[1]
+    tq = NO_TENSOR if q is None else _packed_tensor(q, "q", rows, Hq)
+    p = PackedStruct(B, Hq, Hkv, d, _lengths(cu_q, B + 1, "cu_q", store.device), rows, rows)
+    with torch.cuda.device(store.device):
+        _check(lib().ihip_kv_append(ctypes.byref(p), tq, _packed_tensor(k, "k"), _packed_tensor(v, "v", rows, Hkv),
+                                    _lengths(seq_lens, B, "seq_lens", store.device), max_seq_len,
+                                    cos_sin.ref() if cos_sin is not None else None, store.ref(),
+                                    NO_TENSOR if q is None else _packed_tensor(q_out, "q_out", rows, Hq),
+                                    NO_TENSOR if k_out is None else _packed_tensor(k_out, "k_out", rows, Hkv),
+                                    _stream_of(store.device)))
+    return q_out, k_out
+
+
+def kv_gather(store: KVStore, seq_lens: torch.Tensor, max_seq_len: int, k_out: Optional[torch.Tensor] = None,
+              v_out: Optional[torch.Tensor] = None):
+    """ihip_kv_gather: rows 0 .. seq_lens[b]-1 of every sequence of the store as bf16 [B, Hkv, max_seq_len, d]; made if not
+    given (rows behind a sequence are left as they were).  -> (k_out, v_out)."""
+    B = seq_lens.numel()
+    if B > store.B or max_seq_len > store.tokens:
+        raise IhipError(f"the store holds {store.B} sequences of {store.tokens} tokens")
+    shape = (B, store.Hkv, max_seq_len, 128)
+    k_out, v_out = (torch.empty(shape, dtype=torch.bfloat16, device=store.device) if t is None else t for t in (k_out, v_out))
+    _same_device(store.device, k_out=k_out, v_out=v_out)
+    if k_out.shape != shape or v_out.shape != shape:
+        raise IhipError(f"k_out, v_out: need shape {shape}")
+    with torch.cuda.device(store.device):
+        _check(lib().ihip_kv_gather(store.ref(), B, store.Hkv, 128, _lengths(seq_lens, B, "seq_lens", store.device),
+                                    max_seq_len, _tensor(k_out, "k_out"), _tensor(v_out, "v_out"),
+                                    _stream_of(store.device)))
+    return k_out, v_out

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "common.h"
+#include "api_checks.h"
 #include "select_chain.h"
 #include "prune_nest_args.h"
 
@@ -104,10 +105,8 @@ int32_t launch_attn_prefill(const ihip_shape &, const ihip_tensor &, const ihip_
                             void *, size_t, const ihip_rope *, hipStream_t, const KvFormat * = nullptr);
 size_t attn_prefill_workspace(const ihip_shape &, int, int);
 
-static bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
-
 // FP8 K/V tensors: strides count bytes; rows 16-byte aligned like the bf16 ones
-static int32_t check_tensor8(const ihip_tensor &t, const char *who, const char *name)
+int32_t check_tensor8(const ihip_tensor &t, const char *who, const char *name)
 {
     if (!t.ptr) return fail(IHIP_ERR_INVALID_ARG, "%s: %s.ptr is NULL", who, name);
     if (((uintptr_t)t.ptr | (uintptr_t)t.stride_b | (uintptr_t)t.stride_h | (uintptr_t)t.stride_t) & 15)
@@ -116,7 +115,7 @@ static int32_t check_tensor8(const ihip_tensor &t, const char *who, const char *
     return IHIP_OK;
 }
 // paged K/V: pools through strides (stride_b = elements between pages) + a block table
-static int32_t check_paged(const char *who, const ihip_shape *shape, const ihip_paged_kv *pg, KvFormat *fmt)
+int32_t check_paged(const char *who, const ihip_shape *shape, const ihip_paged_kv *pg, KvFormat *fmt)
 {
     if (!pg || !pg->block_table) return fail(IHIP_ERR_INVALID_ARG, "%s: paged / block_table is NULL", who);
     if (!pow2(pg->page_tokens)) return fail(IHIP_ERR_INVALID_ARG, "%s: page_tokens = %d is not a power of two", who, pg->page_tokens);
@@ -127,14 +126,14 @@ static int32_t check_paged(const char *who, const ihip_shape *shape, const ihip_
     return IHIP_OK;
 }
 
-static int32_t check_scales(const char *who, float k_scale, float v_scale)
+int32_t check_scales(const char *who, float k_scale, float v_scale)
 {
     if (!(k_scale > 0.f) || !(v_scale > 0.f) || k_scale > 3.0e38f || v_scale > 3.0e38f)
         return fail(IHIP_ERR_INVALID_ARG, "%s: scales must be positive and finite", who);
     return IHIP_OK;
 }
 
-static int32_t check_shape(const ihip_shape *s, const char *who)
+int32_t check_shape(const ihip_shape *s, const char *who)
 {
     if (!s) return fail(IHIP_ERR_INVALID_ARG, "%s: shape is NULL", who);
     if (s->B < 0 || s->Hq <= 0 || s->Hkv <= 0 || s->Hq % s->Hkv != 0)
@@ -159,7 +158,7 @@ static int32_t check_shape(const ihip_shape *s, const char *who)
     return IHIP_OK;
 }
 
-static int32_t check_tensor(const ihip_tensor &t, const char *who, const char *name)
+int32_t check_tensor(const ihip_tensor &t, const char *who, const char *name)
 {
     if (!t.ptr) return fail(IHIP_ERR_INVALID_ARG, "%s: %s.ptr is NULL", who, name);
     if (((uintptr_t)t.ptr & 15) || (t.stride_b & 7) || (t.stride_h & 7) || (t.stride_t & 7))
