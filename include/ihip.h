@@ -528,6 +528,24 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
                        const ihip_kv_store *store, ihip_tensor q_out, ihip_tensor k_out, void *stream);
 
 /*
+ * Dense causal attention of whole prompts, packed one behind the other (the
+ * layers that are not pruned, and a prompt's first chunk): query i of the n of
+ * sequence b attends to keys 0 .. i + (t - n) of its t keys, rows
+ * cu_k[b] .. cu_k[b+1]-1 of k and v.
+ *   q, k, v    packed, bf16 [rows, Hq, d], [rows_k, Hkv, d]; query head h reads KV head h / (Hq/Hkv)
+ *   cu_k       device int32 [B+1]; NULL: cu_q (no sequence has keys that precede its
+ *              queries), and rows_k must be packed->rows
+ *   out        bf16 [rows, Hq, d] contiguous
+ *   out_lse    fp32 [rows, Hq] natural-log sum-exp of the scaled scores; may be NULL
+ * QK^T and PV run on the matrix cores (bf16 operands, the probabilities rounded to
+ * bf16, fp32 accumulation), softmax in fp32.  A query that sees no key (t < n)
+ * gets 0, and -INFINITY.  A sequence of more than max_q tokens is not done to its end.
+ */
+int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v,
+                         const int32_t *cu_k, int32_t rows_k, float sm_scale, void *out, float *out_lse,
+                         void *stream);
+
+/*
  * Reads a cache back: rows 0 .. seq_lens[b]-1 (at most max_seq_len) of every sequence and KV head,
  * widened to bf16 (exact for bf16 and MX4 rows whose scale is not 255, and for E4M3 rows
  * whose scale is a power of two; rounded to nearest otherwise).  k_out and v_out

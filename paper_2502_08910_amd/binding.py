@@ -94,6 +94,7 @@ EXPORTS = {
                                          c_f, vp, vp, vp, c_sz, vp]),
     "ihip_prefill_layer": (c_i32, [ctypes.POINTER(Shape), Tensor, Tensor, Tensor, c_i32, vp, vp, c_f,
                                    vp, vp, vp, vp, c_sz, vp]),
+    "ihip_prompt_attn": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, c_f, vp, vp, vp]),
     "ihip_kv_append": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, vp, vp, Tensor, Tensor, vp]),
     "ihip_kv_gather": (c_i32, [vp, c_i32, c_i32, c_i32, vp, c_i32, Tensor, Tensor, vp]),
     "ihip_cache_device_bytes": (c_sz, [c_i32, c_i32, c_i64, c_i32, c_i32, c_i32]),
@@ -869,3 +870,31 @@ def kv_gather(store: KVStore, seq_lens: torch.Tensor, max_seq_len: int, k_out: O
                                     max_seq_len, _tensor(k_out, "k_out"), _tensor(v_out, "v_out"),
                                     _stream_of(store.device)))
     return k_out, v_out
+
+
+def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, max_q: int,
+                cu_k: Optional[torch.Tensor] = None, sm_scale: Optional[float] = None, want_lse: bool = False,
+                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """ihip_prompt_attn: dense causal attention of packed sequences cu_q int32 [B+1] of at most max_q tokens, q [rows, Hq, d]
+    over k, v [rows_k, Hkv, d] (bf16); cu_k: their own offsets, where sequences bring keys that precede their queries.
+    -> (out bf16 [rows, Hq, d], lse fp32 [rows, Hq] or None)."""
+    rows, Hq, d = q.shape
+    rows_k, Hkv, _ = k.shape
+    B = cu_q.numel() - 1
+    sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
+    if out is None:
+        out = torch.empty((rows, Hq, d), dtype=torch.bfloat16, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
+    _same_device(q.device, k=k, v=v, out=out, lse=lse)
+    if out.shape != q.shape or out.dtype != torch.bfloat16 or not out.is_contiguous():
+        raise IhipError("out: need a contiguous bf16 tensor of the shape of q")
+    if lse is not None and (lse.shape != (rows, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise IhipError("lse: need a contiguous fp32 tensor [rows, Hq]")
+    p = PackedStruct(B, Hq, Hkv, d, _lengths(cu_q, B + 1, "cu_q", q.device), rows, max_q)
+    with torch.cuda.device(q.device):
+        _check(lib().ihip_prompt_attn(ctypes.byref(p), _packed_tensor(q, "q"), _packed_tensor(k, "k"),
+                                      _packed_tensor(v, "v", rows_k, Hkv),
+                                      None if cu_k is None else _lengths(cu_k, B + 1, "cu_k", q.device), rows_k, sm_scale,
+                                      _ptr(out), _ptr(lse), _stream_of(q.device)))
+    return out, lse
