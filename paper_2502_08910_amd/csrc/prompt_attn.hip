@@ -1,6 +1,7 @@
 // Dense causal attention of packed prompts on v_mfma_f32_32x32x16_bf16.
 #include "api_checks.h"
 #include "kv_store.h"
+#include <type_traits>
 
 namespace ihip {
 
@@ -13,8 +14,8 @@ constexpr int kPromptRows = 64 * kPromptWaves;       // queries of a workgroup
 constexpr int kTileKeys = 32;
 constexpr int kTileEl = kTileKeys * kD;              // bf16 elements of a K or V tile in LDS
 constexpr int kPromptStages = 3;
-constexpr float kNegBigPrompt = -1.0e30f;            // finite stand-in for -inf in running maxima
-constexpr float kPromptMaxSum = 1024.0f;             // row sum of a tile above which the softmax reference moves
+constexpr float kNegBigPrompt = -1.0e30f;            // finite stand-in for -inf in maxima
+constexpr float kPromptMaxSum = 18446744073709551616.0f;      // 2^64: sum of exponentials beyond which a block is done again
 
 int32_t check_packed(const char *who, const ihip_packed *p);
 
@@ -74,127 +75,201 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     const uint16_t *kb = a.k + (int64_t)k_first * a.k_st + g * a.k_sh;
     const uint16_t *vb = a.v + (int64_t)k_first * a.v_st + g * a.v_sh;
 
-    f32x16 o[2][4];
+    // Loads of a tile: 8 four-row instructions for K and 8 for V, two of each a wave: lane l brings 16 bytes of row 4 j + l / 16 to
+    // base + 16 l.  The base of a tile is scalar; a lane's offset from it changes in a tile that reaches behind the last key only,
+    // whose rows stand for the missing ones.
+    uint32_t k_off[2], v_off[2];
+    auto offsets = [&](int rows, uint32_t (&ko)[2], uint32_t (&vo)[2]) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[s][dt][r] = 0.f;
-    float m_run[2] = {kNegBigPrompt, kNegBigPrompt}, l_run[2] = {0.f, 0.f};
-
-    auto request = [&](int tile) {
-        if (tile >= n_tiles) return;
-        uint16_t *stage = smem + (tile % kPromptStages) * 2 * kTileEl;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = wave + i * kPromptWaves;   // 0..7 K rows 4j.., 8..15 V rows 4(j-8)..
-            const bool is_v = i >= 2;
-            const int key = 4 * (j & 7) + (lane >> 4), slot = lane & 15;
-            const int pos = min(tile * kTileKeys + key, nk - 1);
-            const int chunk = is_v ? slot ^ ((key & 3) << 2) : slot ^ (key & 15);
-            const uint16_t *src = (is_v ? vb + (int64_t)pos * a.v_st : kb + (int64_t)pos * a.k_st) + chunk * 8;
-            const uint32_t dst = __builtin_amdgcn_readfirstlane(
-                (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)(stage + j * 4 * kD));
-            global_to_lds(dst, src);
+        for (int i = 0; i < 2; ++i) {
+            const int key = 4 * (wave + i * kPromptWaves) + (lane >> 4), at = min(key, rows - 1), slot = lane & 15;
+            ko[i] = (uint32_t)(at * (int)a.k_st + ((slot ^ (key & 15)) << 3)) * 2u;
+            vo[i] = (uint32_t)(at * (int)a.v_st + ((slot ^ ((key & 3) << 2)) << 3)) * 2u;
         }
     };
-    int voff[4];
+    offsets(kTileKeys, k_off, v_off);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
+    auto request_k = [&](int tile, int st) {
+        if (tile >= n_tiles) return;
+        const uint16_t *base = kb + (int64_t)tile * kTileKeys * a.k_st;
+        const uint32_t dst = lds0 + (st * kTileEl + wave * 4 * kD) * 2;
+        uint32_t ko[2] = {k_off[0], k_off[1]}, vo[2];
+        if (tile * kTileKeys + kTileKeys > nk) offsets(nk - tile * kTileKeys, ko, vo);
+        global_to_lds(dst, base, ko[0]);
+        global_to_lds(dst + 16 * kD * 2, base, ko[1]);
+    };
+    auto request_v = [&](int tile, int st) {
+        if (tile >= n_tiles) return;
+        const uint16_t *base = vb + (int64_t)tile * kTileKeys * a.v_st;
+        const uint32_t dst = lds0 + ((kPromptStages + st) * kTileEl + wave * 4 * kD) * 2;
+        uint32_t ko[2], vo[2] = {v_off[0], v_off[1]};
+        if (tile * kTileKeys + kTileKeys > nk) offsets(nk - tile * kTileKeys, ko, vo);
+        global_to_lds(dst, base, vo[0]);
+        global_to_lds(dst + 16 * kD * 2, base, vo[1]);
+    };
+    const uint16_t *k_at[8], *v_at[4];               // this lane's addresses in stage 0
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) k_at[ks] = smem + n * kD + ((ks * 2 + half) ^ (n & 15)) * 8;
     {
         const int i = lane & 15, key = 4 * half + (i >> 2);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) {
             const int chunk = dt * 4 + ((n >> 4) << 1) + ((i & 3) >> 1);
-            voff[dt] = key * kD + ((chunk ^ ((key & 3) << 2)) << 3) + ((i & 1) << 2);
+            v_at[dt] = smem + kPromptStages * kTileEl + key * kD + ((chunk ^ ((key & 3) << 2)) << 3) + ((i & 1) << 2);
         }
     }
-    auto v_operand = [&](const uint16_t *cV, int dt, int kk) {
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4 *)(cV + voff[dt] + (16 * kk) * kD));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4 *)(cV + voff[dt] + (16 * kk + 8) * kD));
+    auto k_operand = [&](int st, int ks) { return *reinterpret_cast<const bf16x8 *>(k_at[ks] + st * kTileEl); };
+    auto v_operand = [&](int st, int i) {            // i: 4 kk + dt
+        const uint16_t *at = v_at[i & 3] + st * kTileEl + 16 * (i >> 2) * kD;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 8 * kD));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    auto exponentials = [&](const f32x16 &s, float ref, bf16x8 (&pb)[2]) {
-        float ps = 0.f;
+    f32x16 o[2][4], sc[2];
+    auto scores = [&](int st, int s) {
+        sc[s] = f32x16{};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float pw = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2e, -ref));   // exp2(-inf) = 0
-            ps += pw;
-            pb[r >> 3][r & 7] = (__bf16)pw;
-        }
-        return ps;
+        for (int ks = 0; ks < 8; ++ks) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(st, ks), qb[s][ks], sc[s], 0, 0, 0);
+    };
+    auto mask = [&](int tile, int s) {
+        if (tile * kTileKeys + kTileKeys - 1 <= row0 + s * 32 + ahead) return;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (tile * kTileKeys + 8 * (r >> 2) + 4 * half + (r & 3) > last_key[s]) sc[s][r] = -INFINITY;
+    };
+    auto row_max = [&](const f32x16 &s) {            // scaled; of both halves
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        return fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.scale_log2e;
     };
 
-    request(0);
-    request(1);
-    for (int tile = 0; tile < n_tiles; ++tile) {
-        if (tile + 1 < n_tiles) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        request(tile + 2);
-        const uint16_t *cK = smem + (tile % kPromptStages) * 2 * kTileEl + n * kD, *cV = smem + (tile % kPromptStages) * 2 * kTileEl + kTileEl;
-        f32x16 sc[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sc[s][r] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-            const bf16x8 ka = *reinterpret_cast<const bf16x8 *>(&cK[((ks * 2 + half) ^ (n & 15)) * 8]);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[s][ks], sc[s], 0, 0, 0);
-        }
-        if (tile * kTileKeys + kTileKeys - 1 > row0 + ahead) {
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (tile * kTileKeys + 8 * (r >> 2) + 4 * half + (r & 3) > last_key[s]) sc[s][r] = -INFINITY;
-        }
-        bf16x8 pb[2][2];
+    uint32_t pw[2][8];                               // the probabilities of a set, in pairs of keys
+    float m_ref[2] = {kNegBigPrompt, kNegBigPrompt}, l_run[2] = {0.f, 0.f};
+    // two scores -> two probabilities (exp2(-inf) = 0)
+    auto exponentials = [&](int s, int i) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i], a.scale_log2e, -m_ref[s]));
+        const float y = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i + 1], a.scale_log2e, -m_ref[s]));
+        l_run[s] += x;
+        l_run[s] += y;
+        pw[s][i] = pack_bf16x2(x, y);
+    };
+    auto probabilities = [&](int s, int kk) {
+        return __builtin_bit_cast(bf16x8, make_uint4(pw[s][4 * kk], pw[s][4 * kk + 1], pw[s][4 * kk + 2], pw[s][4 * kk + 3]));
+    };
+    // Period t, for the two sets of 32 queries in turn: first product of tile t + 1 and second product of tile t, and under them the
+    // exponentials of the other set, 16 matrix instructions and 16 scores a lane at a time.  K of tile t + 3 and V of tile t + 2 are
+    // requested as it begins, into the stages that period t - 1 has read, and have landed when period t + 1 ends.
+    auto period = [&](int st, int st1, int st2, int t) {       // stages of tiles t, t + 1, t + 2
+        request_k(t + 3, st);
+        request_v(t + 2, st2);
+        bf16x8 ka[8], va[8];
+        mask(t, 1);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            float ps = exponentials(sc[s], m_run[s], pb[s]);
-            if (__any(!(ps <= kPromptMaxSum))) {
-                float mx = sc[s][0];
+            if (s == 1) mask(t + 1, 0);
 #pragma unroll
-                for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[s][r]);
-                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                const float mn = fmaxf(m_run[s], mx * a.scale_log2e);
-                const float corr = __builtin_amdgcn_exp2f(m_run[s] - mn);
-                m_run[s] = mn;
-                ps = exponentials(sc[s], mn, pb[s]);
-                l_run[s] *= corr;
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt) o[s][dt] *= corr;
+            for (int r = 0; r < 16; ++r) {
+                if (s == 0 && r == 0) {
+                    ka[0] = k_operand(st1, 0);
+                    ka[1] = k_operand(st1, 1);
+                }
+                if (s == 0 && r < 6) ka[r + 2] = k_operand(st1, r + 2);
+                if (s == 0 && r >= 6 && r < 14) va[r - 6] = v_operand(st, r - 6);
+                if (r % 2 == 0) exponentials(1 - s, r / 2);
+                if (r < 8) {
+                    if (r == 0) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[0], qb[s][0], f32x16{}, 0, 0, 0);
+                    else sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[r], qb[s][r], sc[s], 0, 0, 0);
+                } else {
+                    asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][r & 3]) : "v"(va[r - 8]), "v"(probabilities(s, (r - 8) >> 2)));
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            l_run[s] += ps;
+        }
+        if (t + 3 < n_tiles) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    // Exponentials are taken against the row's maximum over the first tile (key 0 is in it, which every query with a key sees), not
+    // against a running one: bf16 and fp32 have exponents to spare, nothing is lost while the scores stay within 2^64 of it.  Where a
+    // row's sum says that they did not, the block is done again against the maxima over all tiles.
+    for (int again = 0; n_tiles > 0 && again < 2; ++again) {
+        if (again) {
+            m_ref[0] = m_ref[1] = kNegBigPrompt;
+            for (int t = 0; t < n_tiles; ++t) {
+                request_k(t, 0);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    scores(0, s);
+                    mask(t, s);
+                    m_ref[s] = fmaxf(m_ref[s], row_max(sc[s]));
+                }
+                __syncthreads();
+            }
         }
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+        for (int s = 0; s < 2; ++s) {
+            l_run[s] = 0.f;
 #pragma unroll
-            for (int dt = 0; dt < 4; ++dt) {
-                const bf16x8 va = v_operand(cV, dt, kk);
+            for (int dt = 0; dt < 4; ++dt) o[s][dt] = f32x16{};
+        }
+        request_k(0, 0);
+        request_k(1, 1);
+        request_k(2, 2);
+        request_v(0, 0);
+        request_v(1, 1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
 #pragma unroll
-                for (int s = 0; s < 2; ++s) o[s][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[s][kk], o[s][dt], 0, 0, 0);
-            }
+        for (int s = 0; s < 2; ++s) {
+            scores(0, s);
+            mask(0, s);
+            if (!again) m_ref[s] = fmaxf(kNegBigPrompt, row_max(sc[s]));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) exponentials(0, i);
+        __syncthreads();                             // K(0) has been read
+        int t = 0, st = 0;
+        for (; t + 3 < n_tiles; t += 3) {
+            period(0, 1, 2, t);
+            period(1, 2, 0, t + 1);
+            period(2, 0, 1, t + 2);
+        }
+        for (; t + 1 < n_tiles; ++t, st = st == 2 ? 0 : st + 1) period(st, st == 2 ? 0 : st + 1, st == 0 ? 2 : st - 1, t);
+        // the last tile, whose first products are done
+        mask(t, 1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) exponentials(1, i);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bf16x8 va = v_operand(st, i);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][i & 3]) : "v"(va), "v"(probabilities(s, i >> 2)));
+        }
+        // (the compiler does not know that there are matrix instructions in the assembly, whose results take up to 19 wait states)
+        asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o[0][0]), "+a"(o[0][1]), "+a"(o[0][2]), "+a"(o[0][3]), "+a"(o[1][0]), "+a"(o[1][1]), "+a"(o[1][2]), "+a"(o[1][3]));
+        l_run[0] += __shfl_xor(l_run[0], 32, 64);
+        l_run[1] += __shfl_xor(l_run[1], 32, 64);
+        if (again || __syncthreads_or(!(l_run[0] <= kPromptMaxSum && l_run[1] <= kPromptMaxSum)) == 0) break;
     }
-
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const float l = l_run[s] + __shfl_xor(l_run[s], 32, 64);
+        const float l = l_run[s];
         const int row = row0 + s * 32 + n;
         if (row >= nq) continue;
-        const float inv = l > 0.f ? 1.0f / l : 0.f;  // a query without keys: 0
+        const float inv = 1.0f / l;
         const int64_t at = (int64_t)(q_first + row) * a.Hq + h;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int r4 = 0; r4 < 4; ++r4)
                 *reinterpret_cast<uint2 *>(a.out + at * kD + dt * 32 + r4 * 8 + half * 4) =
-                    make_uint2(pack_bf16x2(o[s][dt][r4 * 4] * inv, o[s][dt][r4 * 4 + 1] * inv), pack_bf16x2(o[s][dt][r4 * 4 + 2] * inv, o[s][dt][r4 * 4 + 3] * inv));
-        if (a.lse != nullptr && half == 0) a.lse[at] = l > 0.f ? (m_run[s] + log2f(l)) * 0.69314718055994530942f : -INFINITY;
+                    l == 0.f ? make_uint2(0, 0)       // a query without keys
+                             : make_uint2(pack_bf16x2(o[s][dt][r4 * 4] * inv, o[s][dt][r4 * 4 + 1] * inv), pack_bf16x2(o[s][dt][r4 * 4 + 2] * inv, o[s][dt][r4 * 4 + 3] * inv));
+        if (a.lse != nullptr && half == 0) a.lse[at] = l == 0.f ? -INFINITY : (m_ref[s] + log2f(l)) * 0.69314718055994530942f;
     }
 }
 
@@ -221,6 +296,9 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     a.q = (const uint16_t *)q.ptr; a.q_sh = q.stride_h; a.q_st = q.stride_t;
     a.k = (const uint16_t *)k.ptr; a.k_sh = k.stride_h; a.k_st = k.stride_t;
     a.v = (const uint16_t *)v.ptr; a.v_sh = v.stride_h; a.v_st = v.stride_t;
+    // a tile's rows are addressed by 32-bit byte offsets from its first
+    if (a.k_st < 0 || a.v_st < 0 || a.k_st >= (1 << 24) || a.v_st >= (1 << 24))
+        return fail(IHIP_ERR_UNSUPPORTED, "%s: rows of k and v must be less than 2^24 elements apart", who);
     a.scale_log2e = sm_scale * 1.44269504088896340736f;
     a.out = (uint16_t *)out;
     a.lse = out_lse;
