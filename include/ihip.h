@@ -528,6 +528,21 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
                        const ihip_kv_store *store, ihip_tensor q_out, ihip_tensor k_out, void *stream);
 
 /*
+ * ihip_sparse_attn_decode over a store of 4-bit rows (IHIP_KV_MX4): the same
+ * key set, shape, block_starts and outputs.  With n_blocks == 0 (block_starts may
+ * then be NULL) and n_stream >= max_seq_len every key is attended to.  Scores,
+ * exponentials and sums in fp32; the probabilities are rounded to bf16 for the second
+ * product, rows are widened to bf16 (exact).  The output of an idle place of the
+ * batch is 0, its log-sum-exp -INFINITY; so is that of a sequence whose pages all have negative ids
+ * (keys on such pages are left out).
+ *   ws, ws_bytes device scratch of ihip_workspace_bytes(IHIP_OP_ATTN_DECODE_MX4, ...), 8-byte aligned
+ */
+int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_tensor q, const ihip_kv_store *store,
+                                      const int32_t *block_starts, int32_t n_blocks, int32_t block,
+                                      float sm_scale, void *out, float *out_lse, void *ws, size_t ws_bytes,
+                                      void *stream);
+
+/*
  * Dense causal attention of whole prompts, packed one behind the other (the
  * layers that are not pruned, and a prompt's first chunk): query i of the n of
  * sequence b attends to keys 0 .. i + (t - n) of its t keys, rows

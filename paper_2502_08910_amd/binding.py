@@ -94,6 +94,7 @@ EXPORTS = {
                                          c_f, vp, vp, vp, c_sz, vp]),
     "ihip_prefill_layer": (c_i32, [ctypes.POINTER(Shape), Tensor, Tensor, Tensor, c_i32, vp, vp, c_f,
                                    vp, vp, vp, vp, c_sz, vp]),
+    "ihip_sparse_attn_decode_mx4kv": (c_i32, [ctypes.POINTER(Shape), Tensor, vp, vp, c_i32, c_i32, c_f, vp, vp, vp, c_sz, vp]),
     "ihip_prompt_attn": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, c_f, vp, vp, vp]),
     "ihip_kv_append": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, vp, vp, Tensor, Tensor, vp]),
     "ihip_kv_gather": (c_i32, [vp, c_i32, c_i32, c_i32, vp, c_i32, Tensor, Tensor, vp]),
@@ -257,17 +258,17 @@ class Layer:
     """Shape of one attention call plus the device seq_lens; the methods are
     the C entry points of the same names."""
 
-    def __init__(self, q: torch.Tensor, k: torch.Tensor, seq_lens: torch.Tensor, b_q: int, n_sink: int,
+    def __init__(self, q: torch.Tensor, k, seq_lens: torch.Tensor, b_q: int, n_sink: int,
                  n_stream: int, max_seq_len: Optional[int] = None, b_q_range: int = 0):
-        """b_q_range: the first pruning stage's block size when the stages use different ones
+        """k: the K tensor, or the KVStore that is read.  b_q_range: the first pruning stage's block size when the stages use different ones
         (ihip_shape.b_q_range); 0 = b_q."""
         B, Hq, Tq, d = q.shape
-        Hkv = k.shape[1]
+        Hkv, tokens = (k.Hkv, k.tokens) if isinstance(k, KVStore) else (k.shape[1], k.shape[2])
         if seq_lens.dtype != torch.int32 or not seq_lens.is_cuda or seq_lens.numel() != B:
             raise IhipError("seq_lens: need an int32 device tensor [B]")
         self.seq_lens = seq_lens
-        self.max_seq_len = int(k.shape[2] if max_seq_len is None else max_seq_len)
-        if self.max_seq_len > k.shape[2]:
+        self.max_seq_len = int(tokens if max_seq_len is None else max_seq_len)
+        if self.max_seq_len > tokens:
             raise IhipError("max_seq_len exceeds the allocated tokens of K")
         self.shape = Shape(B, Hq, Hkv, d, Tq, b_q, seq_lens.data_ptr(), self.max_seq_len, n_sink, n_stream, b_q_range)
         self.B, self.Hq, self.Hkv, self.d, self.Tq, self.b_q = B, Hq, Hkv, d, Tq, b_q
@@ -897,4 +898,37 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
                                       _packed_tensor(v, "v", rows_k, Hkv),
                                       None if cu_k is None else _lengths(cu_k, B + 1, "cu_k", q.device), rows_k, sm_scale,
                                       _ptr(out), _ptr(lse), _stream_of(q.device)))
+    return out, lse
+
+
+def sparse_attn_decode_mx4(layer: "Layer", q: torch.Tensor, store: KVStore, block_starts: Optional[torch.Tensor] = None,
+                           block: int = 1, sm_scale: Optional[float] = None, want_lse: bool = False,
+                           ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                           lse: Optional[torch.Tensor] = None):
+    """ihip_sparse_attn_decode_mx4kv -> (out bf16 [B,Hq,1,d], lse fp32 [B,Hq,1] or None).  block_starts None: sink and
+    window alone (every key with n_stream >= max_seq_len)."""
+    n_blocks = 0 if block_starts is None else block_starts.shape[-1]
+    sm_scale = 1.0 / math.sqrt(layer.d) if sm_scale is None else sm_scale
+    if store.Hkv != layer.Hkv or store.B < layer.B:
+        raise IhipError(f"the store holds {store.B} sequences of {store.Hkv} heads, the layer has {layer.B} of {layer.Hkv}")
+    if layer.max_seq_len > store.tokens:
+        raise IhipError(f"the store holds {store.tokens} tokens a sequence, max_seq_len is {layer.max_seq_len}")
+    if tuple(q.shape) != (layer.B, layer.Hq, 1, layer.d):
+        raise IhipError(f"q: need the layer's shape, {(layer.B, layer.Hq, 1, layer.d)}")
+    if n_blocks and (block_starts.dtype != torch.int32 or not block_starts.is_contiguous() or block_starts.numel() != layer.P * n_blocks):
+        raise IhipError("block_starts: need a contiguous int32 tensor [B * Hkv, n_blocks]")
+    if out is None:
+        out = torch.empty((layer.B, layer.Hq, 1, layer.d), dtype=torch.bfloat16, device=layer.device)
+    if lse is None and want_lse:
+        lse = torch.empty((layer.B, layer.Hq, 1), dtype=torch.float32, device=layer.device)
+    if ws is None:
+        ws = layer.workspace(OP_ATTN_DECODE_MX4, [block], [max(n_blocks, 1)])
+    _same_device(layer.device, q=q, store=store.k, block_starts=block_starts, out=out, lse=lse, ws=ws)
+    for t, name, dt in ((out, "out", torch.bfloat16), (lse, "lse", torch.float32)):
+        if t is not None and (t.dtype != dt or not t.is_contiguous() or t.numel() != layer.B * layer.Hq * (layer.d if t is out else 1)):
+            raise IhipError(f"{name}: need a contiguous {dt} tensor of the layer's shape")
+    with torch.cuda.device(layer.device):
+        _check(lib().ihip_sparse_attn_decode_mx4kv(ctypes.byref(layer.shape), _tensor(q, "q"), store.ref(), _ptr(block_starts),
+                                                   n_blocks, block, sm_scale, _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
+                                                   _stream_of(layer.device)))
     return out, lse

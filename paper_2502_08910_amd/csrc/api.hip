@@ -100,6 +100,7 @@ void cache_describe(const ihip_cache *, int32_t *, int32_t *, int64_t *, ihip_te
 bool cache_holds_fp8(const ihip_cache *);
 int32_t refuse_capture(const char *, hipStream_t);
 size_t attn_decode_workspace(const ihip_shape &, int, int, bool);
+size_t attn_decode_mx4_workspace(const ihip_shape &, int, int);
 int32_t launch_attn_prefill(const ihip_shape &, const ihip_tensor &, const ihip_tensor &,
                             const ihip_tensor &, const int32_t *, int, int, float, void *, float *,
                             void *, size_t, const ihip_rope *, hipStream_t, const KvFormat * = nullptr);
@@ -1234,6 +1235,8 @@ size_t ihip_workspace_bytes(int32_t op, const ihip_shape *shape, int32_t n_stage
     switch (op) {
     case IHIP_OP_ATTN_DECODE:
         return std::max<size_t>(256, attn_decode_workspace(*shape, keeps[last], chunk_sizes[last], true));
+    case IHIP_OP_ATTN_DECODE_MX4:
+        return std::max<size_t>(256, attn_decode_mx4_workspace(*shape, keeps[last], chunk_sizes[last]));
     case IHIP_OP_ATTN_PREFILL:
         return std::max<size_t>(256, attn_prefill_workspace(*shape, keeps[last], chunk_sizes[last]));
     case IHIP_OP_PRUNE_ALL:         // (never 0, which stands for an error: an empty batch needs nothing)

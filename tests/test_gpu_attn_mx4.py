@@ -1,0 +1,275 @@
+"""Decode attention over 4-bit caches (ihip_sparse_attn_decode_mx4kv) against float64 on the values that the rows stand for.
+
+Tolerances.  Rows are widened exactly.  The probabilities are rounded to bf16 (half a step, 2^-8 of each), the result once more; the
+rest is fp32: scores off by at most 2^-17 of sum |q_i k_i| (128 terms), which moves a probability by as much, relative."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from tests.kv_reference import D, attention, f64, mx4_values  # noqa: E402
+
+SCALE = 1 / np.sqrt(D)
+
+
+@pytest.fixture(scope="module")
+def ihip():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2502_08910_amd as pkg
+    pkg.lib()
+    return pkg
+
+
+class Cache:
+    """Random 4-bit rows where the sequences have keys; everywhere else rows of NaN."""
+
+    def __init__(self, ihip, lens, Hkv, page, seed, T=None):
+        g = torch.Generator().manual_seed(seed)
+        B, T = len(lens), T or max(max(lens), 1)
+        n, self.table, self.page = B, None, page
+        if page:
+            per = -(-T // page)
+            n = B * per + 2
+            self.table = torch.randperm(n, generator=g)[:B * per].to(torch.int32).view(B, per).contiguous()
+        shape = (n, Hkv, page or T)
+        codes = [torch.randint(0, 256, (*shape, D // 2), generator=g, dtype=torch.uint8) for _ in range(2)]
+        scales = [torch.full((*shape, 4), 255, dtype=torch.uint8) for _ in range(2)]
+        for b, t in enumerate(lens):
+            for pos in range(t):
+                p, j = (b, pos) if self.table is None else (int(self.table[b, pos // page]), pos % page)
+                for s in scales:
+                    s[p, :, j] = torch.randint(123, 127, (Hkv, 4), generator=g, dtype=torch.uint8)
+        self.k, self.v, self.ks, self.vs = (t.cuda() for t in (*codes, *scales))
+        self.table = None if self.table is None else self.table.cuda()
+        self.store = ihip.KVStore.mx4(self.k, self.v, self.ks, self.vs, self.table)
+        self.B, self.lens, self.T = B, lens, T
+
+    def rows(self, b, g, pos):
+        if self.table is None:
+            p, j = np.full(len(pos), b), pos
+        else:
+            p, j = self.table.cpu().numpy()[b][pos // self.page], pos % self.page
+        return tuple(mx4_values(c.cpu()[p, g, j], s.cpu()[p, g, j]) for c, s in ((self.k, self.ks), (self.v, self.vs)))
+
+
+def positions(t, n_sink, n_stream, starts, block):
+    """Keys that a query behind t keys attends to."""
+    hi = t - n_stream
+    keep = set(range(min(n_sink, t))) | set(range(max(hi, n_sink), t))
+    for s in starts:
+        if s >= 0:
+            keep |= set(range(s, min(s + block, hi)))
+    return np.array(sorted(keep), dtype=np.int64)
+
+
+def check(c, q, out, lse, n_sink, n_stream, starts=None, block=1, scale=SCALE):
+    B, Hq = q.shape[:2]
+    Hkv = c.k.shape[1]
+    G = Hq // Hkv
+    q, out, lse = f64(q), f64(out), f64(lse)
+    for b in range(B):
+        for g in range(Hkv):
+            pos = positions(c.lens[b], n_sink, n_stream, [] if starts is None else starts[b * Hkv + g].tolist(), block)
+            Q = q[b, g * G:(g + 1) * G, 0]
+            k, v = c.rows(b, g, pos) if len(pos) else (np.zeros((0, D)), np.zeros((0, D)))
+            seen = np.ones((G, len(pos)), dtype=bool)
+            want, want_lse = attention(Q, k, v, scale, seen)
+            mag, _ = attention(Q, k, np.abs(v), scale, seen)
+            off = 2.0 ** -17 * scale * (np.abs(Q) @ np.abs(k).T).max(axis=1, initial=0)
+            got, got_lse = out[b, g * G:(g + 1) * G, 0], lse[b, g * G:(g + 1) * G, 0]
+            # (an exponential below 2^-126 of the reference, which is at most the maximum, is 0 in fp32: as much for every key's value)
+            lost = 2.0 ** -126 * np.abs(v).sum(axis=0)
+            tol = mag * (2.0 ** -8 + 2 * off + 2.0 ** -20)[:, None] + np.abs(want) * 2.0 ** -8 + lost
+            assert bool((np.abs(got - want) <= tol).all()), (b, g, np.abs(got - want).max())
+            if len(pos) == 0:
+                assert (got_lse == -np.inf).all()
+            else:
+                assert (np.abs(got_lse - want_lse) <= off + 2.0 ** -20 * (1 + np.abs(want_lse))).all(), (b, g)
+
+
+def queries(B, Hq, seed, scale=1.0):
+    return (torch.randn((B, Hq, 1, D), generator=torch.Generator().manual_seed(seed)) * scale).bfloat16().cuda()
+
+
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+@pytest.mark.parametrize("page,Hkv,lens", [(0, 2, [1, 0, 31, 32, 33]), (16, 8, [500, 129, 15]), (1, 1, [70]), (64, 3, [1000, 128, 64, 63])])
+def test_all_keys(ihip, G, page, Hkv, lens):
+    c = Cache(ihip, lens, Hkv, page, seed=G)
+    q = queries(len(lens), G * Hkv, 10 + G, scale=2.0)
+    sl = torch.tensor(lens, dtype=torch.int32).cuda()
+    L = ihip.Layer(q, c.store, sl, 1, 0, c.T, max_seq_len=c.T)
+    out, lse = ihip.sparse_attn_decode_mx4(L, q, c.store, want_lse=True)
+    check(c, q, out, lse, 0, c.T)
+
+
+@pytest.mark.parametrize("page,block,n_blocks", [(0, 16, 5), (16, 4, 9), (64, 64, 3), (8, 1, 12)])
+def test_sink_blocks_and_window(ihip, page, block, n_blocks):
+    """Kept blocks, absent ones (-1), one cut at the end of the middle range; a sequence shorter than sink and window."""
+    lens, Hkv, Hq, n_sink, n_stream = [900, 417, 30], 2, 8, 20, 70
+    c = Cache(ihip, lens, Hkv, page, seed=3)
+    q = queries(3, Hq, 4)
+    g = torch.Generator().manual_seed(5)
+    starts = torch.full((3 * Hkv, n_blocks), -1, dtype=torch.int32)
+    for p in range(3 * Hkv):
+        hi = lens[p // Hkv] - n_stream
+        slots = max(0, -(-(hi - n_sink) // block))
+        keep = min(slots, n_blocks - p % 2)
+        at = torch.randperm(slots, generator=g)[:keep].sort().values
+        if keep:
+            at[-1] = slots - 1                       # the block that is cut
+            starts[p, :keep] = (n_sink + at * block).to(torch.int32).unique()[:keep] if len(at.unique()) == keep else n_sink + block * torch.arange(keep, dtype=torch.int32)
+    sl = torch.tensor(lens, dtype=torch.int32).cuda()
+    L = ihip.Layer(q, c.store, sl, 1, n_sink, n_stream, max_seq_len=c.T)
+    out, lse = ihip.sparse_attn_decode_mx4(L, q, c.store, starts.cuda(), block, want_lse=True, sm_scale=0.2)
+    check(c, q, out, lse, n_sink, n_stream, starts, block, scale=0.2)
+
+
+def test_long_sequences_take_several_splits(ihip):
+    lens = [20011, 4097, 9000]
+    c = Cache(ihip, lens, 1, 16, seed=6)
+    q = queries(3, 4, 7, scale=3.0)
+    L = ihip.Layer(q, c.store, torch.tensor(lens, dtype=torch.int32).cuda(), 1, 0, c.T, max_seq_len=c.T)
+    out, lse = ihip.sparse_attn_decode_mx4(L, q, c.store, want_lse=True)
+    check(c, q, out, lse, 0, c.T)
+
+
+def test_scores_that_grow_along_the_keys(ihip):
+    """The running reference follows scores that leave the exponents' range."""
+    lens = [3000]
+    c = Cache(ihip, lens, 1, 0, seed=8)
+    c.ks[0, 0, 1000:] += 4
+    c.ks[0, 0, 2000:] += 5
+    c.ks[0, 0, 2500:] -= 12
+    q = queries(1, 8, 9, scale=2.0)
+    L = ihip.Layer(q, c.store, torch.tensor(lens, dtype=torch.int32).cuda(), 1, 0, c.T, max_seq_len=c.T)
+    out, lse = ihip.sparse_attn_decode_mx4(L, q, c.store, want_lse=True)
+    check(c, q, out, lse, 0, c.T)
+
+
+def test_pages_without_an_id_are_left_out(ihip):
+    lens = [100, 40]
+    c = Cache(ihip, lens, 2, 16, seed=10)
+    table = c.table.clone()
+    table[0, 2] = -1
+    table[1] = -1
+    store = ihip.KVStore.mx4(c.k, c.v, c.ks, c.vs, table)
+    q = queries(2, 4, 11)
+    L = ihip.Layer(q, store, torch.tensor(lens, dtype=torch.int32).cuda(), 1, 0, c.T, max_seq_len=c.T)
+    out, lse = ihip.sparse_attn_decode_mx4(L, q, store, want_lse=True)
+    assert bool((out[1] == 0).all()) and bool((lse[1] == -np.inf).all())
+    pos = np.array([i for i in range(100) if not 32 <= i < 48])
+    for g in range(2):
+        k, v = c.rows(0, g, pos)
+        want, want_lse = attention(f64(q)[0, 2 * g:2 * g + 2, 0], k, v, SCALE, np.ones((2, len(pos)), dtype=bool))
+        assert np.abs(f64(lse)[0, 2 * g:2 * g + 2, 0] - want_lse).max() < 1e-4
+        assert np.abs(f64(out)[0, 2 * g:2 * g + 2, 0] - want).max() <= 2.0 ** -7 * np.abs(v).max()
+
+
+def test_rows_beyond_four_gigabytes(ihip):
+    page, Hkv = 64, 8
+    n = (5 << 30) // (page * Hkv * 64) + 7
+    k, v = (torch.zeros((n, Hkv, page, 64), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((n, Hkv, page, 4), 255, dtype=torch.uint8, device="cuda") for _ in range(2))
+    small = Cache(ihip, [150], Hkv, page, seed=12)
+    table = torch.tensor([[n - 1, 1, n - 3]], dtype=torch.int32).cuda()
+    for i in range(3):
+        for to, src in ((k, small.k), (v, small.v), (ks, small.ks), (vs, small.vs)):
+            to[table[0, i]] = src[small.table[0, i]]
+    store = ihip.KVStore.mx4(k, v, ks, vs, table)
+    q = queries(1, 32, 13)
+    sl = torch.tensor([150], dtype=torch.int32).cuda()
+    got = [ihip.sparse_attn_decode_mx4(ihip.Layer(q, s, sl, 1, 0, 192, max_seq_len=192), q, s, want_lse=True) for s in (store, small_store(ihip, small))]
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+def small_store(ihip, c):
+    """The cache with a table that covers 192 tokens, as the large one's does."""
+    return ihip.KVStore.mx4(c.k, c.v, c.ks, c.vs, c.table[:, :3].contiguous())
+
+
+def test_on_another_stream_and_in_a_graph(ihip):
+    lens = [700, 333]
+    c = Cache(ihip, lens, 2, 16, seed=14)
+    q = queries(2, 8, 15)
+    sl = torch.tensor(lens, dtype=torch.int32).cuda()
+    L = ihip.Layer(q, c.store, sl, 1, 0, c.T, max_seq_len=c.T)
+    ws = L.workspace(ihip.OP_ATTN_DECODE_MX4, [1], [1])
+    out, lse = torch.zeros_like(q), torch.zeros((2, 8, 1), device="cuda")
+
+    def step():
+        ihip.sparse_attn_decode_mx4(L, q, c.store, ws=ws, out=out, lse=lse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    check(c, q, out, lse, 0, c.T)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for i in range(1, 5):
+        q.copy_(queries(2, 8, 20 + i))
+        sl.copy_(torch.tensor([700 - 90 * i, 333 - i], dtype=torch.int32))
+        step()
+        want = out.clone(), lse.clone()
+        out.zero_(), lse.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]), i
+
+
+def test_a_run_of_them_together(ihip):
+    """A prompt in two packed sequences, attended to while its keys go into a 4-bit cache, then decode steps that append and attend;
+    and the cache read back for the library's own decode attention, which has to agree with the 4-bit one."""
+    from tests.kv_reference import fp32_turned, mx4_rounded
+    from workloads import gen
+    B, Hq, Hkv, page, new = 2, 8, 2, 16, [150, 61]
+    T = 160
+    cos, sin = (t.cuda() for t in gen.rope_table(T, D))
+    per = T // page
+    table = torch.randperm(B * per, generator=torch.Generator().manual_seed(1)).to(torch.int32).view(B, per).contiguous().cuda()
+    k, v = (torch.zeros((B * per, Hkv, page, D // 2), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((B * per, Hkv, page, 4), 255, dtype=torch.uint8, device="cuda") for _ in range(2))
+    store = ihip.KVStore.mx4(k, v, ks, vs, table)
+    x = torch.randn((sum(new), Hq + 2 * Hkv, D), generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
+    raw = f64(x)
+    cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32).cuda()
+    sl = torch.tensor(new, dtype=torch.int32).cuda()
+    qx, kx, vx = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    ihip.kv_append(store, kx, vx, cu, sl, T, q=qx, rope=(cos, sin), q_out=qx, k_out=kx)
+    out, lse = ihip.prompt_attn(qx, kx, vx, cu, max(new), want_lse=True)
+    from tests.test_gpu_prompt_attn import check as check_prompt
+    check_prompt(qx, kx, vx, new, new, out, lse)
+    held = [(list(mx4_rounded(fp32_turned(raw[c0:c1, Hq:Hq + Hkv], f64(cos)[:c1 - c0, None], f64(sin)[:c1 - c0, None]))[0]),
+             list(mx4_rounded(raw[c0:c1, Hq + Hkv:])[0])) for c0, c1 in ((0, new[0]), (new[0], sum(new)))]
+    one = torch.tensor([0, 1, 2], dtype=torch.int32).cuda()
+    for step in range(3):
+        y = torch.randn((B, Hq + 2 * Hkv, D), generator=torch.Generator().manual_seed(3 + step)).bfloat16().cuda()
+        sl += 1
+        q, _ = ihip.kv_append(store, y[:, Hq:Hq + Hkv], y[:, Hq + Hkv:], one, sl, T, q=y[:, :Hq], rope=(cos, sin))
+        q = q.view(B, Hq, 1, D)
+        L = ihip.Layer(q, store, sl, 1, 0, T, max_seq_len=T)
+        out, lse = ihip.sparse_attn_decode_mx4(L, q, store, want_lse=True)
+        k16, v16 = ihip.kv_gather(store, sl, T)
+        empty = torch.zeros((L.P, 1), dtype=torch.int32, device="cuda") - 1
+        ref, ref_lse = ihip.Layer(q, k16, sl, 1, 0, T).sparse_attn_decode(q, k16, v16, empty, 1, want_lse=True)
+        # the same values, the probabilities rounded to bf16 here: within 2^-8 of the largest value, and both results' own rounding
+        assert bool(((out.float() - ref.float()).abs() <= 2.0 ** -7 * v16.float().nan_to_num().abs().max()).all())
+        assert bool(((lse - ref_lse).abs() <= 1e-4).all())
+        for b in range(B):
+            pos = new[b] + step
+            r = f64(y[b])
+            held[b][0].append(mx4_rounded(fp32_turned(r[Hq:Hq + Hkv], f64(cos)[pos], f64(sin)[pos]))[0])
+            held[b][1].append(mx4_rounded(r[Hq + Hkv:])[0])
+            K, V = (np.stack(h) for h in held[b])
+            for g in range(Hkv):
+                Q = f64(q)[b, 4 * g:4 * g + 4, 0]
+                seen = np.ones((4, pos + 1), dtype=bool)
+                want, want_lse = attention(Q, K[:, g], V[:, g], SCALE, seen)
+                mag, _ = attention(Q, K[:, g], np.abs(V[:, g]), SCALE, seen)
+                off = 2.0 ** -17 * SCALE * (np.abs(Q) @ np.abs(K[:, g]).T).max(axis=1)
+                assert (np.abs(f64(out)[b, 4 * g:4 * g + 4, 0] - want) <= mag * (2.0 ** -8 + 2 * off + 2.0 ** -20)[:, None] + np.abs(want) * 2.0 ** -8).all()
+                assert (np.abs(f64(lse)[b, 4 * g:4 * g + 4, 0] - want_lse) <= off + 2.0 ** -20 * (1 + np.abs(want_lse))).all()
