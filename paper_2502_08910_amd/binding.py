@@ -796,11 +796,12 @@ class KVStore:
 
 
 def _packed_tensor(t: torch.Tensor, name: str, rows: Optional[int] = None, heads: Optional[int] = None) -> Tensor:
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.stride(2) != 1 or not t.is_cuda:
+    shape, stride = t.shape, t.stride()
+    if t.dtype != torch.bfloat16 or len(shape) != 3 or stride[2] != 1 or not t.is_cuda:
         raise IhipError(f"{name}: need a 3-d bf16 device tensor [rows, heads, d] with contiguous last dim")
-    if (rows is not None and t.shape[0] != rows) or (heads is not None and t.shape[1] != heads):
-        raise IhipError(f"{name}: need {rows} rows of {heads} heads, got {tuple(t.shape[:2])}")
-    return Tensor(t.data_ptr(), 0, t.stride(1), t.stride(0))
+    if rows is not None and (shape[0] != rows or shape[1] != heads):
+        raise IhipError(f"{name}: need {rows} rows of {heads} heads, got {tuple(shape[:2])}")
+    return Tensor(t.data_ptr(), 0, stride[1], stride[0])
 
 
 def _lengths(t: torch.Tensor, n: int, name: str, device) -> int:
@@ -815,8 +816,17 @@ def _same_device(device, **tensors) -> None:
             raise IhipError(f"{name} is on {t.device}, not on {device}")
 
 
-def _stream_of(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+# the raw handle without a Stream object around it, which takes 2 us to make
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _enqueue(device, fn, *args) -> None:
+    """fn(*args, stream) on the device's current stream, with the device as the current one."""
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, _raw_stream(device.index)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _raw_stream(device.index)))
 
 
 def kv_append(store: KVStore, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int,
@@ -833,24 +843,22 @@ def kv_append(store: KVStore, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tens
         raise IhipError(f"the store holds {store.B} sequences of {store.Hkv} heads and {store.tokens} tokens")
     cos_sin = None
     if rope is not None:
-        _same_device(store.device, cos=rope[0], sin=rope[1])
-        cos_sin = Rope(rope[0], rope[1])
-        if rope[0].shape[1] * 2 != d:
-            raise IhipError("rope tables: need d / 2 columns")
+        for t in rope:
+            if t.dtype != torch.float32 or t.device != store.device or not t.is_contiguous() or t.shape != rope[0].shape or \
+                    t.dim() != 2 or t.shape[1] * 2 != d:
+                raise IhipError("rope tables: need contiguous fp32 tensors [n_pos, d / 2] on the store's device")
+        cos_sin = RopeStruct(rope[0].data_ptr(), rope[1].data_ptr(), rope[0].shape[0], ROPE_NONE, ROPE_NONE)
     if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if q is None and q_out is not None:
         raise IhipError("q_out without q")
     Hq = Hkv if q is None else q.shape[1]
     tq = NO_TENSOR if q is None else _packed_tensor(q, "q", rows, Hq)
     p = PackedStruct(B, Hq, Hkv, d, _lengths(cu_q, B + 1, "cu_q", store.device), rows, rows)
-    with torch.cuda.device(store.device):
-        _check(lib().ihip_kv_append(ctypes.byref(p), tq, _packed_tensor(k, "k"), _packed_tensor(v, "v", rows, Hkv),
-                                    _lengths(seq_lens, B, "seq_lens", store.device), max_seq_len,
-                                    cos_sin.ref() if cos_sin is not None else None, store.ref(),
-                                    NO_TENSOR if q is None else _packed_tensor(q_out, "q_out", rows, Hq),
-                                    NO_TENSOR if k_out is None else _packed_tensor(k_out, "k_out", rows, Hkv),
-                                    _stream_of(store.device)))
+    _enqueue(store.device, lib().ihip_kv_append, ctypes.byref(p), tq, _packed_tensor(k, "k"), _packed_tensor(v, "v", rows, Hkv),
+             _lengths(seq_lens, B, "seq_lens", store.device), max_seq_len, None if cos_sin is None else ctypes.byref(cos_sin),
+             store.ref(), NO_TENSOR if q is None else _packed_tensor(q_out, "q_out", rows, Hq),
+             NO_TENSOR if k_out is None else _packed_tensor(k_out, "k_out", rows, Hkv))
     return q_out, k_out
 
 
@@ -866,10 +874,8 @@ def kv_gather(store: KVStore, seq_lens: torch.Tensor, max_seq_len: int, k_out: O
     _same_device(store.device, k_out=k_out, v_out=v_out)
     if k_out.shape != shape or v_out.shape != shape:
         raise IhipError(f"k_out, v_out: need shape {shape}")
-    with torch.cuda.device(store.device):
-        _check(lib().ihip_kv_gather(store.ref(), B, store.Hkv, 128, _lengths(seq_lens, B, "seq_lens", store.device),
-                                    max_seq_len, _tensor(k_out, "k_out"), _tensor(v_out, "v_out"),
-                                    _stream_of(store.device)))
+    _enqueue(store.device, lib().ihip_kv_gather, store.ref(), B, store.Hkv, 128,
+             _lengths(seq_lens, B, "seq_lens", store.device), max_seq_len, _tensor(k_out, "k_out"), _tensor(v_out, "v_out"))
     return k_out, v_out
 
 
@@ -884,7 +890,7 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     B = cu_q.numel() - 1
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
     if out is None:
-        out = torch.empty((rows, Hq, d), dtype=torch.bfloat16, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None and want_lse:
         lse = torch.empty((rows, Hq), dtype=torch.float32, device=q.device)
     _same_device(q.device, k=k, v=v, out=out, lse=lse)
@@ -893,11 +899,9 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     if lse is not None and (lse.shape != (rows, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous()):
         raise IhipError("lse: need a contiguous fp32 tensor [rows, Hq]")
     p = PackedStruct(B, Hq, Hkv, d, _lengths(cu_q, B + 1, "cu_q", q.device), rows, max_q)
-    with torch.cuda.device(q.device):
-        _check(lib().ihip_prompt_attn(ctypes.byref(p), _packed_tensor(q, "q"), _packed_tensor(k, "k"),
-                                      _packed_tensor(v, "v", rows_k, Hkv),
-                                      None if cu_k is None else _lengths(cu_k, B + 1, "cu_k", q.device), rows_k, sm_scale,
-                                      _ptr(out), _ptr(lse), _stream_of(q.device)))
+    _enqueue(q.device, lib().ihip_prompt_attn, ctypes.byref(p), _packed_tensor(q, "q"), _packed_tensor(k, "k"),
+             _packed_tensor(v, "v", rows_k, Hkv), None if cu_k is None else _lengths(cu_k, B + 1, "cu_k", q.device), rows_k,
+             sm_scale, _ptr(out), _ptr(lse))
     return out, lse
 
 
@@ -927,8 +931,6 @@ def sparse_attn_decode_mx4(layer: "Layer", q: torch.Tensor, store: KVStore, bloc
     for t, name, dt in ((out, "out", torch.bfloat16), (lse, "lse", torch.float32)):
         if t is not None and (t.dtype != dt or not t.is_contiguous() or t.numel() != layer.B * layer.Hq * (layer.d if t is out else 1)):
             raise IhipError(f"{name}: need a contiguous {dt} tensor of the layer's shape")
-    with torch.cuda.device(layer.device):
-        _check(lib().ihip_sparse_attn_decode_mx4kv(ctypes.byref(layer.shape), _tensor(q, "q"), store.ref(), _ptr(block_starts),
-                                                   n_blocks, block, sm_scale, _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
-                                                   _stream_of(layer.device)))
+    _enqueue(layer.device, lib().ihip_sparse_attn_decode_mx4kv, ctypes.byref(layer.shape), _tensor(q, "q"), store.ref(),
+             _ptr(block_starts), n_blocks, block, sm_scale, _ptr(out), _ptr(lse), _ptr(ws), ws.numel())
     return out, lse
