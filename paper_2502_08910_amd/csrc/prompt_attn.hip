@@ -13,7 +13,7 @@ constexpr int kPromptWaves = 4;
 constexpr int kPromptRows = 64 * kPromptWaves;       // queries of a workgroup
 constexpr int kTileKeys = 32;
 constexpr int kTileEl = kTileKeys * kD;              // bf16 elements of a K or V tile in LDS
-constexpr int kPromptStages = 3;
+constexpr int kPromptStages = 4;
 constexpr float kNegBigPrompt = -1.0e30f;            // finite stand-in for -inf in maxima
 constexpr float kPromptMaxSum = 18446744073709551616.0f;      // 2^64: sum of exponentials beyond which a block is done again
 
@@ -28,6 +28,13 @@ struct PromptArgs {
     uint16_t *out;                   // [rows_q, Hq, d]
     float *lse;                      // [rows_q, Hq] or null
 };
+
+// 16 bytes a lane from a scalar base and the lane's byte offset to the LDS byte address dst + 16 l (counts on vmcnt).  M0 is left as it is:
+// nothing else in this kernel reads it, and it is not the compiler's to keep values in.
+__device__ inline void prompt_to_lds(uint32_t dst, const uint16_t *base, uint32_t byte_off)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(byte_off), "s"(base) : "memory");
+}
 
 __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const PromptArgs a)
 {
@@ -77,35 +84,41 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 
     // Loads of a tile: 8 four-row instructions for K and 8 for V, two of each a wave: lane l brings 16 bytes of row 4 j + l / 16 to
     // base + 16 l.  The base of a tile is scalar; a lane's offset from it changes in a tile that reaches behind the last key only,
-    // whose rows stand for the missing ones.
-    uint32_t k_off[2], v_off[2];
-    auto offsets = [&](int rows, uint32_t (&ko)[2], uint32_t (&vo)[2]) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int key = 4 * (wave + i * kPromptWaves) + (lane >> 4), at = min(key, rows - 1), slot = lane & 15;
-            ko[i] = (uint32_t)(at * (int)a.k_st + ((slot ^ (key & 15)) << 3)) * 2u;
-            vo[i] = (uint32_t)(at * (int)a.v_st + ((slot ^ ((key & 3) << 2)) << 3)) * 2u;
+    // whose rows stand for the missing ones.  What would come after the last tile is the last tile again, so that every period
+    // has as many loads on their way as any other.
+    auto offset = [&](int i, int rows, int64_t st, bool is_v) {
+        const int key = 4 * (wave + i * kPromptWaves) + (lane >> 4), at = min(key, rows - 1), slot = lane & 15;
+        return (uint32_t)(at * (int)st + ((slot ^ (is_v ? (key & 3) << 2 : key & 15)) << 3)) * 2u;
+    };
+    const uint32_t k_off[2] = {offset(0, kTileKeys, a.k_st, false), offset(1, kTileKeys, a.k_st, false)};
+    const uint32_t v_off[2] = {offset(0, kTileKeys, a.v_st, true), offset(1, kTileKeys, a.v_st, true)};
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem + wave * 4 * kD * 2;
+    const bool cut = n_tiles * kTileKeys > nk;       // the last tile reaches behind the last key
+    const uint16_t *k_next = kb, *v_next = vb;       // of the tiles to be requested next
+    int k_tile = 0, v_tile = 0;
+    auto request_k = [&](int st) {
+        uint32_t off[2] = {k_off[0], k_off[1]};
+        if (cut && k_tile == n_tiles - 1) {
+            off[0] = offset(0, nk - k_tile * kTileKeys, a.k_st, false);
+            off[1] = offset(1, nk - k_tile * kTileKeys, a.k_st, false);
         }
+        prompt_to_lds(lds0 + st * kTileEl * 2, k_next, off[0]);
+        prompt_to_lds(lds0 + st * kTileEl * 2 + 16 * kD * 2, k_next, off[1]);
+        const bool more = k_tile < n_tiles - 1;
+        k_next += more ? kTileKeys * a.k_st : 0;
+        k_tile += more;
     };
-    offsets(kTileKeys, k_off, v_off);
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
-    auto request_k = [&](int tile, int st) {
-        if (tile >= n_tiles) return;
-        const uint16_t *base = kb + (int64_t)tile * kTileKeys * a.k_st;
-        const uint32_t dst = lds0 + (st * kTileEl + wave * 4 * kD) * 2;
-        uint32_t ko[2] = {k_off[0], k_off[1]}, vo[2];
-        if (tile * kTileKeys + kTileKeys > nk) offsets(nk - tile * kTileKeys, ko, vo);
-        global_to_lds(dst, base, ko[0]);
-        global_to_lds(dst + 16 * kD * 2, base, ko[1]);
-    };
-    auto request_v = [&](int tile, int st) {
-        if (tile >= n_tiles) return;
-        const uint16_t *base = vb + (int64_t)tile * kTileKeys * a.v_st;
-        const uint32_t dst = lds0 + ((kPromptStages + st) * kTileEl + wave * 4 * kD) * 2;
-        uint32_t ko[2], vo[2] = {v_off[0], v_off[1]};
-        if (tile * kTileKeys + kTileKeys > nk) offsets(nk - tile * kTileKeys, ko, vo);
-        global_to_lds(dst, base, vo[0]);
-        global_to_lds(dst + 16 * kD * 2, base, vo[1]);
+    auto request_v = [&](int st) {
+        uint32_t off[2] = {v_off[0], v_off[1]};
+        if (cut && v_tile == n_tiles - 1) {
+            off[0] = offset(0, nk - v_tile * kTileKeys, a.v_st, true);
+            off[1] = offset(1, nk - v_tile * kTileKeys, a.v_st, true);
+        }
+        prompt_to_lds(lds0 + (kPromptStages + st) * kTileEl * 2, v_next, off[0]);
+        prompt_to_lds(lds0 + (kPromptStages + st) * kTileEl * 2 + 16 * kD * 2, v_next, off[1]);
+        const bool more = v_tile < n_tiles - 1;
+        v_next += more ? kTileKeys * a.v_st : 0;
+        v_tile += more;
     };
     const uint16_t *k_at[8], *v_at[4];               // this lane's addresses in stage 0
 #pragma unroll
@@ -133,9 +146,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     };
     auto mask = [&](int tile, int s) {
         if (tile * kTileKeys + kTileKeys - 1 <= row0 + s * 32 + ahead) return;
+        const int last = last_key[s] - 4 * half - tile * kTileKeys;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-            if (tile * kTileKeys + 8 * (r >> 2) + 4 * half + (r & 3) > last_key[s]) sc[s][r] = -INFINITY;
+        for (int r = 0; r < 16; ++r) sc[s][r] = 8 * (r >> 2) + (r & 3) > last ? -INFINITY : sc[s][r];
     };
     auto row_max = [&](const f32x16 &s) {            // scaled; of both halves
         float mx = s[0];
@@ -146,48 +159,57 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 
     uint32_t pw[2][8];                               // the probabilities of a set, in pairs of keys
     float m_ref[2] = {kNegBigPrompt, kNegBigPrompt}, l_run[2] = {0.f, 0.f};
-    // two scores -> two probabilities (exp2(-inf) = 0)
+    // two scores -> two probabilities (exp2(-inf) = 0).  The empty assembly keeps them where they are called: left to themselves all
+    // exponentials of a phase would be computed in front of its matrix instructions instead of under them.
     auto exponentials = [&](int s, int i) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i], a.scale_log2e, -m_ref[s]));
-        const float y = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i + 1], a.scale_log2e, -m_ref[s]));
+        float x = fmaf(sc[s][2 * i], a.scale_log2e, -m_ref[s]), y = fmaf(sc[s][2 * i + 1], a.scale_log2e, -m_ref[s]);
+        asm volatile("" : "+v"(x), "+v"(y));
+        x = __builtin_amdgcn_exp2f(x);
+        y = __builtin_amdgcn_exp2f(y);
         l_run[s] += x;
         l_run[s] += y;
         pw[s][i] = pack_bf16x2(x, y);
+        asm volatile("" : "+v"(pw[s][i]), "+v"(l_run[s]));
     };
     auto probabilities = [&](int s, int kk) {
         return __builtin_bit_cast(bf16x8, make_uint4(pw[s][4 * kk], pw[s][4 * kk + 1], pw[s][4 * kk + 2], pw[s][4 * kk + 3]));
     };
     // Period t, for the two sets of 32 queries in turn: first product of tile t + 1 and second product of tile t, and under them the
-    // exponentials of the other set, 16 matrix instructions and 16 scores a lane at a time.  K of tile t + 3 and V of tile t + 2 are
-    // requested as it begins, into the stages that period t - 1 has read, and have landed when period t + 1 ends.
-    auto period = [&](int st, int st1, int st2, int t) {       // stages of tiles t, t + 1, t + 2
-        request_k(t + 3, st);
-        request_v(t + 2, st2);
-        bf16x8 ka[8], va[8];
+    // exponentials of the other set, 16 matrix instructions and 16 scores a lane at a time.  K of tile t + 4 and V of tile t + 3 are
+    // requested into the stages that period t - 1 has read, and have landed when period t + 1 ends; the first operands of period
+    // t + 1 are read from LDS as this one ends.  Matrix instructions are written as assembly: of the 512 registers that the one wave of
+    // a SIMD has, they can keep the accumulators in the upper half ("a") and everything else in the lower one, and they stay where
+    // they are, each with its share of the vector instructions under it.  The compiler does not know the instructions' latency: a set's
+    // scores are read by vector instructions eight matrix instructions after their last one.
+    bf16x8 ka[8], va[8];
+    auto first_operands = [&](int st, int st1) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            ka[i] = k_operand(st1, i);
+            va[i] = v_operand(st, i);
+        }
+    };
+    auto period = [&](int st, int st1, int st2, int st3, int t) {      // stages of tiles t, t + 1, t + 2, t + 3
         mask(t, 1);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             if (s == 1) mask(t + 1, 0);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                if (s == 0 && r == 0) {
-                    ka[0] = k_operand(st1, 0);
-                    ka[1] = k_operand(st1, 1);
-                }
+                const int i = r & 7;
                 if (s == 0 && r < 6) ka[r + 2] = k_operand(st1, r + 2);
-                if (s == 0 && r >= 6 && r < 14) va[r - 6] = v_operand(st, r - 6);
+                if (s == 0 && r >= 6 && r < 12) va[r - 4] = v_operand(st, r - 4);
+                if (s == 1 && r == 10) first_operands(st1, st2);
+                if (r == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=v"(sc[s]) : "v"(ka[0]), "v"(qb[s][0]));
+                else if (r < 8) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(sc[s]) : "v"(ka[r]), "v"(qb[s][r]));
+                else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][i & 3]) : "v"(va[i]), "v"(probabilities(s, i >> 2)));
                 if (r % 2 == 0) exponentials(1 - s, r / 2);
-                if (r < 8) {
-                    if (r == 0) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[0], qb[s][0], f32x16{}, 0, 0, 0);
-                    else sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[r], qb[s][r], sc[s], 0, 0, 0);
-                } else {
-                    asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][r & 3]) : "v"(va[r - 8]), "v"(probabilities(s, (r - 8) >> 2)));
-                }
+                if (s == 0 && r == 3) request_k(st);
+                if (s == 0 && r == 9) request_v(st3);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (t + 3 < n_tiles) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
         __syncthreads();
     };
     // Exponentials are taken against the row's maximum over the first tile (key 0 is in it, which every query with a key sees), not
@@ -196,8 +218,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     for (int again = 0; n_tiles > 0 && again < 2; ++again) {
         if (again) {
             m_ref[0] = m_ref[1] = kNegBigPrompt;
+            k_next = kb;
+            k_tile = 0;
             for (int t = 0; t < n_tiles; ++t) {
-                request_k(t, 0);
+                request_k(0);
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
 #pragma unroll
@@ -215,11 +239,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) o[s][dt] = f32x16{};
         }
-        request_k(0, 0);
-        request_k(1, 1);
-        request_k(2, 2);
-        request_v(0, 0);
-        request_v(1, 1);
+        k_next = kb; v_next = vb;
+        k_tile = v_tile = 0;
+#pragma unroll
+        for (int st = 0; st < 4; ++st) request_k(st);
+#pragma unroll
+        for (int st = 0; st < 3; ++st) request_v(st);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
 #pragma unroll
@@ -231,23 +256,25 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 #pragma unroll
         for (int i = 0; i < 8; ++i) exponentials(0, i);
         __syncthreads();                             // K(0) has been read
-        int t = 0, st = 0;
-        for (; t + 3 < n_tiles; t += 3) {
-            period(0, 1, 2, t);
-            period(1, 2, 0, t + 1);
-            period(2, 0, 1, t + 2);
+        first_operands(0, 1);
+        int t = 0;
+        for (; t + 4 < n_tiles; t += 4) {
+            period(0, 1, 2, 3, t);
+            period(1, 2, 3, 0, t + 1);
+            period(2, 3, 0, 1, t + 2);
+            period(3, 0, 1, 2, t + 3);
         }
-        for (; t + 1 < n_tiles; ++t, st = st == 2 ? 0 : st + 1) period(st, st == 2 ? 0 : st + 1, st == 0 ? 2 : st - 1, t);
+        for (; t + 1 < n_tiles; ++t) period(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t);
         // the last tile, whose first products are done
         mask(t, 1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) exponentials(1, i);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bf16x8 va = v_operand(st, i);
+            const bf16x8 vt = v_operand(t & 3, i);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-                asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][i & 3]) : "v"(va), "v"(probabilities(s, i >> 2)));
+                asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][i & 3]) : "v"(vt), "v"(probabilities(s, i >> 2)));
         }
         // (the compiler does not know that there are matrix instructions in the assembly, whose results take up to 19 wait states)
         asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o[0][0]), "+a"(o[0][1]), "+a"(o[0][2]), "+a"(o[0][3]), "+a"(o[1][0]), "+a"(o[1][1]), "+a"(o[1][2]), "+a"(o[1][3]));
