@@ -36,7 +36,7 @@ struct AttnMx4Args {
     const int32_t *block_starts;
     int n_blocks, block, block_log2;
     float scale_log2e;
-    int n_splits, slots_per_split;
+    int n_splits;
     DecodeGrid grid;
     PagedView paged;
     float *part_ml, *part_acc;       // [P, n_splits, G, 2] (reference in log2 units, sum), [P, n_splits, G, 128]
@@ -62,8 +62,10 @@ __global__ __launch_bounds__(kMxThreads, kMxPerCu) void attn_decode_mx4_kernel(c
     const int n_sink_eff = min(a.ge.n_sink, pr.E), w0 = max(pr.hi, a.ge.n_sink);
     const int block_slots = a.n_blocks << a.block_log2;
     const int total = n_sink_eff + block_slots + max(0, pr.E - w0);
-    const int s0 = split * a.slots_per_split;
-    const int slots = min(a.slots_per_split, total - s0), steps = (slots + kMxStep - 1) / kMxStep;
+    // every problem's own slots in equal parts (the host's bound makes none longer than kMxMaxSplit)
+    const int per = min(kMxMaxSplit, max(kMxMinSplit, ((total + a.n_splits - 1) / a.n_splits + kMxMinSplit - 1) / kMxMinSplit * kMxMinSplit));
+    const int s0 = split * per;
+    const int slots = min(per, total - s0), steps = (slots + kMxStep - 1) / kMxStep;
     const int64_t pbase = ((int64_t)p * a.n_splits + split) * G;
 
     __shared__ __attribute__((aligned(16))) uint32_t sh_row[kMxMaxSplit];     // row of every slot
@@ -285,20 +287,23 @@ __global__ __launch_bounds__(kD * kMxMergeGroups) void attn_decode_mx4_merge_ker
     if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
 }
 
-// Splits of the slot list: what fills the compute units once, or the longest splits
-static int mx4_splits(const ihip_shape &s, int n_blocks, int block, int *slots_per_split)
+// Splits of a problem, which the kernel makes equally long: what fills the compute units once.  Where those would be longer than 1,024 slots,
+// twice: sequences of different lengths keep the units busier so, and beginning and ending a split costs as much as some 128 slots.  32
+// sequences of 7,383 to 16,384 keys, 8 problems each (us): 4 splits a problem 120, 6 (two rounds) 101, 9 103, 12 105, 15 109, 18 112; the
+// same for the longest length 16,384 in splits of 1,024 slots 108.
+static int mx4_splits(const ihip_shape &s, int n_blocks, int block)
 {
     const int64_t total = (int64_t)s.n_sink + (int64_t)n_blocks * block + s.n_stream, P = std::max(1, s.B * s.Hkv);
-    const int64_t want = std::max<int64_t>(1, (int64_t)compute_units() * kMxPerCu / P);
-    const int64_t per = ((total + want - 1) / want + kMxMinSplit - 1) / kMxMinSplit * kMxMinSplit;
-    *slots_per_split = (int)std::min<int64_t>(kMxMaxSplit, std::max<int64_t>(kMxMinSplit, per));
-    return (int)((total + *slots_per_split - 1) / *slots_per_split);
+    const int64_t places = (int64_t)compute_units() * kMxPerCu;
+    int64_t n = std::max<int64_t>(1, places / P);
+    if (total > n * 1024) n = std::max<int64_t>(1, 2 * places / P);
+    n = std::max(n, (total + kMxMaxSplit - 1) / kMxMaxSplit);
+    return (int)std::min(n, (total + kMxMinSplit - 1) / kMxMinSplit);
 }
 
 size_t attn_decode_mx4_workspace(const ihip_shape &s, int n_blocks, int block)
 {
-    int per;
-    return (size_t)s.B * s.Hq * mx4_splits(s, n_blocks, block, &per) * (2 + kD) * sizeof(float);
+    return (size_t)s.B * s.Hq * mx4_splits(s, n_blocks, block) * (2 + kD) * sizeof(float);
 }
 
 }  // namespace ihip
@@ -336,7 +341,7 @@ extern "C" int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_t
     a.block_starts = block_starts;
     a.n_blocks = n_blocks; a.block = block; a.block_log2 = __builtin_ctz(block);
     a.scale_log2e = sm_scale * 1.44269504088896340736f;
-    a.n_splits = mx4_splits(*shape, n_blocks, block, &a.slots_per_split);
+    a.n_splits = mx4_splits(*shape, n_blocks, block);
     a.grid = decode_grid(a.ge, a.n_splits, false);
     a.paged = w.paged;
     const int P = shape->B * shape->Hkv;
