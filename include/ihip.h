@@ -554,11 +554,16 @@ int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_tensor q, co
  *   out_lse    fp32 [rows, Hq] natural-log sum-exp of the scaled scores; may be NULL
  * QK^T and PV run on the matrix cores (bf16 operands, the probabilities rounded to
  * bf16, fp32 accumulation), softmax in fp32.  A query that sees no key (t < n)
- * gets 0, and -INFINITY.  A sequence of more than max_q tokens is not done to its end.
+ * gets 0, and -INFINITY.  A sequence of more than max_q tokens may be done in part only.
+ *   ws, ws_bytes device scratch of ihip_prompt_attn_workspace_bytes(packed, rows_k), 16-byte aligned; may be NULL.  A call with few
+ *                queries on many keys deals its work out to the whole chip in equal shares and merges the parts there;
+ *                with NULL, less or a misaligned pointer it does not (slower; equal up to rounding).  Calls that overlap
+ *                on a GPU need scratch of their own.
  */
+size_t  ihip_prompt_attn_workspace_bytes(const ihip_packed *packed, int32_t rows_k);
 int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v,
                          const int32_t *cu_k, int32_t rows_k, float sm_scale, void *out, float *out_lse,
-                         void *stream);
+                         void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Reads a cache back: rows 0 .. seq_lens[b]-1 (at most max_seq_len) of every sequence and KV head,

@@ -95,7 +95,8 @@ EXPORTS = {
     "ihip_prefill_layer": (c_i32, [ctypes.POINTER(Shape), Tensor, Tensor, Tensor, c_i32, vp, vp, c_f,
                                    vp, vp, vp, vp, c_sz, vp]),
     "ihip_sparse_attn_decode_mx4kv": (c_i32, [ctypes.POINTER(Shape), Tensor, vp, vp, c_i32, c_i32, c_f, vp, vp, vp, c_sz, vp]),
-    "ihip_prompt_attn": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, c_f, vp, vp, vp]),
+    "ihip_prompt_attn_workspace_bytes": (c_sz, [vp, c_i32]),
+    "ihip_prompt_attn": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, c_f, vp, vp, vp, c_sz, vp]),
     "ihip_kv_append": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, vp, vp, Tensor, Tensor, vp]),
     "ihip_kv_gather": (c_i32, [vp, c_i32, c_i32, c_i32, vp, c_i32, Tensor, Tensor, vp]),
     "ihip_cache_device_bytes": (c_sz, [c_i32, c_i32, c_i64, c_i32, c_i32, c_i32]),
@@ -881,10 +882,10 @@ def kv_gather(store: KVStore, seq_lens: torch.Tensor, max_seq_len: int, k_out: O
 
 def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, max_q: int,
                 cu_k: Optional[torch.Tensor] = None, sm_scale: Optional[float] = None, want_lse: bool = False,
-                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """ihip_prompt_attn: dense causal attention of packed sequences cu_q int32 [B+1] of at most max_q tokens, q [rows, Hq, d]
     over k, v [rows_k, Hkv, d] (bf16); cu_k: their own offsets, where sequences bring keys that precede their queries.
-    -> (out bf16 [rows, Hq, d], lse fp32 [rows, Hq] or None)."""
+    ws: device scratch, made if not given and of use (an empty tensor: none).  -> (out bf16 [rows, Hq, d], lse fp32 [rows, Hq] or None)."""
     rows, Hq, d = q.shape
     rows_k, Hkv, _ = k.shape
     B = cu_q.numel() - 1
@@ -899,9 +900,14 @@ def prompt_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     if lse is not None and (lse.shape != (rows, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous()):
         raise IhipError("lse: need a contiguous fp32 tensor [rows, Hq]")
     p = PackedStruct(B, Hq, Hkv, d, _lengths(cu_q, B + 1, "cu_q", q.device), rows, max_q)
+    if ws is None:
+        need = lib().ihip_prompt_attn_workspace_bytes(ctypes.byref(p), rows_k)
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 256 else None
+    elif ws.device != q.device:
+        raise IhipError(f"ws is on {ws.device}, not on {q.device}")
     _enqueue(q.device, lib().ihip_prompt_attn, ctypes.byref(p), _packed_tensor(q, "q"), _packed_tensor(k, "k"),
              _packed_tensor(v, "v", rows_k, Hkv), None if cu_k is None else _lengths(cu_k, B + 1, "cu_k", q.device), rows_k,
-             sm_scale, _ptr(out), _ptr(lse))
+             sm_scale, _ptr(out), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
     return out, lse
 
 

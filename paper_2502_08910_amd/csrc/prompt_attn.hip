@@ -27,7 +27,103 @@ struct PromptArgs {
     float scale_log2e;
     uint16_t *out;                   // [rows_q, Hq, d]
     float *lse;                      // [rows_q, Hq] or null
+    // launches whose work is dealt out in equal shares: partial results of parts of blocks, two a workgroup
+    float4 *part_o;                  // [part][wave][accumulators of a lane, four at a time: 32][lane]
+    float2 *part_ml;                 // [part][wave][64 queries]: reference of the exponentials (log2 units), sum
 };
+
+// ---- shares ------------------------------------------------------------------
+// Where there are too few blocks of 256 queries x heads to keep the compute units busy to the end, the tiles of all blocks are dealt out
+// to one workgroup a unit in equal shares, which begin and end inside blocks; a second kernel merges the parts of a block.  The
+// list goes head by head (the query heads of a KV head next to each other), sequence by sequence, block by block; a block weighs its
+// tiles and kBlockCost for its beginning and end.
+constexpr int kBlockCost = 4, kMinPart = 4, kMinShare = 12;      // tiles
+
+struct PromptSeq {
+    int q_first, nq, k_first, nk;
+    int ahead, blocks, ahead_tiles;
+    __device__ PromptSeq(const PromptArgs &a, int b)
+    {
+        q_first = min(max(a.cu_q[b], 0), a.rows_q);
+        nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
+        k_first = min(max(a.cu_k[b], 0), a.rows_k);
+        nk = min(max(a.cu_k[b + 1], k_first), a.rows_k) - k_first;
+        ahead = nk - nq;                             // query i sees keys 0 .. i + ahead
+        blocks = (nq + kPromptRows - 1) / kPromptRows;
+        ahead_tiles = (ahead + kTileKeys - 1) >> 5;  // rounded up, also below 0
+    }
+    __device__ int tiles(int m) const
+    {
+        return m + 1 < blocks ? max(0, kPromptRows / kTileKeys * (m + 1) + ahead_tiles) : (nk + kTileKeys - 1) / kTileKeys;
+    }
+    __device__ int64_t weight_before(int m) const    // of blocks 0 .. m - 1, m < blocks
+    {
+        const int none = min(m, ahead_tiles < 0 ? -ahead_tiles / 8 : 0);          // blocks whose queries see nothing
+        auto sum = [&](int64_t c) { return 4 * c * (c + 1) + ahead_tiles * c; };
+        return sum(m) - sum(none) + (int64_t)kBlockCost * m;
+    }
+    __device__ int64_t weight() const { return blocks == 0 ? 0 : weight_before(blocks - 1) + tiles(blocks - 1) + kBlockCost; }
+    // A part begins at a multiple of a tile, kMinPart or more from both ends of the block and not behind the tile that its first
+    // query sees the end of (so that every query has a key in a part's first tile); w: weight from the block's beginning.
+    // The block's number of tiles stands for its end.
+    __device__ int part_begin(int m, int64_t w) const
+    {
+        const int t = tiles(m), c = (int)min<int64_t>(max<int64_t>(w - kBlockCost, 0), t);
+        if (c < kMinPart) return 0;
+        if (c > t - kMinPart) return t;
+        const int last = min((m * kPromptRows + ahead) / kTileKeys, t - kMinPart);
+        return c <= last ? c : last < kMinPart ? t : last;
+    }
+};
+__device__ inline int64_t wave_sum_i64(int64_t v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
+    return v;
+}
+__device__ inline int64_t head_weight(const PromptArgs &a, int lane)
+{
+    int64_t w = 0;
+    for (int b = lane; b < a.B; b += 64) w += PromptSeq(a, b).weight();
+    return wave_sum_i64(w);
+}
+struct PromptPlace { int head, b, m, tile; int64_t begin; };        // head in list order; begin: weight in front of the block
+__device__ inline PromptPlace prompt_place(const PromptArgs &a, int64_t x, int64_t per_head, int lane)
+{
+    PromptPlace r{(int)(x / per_head), 0, 0, 0, 0};
+    int64_t y = x % per_head;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int64_t w = b0 + lane < a.B ? PromptSeq(a, b0 + lane).weight() : 0;
+        int64_t incl = w;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int64_t o = __shfl_up(incl, d, 64);
+            if (lane >= d) incl += o;
+        }
+        const unsigned long long past = __ballot(incl > y);
+        if (past != 0) {
+            const int at = __builtin_ctzll(past);
+            r.b = __builtin_amdgcn_readfirstlane(b0 + at);
+            y -= __shfl(incl - w, at, 64);
+            break;
+        }
+        y -= __shfl(incl, 63, 64);
+    }
+    const PromptSeq q(a, r.b);
+    int lo = 0, hi = q.blocks - 1;                   // the last block that begins at or before y
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (q.weight_before(mid) <= y) lo = mid;
+        else hi = mid - 1;
+    }
+    r.m = __builtin_amdgcn_readfirstlane(lo);
+    r.head = __builtin_amdgcn_readfirstlane(r.head);
+    r.tile = __builtin_amdgcn_readfirstlane(q.part_begin(r.m, y - q.weight_before(r.m)));
+    r.begin = x - (y - q.weight_before(r.m));
+    return r;
+}
+// Shares that the whole weight is cut into, at most n
+__device__ inline int prompt_shares(int64_t whole, int n) { return __builtin_amdgcn_readfirstlane((int)min<int64_t>(n, max<int64_t>(1, whole / kMinShare))); }
 
 // 16 bytes a lane from a scalar base and the lane's byte offset to the LDS byte address dst + 16 l (counts on vmcnt).  M0 is left as it is:
 // nothing else in this kernel reads it, and it is not the compiler's to keep values in.
@@ -36,51 +132,94 @@ __device__ inline void prompt_to_lds(uint32_t dst, const uint16_t *base, uint32_
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(byte_off), "s"(base) : "memory");
 }
 
+// SHARES: as above; otherwise a workgroup a block and head, the heads of a block next to each other, those with most keys first.
+template <bool SHARES>
 __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const PromptArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
 
-    // which head, which sequence, which of its blocks
-    const int hs = blockIdx.x % a.Hq, g = hs % a.Hkv, h = g * a.G + hs / a.Hkv;
-    int ti = blockIdx.x / a.Hq, b = -1, m = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        int blocks = 0;
-        if (b0 + lane < a.B) {
-            const int c0 = min(max(a.cu_q[b0 + lane], 0), a.rows_q), c1 = min(max(a.cu_q[b0 + lane + 1], c0), a.rows_q);
-            blocks = (c1 - c0 + kPromptRows - 1) / kPromptRows;
+    // which head, which sequence, which of its blocks, which tiles of the block
+    int head, b = -1, m = 0, tile0 = 0, tile1 = 0, share = 0;
+    PromptPlace end{};
+    if constexpr (SHARES) {
+        const int64_t per_head = head_weight(a, lane), whole = per_head * a.Hq;
+        const int shares = prompt_shares(whole, gridDim.x);
+        // workgroups are dealt to the eight XCDs in turn: each gets shares that follow each other, of one KV head if there are eight
+        share = shares % 8 == 0 && (int)gridDim.x == shares ? (blockIdx.x & 7) * (shares / 8) + (blockIdx.x >> 3) : blockIdx.x;
+        if (share >= shares || __builtin_amdgcn_readfirstlane((int)(whole == 0)) != 0) return;
+        const PromptPlace p = prompt_place(a, share * whole / shares, per_head, lane);
+        head = p.head; b = p.b; m = p.m; tile0 = p.tile;
+        if (share + 1 < shares) end = prompt_place(a, (share + 1) * whole / shares, per_head, lane);
+        else end.head = a.Hq;
+    } else {
+        head = blockIdx.x % a.Hq;
+        head = head % a.Hkv * a.G + head / a.Hkv;    // neighbours read different KV heads, on the XCD of their own if there are eight
+        int ti = blockIdx.x / a.Hq;
+        if (a.B <= 64) {
+            // blocks in the order of their keys, a block's worth of them at a time: key class c of a sequence's block m is base + m
+            const PromptSeq q(a, min(lane, a.B - 1));
+            const int blocks = lane < a.B ? q.blocks : 0, base = max(0, q.ahead) / kPromptRows;
+            auto at_least = [&](int c) { return (int)wave_sum_u32((uint32_t)min(max(base + blocks - c, 0), blocks)); };
+            if (ti >= at_least(0)) return;
+            int lo = 0, hi = (int)wave_reduce_bits((uint32_t)(base + blocks), [](uint32_t x, uint32_t y) { return max(x, y); });
+            while (hi - lo > 1) {                    // at_least(lo) > ti >= at_least(hi)
+                const int mid = lo + (hi - lo) / 2;
+                if (at_least(mid) > ti) lo = mid;
+                else hi = mid;
+            }
+            ti -= at_least(hi);
+            const unsigned long long those = __ballot(base <= lo && lo < base + blocks);
+            const int rank = __popcll(those & ((1ull << lane) - 1));
+            b = __builtin_ctzll(__ballot(((those >> lane) & 1) && rank == ti));
+            m = lo - __builtin_amdgcn_readlane(base, b);
+        } else {
+            for (int b0 = 0; b0 < a.B; b0 += 64) {
+                const int blocks = b0 + lane < a.B ? PromptSeq(a, b0 + lane).blocks : 0;
+                const int incl = (int)wave_scan_u32((uint32_t)blocks, lane);
+                const unsigned long long past = __ballot(incl > ti);
+                if (past != 0) {
+                    const int at = __builtin_ctzll(past);
+                    b = b0 + at;
+                    m = __builtin_amdgcn_readlane(incl, at) - 1 - ti;          // the longest blocks of a sequence come first
+                    break;
+                }
+                ti -= __builtin_amdgcn_readlane(incl, 63);
+            }
+            if (b < 0) return;
         }
-        const int incl = (int)wave_scan_u32((uint32_t)blocks, lane);
-        const unsigned long long past = __ballot(incl > ti);
-        if (past != 0) {
-            const int at = __builtin_ctzll(past);
-            b = b0 + at;
-            m = __builtin_amdgcn_readlane(incl, at) - 1 - ti;          // the longest blocks of a sequence come first
-            break;
-        }
-        ti -= __builtin_amdgcn_readlane(incl, 63);
     }
-    if (b < 0) return;
-    const int q_first = min(max(a.cu_q[b], 0), a.rows_q), nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
-    const int k_first = min(max(a.cu_k[b], 0), a.rows_k), nk = min(max(a.cu_k[b + 1], k_first), a.rows_k) - k_first;
+    for (;;) {                                       // SHARES: blocks and parts of blocks; otherwise once
+    // (the same in all lanes, which the compiler cannot see everywhere)
+    head = __builtin_amdgcn_readfirstlane(head);
+    b = __builtin_amdgcn_readfirstlane(b);
+    m = __builtin_amdgcn_readfirstlane(m);
+    tile0 = __builtin_amdgcn_readfirstlane(tile0);
+    const PromptSeq seq(a, b);
+    const int nq = seq.nq, nk = seq.nk, ahead = seq.ahead;
+    const int all_tiles = __builtin_amdgcn_readfirstlane(seq.tiles(m));
+    const bool is_end = SHARES && __builtin_amdgcn_readfirstlane((int)(head == end.head && b == end.b && m == end.m)) != 0;
+    tile1 = __builtin_amdgcn_readfirstlane(is_end ? end.tile : all_tiles);
+    if (!SHARES || tile0 < tile1 || (all_tiles == 0 && !is_end)) {
+    const int h = head, g = h / a.G;
     const int row0 = m * kPromptRows + wave * 64;    // this wave's first query
-    const int ahead = nk - nq;                       // query i sees keys 0 .. i + ahead
-    const int n_keys = min(m * kPromptRows + kPromptRows, nq) + ahead;
-    const int n_tiles = n_keys > 0 ? (n_keys + kTileKeys - 1) / kTileKeys : 0;
+    const int n_tiles = tile1 - tile0;               // of this part, numbered from its first
 
     bf16x8 qb[2][8];
     int last_key[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const int row = min(row0 + s * 32 + n, nq - 1);
-        last_key[s] = row + ahead;
-        const uint16_t *qp = a.q + (int64_t)(q_first + row) * a.q_st + h * a.q_sh + half * 8;
+        last_key[s] = row + ahead - tile0 * kTileKeys;
+        const uint16_t *qp = a.q + (int64_t)(seq.q_first + row) * a.q_st + h * a.q_sh + half * 8;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) qb[s][ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 16);
     }
-    const uint16_t *kb = a.k + (int64_t)k_first * a.k_st + g * a.k_sh;
-    const uint16_t *vb = a.v + (int64_t)k_first * a.v_st + g * a.v_sh;
+    const int first_last = row0 + ahead - tile0 * kTileKeys;       // the last key of the wave's first query
+    const int keys_here = nk - tile0 * kTileKeys;
+    const uint16_t *kb = a.k + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.k_st + g * a.k_sh;
+    const uint16_t *vb = a.v + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.v_st + g * a.v_sh;
 
     // Loads of a tile: 8 four-row instructions for K and 8 for V, two of each a wave: lane l brings 16 bytes of row 4 j + l / 16 to
     // base + 16 l.  The base of a tile is scalar; a lane's offset from it changes in a tile that reaches behind the last key only,
@@ -93,14 +232,14 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     const uint32_t k_off[2] = {offset(0, kTileKeys, a.k_st, false), offset(1, kTileKeys, a.k_st, false)};
     const uint32_t v_off[2] = {offset(0, kTileKeys, a.v_st, true), offset(1, kTileKeys, a.v_st, true)};
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem + wave * 4 * kD * 2;
-    const bool cut = n_tiles * kTileKeys > nk;       // the last tile reaches behind the last key
+    const bool cut = n_tiles * kTileKeys > keys_here;       // the last tile reaches behind the last key
     const uint16_t *k_next = kb, *v_next = vb;       // of the tiles to be requested next
     int k_tile = 0, v_tile = 0;
     auto request_k = [&](int st) {
         uint32_t off[2] = {k_off[0], k_off[1]};
         if (cut && k_tile == n_tiles - 1) {
-            off[0] = offset(0, nk - k_tile * kTileKeys, a.k_st, false);
-            off[1] = offset(1, nk - k_tile * kTileKeys, a.k_st, false);
+            off[0] = offset(0, keys_here - k_tile * kTileKeys, a.k_st, false);
+            off[1] = offset(1, keys_here - k_tile * kTileKeys, a.k_st, false);
         }
         prompt_to_lds(lds0 + st * kTileEl * 2, k_next, off[0]);
         prompt_to_lds(lds0 + st * kTileEl * 2 + 16 * kD * 2, k_next, off[1]);
@@ -111,8 +250,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     auto request_v = [&](int st) {
         uint32_t off[2] = {v_off[0], v_off[1]};
         if (cut && v_tile == n_tiles - 1) {
-            off[0] = offset(0, nk - v_tile * kTileKeys, a.v_st, true);
-            off[1] = offset(1, nk - v_tile * kTileKeys, a.v_st, true);
+            off[0] = offset(0, keys_here - v_tile * kTileKeys, a.v_st, true);
+            off[1] = offset(1, keys_here - v_tile * kTileKeys, a.v_st, true);
         }
         prompt_to_lds(lds0 + (kPromptStages + st) * kTileEl * 2, v_next, off[0]);
         prompt_to_lds(lds0 + (kPromptStages + st) * kTileEl * 2 + 16 * kD * 2, v_next, off[1]);
@@ -145,7 +284,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         for (int ks = 0; ks < 8; ++ks) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(st, ks), qb[s][ks], sc[s], 0, 0, 0);
     };
     auto mask = [&](int tile, int s) {
-        if (tile * kTileKeys + kTileKeys - 1 <= row0 + s * 32 + ahead) return;
+        if (tile * kTileKeys + kTileKeys - 1 <= first_last + s * 32) return;
         const int last = last_key[s] - 4 * half - tile * kTileKeys;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[s][r] = 8 * (r >> 2) + (r & 3) > last ? -INFINITY : sc[s][r];
@@ -212,7 +351,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
         __syncthreads();
     };
-    // Exponentials are taken against the row's maximum over the first tile (key 0 is in it, which every query with a key sees), not
+    // Exponentials are taken against the row's maximum over the first tile (which holds a key of every query that has any), not
     // against a running one: bf16 and fp32 have exponents to spare, nothing is lost while the scores stay within 2^64 of it.  Where a
     // row's sum says that they did not, the block is done again against the maxima over all tiles.
     for (int again = 0; n_tiles > 0 && again < 2; ++again) {
@@ -282,13 +421,26 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         l_run[1] += __shfl_xor(l_run[1], 32, 64);
         if (again || __syncthreads_or(!(l_run[0] <= kPromptMaxSum && l_run[1] <= kPromptMaxSum)) == 0) break;
     }
+    if (SHARES && n_tiles < all_tiles) {             // a part: its share's first (which does not begin the block) or last one
+        const int64_t unit = (int64_t)(2 * share + (tile0 == 0)) * kPromptWaves + wave;
+        float4 *to = a.part_o + unit * 32 * 64 + lane;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                for (int r4 = 0; r4 < 4; ++r4)
+                    to[(s * 16 + dt * 4 + r4) * 64] = make_float4(o[s][dt][r4 * 4], o[s][dt][r4 * 4 + 1], o[s][dt][r4 * 4 + 2], o[s][dt][r4 * 4 + 3]);
+            if (half == 0) a.part_ml[unit * 64 + s * 32 + n] = make_float2(m_ref[s], l_run[s]);
+        }
+    } else {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const float l = l_run[s];
         const int row = row0 + s * 32 + n;
         if (row >= nq) continue;
         const float inv = 1.0f / l;
-        const int64_t at = (int64_t)(q_first + row) * a.Hq + h;
+        const int64_t at = (int64_t)(seq.q_first + row) * a.Hq + h;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -298,14 +450,103 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
                              : make_uint2(pack_bf16x2(o[s][dt][r4 * 4] * inv, o[s][dt][r4 * 4 + 1] * inv), pack_bf16x2(o[s][dt][r4 * 4 + 2] * inv, o[s][dt][r4 * 4 + 3] * inv));
         if (a.lse != nullptr && half == 0) a.lse[at] = l == 0.f ? -INFINITY : (m_ref[s] + log2f(l)) * 0.69314718055994530942f;
     }
+    }
+    }
+    if (!SHARES || is_end) break;
+    tile0 = 0;
+    if (++m >= seq.blocks) {                         // on to the next block of the list
+        m = 0;
+        do {
+            if (++b == a.B) { b = 0; ++head; }
+        } while (head < a.Hq && PromptSeq(a, b).blocks == 0);
+    }
+    if (head >= a.Hq) break;
+    __syncthreads();                                 // the last tile's values have been read
+    }
 }
+
+// The parts of the block that boundary `blockIdx.x` + 1 of the shares is the first to cut; a wave's 64 queries a workgroup.
+// Wave w of it takes accumulators 8 w .. 8 w + 7 of each lane.
+__global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, int workgroups)
+{
+    const int lane = threadIdx.x & 63, quarter = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y;
+    const int64_t per_head = head_weight(a, lane), whole = per_head * a.Hq;
+    const int shares = prompt_shares(whole, workgroups), j = blockIdx.x + 1;
+    if (whole == 0 || j >= shares) return;
+    const PromptPlace p = prompt_place(a, j * whole / shares, per_head, lane);
+    const PromptSeq seq(a, p.b);
+    const int tiles = seq.tiles(p.m);
+    if (p.tile == 0 || p.tile == tiles) return;      // cuts nothing
+    auto tile_of = [&](int k) {                      // where share k begins in this block, its end if behind it
+        const int64_t w = k * whole / shares - p.begin;
+        return k >= shares || w >= (int64_t)tiles + kBlockCost ? tiles : seq.part_begin(p.m, w);
+    };
+    if ((j - 1) * whole / shares >= p.begin) {
+        const int before = tile_of(j - 1);
+        if (before > 0) return;                      // not the first
+    }
+    const int n = lane & 31, half = lane >> 5, s = quarter >> 1;
+    float M = kNegBigPrompt, L = 0.f;
+    float4 acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    int begin = 0;
+    for (int k = j - 1; begin < tiles; ++k) {
+        const int end = tile_of(k + 1);
+        if (begin < end) {
+            const int64_t unit = (int64_t)(2 * k + (begin == 0)) * kPromptWaves + wave;
+            const float2 ml = a.part_ml[unit * 64 + s * 32 + n];
+            const float4 *from = a.part_o + (unit * 32 + quarter * 8) * 64 + lane;
+            const float top = fmaxf(M, ml.x), old = __builtin_amdgcn_exp2f(M - top), w = __builtin_amdgcn_exp2f(ml.x - top);
+            M = top;
+            L = L * old + ml.y * w;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 x = from[i * 64];
+                acc[i] = make_float4(acc[i].x * old + x.x * w, acc[i].y * old + x.y * w, acc[i].z * old + x.z * w, acc[i].w * old + x.w * w);
+            }
+        }
+        begin = end;
+    }
+    const int row = p.m * kPromptRows + wave * 64 + s * 32 + n;
+    if (row >= seq.nq) return;
+    const float inv = 1.0f / L;
+    const int64_t at = (int64_t)(seq.q_first + row) * a.Hq + p.head;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int dt = (quarter & 1) * 2 + i / 4, r4 = i & 3;
+        *reinterpret_cast<uint2 *>(a.out + at * kD + dt * 32 + r4 * 8 + half * 4) =
+            L == 0.f ? make_uint2(0, 0) : make_uint2(pack_bf16x2(acc[i].x * inv, acc[i].y * inv), pack_bf16x2(acc[i].z * inv, acc[i].w * inv));
+    }
+    if (a.lse != nullptr && half == 0 && (quarter & 1) == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
+}
+
+// Blocks x heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each
+static int64_t prompt_blocks(const ihip_packed &p)
+{
+    const int64_t by_rows = (int64_t)p.rows / kPromptRows + p.B, by_len = (int64_t)p.B * ((p.max_q - 1) / kPromptRows + 1);
+    return (by_rows < by_len ? by_rows : by_len) * p.Hq;
+}
+// Whether a call is dealt out in shares: where its blocks are fewer than four a compute unit, if one of them may have 32 tiles or more
+static bool prompt_in_shares(const ihip_packed &p, int64_t keys)
+{
+    return p.max_q > 0 && p.rows > 0 && prompt_blocks(p) < 4 * (int64_t)compute_units() && keys >= 32 * kTileKeys;
+}
+static size_t prompt_part_bytes() { return (size_t)2 * compute_units() * kPromptWaves * 64 * (32 * sizeof(float4) + sizeof(float2)); }
 
 }  // namespace ihip
 
 using namespace ihip;
 
+extern "C" size_t ihip_prompt_attn_workspace_bytes(const ihip_packed *packed, int32_t rows_k)
+{
+    if (check_packed("ihip_prompt_attn_workspace_bytes", packed) != IHIP_OK) return 0;
+    return prompt_in_shares(*packed, rows_k) ? prompt_part_bytes() : 256;
+}
+
 extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v, const int32_t *cu_k,
-                                    int32_t rows_k, float sm_scale, void *out, float *out_lse, void *stream)
+                                    int32_t rows_k, float sm_scale, void *out, float *out_lse, void *ws, size_t ws_bytes,
+                                    void *stream)
 {
     const char *who = "ihip_prompt_attn";
     int32_t rc;
@@ -329,11 +570,25 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     a.scale_log2e = sm_scale * 1.44269504088896340736f;
     a.out = (uint16_t *)out;
     a.lse = out_lse;
-    // blocks of all sequences: at most a part of one in each beyond the whole ones, and no more than max_q gives each
-    const int64_t by_rows = (int64_t)packed->rows / kPromptRows + packed->B, by_len = (int64_t)packed->B * ((packed->max_q - 1) / kPromptRows + 1);
-    const int64_t groups = (by_rows < by_len ? by_rows : by_len) * packed->Hq;
+    const int64_t groups = prompt_blocks(*packed);
     if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
-    KernelTimer timer("prompt_attn", (hipStream_t)stream);
-    hipLaunchKernelGGL(prompt_attn_kernel, dim3((uint32_t)groups), dim3(64 * kPromptWaves), kPromptStages * 2 * kTileEl * 2, (hipStream_t)stream, a);
+    const hipStream_t st = (hipStream_t)stream;
+    const dim3 threads(64 * kPromptWaves);
+    constexpr int lds = kPromptStages * 2 * kTileEl * 2;
+    if (ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes() && prompt_in_shares(*packed, cu_k ? rows_k : packed->max_q)) {
+        const int n = compute_units();
+        a.part_o = (float4 *)ws;
+        a.part_ml = (float2 *)(a.part_o + (size_t)2 * n * kPromptWaves * 32 * 64);
+        {
+            KernelTimer timer("prompt_attn_shares", st);
+            hipLaunchKernelGGL(prompt_attn_kernel<true>, dim3(n), threads, lds, st, a);
+        }
+        if ((rc = check_launch(who)) != IHIP_OK) return rc;
+        KernelTimer timer("prompt_merge", st);
+        hipLaunchKernelGGL(prompt_merge_kernel, dim3(n, kPromptWaves), dim3(256), 0, st, a, n);
+        return check_launch(who);
+    }
+    KernelTimer timer("prompt_attn", st);
+    hipLaunchKernelGGL(prompt_attn_kernel<false>, dim3((uint32_t)groups), threads, lds, st, a);
     return check_launch(who);
 }

@@ -20,7 +20,7 @@ def test_prompt_attention_refuses(b):
     ok = t(4096, 0, 128, 1024)
 
     def call(packed=P(2, 8, 2, 128, 4096, 10, 10), q=ok, k=ok, v=ok, cu_k=4096, rows_k=20, out=4096):
-        return L.ihip_prompt_attn(ctypes.byref(packed) if packed else None, q, k, v, cu_k, rows_k, 0.1, out, None, None)
+        return L.ihip_prompt_attn(ctypes.byref(packed) if packed else None, q, k, v, cu_k, rows_k, 0.1, out, None, None, 0, None)
 
     assert call(packed=None) == -1
     assert call(packed=P(2, 8, 3, 128, 4096, 10, 10)) == -1
