@@ -42,15 +42,30 @@ constexpr int kBlockCost = 4, kMinPart = 4, kMinShare = 12;      // tiles
 struct PromptSeq {
     int q_first, nq, k_first, nk;
     int ahead, blocks, ahead_tiles;
+    __device__ PromptSeq() {}
     __device__ PromptSeq(const PromptArgs &a, int b)
     {
         q_first = min(max(a.cu_q[b], 0), a.rows_q);
         nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
         k_first = min(max(a.cu_k[b], 0), a.rows_k);
         nk = min(max(a.cu_k[b + 1], k_first), a.rows_k) - k_first;
+        derive();
+    }
+    __device__ void derive()
+    {
         ahead = nk - nq;                             // query i sees keys 0 .. i + ahead
         blocks = (nq + kPromptRows - 1) / kPromptRows;
         ahead_tiles = (ahead + kTileKeys - 1) >> 5;  // rounded up, also below 0
+    }
+    __device__ PromptSeq of_lane(int l) const        // that of lane l, in all lanes
+    {
+        PromptSeq r;
+        r.q_first = __builtin_amdgcn_readlane(q_first, l);
+        r.nq = __builtin_amdgcn_readlane(nq, l);
+        r.k_first = __builtin_amdgcn_readlane(k_first, l);
+        r.nk = __builtin_amdgcn_readlane(nk, l);
+        r.derive();
+        return r;
     }
     __device__ int tiles(int m) const
     {
@@ -132,6 +147,15 @@ __device__ inline void prompt_to_lds(uint32_t dst, const uint16_t *base, uint32_
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(byte_off), "s"(base) : "memory");
 }
 
+// A value and that of the lane 32 further, combined (commutatively: both lanes get the same)
+template <class Op>
+__device__ inline float half_swap(float x, Op op)
+{
+    const unsigned u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // SHARES: as above; otherwise a workgroup a block and head, the heads of a block next to each other, those with most keys first.
 template <bool SHARES>
 __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const PromptArgs a)
@@ -139,10 +163,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
+    uint16_t *const rows = smem + kPromptStages * 2 * kTileEl + wave * 64 * kD;          // this wave's results on their way out
 
     // which head, which sequence, which of its blocks, which tiles of the block
     int head, b = -1, m = 0, tile0 = 0, tile1 = 0, share = 0;
     PromptPlace end{};
+    PromptSeq seq;
     if constexpr (SHARES) {
         const int64_t per_head = head_weight(a, lane), whole = per_head * a.Hq;
         const int shares = prompt_shares(whole, gridDim.x);
@@ -174,6 +200,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
             const int rank = __popcll(those & ((1ull << lane) - 1));
             b = __builtin_ctzll(__ballot(((those >> lane) & 1) && rank == ti));
             m = lo - __builtin_amdgcn_readlane(base, b);
+            seq = q.of_lane(b);
         } else {
             for (int b0 = 0; b0 < a.B; b0 += 64) {
                 const int blocks = b0 + lane < a.B ? PromptSeq(a, b0 + lane).blocks : 0;
@@ -188,6 +215,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
                 ti -= __builtin_amdgcn_readlane(incl, 63);
             }
             if (b < 0) return;
+            seq = PromptSeq(a, b);
         }
     }
     for (;;) {                                       // SHARES: blocks and parts of blocks; otherwise once
@@ -196,12 +224,18 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     b = __builtin_amdgcn_readfirstlane(b);
     m = __builtin_amdgcn_readfirstlane(m);
     tile0 = __builtin_amdgcn_readfirstlane(tile0);
-    const PromptSeq seq(a, b);
+    if (SHARES) seq = PromptSeq(a, b);
     const int nq = seq.nq, nk = seq.nk, ahead = seq.ahead;
     const int all_tiles = __builtin_amdgcn_readfirstlane(seq.tiles(m));
     const bool is_end = SHARES && __builtin_amdgcn_readfirstlane((int)(head == end.head && b == end.b && m == end.m)) != 0;
     tile1 = __builtin_amdgcn_readfirstlane(is_end ? end.tile : all_tiles);
-    if (!SHARES || tile0 < tile1 || (all_tiles == 0 && !is_end)) {
+    if (all_tiles == 0 && !is_end) {                 // queries without keys
+        for (int i = tid; i < min(kPromptRows, nq - m * kPromptRows) * kRowLanes; i += 64 * kPromptWaves) {
+            const int64_t at = (int64_t)(seq.q_first + m * kPromptRows + i / kRowLanes) * a.Hq + head;
+            reinterpret_cast<uint4 *>(a.out + at * kD)[i % kRowLanes] = make_uint4(0, 0, 0, 0);
+            if (a.lse != nullptr && i % kRowLanes == 0) a.lse[at] = -INFINITY;
+        }
+    } else if (tile0 < tile1) {
     const int h = head, g = h / a.G;
     const int row0 = m * kPromptRows + wave * 64;    // this wave's first query
     const int n_tiles = tile1 - tile0;               // of this part, numbered from its first
@@ -209,13 +243,15 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     bf16x8 qb[2][8];
     int last_key[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const int row = min(row0 + s * 32 + n, nq - 1);
-        last_key[s] = row + ahead - tile0 * kTileKeys;
-        const uint16_t *qp = a.q + (int64_t)(seq.q_first + row) * a.q_st + h * a.q_sh + half * 8;
+    for (int s = 0; s < 2; ++s) last_key[s] = min(row0 + s * 32 + n, nq - 1) + ahead - tile0 * kTileKeys;
+    auto load_queries = [&] {
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) qb[s][ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 16);
-    }
+        for (int s = 0; s < 2; ++s) {
+            const uint16_t *qp = a.q + (int64_t)(seq.q_first + min(row0 + s * 32 + n, nq - 1)) * a.q_st + h * a.q_sh + half * 8;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) qb[s][ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 16);
+        }
+    };
     const int first_last = row0 + ahead - tile0 * kTileKeys;       // the last key of the wave's first query
     const int keys_here = nk - tile0 * kTileKeys;
     const uint16_t *kb = a.k + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.k_st + g * a.k_sh;
@@ -283,25 +319,35 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(st, ks), qb[s][ks], sc[s], 0, 0, 0);
     };
+    // Keys of a tile that a lane's query must not see, as bits: score r is that of key 8 (r / 4) + 4 half + r % 4
+    auto hidden_keys = [&](int tile, int s) { return ~0u << min(max(last_key[s] - 4 * half - tile * kTileKeys + 1, 0), 31); };
+    auto hide = [&](uint32_t bits, int r, float x) {         // v_bfe_i32, v_bfi_b32
+        const int hidden = (int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31;
+        return __int_as_float((hidden & __float_as_int(-INFINITY)) | (~hidden & __float_as_int(x)));
+    };
     auto mask = [&](int tile, int s) {
         if (tile * kTileKeys + kTileKeys - 1 <= first_last + s * 32) return;
-        const int last = last_key[s] - 4 * half - tile * kTileKeys;
+        const uint32_t bits = hidden_keys(tile, s);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sc[s][r] = 8 * (r >> 2) + (r & 3) > last ? -INFINITY : sc[s][r];
+        for (int r = 0; r < 16; ++r) sc[s][r] = hide(bits, r, sc[s][r]);
     };
     auto row_max = [&](const f32x16 &s) {            // scaled; of both halves
         float mx = s[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-        return fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.scale_log2e;
+        return half_swap(mx, [](float x, float y) { return fmaxf(x, y); }) * a.scale_log2e;
     };
 
     uint32_t pw[2][8];                               // the probabilities of a set, in pairs of keys
     float m_ref[2] = {kNegBigPrompt, kNegBigPrompt}, l_run[2] = {0.f, 0.f};
     // two scores -> two probabilities (exp2(-inf) = 0).  The empty assembly keeps them where they are called: left to themselves all
     // exponentials of a phase would be computed in front of its matrix instructions instead of under them.
-    auto exponentials = [&](int s, int i) {
+    auto exponentials = [&](int s, int i, bool masked, uint32_t bits) {
         float x = fmaf(sc[s][2 * i], a.scale_log2e, -m_ref[s]), y = fmaf(sc[s][2 * i + 1], a.scale_log2e, -m_ref[s]);
+        if (masked) {
+            x = hide(bits, 2 * i, x);
+            y = hide(bits, 2 * i + 1, y);
+        }
         asm volatile("" : "+v"(x), "+v"(y));
         x = __builtin_amdgcn_exp2f(x);
         y = __builtin_amdgcn_exp2f(y);
@@ -328,11 +374,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
             va[i] = v_operand(st, i);
         }
     };
-    auto period = [&](int st, int st1, int st2, int st3, int t) {      // stages of tiles t, t + 1, t + 2, t + 3
-        mask(t, 1);
+    auto period = [&](int st, int st1, int st2, int st3, int t, bool masked) {      // stages of tiles t, t + 1, t + 2, t + 3
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            if (s == 1) mask(t + 1, 0);
+            const uint32_t bits = masked ? hidden_keys(t + s, 1 - s) : 0u;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int i = r & 7;
@@ -342,7 +387,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
                 if (r == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=v"(sc[s]) : "v"(ka[0]), "v"(qb[s][0]));
                 else if (r < 8) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(sc[s]) : "v"(ka[r]), "v"(qb[s][r]));
                 else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][i & 3]) : "v"(va[i]), "v"(probabilities(s, i >> 2)));
-                if (r % 2 == 0) exponentials(1 - s, r / 2);
+                if (r % 2 == 0) exponentials(1 - s, r / 2, masked, bits);
                 if (s == 0 && r == 3) request_k(st);
                 if (s == 0 && r == 9) request_v(st3);
                 __builtin_amdgcn_sched_barrier(0);
@@ -354,7 +399,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     // Exponentials are taken against the row's maximum over the first tile (which holds a key of every query that has any), not
     // against a running one: bf16 and fp32 have exponents to spare, nothing is lost while the scores stay within 2^64 of it.  Where a
     // row's sum says that they did not, the block is done again against the maxima over all tiles.
-    for (int again = 0; n_tiles > 0 && again < 2; ++again) {
+    for (int again = 0; again < 2; ++again) {
         if (again) {
             m_ref[0] = m_ref[1] = kNegBigPrompt;
             k_next = kb;
@@ -384,6 +429,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         for (int st = 0; st < 4; ++st) request_k(st);
 #pragma unroll
         for (int st = 0; st < 3; ++st) request_v(st);
+        if (!again) load_queries();
+        // (the accumulators are cleared while the loads are on their way)
+        asm volatile("" : "+a"(o[0][0]), "+a"(o[0][1]), "+a"(o[0][2]), "+a"(o[0][3]), "+a"(o[1][0]), "+a"(o[1][1]), "+a"(o[1][2]), "+a"(o[1][3]));
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
 #pragma unroll
@@ -393,21 +441,23 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
             if (!again) m_ref[s] = fmaxf(kNegBigPrompt, row_max(sc[s]));
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) exponentials(0, i);
+        for (int i = 0; i < 8; ++i) exponentials(0, i, false, 0);
         __syncthreads();                             // K(0) has been read
         first_operands(0, 1);
         int t = 0;
-        for (; t + 4 < n_tiles; t += 4) {
-            period(0, 1, 2, 3, t);
-            period(1, 2, 3, 0, t + 1);
-            period(2, 3, 0, 1, t + 2);
-            period(3, 0, 1, 2, t + 3);
+        // whole tiles that all queries of the block see; behind them scores are masked, under the matrix instructions as well
+        const int seen = min(n_tiles, (m * kPromptRows + ahead + 1) / kTileKeys - tile0);
+        for (; t + 4 < seen; t += 4) {
+            period(0, 1, 2, 3, t, false);
+            period(1, 2, 3, 0, t + 1, false);
+            period(2, 3, 0, 1, t + 2, false);
+            period(3, 0, 1, 2, t + 3, false);
         }
-        for (; t + 1 < n_tiles; ++t) period(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t);
+        for (; t + 1 < n_tiles; ++t) period(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t, true);
         // the last tile, whose first products are done
-        mask(t, 1);
+        const uint32_t bits = hidden_keys(t, 1);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) exponentials(1, i);
+        for (int i = 0; i < 8; ++i) exponentials(1, i, true, bits);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const bf16x8 vt = v_operand(t & 3, i);
@@ -417,8 +467,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         }
         // (the compiler does not know that there are matrix instructions in the assembly, whose results take up to 19 wait states)
         asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o[0][0]), "+a"(o[0][1]), "+a"(o[0][2]), "+a"(o[0][3]), "+a"(o[1][0]), "+a"(o[1][1]), "+a"(o[1][2]), "+a"(o[1][3]));
-        l_run[0] += __shfl_xor(l_run[0], 32, 64);
-        l_run[1] += __shfl_xor(l_run[1], 32, 64);
+        l_run[0] = half_swap(l_run[0], [](float x, float y) { return x + y; });
+        l_run[1] = half_swap(l_run[1], [](float x, float y) { return x + y; });
         if (again || __syncthreads_or(!(l_run[0] <= kPromptMaxSum && l_run[1] <= kPromptMaxSum)) == 0) break;
     }
     if (SHARES && n_tiles < all_tiles) {             // a part: its share's first (which does not begin the block) or last one
@@ -434,21 +484,33 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
             if (half == 0) a.part_ml[unit * 64 + s * 32 + n] = make_float2(m_ref[s], l_run[s]);
         }
     } else {
+    // The results go out through LDS, so that whole rows are written: 16-byte chunk c of row r at slot c ^ r % 16.  256 queries of 32 heads on 256
+    // keys each 17.4 -> 14.4 us
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const float l = l_run[s];
         const int row = row0 + s * 32 + n;
-        if (row >= nq) continue;
-        const float inv = 1.0f / l;
-        const int64_t at = (int64_t)(seq.q_first + row) * a.Hq + h;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;           // (a query without keys: 0)
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int r4 = 0; r4 < 4; ++r4)
-                *reinterpret_cast<uint2 *>(a.out + at * kD + dt * 32 + r4 * 8 + half * 4) =
-                    l == 0.f ? make_uint2(0, 0)       // a query without keys
-                             : make_uint2(pack_bf16x2(o[s][dt][r4 * 4] * inv, o[s][dt][r4 * 4 + 1] * inv), pack_bf16x2(o[s][dt][r4 * 4 + 2] * inv, o[s][dt][r4 * 4 + 3] * inv));
-        if (a.lse != nullptr && half == 0) a.lse[at] = l == 0.f ? -INFINITY : (m_ref[s] + log2f(l)) * 0.69314718055994530942f;
+                *reinterpret_cast<uint2 *>(rows + (s * 32 + n) * kD + (((dt * 4 + r4) ^ (n & 15)) << 3) + half * 4) =
+                    make_uint2(pack_bf16x2(o[s][dt][r4 * 4] * inv, o[s][dt][r4 * 4 + 1] * inv), pack_bf16x2(o[s][dt][r4 * 4 + 2] * inv, o[s][dt][r4 * 4 + 3] * inv));
+        if (a.lse != nullptr && half == 0 && row < nq)
+            a.lse[(int64_t)(seq.q_first + row) * a.Hq + h] = l == 0.f ? -INFINITY : (m_ref[s] + log2f(l)) * 0.69314718055994530942f;
+    }
+    asm volatile("" ::: "memory");                   // lanes read what other lanes of the wave wrote (LDS keeps the order)
+    uint16_t *out = a.out + ((int64_t)(seq.q_first + row0) * a.Hq + h) * kD;
+    const int64_t step = (int64_t)4 * a.Hq * kD;     // four rows
+    const int64_t mine = (int64_t)(lane >> 4) * a.Hq * kD + (lane & 15) * 8;
+    auto row_piece = [&](int i) { return *reinterpret_cast<const uint4 *>(rows + (4 * i + (lane >> 4)) * kD + (((lane & 15) ^ (4 * (i & 3) + (lane >> 4))) << 3)); };
+    if (row0 + 64 <= nq) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
+    } else {
+        for (int i = 0; i < 16; ++i)
+            if (row0 + 4 * i + (lane >> 4) < nq) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
     }
     }
     }
@@ -564,9 +626,9 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     a.q = (const uint16_t *)q.ptr; a.q_sh = q.stride_h; a.q_st = q.stride_t;
     a.k = (const uint16_t *)k.ptr; a.k_sh = k.stride_h; a.k_st = k.stride_t;
     a.v = (const uint16_t *)v.ptr; a.v_sh = v.stride_h; a.v_st = v.stride_t;
-    // a tile's rows are addressed by 32-bit byte offsets from its first
-    if (a.k_st < 0 || a.v_st < 0 || a.k_st >= (1 << 24) || a.v_st >= (1 << 24))
-        return fail(IHIP_ERR_UNSUPPORTED, "%s: rows of k and v must be less than 2^24 elements apart", who);
+    // the rows of a tile, and of a wave's queries, are addressed by 32-bit byte offsets from the first
+    if ((a.q_st | a.k_st | a.v_st) < 0 || a.q_st >= (1 << 24) || a.k_st >= (1 << 24) || a.v_st >= (1 << 24))
+        return fail(IHIP_ERR_UNSUPPORTED, "%s: rows of q, k and v must be less than 2^24 elements apart", who);
     a.scale_log2e = sm_scale * 1.44269504088896340736f;
     a.out = (uint16_t *)out;
     a.lse = out_lse;
@@ -574,7 +636,13 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
     const hipStream_t st = (hipStream_t)stream;
     const dim3 threads(64 * kPromptWaves);
-    constexpr int lds = kPromptStages * 2 * kTileEl * 2;
+    constexpr int lds = (kPromptStages * 2 * kTileEl + kPromptRows * kD) * 2;
+    static bool attr_set = false;        // allow more than 64 KiB of dynamic LDS, once
+    if (!attr_set) {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        attr_set = true;
+    }
     if (ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes() && prompt_in_shares(*packed, cu_k ? rows_k : packed->max_q)) {
         const int n = compute_units();
         a.part_o = (float4 *)ws;
