@@ -1,6 +1,8 @@
 // Dense causal attention of packed prompts on v_mfma_f32_32x32x16_bf16.
 #include "api_checks.h"
 #include "kv_store.h"
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace ihip {
@@ -589,10 +591,20 @@ static int64_t prompt_blocks(const ihip_packed &p)
     const int64_t by_rows = (int64_t)p.rows / kPromptRows + p.B, by_len = (int64_t)p.B * ((p.max_q - 1) / kPromptRows + 1);
     return (by_rows < by_len ? by_rows : by_len) * p.Hq;
 }
-// Whether a call is dealt out in shares: where its blocks are fewer than four a compute unit, if one of them may have 32 tiles or more
+// Whether a call is dealt out in shares, from what the host knows of it: total tokens, keys and sequences.  Without shares a launch takes
+// as long as its longest block, or as the rounds of blocks that the compute units do (blocks of the same length in whole rounds; a
+// whole prompt's blocks, of all lengths up to the longest, fill the rounds).  Equal shares take the mean, and kShareCost tiles for their
+// beginnings and ends and for the merge.  Without / with shares (us): 512 queries on 4,608 keys, 32 heads 109 / 73; 2,048 on as many 60 / 78, 4
+// times 1,500 105 / 116; 16 heads, 4,096 103 / 111; 8 heads, 8,192 189 / 170; 16 heads, 1,500 on 13,500 and 700 on 20,711 433 / 273; 32 heads, 8,192 484 / 546.
+constexpr double kShareCost = 65;
 static bool prompt_in_shares(const ihip_packed &p, int64_t keys)
 {
-    return p.max_q > 0 && p.rows > 0 && prompt_blocks(p) < 4 * (int64_t)compute_units() && keys >= 32 * kTileKeys;
+    if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return false;
+    const double cu = compute_units(), before = std::max<double>(0, (double)(keys - p.rows)) / p.B, mean = (double)p.rows / p.B;
+    const double longest = (before + p.max_q) / kTileKeys, tiles = (before + mean / 2) / kTileKeys;
+    const double rounds = std::min<double>((double)prompt_blocks(p), ((double)p.rows / kPromptRows + 0.5 * p.B) * p.Hq) / cu;
+    const double alike = before / (before + mean / 2);
+    return std::max(longest, tiles * (rounds + alike * (std::ceil(rounds) - rounds))) > tiles * rounds + kShareCost;
 }
 static size_t prompt_part_bytes() { return (size_t)2 * compute_units() * kPromptWaves * 64 * (32 * sizeof(float4) + sizeof(float2)); }
 
@@ -643,7 +655,7 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
         (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         attr_set = true;
     }
-    if (ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes() && prompt_in_shares(*packed, cu_k ? rows_k : packed->max_q)) {
+    if (ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes() && prompt_in_shares(*packed, rows_k)) {
         const int n = compute_units();
         a.part_o = (float4 *)ws;
         a.part_ml = (float2 *)(a.part_o + (size_t)2 * n * kPromptWaves * 32 * 64);

@@ -26,23 +26,25 @@ def workspace_bytes(ihip, q, k, cu, max_q):
     return ihip.lib().ihip_prompt_attn_workspace_bytes(ctypes.byref(p), k.shape[0])
 
 
-@pytest.mark.parametrize("Hq,Hkv,new,ctx", [
-    (8, 8, [1], [5000]),
-    (8, 2, [300, 1, 0, 64], [9000, 3, 0, 1200]),
-    (16, 2, [700], [20011]),
-    (3, 1, [257, 255], [4096, 31]),
-    (4, 2, [2500], [0]),
-    (1, 1, [1000, 300, 900], [-700, 4000, -900]),        # blocks whose queries see nothing
-    (2, 1, [17] * 70, [(i * 37) % 300 for i in range(70)]),
-    (1, 1, [40000], [0]),
+@pytest.mark.parametrize("Hq,Hkv,new,ctx,shares", [
+    (8, 8, [1], [5000], True),
+    (8, 2, [300, 1, 0, 64], [9000, 3, 0, 1200], True),
+    (16, 2, [700], [20011], True),
+    (3, 1, [257, 255], [4096, 31], True),
+    (4, 2, [2500], [0], True),
+    (1, 1, [1000, 300, 900], [-700, 4000, -900], False),
+    (1, 1, [1000, 300, 900], [-700, 40000, -900], True),      # blocks whose queries see nothing
+    (2, 1, [17] * 70, [(i * 37) % 300 for i in range(70)], False),
+    (2, 1, [17] * 70, [(i * 373) % 17000 for i in range(70)], True),
+    (1, 1, [40000], [0], True),
 ])
-def test_shares(ihip, Hq, Hkv, new, ctx):
+def test_shares(ihip, Hq, Hkv, new, ctx, shares):
     total = [a + b for a, b in zip(new, ctx)]
     N, K = sum(new), sum(total)
     q, k, v = (torch.full((r + 9, h, D), float("nan"), dtype=torch.bfloat16, device="cuda") for r, h in ((N, Hq), (K, Hkv), (K, Hkv)))
     q[:N], k[:K], v[:K] = normal(1, N, Hq, D, scale=2.0), normal(2, K, Hkv, D), normal(3, K, Hkv, D)
     cu, cu_k = offsets(new), offsets(total)
-    assert workspace_bytes(ihip, q, k, cu, max(new)) > 256
+    assert (workspace_bytes(ihip, q, k, cu, max(new)) > 256) == shares
     out = torch.full(q.shape, 5.0, dtype=torch.bfloat16, device="cuda")
     lse = torch.full(q.shape[:2], 5.0, device="cuda")
     ihip.prompt_attn(q, k, v, cu, max(new), cu_k=cu_k, out=out, lse=lse)
