@@ -10,6 +10,19 @@ namespace ihip {
 constexpr int kStoreThreads = 256;
 constexpr int kStoreGroups = kStoreThreads / kRowLanes;      // rows that a workgroup has in hand at a time
 
+// bf16 rows that are more than the L2 caches keep go past them (non-temporal stores): 128K tokens of 8 heads widened from 4 bits 139 -> 135 us
+// (5.0 TB/s; 142 -> 102 us where the rows are in the memory-side cache), 32K tokens of 32/8 heads appended to 4 bits and read back
+// 197 -> 186 us, 7,937 tokens into bf16 pages 39.2 -> 37.1 us.  The narrow rows of the caches go through them
+// (so do smaller results, which are read next).
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ inline void store_row16(void *row, int l16, const uint4 &w, bool past)
+{
+    const u32x4_t x = {w.x, w.y, w.z, w.w};
+    if (past) __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(row) + l16);
+    else reinterpret_cast<u32x4_t *>(row)[l16] = x;
+}
+constexpr int64_t kPastBytes = 16 << 20;             // half of the eight L2 caches
+
 struct AppendArgs {
     int B, Hq, Hkv, rows, max_len;
     const int32_t *cu, *lens;
@@ -20,14 +33,15 @@ struct AppendArgs {
     uint16_t *qo, *ko;               // may be null
     int64_t qo_sh, qo_st, ko_sh, ko_st;
     int first, per_wg;               // first head slot (Hq without queries) and head slots of a workgroup
+    bool past;
 };
 
-__device__ inline void append_row(uint8_t *row, uint8_t *scales, const uint4 &raw, const float (&f)[8], bool turned, int l16, int format, float scale)
+__device__ inline void append_row(uint8_t *row, uint8_t *scales, const uint4 &raw, const float (&f)[8], bool turned, int l16, int format, float scale, bool past)
 {
     if (format == IHIP_KV_BF16) {
         uint4 w = raw;
         if (turned) w = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-        reinterpret_cast<uint4 *>(row)[l16] = w;
+        store_row16(row, l16, w, past);
     } else if (format == IHIP_KV_E4M3) {
         reinterpret_cast<uint2 *>(row)[l16] = e4m3_quantise(f, scale);
     } else {
@@ -104,15 +118,15 @@ __global__ __launch_bounds__(kStoreThreads) void kv_append_kernel(const AppendAr
                     out += is_q ? slot * a.qo_sh + tok * a.qo_st : (slot - a.Hq) * a.ko_sh + tok * a.ko_st;
                     uint4 w = raw[u];
                     if constexpr (ROPE) w = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-                    reinterpret_cast<uint4 *>(out)[l16] = w;
+                    store_row16(out, l16, w, a.past);
                 }
                 if (!is_q && kept) {
                     const int64_t o = k_row + (slot - a.Hq) * a.to.k_sh;
-                    append_row(a.to.k + o, a.to.ks + o / 16, raw[u], f, ROPE, l16, FORMAT, a.to.k_scale);
+                    append_row(a.to.k + o, a.to.ks + o / 16, raw[u], f, ROPE, l16, FORMAT, a.to.k_scale, a.past);
                 }
             } else if (kept) {
                 const int64_t o = v_row + (slot - a.Hq - a.Hkv) * a.to.v_sh;
-                append_row(a.to.v + o, a.to.vs + o / 16, raw[u], f, false, l16, FORMAT, a.to.v_scale);
+                append_row(a.to.v + o, a.to.vs + o / 16, raw[u], f, false, l16, FORMAT, a.to.v_scale, a.past);
             }
         }
     }
@@ -120,16 +134,18 @@ __global__ __launch_bounds__(kStoreThreads) void kv_append_kernel(const AppendAr
 
 struct GatherArgs {
     int BH, Hkv, max_len;
+    bool past;
     const int32_t *lens;
     StoreView from;
     uint16_t *k, *v;                 // may be null
     int64_t k_sb, k_sh, k_st, v_sb, v_sh, v_st;
 };
 
+constexpr int kGatherRows = 2;       // rows of K, and as many of V, that a lane asks for at once (4-bit rows: 2 97 us, 4 103, 8 103)
 template <int FORMAT>
 __global__ __launch_bounds__(kStoreThreads) void kv_gather_kernel(const GatherArgs a)
 {
-    constexpr int kRows = 4;         // rows of K, and as many of V, that a lane asks for at once
+    constexpr int kRows = kGatherRows;
     using word = typename std::conditional<FORMAT == IHIP_KV_BF16, uint4, typename std::conditional<FORMAT == IHIP_KV_E4M3, uint2, uint32_t>::type>::type;
     const int l16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
     const int bh = blockIdx.x % a.BH, b = bh / a.Hkv, g = bh % a.Hkv;
@@ -183,7 +199,7 @@ __global__ __launch_bounds__(kStoreThreads) void kv_gather_kernel(const GatherAr
                 w = mx4_to_bf16x8(x[kv][u], mx4_scale(s[kv][u]));
                 if (s[kv][u] == 255u) w = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
             }
-            reinterpret_cast<uint4 *>(to + (int64_t)(t0 + u * kStoreGroups + grp) * st)[l16] = w;
+            store_row16(to + (int64_t)(t0 + u * kStoreGroups + grp) * st, l16, w, a.past);
         }
     }
 }
@@ -292,7 +308,11 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
     a.sin = rope ? rope->sin : nullptr;
     a.first = with_q ? 0 : a.Hq;
     const int slots = a.Hq + 2 * a.Hkv - a.first, groups = (a.rows - 1) / kStoreGroups + 1;
+    // Longer runs of heads use a token's place and angles longer, as long as there are workgroups enough (32K tokens, 48 heads, 4 to a
+    // workgroup / 16: 186 / 169 us; a decode step is slower with 16)
     a.per_wg = 4;
+    while (a.per_wg < 16 && (int64_t)groups * slots / (2 * a.per_wg) >= 8 * (int64_t)compute_units()) a.per_wg *= 2;
+    a.past = (int64_t)a.rows * (slots - 2 * a.Hkv + (k_out.ptr ? a.Hkv : 0) + (store->format == IHIP_KV_BF16 ? 2 * a.Hkv : 0)) * kD * 2 > kPastBytes;
     const dim3 grid(groups, (slots + a.per_wg - 1) / a.per_wg);
     if (grid.y > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: %d heads are too many", who, slots);
     KernelTimer timer("kv_append", (hipStream_t)stream);
@@ -323,8 +343,9 @@ int32_t ihip_kv_gather(const ihip_kv_store *store, int32_t B, int32_t Hkv, int32
     lengths.max_seq_len = max_seq_len;
     if ((rc = check_store(who, store, lengths, &a.from)) != IHIP_OK) return rc;
     if (!k_out.ptr && !v_out.ptr) return IHIP_OK;
-    const int64_t groups = (int64_t)B * Hkv * ((max_seq_len - 1) / (4 * kStoreGroups) + 1);
+    const int64_t groups = (int64_t)B * Hkv * ((max_seq_len - 1) / (kGatherRows * kStoreGroups) + 1);
     if ((int64_t)B * Hkv > INT32_MAX || groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: B * Hkv * max_seq_len is too large", who);
+    a.past = (int64_t)B * Hkv * max_seq_len * kD * 2 * ((k_out.ptr != nullptr) + (v_out.ptr != nullptr)) > kPastBytes;
     a.BH = B * Hkv; a.Hkv = Hkv; a.max_len = max_seq_len; a.lens = seq_lens;
     a.k = (uint16_t *)const_cast<void *>(k_out.ptr); a.k_sb = k_out.stride_b; a.k_sh = k_out.stride_h; a.k_st = k_out.stride_t;
     a.v = (uint16_t *)const_cast<void *>(v_out.ptr); a.v_sb = v_out.stride_b; a.v_sh = v_out.stride_h; a.v_st = v_out.stride_t;
