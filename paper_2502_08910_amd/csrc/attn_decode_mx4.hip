@@ -230,6 +230,12 @@ __global__ __launch_bounds__(kMxThreads, kMxPerCu) void attn_decode_mx4_kernel(c
             L = fmaf(x, sh_l[w][h], L);
             A = fmaf(x, sh_acc[w][h][c], A);
         }
+        if (a.n_splits == 1) {                       // nothing to merge
+            const int64_t hq = (int64_t)pr.b * a.ge.Hq + pr.g * G + h;
+            a.out[hq * kD + c] = (uint16_t)f32_to_bf16_bits(L == 0.f ? 0.f : A / L);
+            if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
+            continue;
+        }
         a.part_acc[(pbase + h) * kD + c] = A;
         if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + (pbase + h) * 2) = make_float2(M, L);
     }
@@ -287,18 +293,34 @@ __global__ __launch_bounds__(kD * kMxMergeGroups) void attn_decode_mx4_merge_ker
     if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
 }
 
-// Splits of a problem, which the kernel makes equally long: what fills the compute units once.  Where those would be longer than 1,024 slots,
-// twice: sequences of different lengths keep the units busier so, and beginning and ending a split costs as much as some 128 slots.  32
-// sequences of 7,383 to 16,384 keys, 8 problems each (us): 4 splits a problem 120, 6 (two rounds) 101, 9 103, 12 105, 15 109, 18 112; the
-// same for the longest length 16,384 in splits of 1,024 slots 108.
+// Splits of a problem, which the kernel makes equally long.  A workgroup that has a compute unit to itself takes 10.7 ns a slot (it waits
+// for its loads), three that share one 21 ns (they wait for the memory); a round of workgroups 2 us more than its slots, the launch 3, and the
+// merge with its launch 10.  The least of that over one split (no merge), the splits that give every compute unit one, two or three
+// workgroups, and those that fill two and more rounds.  One split / 768 workgroups or more (us), 8 problems a sequence: 8 sequences of 1,000
+// keys 14.7 / 21.2, 16 of 2,000 25.5 / 20.9, 32 of 1,000 16.9 / 20.2, 32 of 4,000 44.6 / 37.9, 96 of 4,000 88 / 99; 32 of 7,383 to 16,384 in 4, 6
+// (two rounds), 9, 12, 15 and 18 splits 120, 101, 103, 105, 109 and 112.
 static int mx4_splits(const ihip_shape &s, int n_blocks, int block)
 {
     const int64_t total = (int64_t)s.n_sink + (int64_t)n_blocks * block + s.n_stream, P = std::max(1, s.B * s.Hkv);
-    const int64_t places = (int64_t)compute_units() * kMxPerCu;
-    int64_t n = std::max<int64_t>(1, places / P);
-    if (total > n * 1024) n = std::max<int64_t>(1, 2 * places / P);
-    n = std::max(n, (total + kMxMaxSplit - 1) / kMxMaxSplit);
-    return (int)std::min(n, (total + kMxMinSplit - 1) / kMxMinSplit);
+    const int64_t cu = compute_units(), places = cu * kMxPerCu;
+    const int64_t fewest = (total + kMxMaxSplit - 1) / kMxMaxSplit, most = (total + kMxMinSplit - 1) / kMxMinSplit;
+    int64_t best = fewest;
+    double least = 1e300;
+    auto consider = [&](int64_t n) {
+        n = std::min(std::max(n, fewest), most);
+        const int64_t size = ((total + n - 1) / n + kMxMinSplit - 1) / kMxMinSplit * kMxMinSplit;
+        const double share = (double)std::min(P * n, places) / cu, slot = 0.0107 + 0.00515 * std::max(0.0, share - 1);
+        const double time = (double)((P * n + places - 1) / places) * ((double)size * slot + 2) + 3 + (n > 1 ? 10 : 0);
+        if (time < least) {
+            least = time;
+            best = n;
+        }
+    };
+    consider(1);
+    for (int k = 1; k <= kMxPerCu; ++k) consider(k * cu / P);
+    const int64_t rounds = (P * fewest + places - 1) / places;
+    for (int64_t r = std::max<int64_t>(rounds, 2); r < rounds + 4; ++r) consider(r * places / P);
+    return (int)best;
 }
 
 size_t attn_decode_mx4_workspace(const ihip_shape &s, int n_blocks, int block)
@@ -357,7 +379,7 @@ extern "C" int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_t
         if (a.ge.G <= 4) hipLaunchKernelGGL(attn_decode_mx4_kernel<4>, grid, dim3(kMxThreads), 0, st, a);
         else hipLaunchKernelGGL(attn_decode_mx4_kernel<8>, grid, dim3(kMxThreads), 0, st, a);
     }
-    if ((rc = check_launch(who)) != IHIP_OK) return rc;
+    if ((rc = check_launch(who)) != IHIP_OK || a.n_splits == 1) return rc;
     KernelTimer timer("attn_decode_mx4_merge", st);
     hipLaunchKernelGGL(attn_decode_mx4_merge_kernel, dim3(P * a.ge.G), dim3(kD * kMxMergeGroups), 0, st, a);
     return check_launch(who);
