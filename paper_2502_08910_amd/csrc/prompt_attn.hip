@@ -12,7 +12,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPromptWaves = 4;
-constexpr int kPromptRows = 64 * kPromptWaves;       // queries of a workgroup
+constexpr int kPromptRows = 64 * kPromptWaves;       // queries of a workgroup (two sets of 32 a wave)
 constexpr int kTileKeys = 32;
 constexpr int kTileEl = kTileKeys * kD;              // bf16 elements of a K or V tile in LDS
 constexpr int kPromptStages = 4;
@@ -41,11 +41,12 @@ struct PromptArgs {
 // tiles and kBlockCost for its beginning and end.
 constexpr int kBlockCost = 4, kMinPart = 4, kMinShare = 12;      // tiles
 
-struct PromptSeq {
+template <int ROWS>
+struct PromptSeqOf {
     int q_first, nq, k_first, nk;
     int ahead, blocks, ahead_tiles;
-    __device__ PromptSeq() {}
-    __device__ PromptSeq(const PromptArgs &a, int b)
+    __device__ PromptSeqOf() {}
+    __device__ PromptSeqOf(const PromptArgs &a, int b)
     {
         q_first = min(max(a.cu_q[b], 0), a.rows_q);
         nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
@@ -56,12 +57,12 @@ struct PromptSeq {
     __device__ void derive()
     {
         ahead = nk - nq;                             // query i sees keys 0 .. i + ahead
-        blocks = (nq + kPromptRows - 1) / kPromptRows;
+        blocks = (nq + ROWS - 1) / ROWS;
         ahead_tiles = (ahead + kTileKeys - 1) >> 5;  // rounded up, also below 0
     }
-    __device__ PromptSeq of_lane(int l) const        // that of lane l, in all lanes
+    __device__ PromptSeqOf of_lane(int l) const      // that of lane l, in all lanes
     {
-        PromptSeq r;
+        PromptSeqOf r;
         r.q_first = __builtin_amdgcn_readlane(q_first, l);
         r.nq = __builtin_amdgcn_readlane(nq, l);
         r.k_first = __builtin_amdgcn_readlane(k_first, l);
@@ -71,12 +72,13 @@ struct PromptSeq {
     }
     __device__ int tiles(int m) const
     {
-        return m + 1 < blocks ? max(0, kPromptRows / kTileKeys * (m + 1) + ahead_tiles) : (nk + kTileKeys - 1) / kTileKeys;
+        return m + 1 < blocks ? max(0, ROWS / kTileKeys * (m + 1) + ahead_tiles) : (nk + kTileKeys - 1) / kTileKeys;
     }
     __device__ int64_t weight_before(int m) const    // of blocks 0 .. m - 1, m < blocks
     {
-        const int none = min(m, ahead_tiles < 0 ? -ahead_tiles / 8 : 0);          // blocks whose queries see nothing
-        auto sum = [&](int64_t c) { return 4 * c * (c + 1) + ahead_tiles * c; };
+        constexpr int per = ROWS / kTileKeys;
+        const int none = min(m, ahead_tiles < 0 ? -ahead_tiles / per : 0);        // blocks whose queries see nothing
+        auto sum = [&](int64_t c) { return per / 2 * c * (c + 1) + ahead_tiles * c; };
         return sum(m) - sum(none) + (int64_t)kBlockCost * m;
     }
     __device__ int64_t weight() const { return blocks == 0 ? 0 : weight_before(blocks - 1) + tiles(blocks - 1) + kBlockCost; }
@@ -88,10 +90,11 @@ struct PromptSeq {
         const int t = tiles(m), c = (int)min<int64_t>(max<int64_t>(w - kBlockCost, 0), t);
         if (c < kMinPart) return 0;
         if (c > t - kMinPart) return t;
-        const int last = min((m * kPromptRows + ahead) / kTileKeys, t - kMinPart);
+        const int last = min((m * ROWS + ahead) / kTileKeys, t - kMinPart);
         return c <= last ? c : last < kMinPart ? t : last;
     }
 };
+typedef PromptSeqOf<kPromptRows> PromptSeq;
 __device__ inline int64_t wave_sum_i64(int64_t v)
 {
 #pragma unroll
@@ -159,18 +162,26 @@ __device__ inline float half_swap(float x, Op op)
 }
 
 // SHARES: as above; otherwise a workgroup a block and head, the heads of a block next to each other, those with most keys first.
-template <bool SHARES>
+// SETS: sets of 32 queries of a wave, 2, or 1 where there are too few blocks otherwise.  With one, the two tiles of a group take the place of the
+// two sets everywhere below: they are worked on in turn, and both go to the same queries.
+template <int SETS, bool SHARES>
 __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const PromptArgs a)
 {
+    static_assert(SETS == 2 || (SETS == 1 && !SHARES), "shares are made of blocks of two sets a wave");
+    constexpr int kSetRows = 32 * SETS, kRows = kSetRows * kPromptWaves;       // queries of a wave and of the workgroup
+    constexpr int kGroup = 3 - SETS, kGroupKeys = kGroup * kTileKeys, kGroupEl = kGroup * kTileEl;
+    constexpr int kLoads = kGroupKeys / (4 * kPromptWaves);                    // of a wave for K (and for V) of a group
+    typedef PromptSeqOf<kRows> Seq;
     extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
-    uint16_t *const rows = smem + kPromptStages * 2 * kTileEl + wave * 64 * kD;          // this wave's results on their way out
+    // this wave's results on their way out: behind the stages, or, where those take all of LDS, in their place
+    uint16_t *const rows = smem + (SETS == 2 ? kPromptStages * 2 * kGroupEl : 0) + wave * kSetRows * kD;
 
     // which head, which sequence, which of its blocks, which tiles of the block
     int head, b = -1, m = 0, tile0 = 0, tile1 = 0, share = 0;
     PromptPlace end{};
-    PromptSeq seq;
+    Seq seq;
     if constexpr (SHARES) {
         const int64_t per_head = head_weight(a, lane), whole = per_head * a.Hq;
         const int shares = prompt_shares(whole, gridDim.x);
@@ -187,8 +198,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         int ti = blockIdx.x / a.Hq;
         if (a.B <= 64) {
             // blocks in the order of their keys, a block's worth of them at a time: key class c of a sequence's block m is base + m
-            const PromptSeq q(a, min(lane, a.B - 1));
-            const int blocks = lane < a.B ? q.blocks : 0, base = max(0, q.ahead) / kPromptRows;
+            const Seq q(a, min(lane, a.B - 1));
+            const int blocks = lane < a.B ? q.blocks : 0, base = max(0, q.ahead) / kRows;
             auto at_least = [&](int c) { return (int)wave_sum_u32((uint32_t)min(max(base + blocks - c, 0), blocks)); };
             if (ti >= at_least(0)) return;
             int lo = 0, hi = (int)wave_reduce_bits((uint32_t)(base + blocks), [](uint32_t x, uint32_t y) { return max(x, y); });
@@ -205,7 +216,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
             seq = q.of_lane(b);
         } else {
             for (int b0 = 0; b0 < a.B; b0 += 64) {
-                const int blocks = b0 + lane < a.B ? PromptSeq(a, b0 + lane).blocks : 0;
+                const int blocks = b0 + lane < a.B ? Seq(a, b0 + lane).blocks : 0;
                 const int incl = (int)wave_scan_u32((uint32_t)blocks, lane);
                 const unsigned long long past = __ballot(incl > ti);
                 if (past != 0) {
@@ -217,7 +228,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
                 ti -= __builtin_amdgcn_readlane(incl, 63);
             }
             if (b < 0) return;
-            seq = PromptSeq(a, b);
+            seq = Seq(a, b);
         }
     }
     for (;;) {                                       // SHARES: blocks and parts of blocks; otherwise once
@@ -226,29 +237,31 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     b = __builtin_amdgcn_readfirstlane(b);
     m = __builtin_amdgcn_readfirstlane(m);
     tile0 = __builtin_amdgcn_readfirstlane(tile0);
-    if (SHARES) seq = PromptSeq(a, b);
+    if (SHARES) seq = Seq(a, b);
     const int nq = seq.nq, nk = seq.nk, ahead = seq.ahead;
     const int all_tiles = __builtin_amdgcn_readfirstlane(seq.tiles(m));
     const bool is_end = SHARES && __builtin_amdgcn_readfirstlane((int)(head == end.head && b == end.b && m == end.m)) != 0;
     tile1 = __builtin_amdgcn_readfirstlane(is_end ? end.tile : all_tiles);
     if (all_tiles == 0 && !is_end) {                 // queries without keys
-        for (int i = tid; i < min(kPromptRows, nq - m * kPromptRows) * kRowLanes; i += 64 * kPromptWaves) {
-            const int64_t at = (int64_t)(seq.q_first + m * kPromptRows + i / kRowLanes) * a.Hq + head;
+        for (int i = tid; i < min(kRows, nq - m * kRows) * kRowLanes; i += 64 * kPromptWaves) {
+            const int64_t at = (int64_t)(seq.q_first + m * kRows + i / kRowLanes) * a.Hq + head;
             reinterpret_cast<uint4 *>(a.out + at * kD)[i % kRowLanes] = make_uint4(0, 0, 0, 0);
             if (a.lse != nullptr && i % kRowLanes == 0) a.lse[at] = -INFINITY;
         }
     } else if (tile0 < tile1) {
     const int h = head, g = h / a.G;
-    const int row0 = m * kPromptRows + wave * 64;    // this wave's first query
-    const int n_tiles = tile1 - tile0;               // of this part, numbered from its first
+    const int row0 = m * kRows + wave * kSetRows;    // this wave's first query
+    const int n_groups = (tile1 - tile0 + kGroup - 1) / kGroup;      // of tiles of this part, numbered from its first
+    auto qs = [](int s) { return SETS == 2 ? s : 0; };               // the queries of set s, and its tile in group t
+    auto tile_of = [](int t, int s) { return SETS == 2 ? t : 2 * t + s; };
 
-    bf16x8 qb[2][8];
-    int last_key[2];
+    bf16x8 qb[SETS][8];
+    int last_key[SETS];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) last_key[s] = min(row0 + s * 32 + n, nq - 1) + ahead - tile0 * kTileKeys;
+    for (int s = 0; s < SETS; ++s) last_key[s] = min(row0 + s * 32 + n, nq - 1) + ahead - tile0 * kTileKeys;
     auto load_queries = [&] {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < SETS; ++s) {
             const uint16_t *qp = a.q + (int64_t)(seq.q_first + min(row0 + s * 32 + n, nq - 1)) * a.q_st + h * a.q_sh + half * 8;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) qb[s][ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 16);
@@ -259,44 +272,44 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     const uint16_t *kb = a.k + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.k_st + g * a.k_sh;
     const uint16_t *vb = a.v + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.v_st + g * a.v_sh;
 
-    // Loads of a tile: 8 four-row instructions for K and 8 for V, two of each a wave: lane l brings 16 bytes of row 4 j + l / 16 to
-    // base + 16 l.  The base of a tile is scalar; a lane's offset from it changes in a tile that reaches behind the last key only,
-    // whose rows stand for the missing ones.  What would come after the last tile is the last tile again, so that every period
+    // Loads of a group of tiles (32 keys with two sets, 64 with one): four-row instructions, dealt to the waves.  Lane l brings 16 bytes of row
+    // 4 j + l / 16 to base + 16 l.  The base of a group is scalar; a lane's offset from it changes in a group that reaches behind the last key
+    // only, whose rows stand for the missing ones.  What would come after the last group is the last one again, so that every period
     // has as many loads on their way as any other.
     auto offset = [&](int i, int rows, int64_t st, bool is_v) {
         const int key = 4 * (wave + i * kPromptWaves) + (lane >> 4), at = min(key, rows - 1), slot = lane & 15;
         return (uint32_t)(at * (int)st + ((slot ^ (is_v ? (key & 3) << 2 : key & 15)) << 3)) * 2u;
     };
-    const uint32_t k_off[2] = {offset(0, kTileKeys, a.k_st, false), offset(1, kTileKeys, a.k_st, false)};
-    const uint32_t v_off[2] = {offset(0, kTileKeys, a.v_st, true), offset(1, kTileKeys, a.v_st, true)};
+    uint32_t k_off[kLoads], v_off[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        k_off[i] = offset(i, kGroupKeys, a.k_st, false);
+        v_off[i] = offset(i, kGroupKeys, a.v_st, true);
+    }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem + wave * 4 * kD * 2;
-    const bool cut = n_tiles * kTileKeys > keys_here;       // the last tile reaches behind the last key
-    const uint16_t *k_next = kb, *v_next = vb;       // of the tiles to be requested next
-    int k_tile = 0, v_tile = 0;
-    auto request_k = [&](int st) {
-        uint32_t off[2] = {k_off[0], k_off[1]};
-        if (cut && k_tile == n_tiles - 1) {
-            off[0] = offset(0, keys_here - k_tile * kTileKeys, a.k_st, false);
-            off[1] = offset(1, keys_here - k_tile * kTileKeys, a.k_st, false);
+    const bool cut = n_groups * kGroupKeys > keys_here;     // the last group reaches behind the last key
+    const uint16_t *k_next = kb, *v_next = vb;       // of the groups to be requested next
+    int k_group = 0, v_group = 0;
+    auto request = [&](bool is_v, int st) {
+        int &group = is_v ? v_group : k_group;
+        const uint16_t *&next = is_v ? v_next : k_next;
+        const int64_t stride = is_v ? a.v_st : a.k_st;
+        uint32_t off[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) off[i] = is_v ? v_off[i] : k_off[i];
+        if (cut && group == n_groups - 1) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) off[i] = offset(i, keys_here - group * kGroupKeys, stride, is_v);
         }
-        prompt_to_lds(lds0 + st * kTileEl * 2, k_next, off[0]);
-        prompt_to_lds(lds0 + st * kTileEl * 2 + 16 * kD * 2, k_next, off[1]);
-        const bool more = k_tile < n_tiles - 1;
-        k_next += more ? kTileKeys * a.k_st : 0;
-        k_tile += more;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            prompt_to_lds(lds0 + ((is_v ? kPromptStages : 0) + st) * kGroupEl * 2 + i * 4 * kPromptWaves * kD * 2, next, off[i]);
+        const bool more = group < n_groups - 1;
+        next += more ? kGroupKeys * stride : 0;
+        group += more;
     };
-    auto request_v = [&](int st) {
-        uint32_t off[2] = {v_off[0], v_off[1]};
-        if (cut && v_tile == n_tiles - 1) {
-            off[0] = offset(0, keys_here - v_tile * kTileKeys, a.v_st, true);
-            off[1] = offset(1, keys_here - v_tile * kTileKeys, a.v_st, true);
-        }
-        prompt_to_lds(lds0 + (kPromptStages + st) * kTileEl * 2, v_next, off[0]);
-        prompt_to_lds(lds0 + (kPromptStages + st) * kTileEl * 2 + 16 * kD * 2, v_next, off[1]);
-        const bool more = v_tile < n_tiles - 1;
-        v_next += more ? kTileKeys * a.v_st : 0;
-        v_tile += more;
-    };
+    auto request_k = [&](int st) { request(false, st); };
+    auto request_v = [&](int st) { request(true, st); };
     const uint16_t *k_at[8], *v_at[4];               // this lane's addresses in stage 0
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) k_at[ks] = smem + n * kD + ((ks * 2 + half) ^ (n & 15)) * 8;
@@ -305,30 +318,31 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) {
             const int chunk = dt * 4 + ((n >> 4) << 1) + ((i & 3) >> 1);
-            v_at[dt] = smem + kPromptStages * kTileEl + key * kD + ((chunk ^ ((key & 3) << 2)) << 3) + ((i & 1) << 2);
+            v_at[dt] = smem + kPromptStages * kGroupEl + key * kD + ((chunk ^ ((key & 3) << 2)) << 3) + ((i & 1) << 2);
         }
     }
-    auto k_operand = [&](int st, int ks) { return *reinterpret_cast<const bf16x8 *>(k_at[ks] + st * kTileEl); };
-    auto v_operand = [&](int st, int i) {            // i: 4 kk + dt
-        const uint16_t *at = v_at[i & 3] + st * kTileEl + 16 * (i >> 2) * kD;
+    // operand of a stage for set s (with two sets the same tile for both); i: 4 kk + dt
+    auto k_operand = [&](int st, int s, int ks) { return *reinterpret_cast<const bf16x8 *>(k_at[ks] + st * kGroupEl + (SETS == 1 ? s * kTileEl : 0)); };
+    auto v_operand = [&](int st, int s, int i) {
+        const uint16_t *at = v_at[i & 3] + st * kGroupEl + (SETS == 1 ? s * kTileEl : 0) + 16 * (i >> 2) * kD;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 8 * kD));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    f32x16 o[2][4], sc[2];
+    f32x16 o[SETS][4], sc[2];
     auto scores = [&](int st, int s) {
         sc[s] = f32x16{};
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(st, ks), qb[s][ks], sc[s], 0, 0, 0);
+        for (int ks = 0; ks < 8; ++ks) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(st, s, ks), qb[qs(s)][ks], sc[s], 0, 0, 0);
     };
     // Keys of a tile that a lane's query must not see, as bits: score r is that of key 8 (r / 4) + 4 half + r % 4
-    auto hidden_keys = [&](int tile, int s) { return ~0u << min(max(last_key[s] - 4 * half - tile * kTileKeys + 1, 0), 31); };
+    auto hidden_keys = [&](int tile, int s) { return ~0u << min(max(last_key[qs(s)] - 4 * half - tile * kTileKeys + 1, 0), 31); };
     auto hide = [&](uint32_t bits, int r, float x) {         // v_bfe_i32, v_bfi_b32
         const int hidden = (int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31;
         return __int_as_float((hidden & __float_as_int(-INFINITY)) | (~hidden & __float_as_int(x)));
     };
     auto mask = [&](int tile, int s) {
-        if (tile * kTileKeys + kTileKeys - 1 <= first_last + s * 32) return;
+        if (tile * kTileKeys + kTileKeys - 1 <= first_last + qs(s) * 32) return;
         const uint32_t bits = hidden_keys(tile, s);
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[s][r] = hide(bits, r, sc[s][r]);
@@ -341,11 +355,16 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     };
 
     uint32_t pw[2][8];                               // the probabilities of a set, in pairs of keys
-    float m_ref[2] = {kNegBigPrompt, kNegBigPrompt}, l_run[2] = {0.f, 0.f};
+    float m_ref[SETS], l_run[SETS];
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+        m_ref[s] = kNegBigPrompt;
+        l_run[s] = 0.f;
+    }
     // two scores -> two probabilities (exp2(-inf) = 0).  The empty assembly keeps them where they are called: left to themselves all
     // exponentials of a phase would be computed in front of its matrix instructions instead of under them.
     auto exponentials = [&](int s, int i, bool masked, uint32_t bits) {
-        float x = fmaf(sc[s][2 * i], a.scale_log2e, -m_ref[s]), y = fmaf(sc[s][2 * i + 1], a.scale_log2e, -m_ref[s]);
+        float x = fmaf(sc[s][2 * i], a.scale_log2e, -m_ref[qs(s)]), y = fmaf(sc[s][2 * i + 1], a.scale_log2e, -m_ref[qs(s)]);
         if (masked) {
             x = hide(bits, 2 * i, x);
             y = hide(bits, 2 * i + 1, y);
@@ -353,10 +372,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         asm volatile("" : "+v"(x), "+v"(y));
         x = __builtin_amdgcn_exp2f(x);
         y = __builtin_amdgcn_exp2f(y);
-        l_run[s] += x;
-        l_run[s] += y;
+        l_run[qs(s)] += x;
+        l_run[qs(s)] += y;
         pw[s][i] = pack_bf16x2(x, y);
-        asm volatile("" : "+v"(pw[s][i]), "+v"(l_run[s]));
+        asm volatile("" : "+v"(pw[s][i]), "+v"(l_run[qs(s)]));
     };
     auto probabilities = [&](int s, int kk) {
         return __builtin_bit_cast(bf16x8, make_uint4(pw[s][4 * kk], pw[s][4 * kk + 1], pw[s][4 * kk + 2], pw[s][4 * kk + 3]));
@@ -369,33 +388,34 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     // they are, each with its share of the vector instructions under it.  The compiler does not know the instructions' latency: a set's
     // scores are read by vector instructions eight matrix instructions after their last one.
     bf16x8 ka[8], va[8];
-    auto first_operands = [&](int st, int st1) {
+    auto first_operands = [&](int st, int st1, int s) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            ka[i] = k_operand(st1, i);
-            va[i] = v_operand(st, i);
+            ka[i] = k_operand(st1, s, i);
+            va[i] = v_operand(st, s, i);
         }
     };
-    auto period = [&](int st, int st1, int st2, int st3, int t, bool masked) {      // stages of tiles t, t + 1, t + 2, t + 3
+    auto period = [&](int st, int st1, int st2, int st3, int t, bool masked) {      // stages of groups t, t + 1, t + 2, t + 3
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const uint32_t bits = masked ? hidden_keys(t + s, 1 - s) : 0u;
+            const uint32_t bits = masked ? hidden_keys(tile_of(t + s, 1 - s), 1 - s) : 0u;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int i = r & 7;
-                if (s == 0 && r < 6) ka[r + 2] = k_operand(st1, r + 2);
-                if (s == 0 && r >= 6 && r < 12) va[r - 4] = v_operand(st, r - 4);
-                if (s == 1 && r == 10) first_operands(st1, st2);
-                if (r == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=v"(sc[s]) : "v"(ka[0]), "v"(qb[s][0]));
-                else if (r < 8) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(sc[s]) : "v"(ka[r]), "v"(qb[s][r]));
-                else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][i & 3]) : "v"(va[i]), "v"(probabilities(s, i >> 2)));
+                if ((s == 0 || SETS == 1) && r < 6) ka[r + 2] = k_operand(st1, s, r + 2);
+                if ((s == 0 || SETS == 1) && r >= 6 && r < 12) va[r - 4] = v_operand(st, s, r - 4);
+                if (s == 0 && SETS == 1 && r == 10) first_operands(st, st1, 1);
+                if (s == 1 && r == 10) first_operands(st1, st2, 0);
+                if (r == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=v"(sc[s]) : "v"(ka[0]), "v"(qb[qs(s)][0]));
+                else if (r < 8) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(sc[s]) : "v"(ka[r]), "v"(qb[qs(s)][r]));
+                else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[qs(s)][i & 3]) : "v"(va[i]), "v"(probabilities(s, i >> 2)));
                 if (r % 2 == 0) exponentials(1 - s, r / 2, masked, bits);
                 if (s == 0 && r == 3) request_k(st);
                 if (s == 0 && r == 9) request_v(st3);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
         __syncthreads();
     };
     // Exponentials are taken against the row's maximum over the first tile (which holds a key of every query that has any), not
@@ -403,77 +423,87 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     // row's sum says that they did not, the block is done again against the maxima over all tiles.
     for (int again = 0; again < 2; ++again) {
         if (again) {
-            m_ref[0] = m_ref[1] = kNegBigPrompt;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was requested beyond the last group)
             k_next = kb;
-            k_tile = 0;
-            for (int t = 0; t < n_tiles; ++t) {
+            k_group = 0;
+#pragma unroll
+            for (int s = 0; s < SETS; ++s) m_ref[s] = kNegBigPrompt;
+            for (int t = 0; t < n_groups; ++t) {
                 request_k(0);
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     scores(0, s);
-                    mask(t, s);
-                    m_ref[s] = fmaxf(m_ref[s], row_max(sc[s]));
+                    mask(tile_of(t, s), s);
+                    m_ref[qs(s)] = fmaxf(m_ref[qs(s)], row_max(sc[s]));
                 }
                 __syncthreads();
             }
         }
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < SETS; ++s) {
             l_run[s] = 0.f;
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) o[s][dt] = f32x16{};
         }
         k_next = kb; v_next = vb;
-        k_tile = v_tile = 0;
+        k_group = v_group = 0;
 #pragma unroll
         for (int st = 0; st < 4; ++st) request_k(st);
 #pragma unroll
         for (int st = 0; st < 3; ++st) request_v(st);
         if (!again) load_queries();
         // (the accumulators are cleared while the loads are on their way)
-        asm volatile("" : "+a"(o[0][0]), "+a"(o[0][1]), "+a"(o[0][2]), "+a"(o[0][3]), "+a"(o[1][0]), "+a"(o[1][1]), "+a"(o[1][2]), "+a"(o[1][3]));
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) asm volatile("" : "+a"(o[s][0]), "+a"(o[s][1]), "+a"(o[s][2]), "+a"(o[s][3]));
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             scores(0, s);
-            mask(0, s);
-            if (!again) m_ref[s] = fmaxf(kNegBigPrompt, row_max(sc[s]));
+            mask(tile_of(0, s), s);
+            if (!again) m_ref[qs(s)] = fmaxf(SETS == 2 ? kNegBigPrompt : m_ref[0], row_max(sc[s]));
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) exponentials(0, i, false, 0);
         __syncthreads();                             // K(0) has been read
-        first_operands(0, 1);
+        first_operands(0, 1, 0);
         int t = 0;
-        // whole tiles that all queries of the block see; behind them scores are masked, under the matrix instructions as well
-        const int seen = min(n_tiles, (m * kPromptRows + ahead + 1) / kTileKeys - tile0);
+        // groups of whole tiles that all queries of the block see; behind them scores are masked, under the matrix instructions as well
+        const int seen = min(n_groups, ((m * kRows + ahead + 1) / kTileKeys - tile0) / kGroup);
         for (; t + 4 < seen; t += 4) {
             period(0, 1, 2, 3, t, false);
             period(1, 2, 3, 0, t + 1, false);
             period(2, 3, 0, 1, t + 2, false);
             period(3, 0, 1, 2, t + 3, false);
         }
-        for (; t + 1 < n_tiles; ++t) period(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t, true);
-        // the last tile, whose first products are done
-        const uint32_t bits = hidden_keys(t, 1);
+        for (; t + 1 < n_groups; ++t) period(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t, true);
+        // the last group, whose first products are done
+        const uint32_t bits = hidden_keys(tile_of(t, 1), 1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) exponentials(1, i, true, bits);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bf16x8 vt = v_operand(t & 3, i);
+            bf16x8 vt = v_operand(t & 3, 0, i);
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-                asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[s][i & 3]) : "v"(vt), "v"(probabilities(s, i >> 2)));
+            for (int s = 0; s < 2; ++s) {
+                if (SETS == 1 && s == 1) vt = v_operand(t & 3, 1, i);
+                asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[qs(s)][i & 3]) : "v"(vt), "v"(probabilities(s, i >> 2)));
+            }
         }
         // (the compiler does not know that there are matrix instructions in the assembly, whose results take up to 19 wait states)
-        asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o[0][0]), "+a"(o[0][1]), "+a"(o[0][2]), "+a"(o[0][3]), "+a"(o[1][0]), "+a"(o[1][1]), "+a"(o[1][2]), "+a"(o[1][3]));
-        l_run[0] = half_swap(l_run[0], [](float x, float y) { return x + y; });
-        l_run[1] = half_swap(l_run[1], [](float x, float y) { return x + y; });
-        if (again || __syncthreads_or(!(l_run[0] <= kPromptMaxSum && l_run[1] <= kPromptMaxSum)) == 0) break;
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o[s][0]), "+a"(o[s][1]), "+a"(o[s][2]), "+a"(o[s][3]));
+        bool in_range = true;
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) {
+            l_run[s] = half_swap(l_run[s], [](float x, float y) { return x + y; });
+            in_range = in_range && l_run[s] <= kPromptMaxSum;
+        }
+        if (again || __syncthreads_or(!in_range) == 0) break;
     }
-    if (SHARES && n_tiles < all_tiles) {             // a part: its share's first (which does not begin the block) or last one
+    if (SHARES && n_groups < all_tiles) {             // a part: its share's first (which does not begin the block) or last one
         const int64_t unit = (int64_t)(2 * share + (tile0 == 0)) * kPromptWaves + wave;
         float4 *to = a.part_o + unit * 32 * 64 + lane;
 #pragma unroll
@@ -488,8 +518,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     } else {
     // The results go out through LDS, so that whole rows are written: 16-byte chunk c of row r at slot c ^ r % 16.  256 queries of 32 heads on 256
     // keys each 17.4 -> 14.4 us
+    if (SETS == 1) {                                 // in place of the stages, once they have been read and the last requests have come
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < SETS; ++s) {
         const float l = l_run[s];
         const int row = row0 + s * 32 + n;
         const float inv = l == 0.f ? 0.f : 1.0f / l;           // (a query without keys: 0)
@@ -507,11 +541,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     const int64_t step = (int64_t)4 * a.Hq * kD;     // four rows
     const int64_t mine = (int64_t)(lane >> 4) * a.Hq * kD + (lane & 15) * 8;
     auto row_piece = [&](int i) { return *reinterpret_cast<const uint4 *>(rows + (4 * i + (lane >> 4)) * kD + (((lane & 15) ^ (4 * (i & 3) + (lane >> 4))) << 3)); };
-    if (row0 + 64 <= nq) {
+    if (row0 + kSetRows <= nq) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
+        for (int i = 0; i < kSetRows / 4; ++i) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
     } else {
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < kSetRows / 4; ++i)
             if (row0 + 4 * i + (lane >> 4) < nq) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
     }
     }
@@ -522,7 +556,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         m = 0;
         do {
             if (++b == a.B) { b = 0; ++head; }
-        } while (head < a.Hq && PromptSeq(a, b).blocks == 0);
+        } while (head < a.Hq && Seq(a, b).blocks == 0);
     }
     if (head >= a.Hq) break;
     __syncthreads();                                 // the last tile's values have been read
@@ -586,25 +620,34 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
 }
 
 // Blocks x heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each
-static int64_t prompt_blocks(const ihip_packed &p)
+static int64_t prompt_blocks(const ihip_packed &p, int block = kPromptRows)
 {
-    const int64_t by_rows = (int64_t)p.rows / kPromptRows + p.B, by_len = (int64_t)p.B * ((p.max_q - 1) / kPromptRows + 1);
+    const int64_t by_rows = (int64_t)p.rows / block + p.B, by_len = (int64_t)p.B * ((p.max_q - 1) / block + 1);
     return (by_rows < by_len ? by_rows : by_len) * p.Hq;
 }
-// Whether a call is dealt out in shares, from what the host knows of it: total tokens, keys and sequences.  Without shares a launch takes
-// as long as its longest block, or as the rounds of blocks that the compute units do (blocks of the same length in whole rounds; a
-// whole prompt's blocks, of all lengths up to the longest, fill the rounds).  Equal shares take the mean, and kShareCost tiles for their
-// beginnings and ends and for the merge.  Without / with shares (us): 512 queries on 4,608 keys, 32 heads 109 / 73; 2,048 on as many 60 / 78, 4
-// times 1,500 105 / 116; 16 heads, 4,096 103 / 111; 8 heads, 8,192 189 / 170; 16 heads, 1,500 on 13,500 and 700 on 20,711 433 / 273; 32 heads, 8,192 484 / 546.
-constexpr double kShareCost = 65;
-static bool prompt_in_shares(const ihip_packed &p, int64_t keys)
+// How a call is done, from what the host knows of it: total tokens, keys and sequences.  The estimates are in tiles of 32 keys for a block of 256
+// queries (0.7 us, and 14 us for a launch): a launch takes as long as its longest block, or as the rounds of blocks that the compute units do
+// (blocks of the same length in whole rounds; a whole prompt's blocks, of all lengths up to the longest, fill the rounds), where a full chip
+// runs slower than a few blocks and each block begins and ends.  A block of 128 queries takes 0.6 of the time for the same keys: it
+// wins while there are too few blocks of 256.  Equal shares take the mean, and 50 tiles for beginnings, ends and the merge.
+// us with two sets / one / shares, 32 heads: 256 queries 18 / 16 / 40, 512 26 / 19 / 52, 1,024 37 / 26 / 52, 2,048 60 / 51 / 79, 3,000
+// 87 / 99 / 117, 8,192 476 / 545 / 537; 8 heads, 4,096 99 / 64 / 72; 512 on 4,608 keys 109 / 69 / 73; 200 on 8,200 180 / 114 / 81;
+// 16 heads, 1,500 on 13,500 and 700 on 20,700 438 / 353 / 269; 8 heads, 64 on 60,064 1,216 / 734 / 118.
+enum class PromptWay { kTwoSets, kOneSet, kShares };
+static PromptWay prompt_way(const ihip_packed &p, int64_t keys, bool scratch = true)
 {
-    if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return false;
+    if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return PromptWay::kTwoSets;
     const double cu = compute_units(), before = std::max<double>(0, (double)(keys - p.rows)) / p.B, mean = (double)p.rows / p.B;
-    const double longest = (before + p.max_q) / kTileKeys, tiles = (before + mean / 2) / kTileKeys;
-    const double rounds = std::min<double>((double)prompt_blocks(p), ((double)p.rows / kPromptRows + 0.5 * p.B) * p.Hq) / cu;
-    const double alike = before / (before + mean / 2);
-    return std::max(longest, tiles * (rounds + alike * (std::ceil(rounds) - rounds))) > tiles * rounds + kShareCost;
+    const double longest = (before + p.max_q) / kTileKeys, tiles = (before + mean / 2) / kTileKeys, alike = before / (before + mean / 2);
+    auto rounds_of = [&](int block) { return std::min<double>((double)prompt_blocks(p, block), ((double)p.rows / block + 0.5 * p.B) * p.Hq) / cu; };
+    auto whole = [&](int block, double per_tile, double busy) {
+        constexpr double fixed = 8;                  // tiles that a block's beginning and end take
+        const double rounds = rounds_of(block), filled = rounds + alike * (std::ceil(rounds) - rounds);
+        return std::max(per_tile * longest, busy * (per_tile * tiles + fixed) * filled - fixed);
+    };
+    const double two = whole(kPromptRows, 1, 1.3), one = whole(kPromptRows / 2, 0.6, 1.1), shares = 1.4 * tiles * rounds_of(kPromptRows) + 50;
+    if (scratch && shares < two && shares < one) return PromptWay::kShares;
+    return one < two ? PromptWay::kOneSet : PromptWay::kTwoSets;
 }
 static size_t prompt_part_bytes() { return (size_t)2 * compute_units() * kPromptWaves * 64 * (32 * sizeof(float4) + sizeof(float2)); }
 
@@ -615,7 +658,7 @@ using namespace ihip;
 extern "C" size_t ihip_prompt_attn_workspace_bytes(const ihip_packed *packed, int32_t rows_k)
 {
     if (check_packed("ihip_prompt_attn_workspace_bytes", packed) != IHIP_OK) return 0;
-    return prompt_in_shares(*packed, rows_k) ? prompt_part_bytes() : 256;
+    return prompt_way(*packed, rows_k) == PromptWay::kShares ? prompt_part_bytes() : 256;
 }
 
 extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v, const int32_t *cu_k,
@@ -644,24 +687,27 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     a.scale_log2e = sm_scale * 1.44269504088896340736f;
     a.out = (uint16_t *)out;
     a.lse = out_lse;
-    const int64_t groups = prompt_blocks(*packed);
+    const PromptWay way = prompt_way(*packed, rows_k, ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes());
+    const bool one_set = way == PromptWay::kOneSet;
+    const int64_t groups = prompt_blocks(*packed, one_set ? kPromptRows / 2 : kPromptRows);
     if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
     const hipStream_t st = (hipStream_t)stream;
     const dim3 threads(64 * kPromptWaves);
-    constexpr int lds = (kPromptStages * 2 * kTileEl + kPromptRows * kD) * 2;
+    constexpr int lds = kPromptStages * 4 * kTileEl * 2;       // with two sets half of it is the results'
+    static_assert(kPromptStages * 2 * kTileEl >= kPromptRows * kD, "the results of a block fit behind the stages");
     static bool attr_set = false;        // allow more than 64 KiB of dynamic LDS, once
     if (!attr_set) {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<false>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<true>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        for (auto kernel : {&prompt_attn_kernel<2, false>, &prompt_attn_kernel<1, false>, &prompt_attn_kernel<2, true>})
+            (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         attr_set = true;
     }
-    if (ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes() && prompt_in_shares(*packed, rows_k)) {
+    if (way == PromptWay::kShares) {
         const int n = compute_units();
         a.part_o = (float4 *)ws;
         a.part_ml = (float2 *)(a.part_o + (size_t)2 * n * kPromptWaves * 32 * 64);
         {
             KernelTimer timer("prompt_attn_shares", st);
-            hipLaunchKernelGGL(prompt_attn_kernel<true>, dim3(n), threads, lds, st, a);
+            hipLaunchKernelGGL((prompt_attn_kernel<2, true>), dim3(n), threads, lds, st, a);
         }
         if ((rc = check_launch(who)) != IHIP_OK) return rc;
         KernelTimer timer("prompt_merge", st);
@@ -669,6 +715,7 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
         return check_launch(who);
     }
     KernelTimer timer("prompt_attn", st);
-    hipLaunchKernelGGL(prompt_attn_kernel<false>, dim3((uint32_t)groups), threads, lds, st, a);
+    if (one_set) hipLaunchKernelGGL((prompt_attn_kernel<1, false>), dim3((uint32_t)groups), threads, lds, st, a);
+    else hipLaunchKernelGGL((prompt_attn_kernel<2, false>), dim3((uint32_t)groups), threads, lds, st, a);
     return check_launch(who);
 }
