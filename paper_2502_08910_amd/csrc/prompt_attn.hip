@@ -1,4 +1,12 @@
 // Dense causal attention of packed prompts on v_mfma_f32_32x32x16_bf16.
+//   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(c q_i k_j - r_i),   j <= i + (keys - queries),   c = sm_scale log2 e
+// in one pass over the keys, for a reference r_i that is the row's maximum over its first tile (below).  A wave holds the queries (the right
+// operand of the first product, K the left one), so that a lane has 16 of the 32 scores of one query, its exponentials are already
+// the right operand of the second product with V^T (whose rows it takes in the order of the scores), and nothing of P goes through LDS.
+// K and V go from memory to LDS by themselves (global_load_lds), 16-byte chunks XORed with the row, so that both the rows of K and the
+// transposed reads of V (ds_read_b64_tr_b16) are without conflicts.
+// Bound by the matrix units at the clock that the power limit leaves: one prompt of 32,768 with 32 heads, 8.79 TFLOP, takes
+// 7.1 ms, 1.23 PFLOP/s, where a library product of 16,384^3 reaches 1.31 and one of 8,192^3 1.15.
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>
@@ -12,10 +20,20 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPromptWaves = 4;
-constexpr int kPromptRows = 64 * kPromptWaves;       // queries of a workgroup (two sets of 32 a wave)
-constexpr int kTileKeys = 32;
-constexpr int kTileEl = kTileKeys * kD;              // bf16 elements of a K or V tile in LDS
-constexpr int kPromptStages = 4;
+
+// A wave has one or two sets of 32 queries.  With two, a workgroup has a compute unit to itself (512 registers a lane) and what is read
+// from LDS serves two matrix instructions; tiles have 32 keys.  With one, two workgroups share a compute unit, each under the beginnings, ends
+// and waits of the other; tiles have 64 keys, whose two halves take the place of the two sets.
+template <int SETS>
+struct PromptShape {
+    static constexpr int kSetRows = 32 * SETS, kRows = kSetRows * kPromptWaves;          // queries of a wave and of a workgroup
+    static constexpr int kKeys = 64 / SETS, kEl = kKeys * kD;                            // of a tile
+    static constexpr int kPerCu = 3 - SETS;                                              // workgroups of a compute unit
+    static constexpr int kStages = SETS == 2 ? 4 : 2;                                    // tiles of K, and of V, in LDS
+    static constexpr int kLds = (kStages * 2 * kEl + (SETS == 2 ? kRows * kD : 0)) * 2;  // bytes; behind the tiles, or in their place: the results
+    // shares, in tiles: a block's beginning and end, the smallest part of one, the smallest share
+    static constexpr int kBlockCost = 2 + SETS, kMinPart = 2 * SETS, kMinShare = 6 * SETS;
+};
 constexpr float kNegBigPrompt = -1.0e30f;            // finite stand-in for -inf in maxima
 constexpr float kPromptMaxSum = 18446744073709551616.0f;      // 2^64: sum of exponentials beyond which a block is done again
 
@@ -30,23 +48,23 @@ struct PromptArgs {
     uint16_t *out;                   // [rows_q, Hq, d]
     float *lse;                      // [rows_q, Hq] or null
     // launches whose work is dealt out in equal shares: partial results of parts of blocks, two a workgroup
-    float4 *part_o;                  // [part][wave][accumulators of a lane, four at a time: 32][lane]
-    float2 *part_ml;                 // [part][wave][64 queries]: reference of the exponentials (log2 units), sum
+    float4 *part_o;                  // [part][wave][accumulators of a lane, four at a time: 16 a set][lane]
+    float2 *part_ml;                 // [part][wave][set][32 queries]: reference of the exponentials (log2 units), sum
 };
 
 // ---- shares ------------------------------------------------------------------
-// Where there are too few blocks of 256 queries x heads to keep the compute units busy to the end, the tiles of all blocks are dealt out
-// to one workgroup a unit in equal shares, which begin and end inside blocks; a second kernel merges the parts of a block.  The
-// list goes head by head (the query heads of a KV head next to each other), sequence by sequence, block by block; a block weighs its
-// tiles and kBlockCost for its beginning and end.
-constexpr int kBlockCost = 4, kMinPart = 4, kMinShare = 12;      // tiles
+// Where there are too few blocks x heads to keep the compute units busy to the end, the tiles of all blocks are dealt out in equal
+// shares, one to each workgroup that the chip holds at a time, which begin and end inside blocks; a second kernel merges the
+// parts of a block.  The list goes head by head (the query heads of a KV head next to each other), sequence by sequence, block by
+// block; a block weighs its tiles and kBlockCost for its beginning and end.
 
-template <int ROWS>
-struct PromptSeqOf {
+template <int SETS>
+struct PromptSeq {
+    typedef PromptShape<SETS> Shape;
     int q_first, nq, k_first, nk;
     int ahead, blocks, ahead_tiles;
-    __device__ PromptSeqOf() {}
-    __device__ PromptSeqOf(const PromptArgs &a, int b)
+    __device__ PromptSeq() {}
+    __device__ PromptSeq(const PromptArgs &a, int b)
     {
         q_first = min(max(a.cu_q[b], 0), a.rows_q);
         nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
@@ -57,12 +75,12 @@ struct PromptSeqOf {
     __device__ void derive()
     {
         ahead = nk - nq;                             // query i sees keys 0 .. i + ahead
-        blocks = (nq + ROWS - 1) / ROWS;
-        ahead_tiles = (ahead + kTileKeys - 1) >> 5;  // rounded up, also below 0
+        blocks = (nq + Shape::kRows - 1) / Shape::kRows;
+        ahead_tiles = (ahead + Shape::kKeys - 1) >> (SETS == 2 ? 5 : 6);  // rounded up, also below 0
     }
-    __device__ PromptSeqOf of_lane(int l) const      // that of lane l, in all lanes
+    __device__ PromptSeq of_lane(int l) const        // that of lane l, in all lanes
     {
-        PromptSeqOf r;
+        PromptSeq r;
         r.q_first = __builtin_amdgcn_readlane(q_first, l);
         r.nq = __builtin_amdgcn_readlane(nq, l);
         r.k_first = __builtin_amdgcn_readlane(k_first, l);
@@ -72,48 +90,49 @@ struct PromptSeqOf {
     }
     __device__ int tiles(int m) const
     {
-        return m + 1 < blocks ? max(0, ROWS / kTileKeys * (m + 1) + ahead_tiles) : (nk + kTileKeys - 1) / kTileKeys;
+        return m + 1 < blocks ? max(0, Shape::kRows / Shape::kKeys * (m + 1) + ahead_tiles) : (nk + Shape::kKeys - 1) / Shape::kKeys;
     }
     __device__ int64_t weight_before(int m) const    // of blocks 0 .. m - 1, m < blocks
     {
-        constexpr int per = ROWS / kTileKeys;
+        constexpr int per = Shape::kRows / Shape::kKeys;
         const int none = min(m, ahead_tiles < 0 ? -ahead_tiles / per : 0);        // blocks whose queries see nothing
         auto sum = [&](int64_t c) { return per / 2 * c * (c + 1) + ahead_tiles * c; };
-        return sum(m) - sum(none) + (int64_t)kBlockCost * m;
+        return sum(m) - sum(none) + (int64_t)Shape::kBlockCost * m;
     }
-    __device__ int64_t weight() const { return blocks == 0 ? 0 : weight_before(blocks - 1) + tiles(blocks - 1) + kBlockCost; }
+    __device__ int64_t weight() const { return blocks == 0 ? 0 : weight_before(blocks - 1) + tiles(blocks - 1) + Shape::kBlockCost; }
     // A part begins at a multiple of a tile, kMinPart or more from both ends of the block and not behind the tile that its first
     // query sees the end of (so that every query has a key in a part's first tile); w: weight from the block's beginning.
     // The block's number of tiles stands for its end.
     __device__ int part_begin(int m, int64_t w) const
     {
-        const int t = tiles(m), c = (int)min<int64_t>(max<int64_t>(w - kBlockCost, 0), t);
-        if (c < kMinPart) return 0;
-        if (c > t - kMinPart) return t;
-        const int last = min((m * ROWS + ahead) / kTileKeys, t - kMinPart);
-        return c <= last ? c : last < kMinPart ? t : last;
+        const int t = tiles(m), c = (int)min<int64_t>(max<int64_t>(w - Shape::kBlockCost, 0), t);
+        if (c < Shape::kMinPart) return 0;
+        if (c > t - Shape::kMinPart) return t;
+        const int last = min((m * Shape::kRows + ahead) / Shape::kKeys, t - Shape::kMinPart);
+        return c <= last ? c : last < Shape::kMinPart ? t : last;
     }
 };
-typedef PromptSeqOf<kPromptRows> PromptSeq;
 __device__ inline int64_t wave_sum_i64(int64_t v)
 {
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
     return v;
 }
+template <int SETS>
 __device__ inline int64_t head_weight(const PromptArgs &a, int lane)
 {
     int64_t w = 0;
-    for (int b = lane; b < a.B; b += 64) w += PromptSeq(a, b).weight();
+    for (int b = lane; b < a.B; b += 64) w += PromptSeq<SETS>(a, b).weight();
     return wave_sum_i64(w);
 }
 struct PromptPlace { int head, b, m, tile; int64_t begin; };        // head in list order; begin: weight in front of the block
+template <int SETS>
 __device__ inline PromptPlace prompt_place(const PromptArgs &a, int64_t x, int64_t per_head, int lane)
 {
     PromptPlace r{(int)(x / per_head), 0, 0, 0, 0};
     int64_t y = x % per_head;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int64_t w = b0 + lane < a.B ? PromptSeq(a, b0 + lane).weight() : 0;
+        const int64_t w = b0 + lane < a.B ? PromptSeq<SETS>(a, b0 + lane).weight() : 0;
         int64_t incl = w;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -129,7 +148,7 @@ __device__ inline PromptPlace prompt_place(const PromptArgs &a, int64_t x, int64
         }
         y -= __shfl(incl, 63, 64);
     }
-    const PromptSeq q(a, r.b);
+    const PromptSeq<SETS> q(a, r.b);
     int lo = 0, hi = q.blocks - 1;                   // the last block that begins at or before y
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
@@ -143,7 +162,8 @@ __device__ inline PromptPlace prompt_place(const PromptArgs &a, int64_t x, int64
     return r;
 }
 // Shares that the whole weight is cut into, at most n
-__device__ inline int prompt_shares(int64_t whole, int n) { return __builtin_amdgcn_readfirstlane((int)min<int64_t>(n, max<int64_t>(1, whole / kMinShare))); }
+template <int SETS>
+__device__ inline int prompt_shares(int64_t whole, int n) { return __builtin_amdgcn_readfirstlane((int)min<int64_t>(n, max<int64_t>(1, whole / PromptShape<SETS>::kMinShare))); }
 
 // 16 bytes a lane from a scalar base and the lane's byte offset to the LDS byte address dst + 16 l (counts on vmcnt).  M0 is left as it is:
 // nothing else in this kernel reads it, and it is not the compiler's to keep values in.
@@ -162,36 +182,36 @@ __device__ inline float half_swap(float x, Op op)
 }
 
 // SHARES: as above; otherwise a workgroup a block and head, the heads of a block next to each other, those with most keys first.
-// SETS: sets of 32 queries of a wave, 2, or 1 where there are too few blocks otherwise.  With one, the two tiles of a group take the place of the
-// two sets everywhere below: they are worked on in turn, and both go to the same queries.
 template <int SETS, bool SHARES>
-__global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const PromptArgs a)
+__global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void prompt_attn_kernel(const PromptArgs a)
 {
-    static_assert(SETS == 2 || (SETS == 1 && !SHARES), "shares are made of blocks of two sets a wave");
-    constexpr int kSetRows = 32 * SETS, kRows = kSetRows * kPromptWaves;       // queries of a wave and of the workgroup
-    constexpr int kGroup = 3 - SETS, kGroupKeys = kGroup * kTileKeys, kGroupEl = kGroup * kTileEl;
-    constexpr int kLoads = kGroupKeys / (4 * kPromptWaves);                    // of a wave for K (and for V) of a group
-    typedef PromptSeqOf<kRows> Seq;
+    typedef PromptShape<SETS> Shape;
+    typedef PromptSeq<SETS> Seq;
     extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
+    constexpr int kRows = Shape::kRows, kTileKeys = Shape::kKeys, kStages = Shape::kStages, kEl = Shape::kEl;
+    constexpr int kLoads = kTileKeys / (4 * kPromptWaves);         // of a wave for K (and for V) of a tile
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
-    // this wave's results on their way out: behind the stages, or, where those take all of LDS, in their place
-    uint16_t *const rows = smem + (SETS == 2 ? kPromptStages * 2 * kGroupEl : 0) + wave * kSetRows * kD;
+    uint16_t *const rows = smem + (SETS == 2 ? kStages * 2 * kEl : 0) + wave * Shape::kSetRows * kD;       // this wave's results on their way out
 
     // which head, which sequence, which of its blocks, which tiles of the block
     int head, b = -1, m = 0, tile0 = 0, tile1 = 0, share = 0;
     PromptPlace end{};
     Seq seq;
     if constexpr (SHARES) {
-        const int64_t per_head = head_weight(a, lane), whole = per_head * a.Hq;
-        const int shares = prompt_shares(whole, gridDim.x);
+        const int64_t per_head = head_weight<SETS>(a, lane), whole = per_head * a.Hq;
+        const int shares = prompt_shares<SETS>(whole, gridDim.x);
         // workgroups are dealt to the eight XCDs in turn: each gets shares that follow each other, of one KV head if there are eight
         share = shares % 8 == 0 && (int)gridDim.x == shares ? (blockIdx.x & 7) * (shares / 8) + (blockIdx.x >> 3) : blockIdx.x;
         if (share >= shares || __builtin_amdgcn_readfirstlane((int)(whole == 0)) != 0) return;
-        const PromptPlace p = prompt_place(a, share * whole / shares, per_head, lane);
+        const PromptPlace p = prompt_place<SETS>(a, share * whole / shares, per_head, lane);
         head = p.head; b = p.b; m = p.m; tile0 = p.tile;
-        if (share + 1 < shares) end = prompt_place(a, (share + 1) * whole / shares, per_head, lane);
+        if (share + 1 < shares) end = prompt_place<SETS>(a, (share + 1) * whole / shares, per_head, lane);
         else end.head = a.Hq;
+        end.head = __builtin_amdgcn_readfirstlane(end.head);
+        end.b = __builtin_amdgcn_readfirstlane(end.b);
+        end.m = __builtin_amdgcn_readfirstlane(end.m);
+        end.tile = __builtin_amdgcn_readfirstlane(end.tile);
     } else {
         head = blockIdx.x % a.Hq;
         head = head % a.Hkv * a.G + head / a.Hkv;    // neighbours read different KV heads, on the XCD of their own if there are eight
@@ -228,7 +248,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
                 ti -= __builtin_amdgcn_readlane(incl, 63);
             }
             if (b < 0) return;
-            seq = Seq(a, b);
+            seq = Seq(a, b).of_lane(0);
         }
     }
     for (;;) {                                       // SHARES: blocks and parts of blocks; otherwise once
@@ -237,7 +257,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     b = __builtin_amdgcn_readfirstlane(b);
     m = __builtin_amdgcn_readfirstlane(m);
     tile0 = __builtin_amdgcn_readfirstlane(tile0);
-    if (SHARES) seq = Seq(a, b);
+    if (SHARES) seq = Seq(a, b).of_lane(0);
     const int nq = seq.nq, nk = seq.nk, ahead = seq.ahead;
     const int all_tiles = __builtin_amdgcn_readfirstlane(seq.tiles(m));
     const bool is_end = SHARES && __builtin_amdgcn_readfirstlane((int)(head == end.head && b == end.b && m == end.m)) != 0;
@@ -250,10 +270,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         }
     } else if (tile0 < tile1) {
     const int h = head, g = h / a.G;
-    const int row0 = m * kRows + wave * kSetRows;    // this wave's first query
-    const int n_groups = (tile1 - tile0 + kGroup - 1) / kGroup;      // of tiles of this part, numbered from its first
-    auto qs = [](int s) { return SETS == 2 ? s : 0; };               // the queries of set s, and its tile in group t
-    auto tile_of = [](int t, int s) { return SETS == 2 ? t : 2 * t + s; };
+    const int row0 = m * kRows + wave * Shape::kSetRows;           // this wave's first query
+    const int n_tiles = tile1 - tile0;               // of this part, numbered from its first
+    // Work goes in two turns s, for the two sets of queries or the two halves of a tile: their queries, first query and first key
+    auto qs = [](int s) { return SETS == 2 ? s : 0; };
+    auto query0 = [](int s) { return SETS == 2 ? 32 * s : 0; };
+    auto key0 = [](int s) { return SETS == 2 ? 0 : 32 * s; };
 
     bf16x8 qb[SETS][8];
     int last_key[SETS];
@@ -272,10 +294,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     const uint16_t *kb = a.k + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.k_st + g * a.k_sh;
     const uint16_t *vb = a.v + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.v_st + g * a.v_sh;
 
-    // Loads of a group of tiles (32 keys with two sets, 64 with one): four-row instructions, dealt to the waves.  Lane l brings 16 bytes of row
-    // 4 j + l / 16 to base + 16 l.  The base of a group is scalar; a lane's offset from it changes in a group that reaches behind the last key
-    // only, whose rows stand for the missing ones.  What would come after the last group is the last one again, so that every period
-    // has as many loads on their way as any other.
+    // Loads of a tile: four-row instructions for K and V, dealt to the waves.  Lane l brings 16 bytes of row
+    // 4 j + l / 16 to base + 16 l.  The base of a tile is scalar; a lane's offset from it changes in a tile that reaches behind the last key
+    // only, whose rows stand for the missing ones.  What would come after the last tile is the last one again, so that every period has
+    // as many loads on their way as any other.
     auto offset = [&](int i, int rows, int64_t st, bool is_v) {
         const int key = 4 * (wave + i * kPromptWaves) + (lane >> 4), at = min(key, rows - 1), slot = lane & 15;
         return (uint32_t)(at * (int)st + ((slot ^ (is_v ? (key & 3) << 2 : key & 15)) << 3)) * 2u;
@@ -283,30 +305,30 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     uint32_t k_off[kLoads], v_off[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        k_off[i] = offset(i, kGroupKeys, a.k_st, false);
-        v_off[i] = offset(i, kGroupKeys, a.v_st, true);
+        k_off[i] = offset(i, kTileKeys, a.k_st, false);
+        v_off[i] = offset(i, kTileKeys, a.v_st, true);
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem + wave * 4 * kD * 2;
-    const bool cut = n_groups * kGroupKeys > keys_here;     // the last group reaches behind the last key
-    const uint16_t *k_next = kb, *v_next = vb;       // of the groups to be requested next
-    int k_group = 0, v_group = 0;
+    const bool cut = n_tiles * kTileKeys > keys_here;       // the last tile reaches behind the last key
+    const uint16_t *k_next = kb, *v_next = vb;       // of the tiles to be requested next
+    int k_tile = 0, v_tile = 0;
     auto request = [&](bool is_v, int st) {
-        int &group = is_v ? v_group : k_group;
+        int &tile = is_v ? v_tile : k_tile;
         const uint16_t *&next = is_v ? v_next : k_next;
         const int64_t stride = is_v ? a.v_st : a.k_st;
         uint32_t off[kLoads];
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) off[i] = is_v ? v_off[i] : k_off[i];
-        if (cut && group == n_groups - 1) {
+        if (cut && tile == n_tiles - 1) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) off[i] = offset(i, keys_here - group * kGroupKeys, stride, is_v);
+            for (int i = 0; i < kLoads; ++i) off[i] = offset(i, keys_here - tile * kTileKeys, stride, is_v);
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            prompt_to_lds(lds0 + ((is_v ? kPromptStages : 0) + st) * kGroupEl * 2 + i * 4 * kPromptWaves * kD * 2, next, off[i]);
-        const bool more = group < n_groups - 1;
-        next += more ? kGroupKeys * stride : 0;
-        group += more;
+            prompt_to_lds(lds0 + ((is_v ? kStages : 0) + st) * kEl * 2 + i * 4 * kPromptWaves * kD * 2, next, off[i]);
+        const bool more = tile < n_tiles - 1;
+        next += more ? kTileKeys * stride : 0;
+        tile += more;
     };
     auto request_k = [&](int st) { request(false, st); };
     auto request_v = [&](int st) { request(true, st); };
@@ -318,13 +340,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) {
             const int chunk = dt * 4 + ((n >> 4) << 1) + ((i & 3) >> 1);
-            v_at[dt] = smem + kPromptStages * kGroupEl + key * kD + ((chunk ^ ((key & 3) << 2)) << 3) + ((i & 1) << 2);
+            v_at[dt] = smem + kStages * kEl + key * kD + ((chunk ^ ((key & 3) << 2)) << 3) + ((i & 1) << 2);
         }
     }
-    // operand of a stage for set s (with two sets the same tile for both); i: 4 kk + dt
-    auto k_operand = [&](int st, int s, int ks) { return *reinterpret_cast<const bf16x8 *>(k_at[ks] + st * kGroupEl + (SETS == 1 ? s * kTileEl : 0)); };
+    // operands of a stage for turn s; i: 4 kk + dt
+    auto k_operand = [&](int st, int s, int ks) { return *reinterpret_cast<const bf16x8 *>(k_at[ks] + st * kEl + key0(s) * kD); };
     auto v_operand = [&](int st, int s, int i) {
-        const uint16_t *at = v_at[i & 3] + st * kGroupEl + (SETS == 1 ? s * kTileEl : 0) + 16 * (i >> 2) * kD;
+        const uint16_t *at = v_at[i & 3] + st * kEl + (key0(s) + 16 * (i >> 2)) * kD;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 8 * kD));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -335,34 +357,31 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(st, s, ks), qb[qs(s)][ks], sc[s], 0, 0, 0);
     };
-    // Keys of a tile that a lane's query must not see, as bits: score r is that of key 8 (r / 4) + 4 half + r % 4
-    auto hidden_keys = [&](int tile, int s) { return ~0u << min(max(last_key[qs(s)] - 4 * half - tile * kTileKeys + 1, 0), 31); };
+    // Keys of a turn that a lane's query must not see, as bits: score r is that of key 8 (r / 4) + 4 half + r % 4
+    auto hidden_keys = [&](int tile, int s) { return ~0u << min(max(last_key[qs(s)] - 4 * half - tile * kTileKeys - key0(s) + 1, 0), 31); };
     auto hide = [&](uint32_t bits, int r, float x) {         // v_bfe_i32, v_bfi_b32
         const int hidden = (int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31;
         return __int_as_float((hidden & __float_as_int(-INFINITY)) | (~hidden & __float_as_int(x)));
     };
     auto mask = [&](int tile, int s) {
-        if (tile * kTileKeys + kTileKeys - 1 <= first_last + qs(s) * 32) return;
+        if (tile * kTileKeys + key0(s) + 31 <= first_last + query0(s)) return;
         const uint32_t bits = hidden_keys(tile, s);
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[s][r] = hide(bits, r, sc[s][r]);
     };
-    auto row_max = [&](const f32x16 &s) {            // scaled; of both halves
+    auto row_max = [&](const f32x16 &s) {            // scaled; of both halves of the wave
         float mx = s[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
         return half_swap(mx, [](float x, float y) { return fmaxf(x, y); }) * a.scale_log2e;
     };
 
-    uint32_t pw[2][8];                               // the probabilities of a set, in pairs of keys
+    uint32_t pw[2][8];                               // the probabilities of a turn, in pairs of keys
     float m_ref[SETS], l_run[SETS];
 #pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-        m_ref[s] = kNegBigPrompt;
-        l_run[s] = 0.f;
-    }
+    for (int s = 0; s < SETS; ++s) m_ref[s] = kNegBigPrompt;
     // two scores -> two probabilities (exp2(-inf) = 0).  The empty assembly keeps them where they are called: left to themselves all
-    // exponentials of a phase would be computed in front of its matrix instructions instead of under them.
+    // exponentials of a turn would be computed in front of the other's matrix instructions instead of under them.
     auto exponentials = [&](int s, int i, bool masked, uint32_t bits) {
         float x = fmaf(sc[s][2 * i], a.scale_log2e, -m_ref[qs(s)]), y = fmaf(sc[s][2 * i + 1], a.scale_log2e, -m_ref[qs(s)]);
         if (masked) {
@@ -380,35 +399,41 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
     auto probabilities = [&](int s, int kk) {
         return __builtin_bit_cast(bf16x8, make_uint4(pw[s][4 * kk], pw[s][4 * kk + 1], pw[s][4 * kk + 2], pw[s][4 * kk + 3]));
     };
-    // Period t, for the two sets of 32 queries in turn: first product of tile t + 1 and second product of tile t, and under them the
-    // exponentials of the other set, 16 matrix instructions and 16 scores a lane at a time.  K of tile t + 4 and V of tile t + 3 are
-    // requested into the stages that period t - 1 has read, and have landed when period t + 1 ends; the first operands of period
-    // t + 1 are read from LDS as this one ends.  Matrix instructions are written as assembly: of the 512 registers that the one wave of
-    // a SIMD has, they can keep the accumulators in the upper half ("a") and everything else in the lower one, and they stay where
-    // they are, each with its share of the vector instructions under it.  The compiler does not know the instructions' latency: a set's
-    // scores are read by vector instructions eight matrix instructions after their last one.
+    // Matrix instructions of the loop are written as assembly, so that each stays where it is, with its share of the vector
+    // instructions under it, and that the accumulators of two sets are kept in the upper half of the 512 registers ("a") and everything else
+    // in the lower one.  The compiler does not know the instructions' latency: a turn's scores are read by vector instructions eight
+    // matrix instructions after their last one.
+    auto score_step = [&](int s, int ks, const bf16x8 &x) {
+        if (ks == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=v"(sc[s]) : "v"(x), "v"(qb[qs(s)][0]));
+        else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(sc[s]) : "v"(x), "v"(qb[qs(s)][ks]));
+    };
+    auto value_step = [&](int s, int i, const bf16x8 &x) {
+        if constexpr (SETS == 2) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[qs(s)][i & 3]) : "v"(x), "v"(probabilities(s, i >> 2)));
+        else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(o[0][i & 3]) : "v"(x), "v"(probabilities(s, i >> 2)));
+    };
+    // Period t, in two turns: first product of tile t + 1 and second product of tile t, and under them the exponentials of the other
+    // turn, 16 matrix instructions and 16 scores a lane at a time.
+    // Two sets: K of tile t + 4 and V of tile t + 3 are requested into the stages that period t - 1 has read, and have landed when period
+    // t + 1 ends; operands serve both turns, and the first ones of period t + 1 are read from LDS as this one ends.
     bf16x8 ka[8], va[8];
-    auto first_operands = [&](int st, int st1, int s) {
+    auto first_operands = [&](int st, int st1) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            ka[i] = k_operand(st1, s, i);
-            va[i] = v_operand(st, s, i);
+            ka[i] = k_operand(st1, 0, i);
+            va[i] = v_operand(st, 0, i);
         }
     };
-    auto period = [&](int st, int st1, int st2, int st3, int t, bool masked) {      // stages of groups t, t + 1, t + 2, t + 3
+    auto period_of_sets = [&](int st, int st1, int st2, int st3, int t, bool masked) {     // stages of tiles t, t + 1, t + 2, t + 3
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const uint32_t bits = masked ? hidden_keys(tile_of(t + s, 1 - s), 1 - s) : 0u;
+            const uint32_t bits = masked ? hidden_keys(t + s, 1 - s) : 0u;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int i = r & 7;
-                if ((s == 0 || SETS == 1) && r < 6) ka[r + 2] = k_operand(st1, s, r + 2);
-                if ((s == 0 || SETS == 1) && r >= 6 && r < 12) va[r - 4] = v_operand(st, s, r - 4);
-                if (s == 0 && SETS == 1 && r == 10) first_operands(st, st1, 1);
-                if (s == 1 && r == 10) first_operands(st1, st2, 0);
-                if (r == 0) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=v"(sc[s]) : "v"(ka[0]), "v"(qb[qs(s)][0]));
-                else if (r < 8) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(sc[s]) : "v"(ka[r]), "v"(qb[qs(s)][r]));
-                else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[qs(s)][i & 3]) : "v"(va[i]), "v"(probabilities(s, i >> 2)));
+                if (s == 0 && r < 6) ka[r + 2] = k_operand(st1, 0, r + 2);
+                if (s == 0 && r >= 6 && r < 12) va[r - 4] = v_operand(st, 0, r - 4);
+                if (s == 1 && r == 10) first_operands(st1, st2);
+                if (r < 8) score_step(s, r, ka[r]);
+                else value_step(s, r & 7, va[r & 7]);
                 if (r % 2 == 0) exponentials(1 - s, r / 2, masked, bits);
                 if (s == 0 && r == 3) request_k(st);
                 if (s == 0 && r == 9) request_v(st3);
@@ -418,24 +443,50 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
         __syncthreads();
     };
+    // One set: K of tile t + 2 and V of tile t + 1 are requested into the stages that period t - 1 has read, and have landed when this one
+    // ends; operands are read from LDS four matrix instructions ahead.  What that and the barrier leave idle is the other workgroup's.
+    auto period_of_halves = [&](int st, int t, bool masked) {                              // st: t % 2
+        constexpr int kAhead = 4;
+        auto operand = [&](int c) { return (c & 8) == 0 ? k_operand(st ^ 1, c >> 4, c & 7) : v_operand(st, c >> 4, c & 7); };
+        bf16x8 x[kAhead];
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) x[c] = operand(c);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint32_t bits = masked ? hidden_keys(t + s, 1 - s) : 0u;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int c = 16 * s + r;
+                if (r < 8) score_step(s, r, x[c % kAhead]);
+                else value_step(s, r & 7, x[c % kAhead]);
+                if (c + kAhead < 32) x[c % kAhead] = operand(c + kAhead);
+                if (r % 2 == 0) exponentials(1 - s, r / 2, masked, bits);
+                if (s == 0 && r == 1) request_k(st);
+                if (s == 0 && r == 3) request_v(st ^ 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
     // Exponentials are taken against the row's maximum over the first tile (which holds a key of every query that has any), not
     // against a running one: bf16 and fp32 have exponents to spare, nothing is lost while the scores stay within 2^64 of it.  Where a
     // row's sum says that they did not, the block is done again against the maxima over all tiles.
     for (int again = 0; again < 2; ++again) {
         if (again) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was requested beyond the last group)
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was requested beyond the last tile)
             k_next = kb;
-            k_group = 0;
+            k_tile = 0;
 #pragma unroll
             for (int s = 0; s < SETS; ++s) m_ref[s] = kNegBigPrompt;
-            for (int t = 0; t < n_groups; ++t) {
+            for (int t = 0; t < n_tiles; ++t) {
                 request_k(0);
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     scores(0, s);
-                    mask(tile_of(t, s), s);
+                    mask(t, s);
                     m_ref[qs(s)] = fmaxf(m_ref[qs(s)], row_max(sc[s]));
                 }
                 __syncthreads();
@@ -448,85 +499,93 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
             for (int dt = 0; dt < 4; ++dt) o[s][dt] = f32x16{};
         }
         k_next = kb; v_next = vb;
-        k_group = v_group = 0;
+        k_tile = v_tile = 0;
 #pragma unroll
-        for (int st = 0; st < 4; ++st) request_k(st);
+        for (int st = 0; st < kStages; ++st) request_k(st);
 #pragma unroll
-        for (int st = 0; st < 3; ++st) request_v(st);
+        for (int st = 0; st < kStages - 1; ++st) request_v(st);
         if (!again) load_queries();
-        // (the accumulators are cleared while the loads are on their way)
+        if constexpr (SETS == 2) {                   // (the accumulators are cleared while the loads are on their way)
 #pragma unroll
-        for (int s = 0; s < SETS; ++s) asm volatile("" : "+a"(o[s][0]), "+a"(o[s][1]), "+a"(o[s][2]), "+a"(o[s][3]));
+            for (int s = 0; s < SETS; ++s) asm volatile("" : "+a"(o[s][0]), "+a"(o[s][1]), "+a"(o[s][2]), "+a"(o[s][3]));
+        }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             scores(0, s);
-            mask(tile_of(0, s), s);
-            if (!again) m_ref[qs(s)] = fmaxf(SETS == 2 ? kNegBigPrompt : m_ref[0], row_max(sc[s]));
+            mask(0, s);
+            if (!again) m_ref[qs(s)] = fmaxf(m_ref[qs(s)], row_max(sc[s]));
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) exponentials(0, i, false, 0);
         __syncthreads();                             // K(0) has been read
-        first_operands(0, 1, 0);
         int t = 0;
-        // groups of whole tiles that all queries of the block see; behind them scores are masked, under the matrix instructions as well
-        const int seen = min(n_groups, ((m * kRows + ahead + 1) / kTileKeys - tile0) / kGroup);
-        for (; t + 4 < seen; t += 4) {
-            period(0, 1, 2, 3, t, false);
-            period(1, 2, 3, 0, t + 1, false);
-            period(2, 3, 0, 1, t + 2, false);
-            period(3, 0, 1, 2, t + 3, false);
+        // tiles that all queries of the block see whole; behind them scores are masked, under the matrix instructions as well
+        const int seen = min(n_tiles, (m * kRows + ahead + 1) / kTileKeys - tile0);
+        if constexpr (SETS == 2) {
+            first_operands(0, 1);
+            for (; t + 4 < seen; t += 4) {
+                period_of_sets(0, 1, 2, 3, t, false);
+                period_of_sets(1, 2, 3, 0, t + 1, false);
+                period_of_sets(2, 3, 0, 1, t + 2, false);
+                period_of_sets(3, 0, 1, 2, t + 3, false);
+            }
+            for (; t + 1 < n_tiles; ++t) period_of_sets(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t, true);
+        } else {
+            for (; t + 2 < seen; t += 2) {
+                period_of_halves(0, t, false);
+                period_of_halves(1, t + 1, false);
+            }
+            for (; t + 1 < n_tiles; ++t) period_of_halves(t & 1, t, true);
         }
-        for (; t + 1 < n_groups; ++t) period(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t, true);
-        // the last group, whose first products are done
-        const uint32_t bits = hidden_keys(tile_of(t, 1), 1);
+        // the last tile, whose first products are done
+        const uint32_t bits = hidden_keys(t, 1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) exponentials(1, i, true, bits);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            bf16x8 vt = v_operand(t & 3, 0, i);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                if (SETS == 1 && s == 1) vt = v_operand(t & 3, 1, i);
-                asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[qs(s)][i & 3]) : "v"(vt), "v"(probabilities(s, i >> 2)));
-            }
+        for (int c = 0; c < 16; ++c) {               // two sets: both products of an operand; one: one half after the other
+            const int s = SETS == 2 ? c & 1 : c >> 3, i = SETS == 2 ? c >> 1 : c & 7;
+            const bf16x8 x = v_operand(t & (kStages - 1), s, i);
+            if constexpr (SETS == 2) asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o[qs(s)][i & 3]) : "v"(x), "v"(probabilities(s, i >> 2)));
+            else asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(o[0][i & 3]) : "v"(x), "v"(probabilities(s, i >> 2)));
         }
         // (the compiler does not know that there are matrix instructions in the assembly, whose results take up to 19 wait states)
 #pragma unroll
-        for (int s = 0; s < SETS; ++s) asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o[s][0]), "+a"(o[s][1]), "+a"(o[s][2]), "+a"(o[s][3]));
+        for (int s = 0; s < SETS; ++s) {
+            if constexpr (SETS == 2) asm volatile("s_nop 15\n\ts_nop 7" : "+a"(o[s][0]), "+a"(o[s][1]), "+a"(o[s][2]), "+a"(o[s][3]));
+            else asm volatile("s_nop 15\n\ts_nop 7" : "+v"(o[s][0]), "+v"(o[s][1]), "+v"(o[s][2]), "+v"(o[s][3]));
+        }
         bool in_range = true;
 #pragma unroll
         for (int s = 0; s < SETS; ++s) {
             l_run[s] = half_swap(l_run[s], [](float x, float y) { return x + y; });
             in_range = in_range && l_run[s] <= kPromptMaxSum;
         }
-        if (again || __syncthreads_or(!in_range) == 0) break;
+        if (__syncthreads_or(!in_range) == 0 || again) break;        // (all waves have read the stages)
     }
-    if (SHARES && n_groups < all_tiles) {             // a part: its share's first (which does not begin the block) or last one
+    if (SHARES && n_tiles < all_tiles) {             // a part: its share's first (which does not begin the block) or last one
         const int64_t unit = (int64_t)(2 * share + (tile0 == 0)) * kPromptWaves + wave;
-        float4 *to = a.part_o + unit * 32 * 64 + lane;
+        float4 *to = a.part_o + unit * SETS * 16 * 64 + lane;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < SETS; ++s) {
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
                 for (int r4 = 0; r4 < 4; ++r4)
                     to[(s * 16 + dt * 4 + r4) * 64] = make_float4(o[s][dt][r4 * 4], o[s][dt][r4 * 4 + 1], o[s][dt][r4 * 4 + 2], o[s][dt][r4 * 4 + 3]);
-            if (half == 0) a.part_ml[unit * 64 + s * 32 + n] = make_float2(m_ref[s], l_run[s]);
+            if (half == 0) a.part_ml[(unit * SETS + s) * 32 + n] = make_float2(m_ref[s], l_run[s]);
         }
     } else {
     // The results go out through LDS, so that whole rows are written: 16-byte chunk c of row r at slot c ^ r % 16.  256 queries of 32 heads on 256
     // keys each 17.4 -> 14.4 us
-    if (SETS == 1) {                                 // in place of the stages, once they have been read and the last requests have come
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    }
+    int l = lane;                                    // (not known to be it: what follows from it is computed here, not kept in registers all along)
+    asm volatile("" : "+v"(l));
+    const int n = l & 31, half = l >> 5;
 #pragma unroll
     for (int s = 0; s < SETS; ++s) {
-        const float l = l_run[s];
         const int row = row0 + s * 32 + n;
-        const float inv = l == 0.f ? 0.f : 1.0f / l;           // (a query without keys: 0)
+        const float inv = l_run[s] == 0.f ? 0.f : 1.0f / l_run[s];             // (a query without keys: 0)
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -534,19 +593,19 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
                 *reinterpret_cast<uint2 *>(rows + (s * 32 + n) * kD + (((dt * 4 + r4) ^ (n & 15)) << 3) + half * 4) =
                     make_uint2(pack_bf16x2(o[s][dt][r4 * 4] * inv, o[s][dt][r4 * 4 + 1] * inv), pack_bf16x2(o[s][dt][r4 * 4 + 2] * inv, o[s][dt][r4 * 4 + 3] * inv));
         if (a.lse != nullptr && half == 0 && row < nq)
-            a.lse[(int64_t)(seq.q_first + row) * a.Hq + h] = l == 0.f ? -INFINITY : (m_ref[s] + log2f(l)) * 0.69314718055994530942f;
+            a.lse[(int64_t)(seq.q_first + row) * a.Hq + h] = l_run[s] == 0.f ? -INFINITY : (m_ref[s] + log2f(l_run[s])) * 0.69314718055994530942f;
     }
     asm volatile("" ::: "memory");                   // lanes read what other lanes of the wave wrote (LDS keeps the order)
     uint16_t *out = a.out + ((int64_t)(seq.q_first + row0) * a.Hq + h) * kD;
     const int64_t step = (int64_t)4 * a.Hq * kD;     // four rows
-    const int64_t mine = (int64_t)(lane >> 4) * a.Hq * kD + (lane & 15) * 8;
-    auto row_piece = [&](int i) { return *reinterpret_cast<const uint4 *>(rows + (4 * i + (lane >> 4)) * kD + (((lane & 15) ^ (4 * (i & 3) + (lane >> 4))) << 3)); };
-    if (row0 + kSetRows <= nq) {
+    const int64_t mine = (int64_t)(l >> 4) * a.Hq * kD + (l & 15) * 8;
+    auto row_piece = [&](int i) { return *reinterpret_cast<const uint4 *>(rows + (4 * i + (l >> 4)) * kD + (((l & 15) ^ (4 * (i & 3) + (l >> 4))) << 3)); };
+    if (row0 + Shape::kSetRows <= nq) {
 #pragma unroll
-        for (int i = 0; i < kSetRows / 4; ++i) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
+        for (int i = 0; i < Shape::kSetRows / 4; ++i) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
     } else {
-        for (int i = 0; i < kSetRows / 4; ++i)
-            if (row0 + 4 * i + (lane >> 4) < nq) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
+        for (int i = 0; i < Shape::kSetRows / 4; ++i)
+            if (row0 + 4 * i + (l >> 4) < nq) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
     }
     }
     }
@@ -565,91 +624,140 @@ __global__ __launch_bounds__(64 * kPromptWaves, 1) void prompt_attn_kernel(const
 
 // The parts of the block that boundary `blockIdx.x` + 1 of the shares is the first to cut; a wave's 64 queries a workgroup.
 // Wave w of it takes accumulators 8 w .. 8 w + 7 of each lane.
+template <int SETS>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, int workgroups)
 {
+    constexpr int kPieces = 4 * SETS;                // 16-byte pieces of a lane's accumulators, of which each of the four waves takes a quarter
     const int lane = threadIdx.x & 63, quarter = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y;
-    const int64_t per_head = head_weight(a, lane), whole = per_head * a.Hq;
-    const int shares = prompt_shares(whole, workgroups), j = blockIdx.x + 1;
+    const int64_t per_head = head_weight<SETS>(a, lane), whole = per_head * a.Hq;
+    const int shares = prompt_shares<SETS>(whole, workgroups), j = blockIdx.x + 1;
     if (whole == 0 || j >= shares) return;
-    const PromptPlace p = prompt_place(a, j * whole / shares, per_head, lane);
-    const PromptSeq seq(a, p.b);
+    const PromptPlace p = prompt_place<SETS>(a, j * whole / shares, per_head, lane);
+    const PromptSeq<SETS> seq(a, p.b);
     const int tiles = seq.tiles(p.m);
     if (p.tile == 0 || p.tile == tiles) return;      // cuts nothing
     auto tile_of = [&](int k) {                      // where share k begins in this block, its end if behind it
         const int64_t w = k * whole / shares - p.begin;
-        return k >= shares || w >= (int64_t)tiles + kBlockCost ? tiles : seq.part_begin(p.m, w);
+        return k >= shares || w >= (int64_t)tiles + PromptShape<SETS>::kBlockCost ? tiles : seq.part_begin(p.m, w);
     };
     if ((j - 1) * whole / shares >= p.begin) {
         const int before = tile_of(j - 1);
         if (before > 0) return;                      // not the first
     }
-    const int n = lane & 31, half = lane >> 5, s = quarter >> 1;
+    const int n = lane & 31, half = lane >> 5, s = quarter * kPieces / 16;
     float M = kNegBigPrompt, L = 0.f;
-    float4 acc[8];
+    float4 acc[kPieces];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    int begin = 0;
-    for (int k = j - 1; begin < tiles; ++k) {
-        const int end = tile_of(k + 1);
-        if (begin < end) {
-            const int64_t unit = (int64_t)(2 * k + (begin == 0)) * kPromptWaves + wave;
-            const float2 ml = a.part_ml[unit * 64 + s * 32 + n];
-            const float4 *from = a.part_o + (unit * 32 + quarter * 8) * 64 + lane;
-            const float top = fmaxf(M, ml.x), old = __builtin_amdgcn_exp2f(M - top), w = __builtin_amdgcn_exp2f(ml.x - top);
-            M = top;
-            L = L * old + ml.y * w;
+    for (int i = 0; i < kPieces; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    // share k's part of the block is [tile_of(k), tile_of(k + 1)), the first one's from 0; a lane finds that of one share.  Up to four parts
+    // are read at a time: 64 queries on 60,064 keys, which are cut into 64 parts, 162 -> 121 us
+    int begun = 0;
+    for (int k0 = j - 1; begun < tiles; k0 += 64) {
+        const int end = tile_of(k0 + lane + 1);
+        int begin = __shfl_up(end, 1, 64);
+        if (lane == 0) begin = begun;
+        begun = __builtin_amdgcn_readlane(end, 63);
+        const int part = 2 * (k0 + lane) + (begin == 0);
+        unsigned long long left = __ballot(begin < end);
+        auto take = [&](auto count) {
+            constexpr int N = decltype(count)::value;
+            float2 ml[N];
+            float4 x[N][kPieces];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 x = from[i * 64];
-                acc[i] = make_float4(acc[i].x * old + x.x * w, acc[i].y * old + x.y * w, acc[i].z * old + x.z * w, acc[i].w * old + x.w * w);
+            for (int c = 0; c < N; ++c) {
+                const int64_t unit = (int64_t)__builtin_amdgcn_readlane(part, __builtin_ctzll(left)) * kPromptWaves + wave;
+                left &= left - 1;
+                ml[c] = a.part_ml[(unit * SETS + s) * 32 + n];
+                const float4 *from = a.part_o + (unit * SETS * 16 + quarter * kPieces) * 64 + lane;
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) x[c][i] = from[i * 64];
             }
-        }
-        begin = end;
+            float top = M;
+#pragma unroll
+            for (int c = 0; c < N; ++c) top = fmaxf(top, ml[c].x);
+            const float old = __builtin_amdgcn_exp2f(M - top);
+            M = top;
+            L *= old;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) acc[i] = make_float4(acc[i].x * old, acc[i].y * old, acc[i].z * old, acc[i].w * old);
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                const float w = __builtin_amdgcn_exp2f(ml[c].x - top);
+                L += ml[c].y * w;
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i)
+                    acc[i] = make_float4(acc[i].x + x[c][i].x * w, acc[i].y + x[c][i].y * w, acc[i].z + x[c][i].z * w, acc[i].w + x[c][i].w * w);
+            }
+        };
+        while (__popcll(left) >= 4) take(std::integral_constant<int, 4>{});
+        if (__popcll(left) >= 2) take(std::integral_constant<int, 2>{});
+        if (left != 0) take(std::integral_constant<int, 1>{});
     }
-    const int row = p.m * kPromptRows + wave * 64 + s * 32 + n;
+    const int row = p.m * PromptShape<SETS>::kRows + wave * PromptShape<SETS>::kSetRows + s * 32 + n;
     if (row >= seq.nq) return;
     const float inv = 1.0f / L;
     const int64_t at = (int64_t)(seq.q_first + row) * a.Hq + p.head;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int dt = (quarter & 1) * 2 + i / 4, r4 = i & 3;
-        *reinterpret_cast<uint2 *>(a.out + at * kD + dt * 32 + r4 * 8 + half * 4) =
+    for (int i = 0; i < kPieces; ++i) {
+        const int piece = quarter * kPieces + i - 16 * s;
+        *reinterpret_cast<uint2 *>(a.out + at * kD + piece * 8 + half * 4) =
             L == 0.f ? make_uint2(0, 0) : make_uint2(pack_bf16x2(acc[i].x * inv, acc[i].y * inv), pack_bf16x2(acc[i].z * inv, acc[i].w * inv));
     }
-    if (a.lse != nullptr && half == 0 && (quarter & 1) == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
+    if (a.lse != nullptr && half == 0 && quarter * kPieces == 16 * s) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
 }
 
 // Blocks x heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each
-static int64_t prompt_blocks(const ihip_packed &p, int block = kPromptRows)
+static int64_t prompt_blocks(const ihip_packed &p, int rows)
 {
-    const int64_t by_rows = (int64_t)p.rows / block + p.B, by_len = (int64_t)p.B * ((p.max_q - 1) / block + 1);
+    const int64_t by_rows = (int64_t)p.rows / rows + p.B, by_len = (int64_t)p.B * ((p.max_q - 1) / rows + 1);
     return (by_rows < by_len ? by_rows : by_len) * p.Hq;
 }
-// How a call is done, from what the host knows of it: total tokens, keys and sequences.  The estimates are in tiles of 32 keys for a block of 256
-// queries (0.7 us, and 14 us for a launch): a launch takes as long as its longest block, or as the rounds of blocks that the compute units do
-// (blocks of the same length in whole rounds; a whole prompt's blocks, of all lengths up to the longest, fill the rounds), where a full chip
-// runs slower than a few blocks and each block begins and ends.  A block of 128 queries takes 0.6 of the time for the same keys: it
-// wins while there are too few blocks of 256.  Equal shares take the mean, and 50 tiles for beginnings, ends and the merge.
-// us with two sets / one / shares, 32 heads: 256 queries 18 / 16 / 40, 512 26 / 19 / 52, 1,024 37 / 26 / 52, 2,048 60 / 51 / 79, 3,000
-// 87 / 99 / 117, 8,192 476 / 545 / 537; 8 heads, 4,096 99 / 64 / 72; 512 on 4,608 keys 109 / 69 / 73; 200 on 8,200 180 / 114 / 81;
-// 16 heads, 1,500 on 13,500 and 700 on 20,700 438 / 353 / 269; 8 heads, 64 on 60,064 1,216 / 734 / 118.
-enum class PromptWay { kTwoSets, kOneSet, kShares };
-static PromptWay prompt_way(const ihip_packed &p, int64_t keys, bool scratch = true)
+// How a call is done: blocks by themselves (of 128 queries, one set a wave; 0 here), or equal shares with one set or two.  From what the host knows of
+// it, total tokens, keys and sequences, in units of 32 keys for 256 queries of one compute unit (0.7 us; a launch takes 14 us):
+// blocks by themselves take as long as the longest, or as the rounds of them that the compute units do (blocks of the same length in
+// whole rounds; a whole prompt's blocks, of all lengths up to the longest, fill the rounds), and each begins and ends.  Shares take the
+// mean, and some time for beginnings, ends and the merge: more of it with two sets, which read the keys half as often, but keep
+// twice as many queries that may not be there.  Of 56 calls the estimate takes the fastest on 55.
+// us by themselves / shares of one set / of two, 32 heads: 1,024 queries 26 / 49 / 51, 8,192 469 / 535 / 534; 64 on 2,064 keys 37 / 34 / 45; 200
+// on 8,200 111 / 81 / 82; 128, 256, 64 and 500 on 3,000 to 12,000 158 / 107 / 133; 8 heads, 64 on 60,064 752 / 121 / 117; 16 heads, 1,500 on
+// 13,500 and 700 on 20,700 328 / 292 / 273.  Blocks of two sets by themselves would be slower almost everywhere (1,024 queries 37, 20
+// times 333 90 against 61) and at best 3 % faster (16 heads, 8,192: 247 against 254).
+static int prompt_shares_of(const ihip_packed &p, int64_t keys)
 {
-    if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return PromptWay::kTwoSets;
+    if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return 0;
     const double cu = compute_units(), before = std::max<double>(0, (double)(keys - p.rows)) / p.B, mean = (double)p.rows / p.B;
-    const double longest = (before + p.max_q) / kTileKeys, tiles = (before + mean / 2) / kTileKeys, alike = before / (before + mean / 2);
+    const double longest = (before + p.max_q) / 32, tiles = (before + mean / 2) / 32, alike = before / (before + mean / 2);
     auto rounds_of = [&](int block) { return std::min<double>((double)prompt_blocks(p, block), ((double)p.rows / block + 0.5 * p.B) * p.Hq) / cu; };
-    auto whole = [&](int block, double per_tile, double busy) {
-        constexpr double fixed = 8;                  // tiles that a block's beginning and end take
-        const double rounds = rounds_of(block), filled = rounds + alike * (std::ceil(rounds) - rounds);
-        return std::max(per_tile * longest, busy * (per_tile * tiles + fixed) * filled - fixed);
-    };
-    const double two = whole(kPromptRows, 1, 1.3), one = whole(kPromptRows / 2, 0.6, 1.1), shares = 1.4 * tiles * rounds_of(kPromptRows) + 50;
-    if (scratch && shares < two && shares < one) return PromptWay::kShares;
-    return one < two ? PromptWay::kOneSet : PromptWay::kTwoSets;
+    const double one = rounds_of(128), two = rounds_of(256);
+    const double alone = std::max(0.55 * longest, (0.55 * tiles + 4) * (one + alike * (std::ceil(one) - one)) - 4);
+    const double shares1 = 0.8 * tiles * one + 25, shares2 = 1.3 * tiles * two + 40;
+    return alone <= shares1 && alone <= shares2 ? 0 : shares1 <= shares2 ? 1 : 2;
 }
+// Parts of all workgroups of a launch in shares: the same with one set and two
 static size_t prompt_part_bytes() { return (size_t)2 * compute_units() * kPromptWaves * 64 * (32 * sizeof(float4) + sizeof(float2)); }
+
+template <int SETS>
+static int32_t launch_shares(const char *who, PromptArgs &a, void *ws, hipStream_t st)
+{
+    typedef PromptShape<SETS> Shape;
+    static bool attr_set = Shape::kLds <= 65536;     // allow more than 64 KiB of dynamic LDS, once
+    if (!attr_set) {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<SETS, true>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::kLds);
+        attr_set = true;
+    }
+    const int n = Shape::kPerCu * compute_units();
+    a.part_o = (float4 *)ws;
+    a.part_ml = (float2 *)(a.part_o + (size_t)2 * n * kPromptWaves * SETS * 16 * 64);
+    {
+        KernelTimer timer("prompt_attn_shares", st);
+        hipLaunchKernelGGL((prompt_attn_kernel<SETS, true>), dim3(n), dim3(64 * kPromptWaves), Shape::kLds, st, a);
+    }
+    int32_t rc;
+    if ((rc = check_launch(who)) != IHIP_OK) return rc;
+    KernelTimer timer("prompt_merge", st);
+    hipLaunchKernelGGL(prompt_merge_kernel<SETS>, dim3(n, kPromptWaves), dim3(256), 0, st, a, n);
+    return check_launch(who);
+}
 
 }  // namespace ihip
 
@@ -658,7 +766,7 @@ using namespace ihip;
 extern "C" size_t ihip_prompt_attn_workspace_bytes(const ihip_packed *packed, int32_t rows_k)
 {
     if (check_packed("ihip_prompt_attn_workspace_bytes", packed) != IHIP_OK) return 0;
-    return prompt_way(*packed, rows_k) == PromptWay::kShares ? prompt_part_bytes() : 256;
+    return prompt_shares_of(*packed, rows_k) != 0 ? prompt_part_bytes() : 256;
 }
 
 extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v, const int32_t *cu_k,
@@ -687,35 +795,15 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     a.scale_log2e = sm_scale * 1.44269504088896340736f;
     a.out = (uint16_t *)out;
     a.lse = out_lse;
-    const PromptWay way = prompt_way(*packed, rows_k, ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes());
-    const bool one_set = way == PromptWay::kOneSet;
-    const int64_t groups = prompt_blocks(*packed, one_set ? kPromptRows / 2 : kPromptRows);
-    if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
     const hipStream_t st = (hipStream_t)stream;
-    const dim3 threads(64 * kPromptWaves);
-    constexpr int lds = kPromptStages * 4 * kTileEl * 2;       // with two sets half of it is the results'
-    static_assert(kPromptStages * 2 * kTileEl >= kPromptRows * kD, "the results of a block fit behind the stages");
-    static bool attr_set = false;        // allow more than 64 KiB of dynamic LDS, once
-    if (!attr_set) {
-        for (auto kernel : {&prompt_attn_kernel<2, false>, &prompt_attn_kernel<1, false>, &prompt_attn_kernel<2, true>})
-            (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        attr_set = true;
+    if (ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes()) {
+        const int sets = prompt_shares_of(*packed, rows_k);
+        if (sets != 0) return sets == 1 ? launch_shares<1>(who, a, ws, st) : launch_shares<2>(who, a, ws, st);
     }
-    if (way == PromptWay::kShares) {
-        const int n = compute_units();
-        a.part_o = (float4 *)ws;
-        a.part_ml = (float2 *)(a.part_o + (size_t)2 * n * kPromptWaves * 32 * 64);
-        {
-            KernelTimer timer("prompt_attn_shares", st);
-            hipLaunchKernelGGL((prompt_attn_kernel<2, true>), dim3(n), threads, lds, st, a);
-        }
-        if ((rc = check_launch(who)) != IHIP_OK) return rc;
-        KernelTimer timer("prompt_merge", st);
-        hipLaunchKernelGGL(prompt_merge_kernel, dim3(n, kPromptWaves), dim3(256), 0, st, a, n);
-        return check_launch(who);
-    }
+    typedef PromptShape<1> Shape;
+    const int64_t groups = prompt_blocks(*packed, Shape::kRows);
+    if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
     KernelTimer timer("prompt_attn", st);
-    if (one_set) hipLaunchKernelGGL((prompt_attn_kernel<1, false>), dim3((uint32_t)groups), threads, lds, st, a);
-    else hipLaunchKernelGGL((prompt_attn_kernel<2, false>), dim3((uint32_t)groups), threads, lds, st, a);
+    hipLaunchKernelGGL((prompt_attn_kernel<1, false>), dim3((uint32_t)groups), dim3(64 * kPromptWaves), Shape::kLds, st, a);
     return check_launch(who);
 }

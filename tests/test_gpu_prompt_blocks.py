@@ -1,4 +1,4 @@
-"""Prompt attention with more work than one round of blocks, which is done in blocks of 256 queries (smaller calls: 128): the same
+"""Prompt attention with more work than the chip holds at a time, in blocks that end inside and outside of tiles: the same
 corners and tolerances as for those (test_gpu_prompt_attn)."""
 import pytest
 import torch
