@@ -10,7 +10,9 @@
 //   output   v_mfma_f32_16x16x32_bf16 again, 16 heads x 32 keys x 16 dims, eight times: a lane's eight probabilities are its part of
 //            the left operand as they are, key 16 (i / 4) + 4 g + i % 4 for element i; for the right one it brings the
 //            four bytes of dims 8 n .. 8 n + 7 of the same keys, and column n of product j is dim 8 n + j.
-// Probabilities go in as bf16 (2^-9 of each, of either sign); the sum that divides takes them as they were.
+// Probabilities go in as bf16 (off by at most 2^-8 of each, either way); the sum that divides takes them as they were.
+// Bound by memory: 68 bytes a row.  32 sequences of 7,383 to 16,384 tokens, 8 KV heads, 416 MB, take 98 us with the merge, 91 without (4.6
+// TB/s; a copy of 4 GB moves 4.8); one of 4,099 5.4 us and 5.0 for the merge, which is a chain of latencies.
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>

@@ -1,6 +1,9 @@
 // Filling a KV cache with new tokens (rotated and quantised on the way) and reading it back as bf16.
 //
-// Both are one pass over memory: 16 lanes share a row of 128 elements, eight elements a lane.
+// Both are one pass over memory: 16 lanes share a row of 128 elements, eight elements a lane, so that a row is read and written in whole
+// lines and a scale's 32 elements are four neighbouring lanes.  Bound by memory: 7,937 tokens with 32 query and 8 KV heads into
+// bf16 pages, 172 MB, take 35 us (4.9 TB/s; a copy of 4 GB moves 4.8), 128K tokens of 8 heads out of 4 bits, 679 MB, 135 us
+// (5.0).  One token of each of 32 sequences takes 5.4 us, a chain of latencies: offsets, lengths, page, rows.
 #include "api_checks.h"
 #include "kv_store.h"
 #include <type_traits>

@@ -40,3 +40,19 @@ def test_scores_that_grow_and_shrink_along_the_keys(ihip):  # noqa: F811
     k[50] = q[600] * 4
     out, lse = ihip.prompt_attn(q, k, v, offsets([n]), n, want_lse=True)
     check(q, k, v, [n], [n], out, lse)
+
+
+@pytest.mark.parametrize("new", [
+    [1] * 4200,
+    [(i * 7919) % 131 for i in range(700)],
+    [0] * 100 + [300] + [0] * 200 + [128, 129, 1] + [0] * 90,
+    [0] * 65,
+    [256] + [0] * 64,
+])
+def test_many_sequences(ihip, new):  # noqa: F811
+    N = sum(new)
+    q, k, v = normal(1, N + 5, 4, D), normal(2, N + 5, 2, D), normal(3, N + 5, 2, D)
+    out, lse = torch.full_like(q, 5.0), torch.full((N + 5, 4), 5.0, device="cuda")
+    ihip.prompt_attn(q, k, v, offsets(new), max(new + [1]), out=out, lse=lse)
+    check(q, k, v, new, new, out, lse)
+    assert bool((out[N:] == 5).all()) and bool((lse[N:] == 5).all())
