@@ -46,6 +46,8 @@ struct PromptArgs {
     const uint16_t *q, *k, *v;
     int64_t q_sh, q_st, k_sh, k_st, v_sh, v_st;
     float scale_log2e;
+    bool ordered;                    // blocks by themselves: in the order of their keys; otherwise
+    int places;                      // of every sequence in the list of blocks, 0: as its rows are
     uint16_t *out;                   // [rows_q, Hq, d]
     float *lse;                      // [rows_q, Hq] or null
     // launches whose work is dealt out in equal shares: partial results of parts of blocks, two a workgroup
@@ -217,7 +219,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
         head = blockIdx.x % a.Hq;
         head = head % a.Hkv * a.G + head / a.Hkv;    // neighbours read different KV heads, on the XCD of their own if there are eight
         int ti = blockIdx.x / a.Hq;
-        if (a.B <= kOrderedSeqs) {
+        if (a.ordered) {
             // blocks in the order of their keys, a block's worth of them at a time: key class c of a sequence's block m is base + m
             const Seq q(a, min(lane, a.B - 1));
             const int blocks = lane < a.B ? q.blocks : 0, base = max(0, q.ahead) / kRows;
@@ -236,17 +238,26 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             m = lo - __builtin_amdgcn_readlane(base, b);
             seq = q.of_lane(b);
         } else {
-            // a sequence has the places from first row / kRows + b on, at least as many as it has blocks; its longest blocks come first
-            auto first_place = [&](int b) { return min(max(a.cu_q[b], 0), a.rows_q) / kRows + b; };
-            b = 0;
-            for (int range = a.B; range > 1;) {      // the last sequence whose places begin at or before ti, of b .. b + range - 1
-                const int step = (range + 63) / 64, at = lane * step;
-                const int c = __popcll(__ballot(lane == 0 || (at < range && first_place(b + at) <= ti))) - 1;
-                b += c * step;
-                range = min(step, range - c * step);
+            // a sequence's longest blocks come first, of as many places as the longest sequence needs ...
+            int at = ti % max(a.places, 1);
+            if (a.places > 0) {
+                b = ti / a.places;
+                seq = Seq(a, b).of_lane(0);
+            } else {
+                // ... or from first row / kRows + b on, where there are at least as many as it has blocks
+                b = 0;
+                for (int range = a.B, step = 2; step > 1;) {         // the last one whose places begin at or before ti, of b .. b + range - 1
+                    step = (range + 63) / 64;
+                    const int i = lane * step;
+                    const Seq q(a, min(b + i, a.B - 1));
+                    const int c = __popcll(__ballot(lane == 0 || (i < range && q.q_first / kRows + b + i <= ti))) - 1;
+                    b += c * step;
+                    range = min(step, range - c * step);
+                    seq = q.of_lane(c);
+                }
+                at = ti - seq.q_first / kRows - b;
             }
-            seq = Seq(a, b).of_lane(0);
-            m = __builtin_amdgcn_readfirstlane(seq.blocks - 1 - (ti - first_place(b)));
+            m = __builtin_amdgcn_readfirstlane(seq.blocks - 1 - at);
             if (m < 0 || m >= seq.blocks) return;
         }
     }
@@ -798,12 +809,11 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
     if (a.lse != nullptr && half == 0 && quarter * kPieces == 16 * s) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
 }
 
-// Blocks x heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each (where
-// blocks are found by their rows, all those places)
+// Blocks x heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each
 static int64_t prompt_blocks(const ihip_packed &p, int rows)
 {
     const int64_t by_rows = (int64_t)p.rows / rows + p.B, by_len = (int64_t)p.B * ((p.max_q - 1) / rows + 1);
-    return (p.B > kOrderedSeqs || by_rows < by_len ? by_rows : by_len) * p.Hq;
+    return std::min(by_rows, by_len) * p.Hq;
 }
 // How a call is done: blocks by themselves (of 128 queries, one set a wave; 0 here), or equal shares with one set or two.  From what the host knows of
 // it, total tokens, keys and sequences, in units of 32 keys for 256 queries of one compute unit (0.7 us; a launch takes 14 us):
@@ -896,7 +906,11 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     typedef PromptShape<1> Shape;
     // (A workgroup a block, handed out by the hardware.  512 that stay, each with every 512th block and the first tiles of its next one
     // on their way under the end of the present one: 8 prompts of 640 to 2,048 172 -> 185 us, one of 32,768 7.17 -> 7.52 ms.)
+    // The order of the blocks matters where some compute unit has two.  Finding them without it is shorter: 512 queries, 32 heads 18.5 -> 17.6 us
     const int64_t groups = prompt_blocks(*packed, Shape::kRows);
+    a.ordered = packed->B <= kOrderedSeqs && groups > compute_units();
+    const int places = (packed->max_q - 1) / Shape::kRows + 1;
+    a.places = groups == (int64_t)places * packed->B * packed->Hq ? places : 0;
     if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
     KernelTimer timer("prompt_attn", st);
     hipLaunchKernelGGL((prompt_attn_kernel<1, false>), dim3((uint32_t)groups), dim3(64 * kPromptWaves), Shape::kLds, st, a);
