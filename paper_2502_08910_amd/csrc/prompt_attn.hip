@@ -529,24 +529,28 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
 #pragma unroll
             for (int i = 0; i < 8; ++i) exponentials(0, i, false, 0);
             __syncthreads();                                 // K(0) has been read
+            // This wave's last tile with a key that one of its queries sees.  Behind it, it only keeps the others company: the matrix units are
+            // the other workgroup's meanwhile
+            const int last_seen = min(row0 + Shape::kSetRows, nq) - 1 + ahead - tile0 * kTileKeys;
+            const int mine = row0 >= nq ? 1 : min(max(last_seen, 0) / kTileKeys + 1, n_tiles), unmasked = min(seen, mine);
             int t = 0;
             if constexpr (SETS == 2) {
                 first_operands(0, 1);
-                for (; t + 4 < seen; t += 4) {
+                for (; t + 4 < unmasked; t += 4) {
                     period_of_sets(0, 1, 2, 3, t, false);
                     period_of_sets(1, 2, 3, 0, t + 1, false);
                     period_of_sets(2, 3, 0, 1, t + 2, false);
                     period_of_sets(3, 0, 1, 2, t + 3, false);
                 }
-                for (; t + 1 < n_tiles; ++t) period_of_sets(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t, true);
+                for (; t + 1 < mine; ++t) period_of_sets(t & 3, (t + 1) & 3, (t + 2) & 3, (t + 3) & 3, t, true);
             } else {
-                for (; t + 2 < seen; t += 2) {
+                for (; t + 2 < unmasked; t += 2) {
                     period_of_halves(0, t, false);
                     period_of_halves(1, t + 1, false);
                 }
-                for (; t + 1 < n_tiles; ++t) period_of_halves(t & 1, t, true);
+                for (; t + 1 < mine; ++t) period_of_halves(t & 1, t, true);
             }
-            // the last tile, whose first products are done
+            // its last tile, whose first products are done
             const uint32_t bits = hidden_keys(t, 1);
 #pragma unroll
             for (int i = 0; i < 8; ++i) exponentials(1, i, true, bits);
@@ -554,6 +558,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             for (int c = 0; c < 16; ++c) {                   // two sets: both products of an operand; one: one half after the other
                 const int s = SETS == 2 ? c & 1 : c >> 3, i = SETS == 2 ? c >> 1 : c & 7;
                 product(s, i, v_operand(t & (kStages - 1), s, i), probabilities(s, i >> 2));
+            }
+            for (; t + 1 < n_tiles; ++t) {
+                request_k(t & (kStages - 1));
+                request_v((t + kStages - 1) & (kStages - 1));
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(SETS == 2 ? 2 * kLoads : 0) : "memory");
+                __syncthreads();
             }
             settle();
             // Where a row's sum says that its scores left that range, or a result is not finite, the block is done again, a tile at a time and
