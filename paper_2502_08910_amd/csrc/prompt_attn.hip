@@ -45,7 +45,7 @@ struct PromptArgs {
     const int32_t *cu_q, *cu_k;
     const uint16_t *q, *k, *v;
     int64_t q_sh, q_st, k_sh, k_st, v_sh, v_st;
-    float scale_log2e;
+    float scale_log2e, inv_G;
     bool ordered;                    // blocks by themselves: in the order of their keys; otherwise
     int places;                      // of every sequence in the list of blocks, 0: as its rows are
     uint16_t *out;                   // [rows_q, Hq, d]
@@ -61,25 +61,27 @@ struct PromptArgs {
 // parts of a block.  The list goes head by head (the query heads of a KV head next to each other), sequence by sequence, block by
 // block; a block weighs its tiles and kBlockCost for its beginning and end.
 
+// A sequence and its blocks of rows.  A row is a query, or, where `pack` query heads go together, one head of a query: row query * pack + head
 template <int SETS>
 struct PromptSeq {
     typedef PromptShape<SETS> Shape;
-    int q_first, nq, k_first, nk;
-    int ahead, blocks, ahead_tiles;
+    int q_first, nq, k_first, nk, pack;
+    int ahead, rows, blocks;
     __device__ PromptSeq() {}
-    __device__ PromptSeq(const PromptArgs &a, int b)
+    __device__ PromptSeq(const PromptArgs &a, int b, int pack_ = 1)
     {
         q_first = min(max(a.cu_q[b], 0), a.rows_q);
         nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
         k_first = min(max(a.cu_k[b], 0), a.rows_k);
         nk = min(max(a.cu_k[b + 1], k_first), a.rows_k) - k_first;
+        pack = pack_;
         derive();
     }
     __device__ void derive()
     {
         ahead = nk - nq;                             // query i sees keys 0 .. i + ahead
-        blocks = (nq + Shape::kRows - 1) / Shape::kRows;
-        ahead_tiles = (ahead + Shape::kKeys - 1) >> (SETS == 2 ? 5 : 6);  // rounded up, also below 0
+        rows = nq * pack;
+        blocks = (rows + Shape::kRows - 1) / Shape::kRows;
     }
     __device__ PromptSeq of_lane(int l) const        // that of lane l, in all lanes
     {
@@ -88,16 +90,18 @@ struct PromptSeq {
         r.nq = __builtin_amdgcn_readlane(nq, l);
         r.k_first = __builtin_amdgcn_readlane(k_first, l);
         r.nk = __builtin_amdgcn_readlane(nk, l);
+        r.pack = pack;
         r.derive();
         return r;
     }
-    __device__ int tiles(int m) const
+    __device__ int tiles(int m) const                // up to the last key that the block's last query sees
     {
-        return m + 1 < blocks ? max(0, Shape::kRows / Shape::kKeys * (m + 1) + ahead_tiles) : (nk + Shape::kKeys - 1) / Shape::kKeys;
+        return (max(0, (min((m + 1) * Shape::kRows, rows) - 1) / pack + 1 + ahead) + Shape::kKeys - 1) / Shape::kKeys;
     }
-    __device__ int64_t weight_before(int m) const    // of blocks 0 .. m - 1, m < blocks
+    __device__ int64_t weight_before(int m) const    // of blocks 0 .. m - 1, m < blocks; shares: pack is 1
     {
         constexpr int per = Shape::kRows / Shape::kKeys;
+        const int ahead_tiles = (ahead + Shape::kKeys - 1) >> (SETS == 2 ? 5 : 6);       // rounded up, also below 0
         const int none = min(m, ahead_tiles < 0 ? -ahead_tiles / per : 0);        // blocks whose queries see nothing
         auto sum = [&](int64_t c) { return per / 2 * c * (c + 1) + ahead_tiles * c; };
         return sum(m) - sum(none) + (int64_t)Shape::kBlockCost * m;
@@ -198,6 +202,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
     uint16_t *const rows = smem + (SETS == 2 ? kStages * 2 * kEl : 0) + wave * Shape::kSetRows * kD;       // this wave's results on their way out
 
     // which head, which sequence, which of its blocks, which tiles of the block
+    const int pack = SHARES ? 1 : a.G;               // query heads that go together; `head` is then the KV head
     int head, b = -1, m = 0, tile0 = 0, tile1 = 0, share = 0;
     PromptPlace end{};
     Seq seq;
@@ -216,13 +221,14 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
         end.m = __builtin_amdgcn_readfirstlane(end.m);
         end.tile = __builtin_amdgcn_readfirstlane(end.tile);
     } else {
-        head = blockIdx.x % a.Hq;
-        head = head % a.Hkv * a.G + head / a.Hkv;    // neighbours read different KV heads, on the XCD of their own if there are eight
-        int ti = blockIdx.x / a.Hq;
+        // The query heads of a KV head go together: fewer keys that only some rows of a block see, and less of the last block is empty.
+        // Neighbours read different KV heads, on the XCD of their own if there are eight.
+        head = blockIdx.x % a.Hkv;
+        int ti = blockIdx.x / a.Hkv;
         if (a.ordered) {
             // blocks in the order of their keys, a block's worth of them at a time: key class c of a sequence's block m is base + m
-            const Seq q(a, min(lane, a.B - 1));
-            const int blocks = lane < a.B ? q.blocks : 0, base = max(0, q.ahead) / kRows;
+            const Seq q(a, min(lane, a.B - 1), pack);
+            const int blocks = lane < a.B ? q.blocks : 0, base = (int)min((int64_t)max(0, q.ahead) * pack / kRows, (int64_t)1 << 30);
             auto at_least = [&](int c) { return (int)wave_sum_u32((uint32_t)min(max(base + blocks - c, 0), blocks)); };
             if (ti >= at_least(0)) return;
             int lo = 0, hi = (int)wave_reduce_bits((uint32_t)(base + blocks), [](uint32_t x, uint32_t y) { return max(x, y); });
@@ -242,20 +248,20 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             int at = ti % max(a.places, 1);
             if (a.places > 0) {
                 b = ti / a.places;
-                seq = Seq(a, b).of_lane(0);
+                seq = Seq(a, b, pack).of_lane(0);
             } else {
                 // ... or from first row / kRows + b on, where there are at least as many as it has blocks
                 b = 0;
                 for (int range = a.B, step = 2; step > 1;) {         // the last one whose places begin at or before ti, of b .. b + range - 1
                     step = (range + 63) / 64;
                     const int i = lane * step;
-                    const Seq q(a, min(b + i, a.B - 1));
-                    const int c = __popcll(__ballot(lane == 0 || (i < range && q.q_first / kRows + b + i <= ti))) - 1;
+                    const Seq q(a, min(b + i, a.B - 1), pack);
+                    const int c = __popcll(__ballot(lane == 0 || (i < range && q.q_first * pack / kRows + b + i <= ti))) - 1;
                     b += c * step;
                     range = min(step, range - c * step);
                     seq = q.of_lane(c);
                 }
-                at = ti - seq.q_first / kRows - b;
+                at = ti - seq.q_first * pack / kRows - b;
             }
             m = __builtin_amdgcn_readfirstlane(seq.blocks - 1 - at);
             if (m < 0 || m >= seq.blocks) return;
@@ -268,41 +274,60 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
         m = __builtin_amdgcn_readfirstlane(m);
         tile0 = __builtin_amdgcn_readfirstlane(tile0);
         if (SHARES) seq = Seq(a, b).of_lane(0);
-        const int nq = seq.nq, nk = seq.nk, ahead = seq.ahead;
+        const int nk = seq.nk, ahead = seq.ahead, n_rows = seq.rows;
+        // the query of row i of the block, and how far its head is from the block's first
+        const int query0 = m * kRows / pack, over0 = m * kRows % pack;
+        const int head0 = SHARES ? head : head * pack;
+        auto query_of = [&](int i, int &of) {
+            if (SHARES) {
+                of = 0;
+                return m * kRows + i;
+            }
+            const int q = (int)((i + over0 + 0.5f) * a.inv_G);       // (less than 2^21 of them: exact)
+            of = i + over0 - q * pack;
+            return query0 + q;
+        };
         const int all_tiles = __builtin_amdgcn_readfirstlane(seq.tiles(m));
         const bool is_end = SHARES && __builtin_amdgcn_readfirstlane((int)(head == end.head && b == end.b && m == end.m)) != 0;
         tile1 = __builtin_amdgcn_readfirstlane(is_end ? end.tile : all_tiles);
         if (all_tiles == 0 && !is_end) {                 // queries without keys
-            for (int i = tid; i < min(kRows, nq - m * kRows) * kRowLanes; i += 64 * kPromptWaves) {
-                const int64_t at = (int64_t)(seq.q_first + m * kRows + i / kRowLanes) * a.Hq + head;
+            for (int i = tid; i < min(kRows, n_rows - m * kRows) * kRowLanes; i += 64 * kPromptWaves) {
+                int of;
+                const int q = query_of(i / kRowLanes, of);
+                const int64_t at = (int64_t)(seq.q_first + q) * a.Hq + head0 + of;
                 reinterpret_cast<uint4 *>(a.out + at * kD)[i % kRowLanes] = make_uint4(0, 0, 0, 0);
                 if (a.lse != nullptr && i % kRowLanes == 0) a.lse[at] = -INFINITY;
             }
         } else if (tile0 < tile1) {
-            const int h = head, g = h / a.G;
-            const int row0 = m * kRows + wave * Shape::kSetRows;           // this wave's first query
+            const int g = SHARES ? head / a.G : head;
+            const int row0 = m * kRows + wave * Shape::kSetRows;           // this wave's first row
             const int n_tiles = tile1 - tile0;               // of this part, numbered from its first
-            // Work goes in two turns s, for the two sets of queries or the two halves of a tile: their queries, first query and first key
+            // Work goes in two turns s, for the two sets of queries or the two halves of a tile: their queries, first row and first key
             auto qs = [](int s) { return SETS == 2 ? s : 0; };
-            auto query0 = [](int s) { return SETS == 2 ? 32 * s : 0; };
+            auto set0 = [](int s) { return SETS == 2 ? 32 * s : 0; };
             auto key0 = [](int s) { return SETS == 2 ? 0 : 32 * s; };
 
             bf16x8 qb[SETS][8];
             int last_key[SETS];
 #pragma unroll
-            for (int s = 0; s < SETS; ++s) last_key[s] = min(row0 + s * 32 + n, nq - 1) + ahead - tile0 * kTileKeys;
+            for (int s = 0; s < SETS; ++s) {
+                int of;
+                last_key[s] = query_of(min(wave * Shape::kSetRows + s * 32 + n, n_rows - 1 - m * kRows), of) + ahead - tile0 * kTileKeys;
+            }
             auto load_queries = [&] {
                 int l = lane;                                // (not known to be it: what follows from it is computed here, not kept in registers all along)
                 asm volatile("" : "+v"(l));
                 const int n = l & 31, half = l >> 5;
 #pragma unroll
                 for (int s = 0; s < SETS; ++s) {
-                    const uint16_t *qp = a.q + (int64_t)(seq.q_first + min(row0 + s * 32 + n, nq - 1)) * a.q_st + h * a.q_sh + half * 8;
+                    int of;
+                    const int q = query_of(min(wave * Shape::kSetRows + s * 32 + n, n_rows - 1 - m * kRows), of);
+                    const uint16_t *qp = a.q + (int64_t)(seq.q_first + q) * a.q_st + (head0 + of) * a.q_sh + half * 8;
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) qb[s][ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 16);
                 }
             };
-            const int first_last = row0 + ahead - tile0 * kTileKeys;       // the last key of the wave's first query
+            const int first_last = row0 / pack + ahead - tile0 * kTileKeys;          // the last key of the wave's first row
             const int keys_here = nk - tile0 * kTileKeys;
             const uint16_t *kb = a.k + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.k_st + g * a.k_sh;
             const uint16_t *vb = a.v + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.v_st + g * a.v_sh;
@@ -377,7 +402,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 return __int_as_float((hidden & __float_as_int(-INFINITY)) | (~hidden & __float_as_int(x)));
             };
             auto mask = [&](int tile, int s) {
-                if (tile * kTileKeys + key0(s) + 31 <= first_last + query0(s)) return;
+                if (tile * kTileKeys + key0(s) + 31 <= first_last + set0(s)) return;
                 const uint32_t bits = hidden_keys(tile, s);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sc[s][r] = hide(bits, r, sc[s][r]);
@@ -508,7 +533,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 }
             };
             // tiles that all queries of the block see whole; behind them scores are masked, under the matrix instructions as well
-            const int seen = min(n_tiles, (m * kRows + ahead + 1) / kTileKeys - tile0);
+            const int seen = min(n_tiles, (query0 + ahead + 1) / kTileKeys - tile0);
 
             // Exponentials are taken against the row's maximum over the first tile (which holds a key of every query that has any), not
             // against a running one: bf16 and fp32 have exponents to spare, nothing is lost while the scores stay within 2^64 of it.
@@ -531,8 +556,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             __syncthreads();                                 // K(0) has been read
             // This wave's last tile with a key that one of its queries sees.  Behind it, it only keeps the others company: the matrix units are
             // the other workgroup's meanwhile
-            const int last_seen = min(row0 + Shape::kSetRows, nq) - 1 + ahead - tile0 * kTileKeys;
-            const int mine = row0 >= nq ? 1 : min(max(last_seen, 0) / kTileKeys + 1, n_tiles), unmasked = min(seen, mine);
+            const int last_seen = (min(row0 + Shape::kSetRows, n_rows) - 1) / pack + ahead - tile0 * kTileKeys;
+            const int mine = row0 >= n_rows ? 1 : min(max(last_seen, 0) / kTileKeys + 1, n_tiles), unmasked = min(seen, mine);
             int t = 0;
             if constexpr (SETS == 2) {
                 first_operands(0, 1);
@@ -697,7 +722,6 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 const int n = l & 31, half = l >> 5;
 #pragma unroll
                 for (int s = 0; s < SETS; ++s) {
-                    const int row = row0 + s * 32 + n;
                     const float inv = l_run[s] == 0.f ? 0.f : 1.0f / l_run[s];             // (a query without keys: 0)
 #pragma unroll
                     for (int dt = 0; dt < 4; ++dt)
@@ -705,20 +729,26 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                         for (int r4 = 0; r4 < 4; ++r4)
                             *reinterpret_cast<uint2 *>(rows + (s * 32 + n) * kD + (((dt * 4 + r4) ^ (n & 15)) << 3) + half * 4) =
                                 make_uint2(pack_bf16x2(o[s][dt][r4 * 4] * inv, o[s][dt][r4 * 4 + 1] * inv), pack_bf16x2(o[s][dt][r4 * 4 + 2] * inv, o[s][dt][r4 * 4 + 3] * inv));
-                    if (a.lse != nullptr && half == 0 && row < nq)
-                        a.lse[(int64_t)(seq.q_first + row) * a.Hq + h] = l_run[s] == 0.f ? -INFINITY : (m_ref[s] + log2f(l_run[s])) * 0.69314718055994530942f;
+                    int of;
+                    const int q = query_of(wave * Shape::kSetRows + s * 32 + n, of);
+                    if (a.lse != nullptr && half == 0 && row0 + s * 32 + n < n_rows)
+                        a.lse[(int64_t)(seq.q_first + q) * a.Hq + head0 + of] = l_run[s] == 0.f ? -INFINITY : (m_ref[s] + log2f(l_run[s])) * 0.69314718055994530942f;
                 }
                 asm volatile("" ::: "memory");                   // lanes read what other lanes of the wave wrote (LDS keeps the order)
-                uint16_t *out = a.out + ((int64_t)(seq.q_first + row0) * a.Hq + h) * kD;
-                const int64_t step = (int64_t)4 * a.Hq * kD;     // four rows
-                const int64_t mine = (int64_t)(l >> 4) * a.Hq * kD + (l & 15) * 8;
-                auto row_piece = [&](int i) { return *reinterpret_cast<const uint4 *>(rows + (4 * i + (l >> 4)) * kD + (((l & 15) ^ (4 * (i & 3) + (l >> 4))) << 3)); };
-                if (row0 + Shape::kSetRows <= nq) {
+                // four rows at a time: 4 / pack queries and 4 % pack heads further, or a query more and as many heads less
+                const int row = l >> 4, slot = l & 15;
+                int of;
+                const int q = query_of(wave * Shape::kSetRows + row, of);
+                uint16_t *out = a.out + ((int64_t)(seq.q_first + query0) * a.Hq + head0) * kD;
+                int at = ((q - query0) * a.Hq + of) * kD + slot * 8;
+                const int heads = 4 % pack, step = (4 / pack * a.Hq + heads) * kD, wrap = (a.Hq - pack) * kD;
+                auto row_piece = [&](int i) { return *reinterpret_cast<const uint4 *>(rows + (4 * i + row) * kD + ((slot ^ (4 * (i & 3) + row)) << 3)); };
 #pragma unroll
-                    for (int i = 0; i < Shape::kSetRows / 4; ++i) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
-                } else {
-                    for (int i = 0; i < Shape::kSetRows / 4; ++i)
-                        if (row0 + 4 * i + (l >> 4) < nq) *reinterpret_cast<uint4 *>(out + i * step + mine) = row_piece(i);
+                for (int i = 0; i < Shape::kSetRows / 4; ++i) {
+                    if (row0 + Shape::kSetRows <= n_rows || row0 + 4 * i + row < n_rows) *reinterpret_cast<uint4 *>(out + at) = row_piece(i);
+                    of += heads;
+                    at += step + (of >= pack ? wrap : 0);
+                    of -= of >= pack ? pack : 0;
                 }
             }
         }
@@ -820,30 +850,34 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
 }
 
 // Blocks x heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each
-static int64_t prompt_blocks(const ihip_packed &p, int rows)
+static int64_t prompt_blocks(const ihip_packed &p, int block, int pack)
 {
-    const int64_t by_rows = (int64_t)p.rows / rows + p.B, by_len = (int64_t)p.B * ((p.max_q - 1) / rows + 1);
-    return std::min(by_rows, by_len) * p.Hq;
+    const int64_t by_rows = (int64_t)p.rows * pack / block + p.B, by_len = p.B * (((int64_t)p.max_q * pack - 1) / block + 1);
+    return std::min(by_rows, by_len) * (p.Hq / pack);
 }
-// How a call is done: blocks by themselves (of 128 queries, one set a wave; 0 here), or equal shares with one set or two.  From what the host knows of
+// How a call is done: blocks by themselves (of 128 rows, one set a wave; 0 here), or equal shares with one set or two.  From what the host knows of
 // it, total tokens, keys and sequences, in units of 32 keys for 256 queries of one compute unit (0.7 us; a launch takes 14 us):
 // blocks by themselves take as long as the longest, or as the rounds of them that the compute units do (blocks of the same length in
 // whole rounds; a whole prompt's blocks, of all lengths up to the longest, fill the rounds), and each begins and ends.  Shares take the
 // mean, and some time for beginnings, ends and the merge: more of it with two sets, which read the keys half as often, but keep
-// twice as many queries that may not be there.  Of 56 calls the estimate takes the fastest on 55.
-// us by themselves / shares of one set / of two, 32 heads: 1,024 queries 26 / 49 / 51, 8,192 469 / 535 / 534; 64 on 2,064 keys 37 / 34 / 45; 200
-// on 8,200 111 / 81 / 82; 128, 256, 64 and 500 on 3,000 to 12,000 158 / 107 / 133; 8 heads, 64 on 60,064 752 / 121 / 117; 16 heads, 1,500 on
-// 13,500 and 700 on 20,700 328 / 292 / 273.  Blocks of two sets by themselves would be slower almost everywhere (1,024 queries 37, 20
-// times 333 90 against 61) and at best 3 % faster (16 heads, 8,192: 247 against 254).
+// twice as many queries that may not be there.  The longest of several sequences with keys ahead is not known; it is taken for 2.5 times the
+// mean, since shares cost a little where all are alike and the others a lot where they are not.  Of 58 calls the estimate takes the fastest
+// on 56, and what is 11 and 15 % slower on two.
+// us by themselves / shares of one set / of two, 32 heads on 8: 1,024 queries 24 / 47 / 50, 8,192 476 / 538 / 535; 64 on 2,064 keys 36 / 35 / 45; 200
+// on 8,200 109 / 79 / 81; 128, 256, 64 and 500 on 3,000 to 12,000 156 / 102 / 124; 8 heads, 64 on 60,064 694 / 119 / 107; 16 heads, 1,500 on
+// 13,500 and 700 on 20,700 327 / 286 / 267.  Blocks of two sets by themselves would be slower almost everywhere (1,024 queries 37, 20
+// times 333 90 against 48) and at best 3 % faster (16 heads, 8,192: 247 against 256).
 static int prompt_shares_of(const ihip_packed &p, int64_t keys)
 {
     if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return 0;
     const double cu = compute_units(), before = std::max<double>(0, (double)(keys - p.rows)) / p.B, mean = (double)p.rows / p.B;
-    const double longest = (before + p.max_q) / 32, tiles = (before + mean / 2) / 32, alike = before / (before + mean / 2);
-    auto rounds_of = [&](int block) { return std::min<double>((double)prompt_blocks(p, block), ((double)p.rows / block + 0.5 * p.B) * p.Hq) / cu; };
-    const double one = rounds_of(128), two = rounds_of(256);
-    const double alone = std::max(0.55 * longest, (0.55 * tiles + 4) * (one + alike * (std::ceil(one) - one)) - 4);
-    const double shares1 = 0.8 * tiles * one + 25, shares2 = 1.3 * tiles * two + 40;
+    const double longest = ((p.B > 1 ? 2.5 : 1) * before + p.max_q) / 32, tiles = (before + mean / 2) / 32, alike = before / (before + mean / 2);
+    auto rounds_of = [&](int block, int pack) {
+        return std::min((double)prompt_blocks(p, block, pack), ((double)p.rows * pack / block + 0.5 * p.B) * p.Hq / pack) / cu;
+    };
+    const double by_itself = rounds_of(128, p.Hq / p.Hkv);
+    const double alone = std::max(0.55 * longest, (0.55 * tiles + 5) * (by_itself + alike * (std::ceil(by_itself) - by_itself)) - 5);
+    const double shares1 = (0.8 * tiles + 3) * rounds_of(128, 1) + 25, shares2 = (1.3 * tiles + 6) * rounds_of(256, 1) + 35;
     return alone <= shares1 && alone <= shares2 ? 0 : shares1 <= shares2 ? 1 : 2;
 }
 // Parts of all workgroups of a launch in shares: the same with one set and two
@@ -906,6 +940,7 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     if ((a.q_st | a.k_st | a.v_st) < 0 || a.q_st >= (1 << 24) || a.k_st >= (1 << 24) || a.v_st >= (1 << 24))
         return fail(IHIP_ERR_UNSUPPORTED, "%s: rows of q, k and v must be less than 2^24 elements apart", who);
     a.scale_log2e = sm_scale * 1.44269504088896340736f;
+    a.inv_G = 1.0f / a.G;
     a.out = (uint16_t *)out;
     a.lse = out_lse;
     const hipStream_t st = (hipStream_t)stream;
@@ -917,10 +952,10 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     // (A workgroup a block, handed out by the hardware.  512 that stay, each with every 512th block and the first tiles of its next one
     // on their way under the end of the present one: 8 prompts of 640 to 2,048 172 -> 185 us, one of 32,768 7.17 -> 7.52 ms.)
     // The order of the blocks matters where some compute unit has two.  Finding them without it is shorter: 512 queries, 32 heads 18.5 -> 17.6 us
-    const int64_t groups = prompt_blocks(*packed, Shape::kRows);
+    const int64_t groups = prompt_blocks(*packed, Shape::kRows, a.G);
     a.ordered = packed->B <= kOrderedSeqs && groups > compute_units();
-    const int places = (packed->max_q - 1) / Shape::kRows + 1;
-    a.places = groups == (int64_t)places * packed->B * packed->Hq ? places : 0;
+    const int64_t places = ((int64_t)packed->max_q * a.G - 1) / Shape::kRows + 1;
+    a.places = groups == places * packed->B * packed->Hkv ? (int)places : 0;
     if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
     KernelTimer timer("prompt_attn", st);
     hipLaunchKernelGGL((prompt_attn_kernel<1, false>), dim3((uint32_t)groups), dim3(64 * kPromptWaves), Shape::kLds, st, a);
