@@ -21,9 +21,9 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPromptWaves = 4;
 
-// A wave has one or two sets of 32 queries.  With two, a workgroup has a compute unit to itself (512 registers a lane) and what is read
-// from LDS serves two matrix instructions; tiles have 32 keys.  With one, two workgroups share a compute unit, each under the beginnings, ends
-// and waits of the other; tiles have 64 keys, whose two halves take the place of the two sets.
+// A wave has one or two sets of 32 rows.  With one, two workgroups share a compute unit, each under the beginnings, ends and waits of the
+// other; tiles have 64 keys, whose two halves take the place of two sets.  With two, a workgroup has a compute unit to itself (512 registers a
+// lane), what is read from LDS serves two matrix instructions, and the keys are read half as often; tiles have 32 keys.
 template <int SETS>
 struct PromptShape {
     static constexpr int kSetRows = 32 * SETS, kRows = kSetRows * kPromptWaves;          // queries of a wave and of a workgroup
@@ -32,7 +32,7 @@ struct PromptShape {
     static constexpr int kStages = SETS == 2 ? 4 : 2;                                    // tiles of K, and of V, in LDS
     static constexpr int kLds = (kStages * 2 * kEl + (SETS == 2 ? kRows * kD : 0)) * 2;  // bytes; behind the tiles, or in their place: the results
     // shares, in tiles: a block's beginning and end, the smallest part of one, the smallest share
-    static constexpr int kBlockCost = 2 + SETS, kMinPart = 2 * SETS, kMinShare = 6 * SETS;
+    static constexpr int kBlockCost = 4, kMinPart = 4, kMinShare = 12;
 };
 constexpr int kOrderedSeqs = 64;                     // up to so many sequences, one a lane, blocks go in the order of their keys
 constexpr float kNegBigPrompt = -1.0e30f;            // finite stand-in for -inf in maxima
@@ -45,7 +45,8 @@ struct PromptArgs {
     const int32_t *cu_q, *cu_k;
     const uint16_t *q, *k, *v;
     int64_t q_sh, q_st, k_sh, k_st, v_sh, v_st;
-    float scale_log2e, inv_G;
+    int log2_G;                      // -1: G is not a power of two
+    float scale_log2e;
     bool ordered;                    // blocks by themselves: in the order of their keys; otherwise
     int places;                      // of every sequence in the list of blocks, 0: as its rows are
     uint16_t *out;                   // [rows_q, Hq, d]
@@ -58,29 +59,31 @@ struct PromptArgs {
 // ---- shares ------------------------------------------------------------------
 // Where there are too few blocks x heads to keep the compute units busy to the end, the tiles of all blocks are dealt out in equal
 // shares, one to each workgroup that the chip holds at a time, which begin and end inside blocks; a second kernel merges the
-// parts of a block.  The list goes head by head (the query heads of a KV head next to each other), sequence by sequence, block by
+// parts of a block.  The list goes KV head by KV head, sequence by sequence, block by
 // block; a block weighs its tiles and kBlockCost for its beginning and end.
 
-// A sequence and its blocks of rows.  A row is a query, or, where `pack` query heads go together, one head of a query: row query * pack + head
+// A sequence and its blocks of rows.  The G query heads of a KV head go together: row query * G + head.  Fewer keys that only some rows of a
+// block see, fuller last blocks, and keys are read once for all of them.
 template <int SETS>
 struct PromptSeq {
     typedef PromptShape<SETS> Shape;
-    int q_first, nq, k_first, nk, pack;
+    int q_first, nq, k_first, nk, G, log2_G;
     int ahead, rows, blocks;
     __device__ PromptSeq() {}
-    __device__ PromptSeq(const PromptArgs &a, int b, int pack_ = 1)
+    __device__ PromptSeq(const PromptArgs &a, int b)
     {
         q_first = min(max(a.cu_q[b], 0), a.rows_q);
         nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
         k_first = min(max(a.cu_k[b], 0), a.rows_k);
         nk = min(max(a.cu_k[b + 1], k_first), a.rows_k) - k_first;
-        pack = pack_;
+        G = a.G;
+        log2_G = a.log2_G;
         derive();
     }
     __device__ void derive()
     {
         ahead = nk - nq;                             // query i sees keys 0 .. i + ahead
-        rows = nq * pack;
+        rows = nq * G;
         blocks = (rows + Shape::kRows - 1) / Shape::kRows;
     }
     __device__ PromptSeq of_lane(int l) const        // that of lane l, in all lanes
@@ -90,23 +93,26 @@ struct PromptSeq {
         r.nq = __builtin_amdgcn_readlane(nq, l);
         r.k_first = __builtin_amdgcn_readlane(k_first, l);
         r.nk = __builtin_amdgcn_readlane(nk, l);
-        r.pack = pack;
+        r.G = G;
+        r.log2_G = log2_G;
         r.derive();
         return r;
     }
+    __device__ int query(int row) const { return log2_G >= 0 ? row >> log2_G : row / G; }
     __device__ int tiles(int m) const                // up to the last key that the block's last query sees
     {
-        return (max(0, (min((m + 1) * Shape::kRows, rows) - 1) / pack + 1 + ahead) + Shape::kKeys - 1) / Shape::kKeys;
+        return (max(0, query(min((m + 1) * Shape::kRows, rows) - 1) + 1 + ahead) + Shape::kKeys - 1) / Shape::kKeys;
     }
-    __device__ int64_t weight_before(int m) const    // of blocks 0 .. m - 1, m < blocks; shares: pack is 1
+    // Weight of blocks 0 .. m - 1, m <= blocks: the sum of (ahead + kKeys + kRows (j + 1) / G) / kKeys, which is no less than tiles(j), where
+    // that is positive, rounded down, and kBlockCost for each: with that a block weighs no less than its tiles and kBlockCost
+    __device__ int64_t weight_before(int m) const
     {
-        constexpr int per = Shape::kRows / Shape::kKeys;
-        const int ahead_tiles = (ahead + Shape::kKeys - 1) >> (SETS == 2 ? 5 : 6);       // rounded up, also below 0
-        const int none = min(m, ahead_tiles < 0 ? -ahead_tiles / per : 0);        // blocks whose queries see nothing
-        auto sum = [&](int64_t c) { return per / 2 * c * (c + 1) + ahead_tiles * c; };
-        return sum(m) - sum(none) + (int64_t)Shape::kBlockCost * m;
+        const int64_t first = ahead + Shape::kKeys, none = first >= 0 ? 0 : min((int64_t)m, -first * G / Shape::kRows);
+        const int64_t sum = 2 * G * first * (m - none) + Shape::kRows * (m * (m + 1ll) - none * (none + 1));
+        constexpr int log2 = SETS == 2 ? 6 : 7;      // of 2 kKeys
+        return (log2_G >= 0 ? sum >> (log2 + log2_G) : sum / ((int64_t)G << log2)) + (int64_t)Shape::kBlockCost * m;
     }
-    __device__ int64_t weight() const { return blocks == 0 ? 0 : weight_before(blocks - 1) + tiles(blocks - 1) + Shape::kBlockCost; }
+    __device__ int64_t weight() const { return weight_before(blocks); }
     // A part begins at a multiple of a tile, kMinPart or more from both ends of the block and not behind the tile that its first
     // query sees the end of (so that every query has a key in a part's first tile); w: weight from the block's beginning.
     // The block's number of tiles stands for its end.
@@ -115,7 +121,7 @@ struct PromptSeq {
         const int t = tiles(m), c = (int)min<int64_t>(max<int64_t>(w - Shape::kBlockCost, 0), t);
         if (c < Shape::kMinPart) return 0;
         if (c > t - Shape::kMinPart) return t;
-        const int last = min((m * Shape::kRows + ahead) / Shape::kKeys, t - Shape::kMinPart);
+        const int last = min((query(m * Shape::kRows) + ahead) / Shape::kKeys, t - Shape::kMinPart);
         return c <= last ? c : last < Shape::kMinPart ? t : last;
     }
 };
@@ -125,21 +131,19 @@ __device__ inline int64_t wave_sum_i64(int64_t v)
     for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
     return v;
 }
-template <int SETS>
 __device__ inline int64_t head_weight(const PromptArgs &a, int lane)
 {
     int64_t w = 0;
-    for (int b = lane; b < a.B; b += 64) w += PromptSeq<SETS>(a, b).weight();
+    for (int b = lane; b < a.B; b += 64) w += PromptSeq<2>(a, b).weight();
     return wave_sum_i64(w);
 }
 struct PromptPlace { int head, b, m, tile; int64_t begin; };        // head in list order; begin: weight in front of the block
-template <int SETS>
 __device__ inline PromptPlace prompt_place(const PromptArgs &a, int64_t x, int64_t per_head, int lane)
 {
     PromptPlace r{(int)(x / per_head), 0, 0, 0, 0};
     int64_t y = x % per_head;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int64_t w = b0 + lane < a.B ? PromptSeq<SETS>(a, b0 + lane).weight() : 0;
+        const int64_t w = b0 + lane < a.B ? PromptSeq<2>(a, b0 + lane).weight() : 0;
         int64_t incl = w;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -155,7 +159,7 @@ __device__ inline PromptPlace prompt_place(const PromptArgs &a, int64_t x, int64
         }
         y -= __shfl(incl, 63, 64);
     }
-    const PromptSeq<SETS> q(a, r.b);
+    const PromptSeq<2> q(a, r.b);
     int lo = 0, hi = q.blocks - 1;                   // the last block that begins at or before y
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
@@ -169,8 +173,7 @@ __device__ inline PromptPlace prompt_place(const PromptArgs &a, int64_t x, int64
     return r;
 }
 // Shares that the whole weight is cut into, at most n
-template <int SETS>
-__device__ inline int prompt_shares(int64_t whole, int n) { return __builtin_amdgcn_readfirstlane((int)min<int64_t>(n, max<int64_t>(1, whole / PromptShape<SETS>::kMinShare))); }
+__device__ inline int prompt_shares(int64_t whole, int n) { return __builtin_amdgcn_readfirstlane((int)min<int64_t>(n, max<int64_t>(1, whole / PromptShape<2>::kMinShare))); }
 
 // 16 bytes a lane from a scalar base and the lane's byte offset to the LDS byte address dst + 16 l (counts on vmcnt).  M0 is left as it is:
 // nothing else in this kernel reads it, and it is not the compiler's to keep values in.
@@ -188,12 +191,13 @@ __device__ inline float half_swap(float x, Op op)
     return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// SHARES: as above; otherwise a workgroup a block and head, the heads of a block next to each other, those with most keys first.
-template <int SETS, bool SHARES>
+// Two sets: shares, as above; one: a workgroup a block and KV head, the heads of a block next to each other, those with most keys first.
+template <int SETS>
 __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void prompt_attn_kernel(const PromptArgs a)
 {
     typedef PromptShape<SETS> Shape;
     typedef PromptSeq<SETS> Seq;
+    constexpr bool SHARES = SETS == 2;
     extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
     constexpr int kRows = Shape::kRows, kTileKeys = Shape::kKeys, kStages = Shape::kStages, kEl = Shape::kEl;
     constexpr int kLoads = kTileKeys / (4 * kPromptWaves);         // of a wave for K (and for V) of a tile
@@ -201,34 +205,31 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
     const int n = lane & 31, half = lane >> 5;
     uint16_t *const rows = smem + (SETS == 2 ? kStages * 2 * kEl : 0) + wave * Shape::kSetRows * kD;       // this wave's results on their way out
 
-    // which head, which sequence, which of its blocks, which tiles of the block
-    const int pack = SHARES ? 1 : a.G;               // query heads that go together; `head` is then the KV head
+    // which KV head, which sequence, which of its blocks, which tiles of the block
     int head, b = -1, m = 0, tile0 = 0, tile1 = 0, share = 0;
     PromptPlace end{};
     Seq seq;
     if constexpr (SHARES) {
-        const int64_t per_head = head_weight<SETS>(a, lane), whole = per_head * a.Hq;
-        const int shares = prompt_shares<SETS>(whole, gridDim.x);
+        const int64_t per_head = head_weight(a, lane), whole = per_head * a.Hkv;
+        const int shares = prompt_shares(whole, gridDim.x);
         // workgroups are dealt to the eight XCDs in turn: each gets shares that follow each other, of one KV head if there are eight
         share = shares % 8 == 0 && (int)gridDim.x == shares ? (blockIdx.x & 7) * (shares / 8) + (blockIdx.x >> 3) : blockIdx.x;
         if (share >= shares || __builtin_amdgcn_readfirstlane((int)(whole == 0)) != 0) return;
-        const PromptPlace p = prompt_place<SETS>(a, share * whole / shares, per_head, lane);
+        const PromptPlace p = prompt_place(a, share * whole / shares, per_head, lane);
         head = p.head; b = p.b; m = p.m; tile0 = p.tile;
-        if (share + 1 < shares) end = prompt_place<SETS>(a, (share + 1) * whole / shares, per_head, lane);
-        else end.head = a.Hq;
+        if (share + 1 < shares) end = prompt_place(a, (share + 1) * whole / shares, per_head, lane);
+        else end.head = a.Hkv;
         end.head = __builtin_amdgcn_readfirstlane(end.head);
         end.b = __builtin_amdgcn_readfirstlane(end.b);
         end.m = __builtin_amdgcn_readfirstlane(end.m);
         end.tile = __builtin_amdgcn_readfirstlane(end.tile);
     } else {
-        // The query heads of a KV head go together: fewer keys that only some rows of a block see, and less of the last block is empty.
-        // Neighbours read different KV heads, on the XCD of their own if there are eight.
-        head = blockIdx.x % a.Hkv;
+        head = blockIdx.x % a.Hkv;                   // neighbours read different KV heads, on the XCD of their own if there are eight
         int ti = blockIdx.x / a.Hkv;
         if (a.ordered) {
             // blocks in the order of their keys, a block's worth of them at a time: key class c of a sequence's block m is base + m
-            const Seq q(a, min(lane, a.B - 1), pack);
-            const int blocks = lane < a.B ? q.blocks : 0, base = (int)min((int64_t)max(0, q.ahead) * pack / kRows, (int64_t)1 << 30);
+            const Seq q(a, min(lane, a.B - 1));
+            const int blocks = lane < a.B ? q.blocks : 0, base = (int)min((int64_t)max(0, q.ahead) * a.G / kRows, (int64_t)1 << 30);
             auto at_least = [&](int c) { return (int)wave_sum_u32((uint32_t)min(max(base + blocks - c, 0), blocks)); };
             if (ti >= at_least(0)) return;
             int lo = 0, hi = (int)wave_reduce_bits((uint32_t)(base + blocks), [](uint32_t x, uint32_t y) { return max(x, y); });
@@ -248,20 +249,20 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             int at = ti % max(a.places, 1);
             if (a.places > 0) {
                 b = ti / a.places;
-                seq = Seq(a, b, pack).of_lane(0);
+                seq = Seq(a, b).of_lane(0);
             } else {
                 // ... or from first row / kRows + b on, where there are at least as many as it has blocks
                 b = 0;
                 for (int range = a.B, step = 2; step > 1;) {         // the last one whose places begin at or before ti, of b .. b + range - 1
                     step = (range + 63) / 64;
                     const int i = lane * step;
-                    const Seq q(a, min(b + i, a.B - 1), pack);
-                    const int c = __popcll(__ballot(lane == 0 || (i < range && q.q_first * pack / kRows + b + i <= ti))) - 1;
+                    const Seq q(a, min(b + i, a.B - 1));
+                    const int c = __popcll(__ballot(lane == 0 || (i < range && q.q_first * a.G / kRows + b + i <= ti))) - 1;
                     b += c * step;
                     range = min(step, range - c * step);
                     seq = q.of_lane(c);
                 }
-                at = ti - seq.q_first * pack / kRows - b;
+                at = ti - seq.q_first * a.G / kRows - b;
             }
             m = __builtin_amdgcn_readfirstlane(seq.blocks - 1 - at);
             if (m < 0 || m >= seq.blocks) return;
@@ -275,16 +276,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
         tile0 = __builtin_amdgcn_readfirstlane(tile0);
         if (SHARES) seq = Seq(a, b).of_lane(0);
         const int nk = seq.nk, ahead = seq.ahead, n_rows = seq.rows;
-        // the query of row i of the block, and how far its head is from the block's first
-        const int query0 = m * kRows / pack, over0 = m * kRows % pack;
-        const int head0 = SHARES ? head : head * pack;
+        // the query of row i of the block, and its head among the KV head's
+        const int query0 = seq.query(m * kRows), over0 = m * kRows - query0 * a.G, head0 = head * a.G;
         auto query_of = [&](int i, int &of) {
-            if (SHARES) {
-                of = 0;
-                return m * kRows + i;
-            }
-            const int q = (int)((i + over0 + 0.5f) * a.inv_G);       // (less than 2^21 of them: exact)
-            of = i + over0 - q * pack;
+            const int q = seq.query(i + over0);
+            of = i + over0 - q * a.G;
             return query0 + q;
         };
         const int all_tiles = __builtin_amdgcn_readfirstlane(seq.tiles(m));
@@ -299,20 +295,20 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 if (a.lse != nullptr && i % kRowLanes == 0) a.lse[at] = -INFINITY;
             }
         } else if (tile0 < tile1) {
-            const int g = SHARES ? head / a.G : head;
+            const int g = head;
             const int row0 = m * kRows + wave * Shape::kSetRows;           // this wave's first row
             const int n_tiles = tile1 - tile0;               // of this part, numbered from its first
-            // Work goes in two turns s, for the two sets of queries or the two halves of a tile: their queries, first row and first key
+            // Work goes in two turns s, for the two sets of queries or the two halves of a tile: their queries and first key
             auto qs = [](int s) { return SETS == 2 ? s : 0; };
-            auto set0 = [](int s) { return SETS == 2 ? 32 * s : 0; };
             auto key0 = [](int s) { return SETS == 2 ? 0 : 32 * s; };
 
             bf16x8 qb[SETS][8];
-            int last_key[SETS];
+            int last_key[SETS], first_last[SETS];            // the last key of a lane's query, and of a set's first
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
                 int of;
                 last_key[s] = query_of(min(wave * Shape::kSetRows + s * 32 + n, n_rows - 1 - m * kRows), of) + ahead - tile0 * kTileKeys;
+                first_last[s] = seq.query(row0 + s * 32) + ahead - tile0 * kTileKeys;
             }
             auto load_queries = [&] {
                 int l = lane;                                // (not known to be it: what follows from it is computed here, not kept in registers all along)
@@ -327,7 +323,6 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                     for (int ks = 0; ks < 8; ++ks) qb[s][ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 16);
                 }
             };
-            const int first_last = row0 / pack + ahead - tile0 * kTileKeys;          // the last key of the wave's first row
             const int keys_here = nk - tile0 * kTileKeys;
             const uint16_t *kb = a.k + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.k_st + g * a.k_sh;
             const uint16_t *vb = a.v + ((int64_t)seq.k_first + (int64_t)tile0 * kTileKeys) * a.v_st + g * a.v_sh;
@@ -402,7 +397,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 return __int_as_float((hidden & __float_as_int(-INFINITY)) | (~hidden & __float_as_int(x)));
             };
             auto mask = [&](int tile, int s) {
-                if (tile * kTileKeys + key0(s) + 31 <= first_last + set0(s)) return;
+                if (tile * kTileKeys + key0(s) + 31 <= first_last[qs(s)]) return;
                 const uint32_t bits = hidden_keys(tile, s);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sc[s][r] = hide(bits, r, sc[s][r]);
@@ -556,7 +551,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             __syncthreads();                                 // K(0) has been read
             // This wave's last tile with a key that one of its queries sees.  Behind it, it only keeps the others company: the matrix units are
             // the other workgroup's meanwhile
-            const int last_seen = (min(row0 + Shape::kSetRows, n_rows) - 1) / pack + ahead - tile0 * kTileKeys;
+            const int last_seen = seq.query(min(row0 + Shape::kSetRows, n_rows) - 1) + ahead - tile0 * kTileKeys;
             const int mine = row0 >= n_rows ? 1 : min(max(last_seen, 0) / kTileKeys + 1, n_tiles), unmasked = min(seen, mine);
             int t = 0;
             if constexpr (SETS == 2) {
@@ -735,20 +730,20 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                         a.lse[(int64_t)(seq.q_first + q) * a.Hq + head0 + of] = l_run[s] == 0.f ? -INFINITY : (m_ref[s] + log2f(l_run[s])) * 0.69314718055994530942f;
                 }
                 asm volatile("" ::: "memory");                   // lanes read what other lanes of the wave wrote (LDS keeps the order)
-                // four rows at a time: 4 / pack queries and 4 % pack heads further, or a query more and as many heads less
+                // four rows at a time: 4 / G queries and 4 % G heads further, or a query more and G heads less
                 const int row = l >> 4, slot = l & 15;
                 int of;
                 const int q = query_of(wave * Shape::kSetRows + row, of);
                 uint16_t *out = a.out + ((int64_t)(seq.q_first + query0) * a.Hq + head0) * kD;
                 int at = ((q - query0) * a.Hq + of) * kD + slot * 8;
-                const int heads = 4 % pack, step = (4 / pack * a.Hq + heads) * kD, wrap = (a.Hq - pack) * kD;
+                const int heads = 4 % a.G, step = (4 / a.G * a.Hq + heads) * kD, wrap = (a.Hq - a.G) * kD;
                 auto row_piece = [&](int i) { return *reinterpret_cast<const uint4 *>(rows + (4 * i + row) * kD + ((slot ^ (4 * (i & 3) + row)) << 3)); };
 #pragma unroll
                 for (int i = 0; i < Shape::kSetRows / 4; ++i) {
                     if (row0 + Shape::kSetRows <= n_rows || row0 + 4 * i + row < n_rows) *reinterpret_cast<uint4 *>(out + at) = row_piece(i);
                     of += heads;
-                    at += step + (of >= pack ? wrap : 0);
-                    of -= of >= pack ? pack : 0;
+                    at += step + (of >= a.G ? wrap : 0);
+                    of -= of >= a.G ? a.G : 0;
                 }
             }
         }
@@ -758,30 +753,29 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             m = 0;
             do {
                 if (++b == a.B) { b = 0; ++head; }
-            } while (head < a.Hq && Seq(a, b).blocks == 0);
+            } while (head < a.Hkv && Seq(a, b).blocks == 0);
         }
-        if (head >= a.Hq) break;
+        if (head >= a.Hkv) break;
         __syncthreads();                                 // the last tile's values have been read
     }
 }
 
 // The parts of the block that boundary `blockIdx.x` + 1 of the shares is the first to cut; the queries of one of its waves a workgroup, a
 // quarter of each lane's accumulators a wave.
-template <int SETS>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, int workgroups)
 {
-    constexpr int kPieces = 4 * SETS;                // 16-byte pieces of a lane's accumulators, of which each of the four waves takes a quarter
+    constexpr int kPieces = 8;                       // 16-byte pieces of a lane's accumulators, of which each of the four waves takes a quarter
     const int lane = threadIdx.x & 63, quarter = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.y;
-    const int64_t per_head = head_weight<SETS>(a, lane), whole = per_head * a.Hq;
-    const int shares = prompt_shares<SETS>(whole, workgroups), j = blockIdx.x + 1;
+    const int64_t per_head = head_weight(a, lane), whole = per_head * a.Hkv;
+    const int shares = prompt_shares(whole, workgroups), j = blockIdx.x + 1;
     if (whole == 0 || j >= shares) return;
-    const PromptPlace p = prompt_place<SETS>(a, j * whole / shares, per_head, lane);
-    const PromptSeq<SETS> seq(a, p.b);
+    const PromptPlace p = prompt_place(a, j * whole / shares, per_head, lane);
+    const PromptSeq<2> seq(a, p.b);
     const int tiles = seq.tiles(p.m);
     if (p.tile == 0 || p.tile == tiles) return;      // cuts nothing
     auto tile_of = [&](int k) {                      // where share k begins in this block, its end if behind it
         const int64_t w = k * whole / shares - p.begin;
-        return k >= shares || w >= (int64_t)tiles + PromptShape<SETS>::kBlockCost ? tiles : seq.part_begin(p.m, w);
+        return k >= shares || w >= (int64_t)tiles + PromptShape<2>::kBlockCost ? tiles : seq.part_begin(p.m, w);
     };
     if ((j - 1) * whole / shares >= p.begin) {
         const int before = tile_of(j - 1);
@@ -793,7 +787,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     // share k's part of the block is [tile_of(k), tile_of(k + 1)), the first one's from 0; a lane finds that of one share.  Up to four parts
-    // are read at a time: 64 queries on 60,064 keys, which are cut into 64 parts, 162 -> 121 us
+    // are read at a time: 64 queries on 60,064 keys, which are cut into 64 parts, 117 -> 107 us
     int begun = 0;
     for (int k0 = j - 1; begun < tiles; k0 += 64) {
         const int end = tile_of(k0 + lane + 1);
@@ -810,8 +804,8 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
             for (int c = 0; c < N; ++c) {
                 const int64_t unit = (int64_t)__builtin_amdgcn_readlane(part, __builtin_ctzll(left)) * kPromptWaves + wave;
                 left &= left - 1;
-                ml[c] = a.part_ml[(unit * SETS + s) * 32 + n];
-                const float4 *from = a.part_o + (unit * SETS * 16 + quarter * kPieces) * 64 + lane;
+                ml[c] = a.part_ml[(unit * 2 + s) * 32 + n];
+                const float4 *from = a.part_o + (unit * 32 + quarter * kPieces) * 64 + lane;
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) x[c][i] = from[i * 64];
             }
@@ -836,10 +830,11 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
         if (__popcll(left) >= 2) take(std::integral_constant<int, 2>{});
         if (left != 0) take(std::integral_constant<int, 1>{});
     }
-    const int row = p.m * PromptShape<SETS>::kRows + wave * PromptShape<SETS>::kSetRows + s * 32 + n;
-    if (row >= seq.nq) return;
+    const int row = p.m * PromptShape<2>::kRows + wave * PromptShape<2>::kSetRows + s * 32 + n;
+    if (row >= seq.rows) return;
     const float inv = 1.0f / L;
-    const int64_t at = (int64_t)(seq.q_first + row) * a.Hq + p.head;
+    const int query = seq.query(row);
+    const int64_t at = (int64_t)(seq.q_first + query) * a.Hq + p.head * a.G + (row - query * a.G);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
         const int piece = quarter * kPieces + i - 16 * s;
@@ -849,62 +844,38 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
     if (a.lse != nullptr && half == 0 && quarter * kPieces == 16 * s) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
 }
 
-// Blocks x heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each
-static int64_t prompt_blocks(const ihip_packed &p, int block, int pack)
+// Blocks x KV heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each
+static int64_t prompt_blocks(const ihip_packed &p, int rows)
 {
-    const int64_t by_rows = (int64_t)p.rows * pack / block + p.B, by_len = p.B * (((int64_t)p.max_q * pack - 1) / block + 1);
-    return std::min(by_rows, by_len) * (p.Hq / pack);
+    const int64_t G = p.Hq / p.Hkv, by_rows = p.rows * G / rows + p.B, by_len = p.B * ((p.max_q * G - 1) / rows + 1);
+    return std::min(by_rows, by_len) * p.Hkv;
 }
-// How a call is done: blocks by themselves (of 128 rows, one set a wave; 0 here), or equal shares with one set or two.  From what the host knows of
-// it, total tokens, keys and sequences, in units of 32 keys for 256 queries of one compute unit (0.7 us; a launch takes 14 us):
-// blocks by themselves take as long as the longest, or as the rounds of them that the compute units do (blocks of the same length in
-// whole rounds; a whole prompt's blocks, of all lengths up to the longest, fill the rounds), and each begins and ends.  Shares take the
-// mean, and some time for beginnings, ends and the merge: more of it with two sets, which read the keys half as often, but keep
-// twice as many queries that may not be there.  The longest of several sequences with keys ahead is not known; it is taken for 2.5 times the
-// mean, since shares cost a little where all are alike and the others a lot where they are not.  Of 58 calls the estimate takes the fastest
-// on 56, and what is 11 and 15 % slower on two.
-// us by themselves / shares of one set / of two, 32 heads on 8: 1,024 queries 24 / 47 / 50, 8,192 476 / 538 / 535; 64 on 2,064 keys 36 / 35 / 45; 200
-// on 8,200 109 / 79 / 81; 128, 256, 64 and 500 on 3,000 to 12,000 156 / 102 / 124; 8 heads, 64 on 60,064 694 / 119 / 107; 16 heads, 1,500 on
-// 13,500 and 700 on 20,700 327 / 286 / 267.  Blocks of two sets by themselves would be slower almost everywhere (1,024 queries 37, 20
-// times 333 90 against 48) and at best 3 % faster (16 heads, 8,192: 247 against 256).
-static int prompt_shares_of(const ihip_packed &p, int64_t keys)
+// Whether a call is dealt out in shares.  From what the host knows of it, total tokens, keys and sequences, in units of 32 keys for 256
+// rows of one compute unit (0.7 us; a launch takes 14 us): blocks by themselves (of 128 rows, one set a wave) take as long as the
+// longest, or as the rounds of them that the compute units do (blocks of the same length in whole rounds; a whole prompt's blocks, of all
+// lengths up to the longest, fill the rounds), and each begins and ends.  Shares take the mean, and some time for beginnings, ends and the
+// merge.  The longest of several sequences with keys ahead is not known; it is taken for twice the mean, since shares cost a
+// little where all are alike and the others a lot where they are not.  Of 65 calls the estimate takes the faster way on 62, and what is
+// 1, 13 and 14 % slower on three.
+// us by themselves / in shares, 32 heads on 8: 1,024 queries 24 / 53, 8,192 469 / 578; 64 on 2,064 keys 36 / 47, 512 on 4,608 66 / 75; 200 on 8,200
+// 109 / 79; 128, 256, 64 and 500 on 3,000 to 12,000 156 / 102; one each of 16 sequences on 8,000 161 / 127; 8 heads, 64 on 60,064 681 /
+// 109; 16 heads on 8, 1,500 on 13,500 and 700 on 20,700 326 / 267, 1,000 on 101,000 1,514 / 707.
+// The other pairs were slower nearly everywhere: blocks of two sets by themselves (1,024 queries 37, 20 times 333 90 against 48; 16 heads,
+// 8,192 247 against 253), shares of one set (1,500 and 700 276, 1,000 on 101,000 783; 200 on 8,200 70).
+static bool prompt_in_shares(const ihip_packed &p, int64_t keys)
 {
-    if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return 0;
+    if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return false;
     const double cu = compute_units(), before = std::max<double>(0, (double)(keys - p.rows)) / p.B, mean = (double)p.rows / p.B;
-    const double longest = ((p.B > 1 ? 2.5 : 1) * before + p.max_q) / 32, tiles = (before + mean / 2) / 32, alike = before / (before + mean / 2);
-    auto rounds_of = [&](int block, int pack) {
-        return std::min((double)prompt_blocks(p, block, pack), ((double)p.rows * pack / block + 0.5 * p.B) * p.Hq / pack) / cu;
+    const double longest = ((p.B > 1 ? 2 : 1) * before + p.max_q) / 32, tiles = (before + mean / 2) / 32, alike = before / (before + mean / 2);
+    auto rounds_of = [&](int rows) {
+        return std::min((double)prompt_blocks(p, rows), (double)p.rows * p.Hq / rows + 0.5 * p.B * p.Hkv) / cu;
     };
-    const double by_itself = rounds_of(128, p.Hq / p.Hkv);
-    const double alone = std::max(0.55 * longest, (0.55 * tiles + 5) * (by_itself + alike * (std::ceil(by_itself) - by_itself)) - 5);
-    const double shares1 = (0.8 * tiles + 3) * rounds_of(128, 1) + 25, shares2 = (1.3 * tiles + 6) * rounds_of(256, 1) + 35;
-    return alone <= shares1 && alone <= shares2 ? 0 : shares1 <= shares2 ? 1 : 2;
+    const double one = rounds_of(128);
+    const double alone = std::max(0.5 * longest, (0.5 * tiles + 4) * (one + alike * (std::ceil(one) - one)) - 4);
+    return (1.1 * tiles + 6) * rounds_of(256) + 40 < alone;
 }
-// Parts of all workgroups of a launch in shares: the same with one set and two
+// Parts of all workgroups of a launch in shares
 static size_t prompt_part_bytes() { return (size_t)2 * compute_units() * kPromptWaves * 64 * (32 * sizeof(float4) + sizeof(float2)); }
-
-template <int SETS>
-static int32_t launch_shares(const char *who, PromptArgs &a, void *ws, hipStream_t st)
-{
-    typedef PromptShape<SETS> Shape;
-    static bool attr_set = Shape::kLds <= 65536;     // allow more than 64 KiB of dynamic LDS, once
-    if (!attr_set) {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<SETS, true>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::kLds);
-        attr_set = true;
-    }
-    const int n = Shape::kPerCu * compute_units();
-    a.part_o = (float4 *)ws;
-    a.part_ml = (float2 *)(a.part_o + (size_t)2 * n * kPromptWaves * SETS * 16 * 64);
-    {
-        KernelTimer timer("prompt_attn_shares", st);
-        hipLaunchKernelGGL((prompt_attn_kernel<SETS, true>), dim3(n), dim3(64 * kPromptWaves), Shape::kLds, st, a);
-    }
-    int32_t rc;
-    if ((rc = check_launch(who)) != IHIP_OK) return rc;
-    KernelTimer timer("prompt_merge", st);
-    hipLaunchKernelGGL(prompt_merge_kernel<SETS>, dim3(n, kPromptWaves), dim3(256), 0, st, a, n);
-    return check_launch(who);
-}
 
 }  // namespace ihip
 
@@ -913,7 +884,7 @@ using namespace ihip;
 extern "C" size_t ihip_prompt_attn_workspace_bytes(const ihip_packed *packed, int32_t rows_k)
 {
     if (check_packed("ihip_prompt_attn_workspace_bytes", packed) != IHIP_OK) return 0;
-    return prompt_shares_of(*packed, rows_k) != 0 ? prompt_part_bytes() : 256;
+    return prompt_in_shares(*packed, rows_k) ? prompt_part_bytes() : 256;
 }
 
 extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v, const int32_t *cu_k,
@@ -940,24 +911,39 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     if ((a.q_st | a.k_st | a.v_st) < 0 || a.q_st >= (1 << 24) || a.k_st >= (1 << 24) || a.v_st >= (1 << 24))
         return fail(IHIP_ERR_UNSUPPORTED, "%s: rows of q, k and v must be less than 2^24 elements apart", who);
     a.scale_log2e = sm_scale * 1.44269504088896340736f;
-    a.inv_G = 1.0f / a.G;
+    a.log2_G = pow2(a.G) ? __builtin_ctz(a.G) : -1;
     a.out = (uint16_t *)out;
     a.lse = out_lse;
     const hipStream_t st = (hipStream_t)stream;
-    if (ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes()) {
-        const int sets = prompt_shares_of(*packed, rows_k);
-        if (sets != 0) return sets == 1 ? launch_shares<1>(who, a, ws, st) : launch_shares<2>(who, a, ws, st);
+    if (ws && !((uintptr_t)ws & 15) && ws_bytes >= prompt_part_bytes() && prompt_in_shares(*packed, rows_k)) {
+        constexpr int lds = PromptShape<2>::kLds;
+        static bool attr_set = false;        // allow more than 64 KiB of dynamic LDS, once
+        if (!attr_set) {
+            (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<2>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            attr_set = true;
+        }
+        const int n = PromptShape<2>::kPerCu * compute_units();
+        a.part_o = (float4 *)ws;
+        a.part_ml = (float2 *)(a.part_o + (size_t)2 * n * kPromptWaves * 32 * 64);
+        {
+            KernelTimer timer("prompt_attn_shares", st);
+            hipLaunchKernelGGL(prompt_attn_kernel<2>, dim3(n), dim3(64 * kPromptWaves), lds, st, a);
+        }
+        if ((rc = check_launch(who)) != IHIP_OK) return rc;
+        KernelTimer timer("prompt_merge", st);
+        hipLaunchKernelGGL(prompt_merge_kernel, dim3(n, kPromptWaves), dim3(256), 0, st, a, n);
+        return check_launch(who);
     }
     typedef PromptShape<1> Shape;
     // (A workgroup a block, handed out by the hardware.  512 that stay, each with every 512th block and the first tiles of its next one
     // on their way under the end of the present one: 8 prompts of 640 to 2,048 172 -> 185 us, one of 32,768 7.17 -> 7.52 ms.)
     // The order of the blocks matters where some compute unit has two.  Finding them without it is shorter: 512 queries, 32 heads 18.5 -> 17.6 us
-    const int64_t groups = prompt_blocks(*packed, Shape::kRows, a.G);
+    const int64_t groups = prompt_blocks(*packed, Shape::kRows);
     a.ordered = packed->B <= kOrderedSeqs && groups > compute_units();
     const int64_t places = ((int64_t)packed->max_q * a.G - 1) / Shape::kRows + 1;
     a.places = groups == places * packed->B * packed->Hkv ? (int)places : 0;
     if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
     KernelTimer timer("prompt_attn", st);
-    hipLaunchKernelGGL((prompt_attn_kernel<1, false>), dim3((uint32_t)groups), dim3(64 * kPromptWaves), Shape::kLds, st, a);
+    hipLaunchKernelGGL(prompt_attn_kernel<1>, dim3((uint32_t)groups), dim3(64 * kPromptWaves), Shape::kLds, st, a);
     return check_launch(who);
 }

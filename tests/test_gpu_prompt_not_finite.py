@@ -31,7 +31,7 @@ def reference(q, k, v):
 @pytest.mark.parametrize("Hq,n,ahead", [
     (4, 1, 0), (4, 200, 0), (8, 517, 77), (2, 300, -150),
     (96, 700, 0),                                        # more blocks than the chip holds at a time
-    (8, 300, 20000), (16, 512, 16000),                   # shares of one set of queries a wave, and of two
+    (8, 300, 20000), (16, 512, 16000),                   # equal shares
 ])
 @pytest.mark.parametrize("what", ["values", "keys", "both"])
 def test_what_is_not_finite_stays_with_those_who_see_it(ihip, Hq, n, ahead, what):  # noqa: F811
