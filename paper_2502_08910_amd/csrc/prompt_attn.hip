@@ -5,7 +5,7 @@
 // the right operand of the second product with V^T (whose rows it takes in the order of the scores), and nothing of P goes through LDS.
 // K and V go from memory to LDS by themselves (global_load_lds), 16-byte chunks XORed with the row, so that both the rows of K and the
 // transposed reads of V (ds_read_b64_tr_b16) are without conflicts.
-// Bound by the matrix units at the clock that the power limit leaves: one prompt of 32,768 with 32 heads, 8.79 TFLOP, takes
+// Bound by the matrix units at the clock that the power limit leaves: one prompt of 32,749 with 32 heads, 8.79 TFLOP, takes
 // 7.1 ms, 1.23 PFLOP/s, where a library product of 16,384^3 reaches 1.31 and one of 8,192^3 1.15.
 #include "api_checks.h"
 #include "kv_store.h"
@@ -711,7 +711,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 }
             } else {
                 // The results go out through LDS, so that whole rows are written: 16-byte chunk c of row r at slot c ^ r % 16.  256 queries of 32 heads on 256
-                // keys each 17.4 -> 14.4 us
+                // keys each 17.4 -> 15.9 us
                 int l = lane;                                    // (as above)
                 asm volatile("" : "+v"(l));
                 const int n = l & 31, half = l >> 5;
@@ -936,7 +936,7 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     }
     typedef PromptShape<1> Shape;
     // (A workgroup a block, handed out by the hardware.  512 that stay, each with every 512th block and the first tiles of its next one
-    // on their way under the end of the present one: 8 prompts of 640 to 2,048 172 -> 185 us, one of 32,768 7.17 -> 7.52 ms.)
+    // on their way under the end of the present one: 8 prompts of 640 to 2,048 172 -> 185 us, one of 32,749 7.17 -> 7.52 ms.)
     // The order of the blocks matters where some compute unit has two.  Finding them without it is shorter: 512 queries, 32 heads 18.5 -> 17.6 us
     const int64_t groups = prompt_blocks(*packed, Shape::kRows);
     a.ordered = packed->B <= kOrderedSeqs && groups > compute_units();
