@@ -532,7 +532,7 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
  * key set, shape, block_starts and outputs.  With n_blocks == 0 (block_starts may
  * then be NULL) and n_stream >= max_seq_len every key is attended to.  Scores,
  * exponentials and sums in fp32; the probabilities are rounded to bf16 for the second
- * product, rows are widened to bf16 (exact).  The output of an idle place of the
+ * product, rows are widened to bf16 (exact).  sm_scale is finite and not negative.  The output of an idle place of the
  * batch is 0, its log-sum-exp -INFINITY; so is that of a sequence whose pages all have negative ids
  * (keys on such pages are left out).
  *   ws, ws_bytes device scratch of ihip_workspace_bytes(IHIP_OP_ATTN_DECODE_MX4, ...), 8-byte aligned
@@ -555,7 +555,7 @@ int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_tensor q, co
  * QK^T and PV run on the matrix cores (bf16 operands, the probabilities rounded to
  * bf16, fp32 accumulation), softmax in fp32.  A query that sees no key (t < n)
  * gets 0, and -INFINITY.  A sequence of more than max_q tokens may be done in part only.
- * A key or a value that is not finite makes only those results NaN or infinite that see it.
+ * sm_scale is finite and not negative.  A key or a value that is not finite makes only those results NaN or infinite that see it.
  *   ws, ws_bytes device scratch of ihip_prompt_attn_workspace_bytes(packed, rows_k), 16-byte aligned; may be NULL.  A call with few
  *                queries on many keys deals its work out to the whole chip in equal shares and merges the parts there;
  *                with NULL, less or a misaligned pointer it does not (slower; equal up to rounding).  Calls that overlap

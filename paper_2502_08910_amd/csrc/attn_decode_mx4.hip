@@ -364,7 +364,7 @@ extern "C" int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_t
     a.sb = (uint32_t)(w.k_sb / 64); a.sh = w.k_sh / 64; a.st = (uint32_t)(w.k_st / 64);
     a.block_starts = block_starts;
     a.n_blocks = n_blocks; a.block = block; a.block_log2 = __builtin_ctz(block);
-    a.scale_log2e = sm_scale * 1.44269504088896340736f;
+    if ((rc = check_sm_scale(who, sm_scale, &a.scale_log2e)) != IHIP_OK) return rc;
     a.n_splits = mx4_splits(*shape, n_blocks, block);
     a.grid = decode_grid(a.ge, a.n_splits, false);
     a.paged = w.paged;

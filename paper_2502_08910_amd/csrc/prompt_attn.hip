@@ -910,7 +910,7 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     // the rows of a tile, and of a wave's queries, are addressed by 32-bit byte offsets from the first
     if ((a.q_st | a.k_st | a.v_st) < 0 || a.q_st >= (1 << 24) || a.k_st >= (1 << 24) || a.v_st >= (1 << 24))
         return fail(IHIP_ERR_UNSUPPORTED, "%s: rows of q, k and v must be less than 2^24 elements apart", who);
-    a.scale_log2e = sm_scale * 1.44269504088896340736f;
+    if ((rc = check_sm_scale(who, sm_scale, &a.scale_log2e)) != IHIP_OK) return rc;
     a.log2_G = pow2(a.G) ? __builtin_ctz(a.G) : -1;
     a.out = (uint16_t *)out;
     a.lse = out_lse;

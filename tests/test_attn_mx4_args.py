@@ -26,8 +26,8 @@ def test_decode_attention_over_4_bit_rows_refuses(b):
         return s
 
     def call(shape=b.Shape(2, 8, 2, 128, 1, 1, 4096, 1000, 4, 64, 0), q=t(4096, 1024, 128, 128), s=store(), starts=4096, n=4, block=16, out=4096,
-             ws=4096, size=1 << 30):
-        return L.ihip_sparse_attn_decode_mx4kv(ctypes.byref(shape), q, ctypes.byref(s) if s else None, starts, n, block, 0.1, out, None, ws, size, None)
+             ws=4096, size=1 << 30, scale=0.1):
+        return L.ihip_sparse_attn_decode_mx4kv(ctypes.byref(shape), q, ctypes.byref(s) if s else None, starts, n, block, scale, out, None, ws, size, None)
 
     Shape = b.Shape
     assert call(shape=Shape(2, 8, 2, 64, 1, 1, 4096, 1000, 4, 64, 0)) == -4
@@ -42,6 +42,8 @@ def test_decode_attention_over_4_bit_rows_refuses(b):
     assert call(s=store(k=back, v=back)) == -4 and b"strides" in L.ihip_last_error()
     pg = b.PagedStruct(4096, 10, 64)                                     # 640 of 1,000 tokens
     assert call(s=store(paged=ctypes.cast(ctypes.pointer(pg), ctypes.c_void_p))) == -1
+    for scale in (-0.1, float("nan"), float("inf")):
+        assert call(scale=scale) == -1 and b"sm_scale" in L.ihip_last_error()
     assert call(n=-1) == -1 and call(block=12) == -1 and call(starts=None) == -1 and call(out=None) == -1
     assert call(n=1 << 20, block=4096) == -4 and b"slots" in L.ihip_last_error()
     assert call(ws=None) == -2 and call(ws=4100) == -2 and call(size=100) == -2 and b"workspace" in L.ihip_last_error()

@@ -148,6 +148,15 @@ def test_scores_that_grow_along_the_keys(ihip):
     check(c, q, out, lse, 0, c.T)
 
 
+def test_a_scale_of_zero_gives_the_mean(ihip):
+    lens = [300, 45, 1]
+    c = Cache(ihip, lens, 2, 16, seed=21)
+    q = queries(3, 8, 22)
+    sl = torch.tensor(lens, dtype=torch.int32).cuda()
+    out, lse = ihip.sparse_attn_decode_mx4(ihip.Layer(q, c.store, sl, 1, 0, c.T, max_seq_len=c.T), q, c.store, want_lse=True, sm_scale=0.0)
+    check(c, q, out, lse, 0, c.T, scale=0.0)
+
+
 def test_pages_without_an_id_are_left_out(ihip):
     lens = [100, 40]
     c = Cache(ihip, lens, 2, 16, seed=10)

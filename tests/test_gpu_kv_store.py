@@ -232,7 +232,6 @@ def test_gather(ihip, fmt, page, Hkv, lens):
 
 
 def test_gather_of_keys_alone_and_of_lengths_beyond_the_bound(ihip):
-    import ctypes
     from paper_2502_08910_amd.binding import NO_TENSOR, _tensor
     c = Cache(ihip, "mx4", 2, 2, 40, 0)
     lens = torch.tensor([1 << 30, 9], dtype=torch.int32).cuda()
@@ -242,7 +241,6 @@ def test_gather_of_keys_alone_and_of_lengths_beyond_the_bound(ihip):
     want = np.full((2, 2, 24, D), 5.0)
     want[0, :, :20], want[1, :, :9] = c.values()[0][0, :, :20], c.values()[0][1, :, :9]
     assert np.array_equal(f64(out), want)
-    _ = ctypes
 
 
 @pytest.mark.parametrize("fmt", FORMATS)

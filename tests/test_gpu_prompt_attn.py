@@ -9,7 +9,7 @@ import torch
 
 pytestmark = pytest.mark.gpu
 
-from tests.kv_reference import D, f64  # noqa: E402
+from tests.kv_reference import D  # noqa: E402
 
 SCALE = 1 / np.sqrt(D)
 
@@ -131,6 +131,27 @@ def test_offsets_beyond_the_rows_stay_inside(ihip):
     check(q, k, v, [60, 40], [60, 40], out, lse)
 
 
+def test_a_scale_of_zero_gives_the_mean(ihip):
+    q, k, v = normal(17, 300, 4, D), normal(18, 300, 2, D), normal(19, 300, 2, D)
+    out, lse = ihip.prompt_attn(q, k, v, offsets([33, 267]), 267, sm_scale=0.0, want_lse=True)
+    check(q, k, v, [33, 267], [33, 267], out, lse, scale=0.0)
+
+
+@pytest.mark.parametrize("ctx,shares", [(0, False), (30000, True)])
+def test_rows_beyond_four_gigabytes(ihip, ctx, shares):
+    """Keys behind 2^32 bytes of other sequences' keys, queries 2^32 bytes apart from first to last."""
+    n, far, step = 300, (1 << 32) // (2 * D * 2) + 13, (1 << 23)
+    total = n + ctx
+    k, v = (torch.empty((far + total, 2, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k[far:], v[far:] = normal(20, total, 2, D), normal(21, total, 2, D)
+    wide = torch.empty((n * step,), dtype=torch.bfloat16, device="cuda").view(n, step)
+    q = wide[:, :4 * D].unflatten(1, (4, D))
+    q.copy_(normal(22, n, 4, D))
+    cu, cu_k = offsets([0, n]), offsets([far, total])
+    out, lse = ihip.prompt_attn(q, k, v, cu, n, cu_k=cu_k, want_lse=True, ws=None if shares else torch.empty(0, dtype=torch.uint8, device="cuda"))
+    check(q, k[far:], v[far:], [n], [total], out, lse)
+
+
 def test_on_another_stream_and_in_a_graph(ihip):
     q, k, v = (torch.empty((400, h, D), dtype=torch.bfloat16, device="cuda") for h in (8, 2, 2))
     cu = offsets([130, 270])
@@ -161,4 +182,3 @@ def test_on_another_stream_and_in_a_graph(ihip):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
-    _ = f64

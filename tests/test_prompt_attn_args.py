@@ -19,8 +19,8 @@ def test_prompt_attention_refuses(b):
     t, P, L = b.Tensor, b.PackedStruct, b.lib()
     ok = t(4096, 0, 128, 1024)
 
-    def call(packed=P(2, 8, 2, 128, 4096, 10, 10), q=ok, k=ok, v=ok, cu_k=4096, rows_k=20, out=4096):
-        return L.ihip_prompt_attn(ctypes.byref(packed) if packed else None, q, k, v, cu_k, rows_k, 0.1, out, None, None, 0, None)
+    def call(packed=P(2, 8, 2, 128, 4096, 10, 10), q=ok, k=ok, v=ok, cu_k=4096, rows_k=20, out=4096, scale=0.1):
+        return L.ihip_prompt_attn(ctypes.byref(packed) if packed else None, q, k, v, cu_k, rows_k, scale, out, None, None, 0, None)
 
     assert call(packed=None) == -1
     assert call(packed=P(2, 8, 3, 128, 4096, 10, 10)) == -1
@@ -31,6 +31,8 @@ def test_prompt_attention_refuses(b):
     assert call(k=t(4096, 0, 128, 64)) == -1
     assert call(out=None) == -1 and call(out=4100) == -1
     assert call(rows_k=-1) == -1
+    for scale in (-0.1, float("nan"), float("inf")):
+        assert call(scale=scale) == -1 and b"sm_scale" in L.ihip_last_error()
     assert call(cu_k=None, rows_k=20) == -1 and b"rows_k" in L.ihip_last_error()      # whole prompts: as many keys as queries
     assert call(packed=P(1, 1 << 20, 1 << 20, 128, 4096, 1 << 30, 1 << 30)) == -4 and b"workgroups" in L.ihip_last_error()
     # nothing to do
