@@ -5,7 +5,8 @@
 // the right operand of the second product with V^T (whose rows it takes in the order of the scores), and nothing of P goes through LDS.
 // K and V go from memory to LDS by themselves (global_load_lds), 16-byte chunks XORed with the row, so that both the rows of K and the
 // transposed reads of V (ds_read_b64_tr_b16) are without conflicts.
-// Bound by the matrix units at the clock that the power limit leaves: one prompt of 32,749 with 32 heads, 8.79 TFLOP, takes
+// Bound by the matrix units (32 cycles an instruction) and the vector units (four instructions a product, 28 cycles, 16 of them for the
+// exponential) of a SIMD's two waves, at the clock that the power limit leaves: one prompt of 32,749 with 32 heads, 8.79 TFLOP, takes
 // 7.1 ms, 1.23 PFLOP/s, where a library product of 16,384^3 reaches 1.31 and one of 8,192^3 1.15.
 #include "api_checks.h"
 #include "kv_store.h"
@@ -572,13 +573,18 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             }
             // its last tile, whose first products are done
             const uint32_t bits = hidden_keys(t, 1);
+            // two sets: both products of an operand; one: one half after the other
+            auto turn_of = [](int c) { return SETS == 2 ? c & 1 : c >> 3; };
+            auto step_of = [](int c) { return SETS == 2 ? c >> 1 : c & 7; };
+            bf16x8 x[16 / SETS];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = v_operand(t & (kStages - 1), turn_of(c * SETS), step_of(c * SETS));
 #pragma unroll
             for (int i = 0; i < 8; ++i) exponentials(1, i, true, bits);
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {                   // two sets: both products of an operand; one: one half after the other
-                const int s = SETS == 2 ? c & 1 : c >> 3, i = SETS == 2 ? c >> 1 : c & 7;
-                product(s, i, v_operand(t & (kStages - 1), s, i), probabilities(s, i >> 2));
-            }
+            for (int c = 4; c < 16 / SETS; ++c) x[c] = v_operand(t & (kStages - 1), turn_of(c * SETS), step_of(c * SETS));
+#pragma unroll
+            for (int c = 0; c < 16; ++c) product(turn_of(c), step_of(c), x[c / SETS], probabilities(turn_of(c), step_of(c) >> 2));
             for (; t + 1 < n_tiles; ++t) {
                 request_k(t & (kStages - 1));
                 request_v((t + kStages - 1) & (kStages - 1));
@@ -594,12 +600,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
                 l_run[s] = half_swap(l_run[s], [](float x, float y) { return x + y; });
-                float zero = 0.f;
+                float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int dt = 0; dt < 4; ++dt)
+                for (int r = 0; r < 16; ++r)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) zero = fmaf(o[s][dt][r], 0.f, zero);
-                fine = fine && l_run[s] <= kPromptMaxSum && zero == 0.f;
+                    for (int dt = 0; dt < 4; ++dt) zero[dt] = fmaf(o[s][dt][r], 0.f, zero[dt]);
+                fine = fine && l_run[s] <= kPromptMaxSum && zero[0] + zero[1] + zero[2] + zero[3] == 0.f;
             }
             if (__syncthreads_or(!fine) != 0) {              // (all waves have read the stages)
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was requested beyond the last tile)
@@ -738,9 +744,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 int at = ((q - query0) * a.Hq + of) * kD + slot * 8;
                 const int heads = 4 % a.G, step = (4 / a.G * a.Hq + heads) * kD, wrap = (a.Hq - a.G) * kD;
                 auto row_piece = [&](int i) { return *reinterpret_cast<const uint4 *>(rows + (4 * i + row) * kD + ((slot ^ (4 * (i & 3) + row)) << 3)); };
+                uint4 piece[Shape::kSetRows / 4];
+#pragma unroll
+                for (int i = 0; i < Shape::kSetRows / 4; ++i) piece[i] = row_piece(i);
 #pragma unroll
                 for (int i = 0; i < Shape::kSetRows / 4; ++i) {
-                    if (row0 + Shape::kSetRows <= n_rows || row0 + 4 * i + row < n_rows) *reinterpret_cast<uint4 *>(out + at) = row_piece(i);
+                    if (row0 + 4 * i + row < n_rows) *reinterpret_cast<uint4 *>(out + at) = piece[i];
                     of += heads;
                     at += step + (of >= a.G ? wrap : 0);
                     of -= of >= a.G ? a.G : 0;
