@@ -315,3 +315,44 @@ def test_append_and_gather_on_another_stream_and_in_a_graph(ihip):
             assert torch.equal(got, w), i
         for b, n in enumerate(lens.tolist()):
             assert torch.equal(k_out[b, :, :n], want[1][b, :, :n]) and torch.equal(v_out[b, :, :n], want[2][b, :, :n])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("page", [0, 16])
+def test_caches_whose_tokens_hold_all_heads(ihip, fmt, page):
+    """[.., tokens, heads, d] in memory, more of it between the rows, a cache that begins inside a larger one: the same as head by head."""
+    c = Cache(ihip, fmt, 2, 3, 64, page, seed=31)
+
+    def spread(t):
+        n, H, T, w = t.shape
+        big = torch.full((n + 1, T, H + 2, w), 7, dtype=t.dtype, device="cuda")
+        view = big[1:, :, 1:H + 1].transpose(1, 2)
+        view.copy_(t)
+        return big, view
+
+    big_k, k = spread(c.k)
+    big_v, v = spread(c.v)
+    if fmt == "mx4":
+        (big_ks, ks), (big_vs, vs) = spread(c.ks), spread(c.vs)
+        other = ihip.KVStore.mx4(k, v, ks, vs, c.table)
+    else:
+        other = ihip.KVStore.bf16(k, v, c.table) if fmt == "bf16" else ihip.KVStore.e4m3(k, v, SCALES, c.table)
+    new, lens = [9, 30], torch.tensor([40, 61], dtype=torch.int32).cuda()
+    nk, nv = normal(32, 39, 3, D).cuda(), normal(33, 39, 3, D).cuda()
+    angles = torch.rand((64, D // 2), generator=torch.Generator().manual_seed(34))
+    rope = angles.cos().cuda(), angles.sin().cuda()
+    got = []
+    for store in (c.store, other):
+        ihip.kv_append(store, nk, nv, offsets(new).cuda(), lens, 64, rope=rope)
+        out = [torch.zeros((2, 3, 64, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        got.append(ihip.kv_gather(store, lens, 64, *out))
+    for a, b in zip(*got):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+    for a, b in ((c.k, k), (c.v, v)) + (((c.ks, ks), (c.vs, vs)) if fmt == "mx4" else ()):
+        assert torch.equal(a.view(torch.int16) if fmt == "bf16" else a, b.contiguous().view(torch.int16) if fmt == "bf16" else b)
+    for big in (big_k, big_v):                           # what lies between the rows
+        assert bool((big[0] == 7).all()) and bool((big[:, :, 0] == 7).all()) and bool((big[:, :, 4:] == 7).all())
+    if fmt == "mx4":
+        q = normal(35, 2, 6, 1, D).cuda()
+        a, b = (ihip.sparse_attn_decode_mx4(ihip.Layer(q, x, lens, 1, 0, 64, max_seq_len=64), q, x)[0] for x in (c.store, other))
+        assert torch.equal(a, b)

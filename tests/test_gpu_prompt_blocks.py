@@ -56,3 +56,52 @@ def test_many_sequences(ihip, new):  # noqa: F811
     ihip.prompt_attn(q, k, v, offsets(new), max(new + [1]), out=out, lse=lse)
     check(q, k, v, new, new, out, lse)
     assert bool((out[N:] == 5).all()) and bool((lse[N:] == 5).all())
+
+
+@pytest.mark.parametrize("Hq,Hkv,lists", [
+    (8, 2, [[300, 1, 99], [100, 200, 100], [0, 0, 400], [398, 1, 1]]),                            # all at once
+    (128, 16, [[300, 500, 99], [500, 399, 0], [1, 400, 498]]),                                    # in the order of their keys
+    (6, 2, [[(i * 7) % 40 for i in range(70)], [(i * 11) % 40 for i in range(70)], [0] * 69 + [40]]),        # found by their rows
+])
+def test_lengths_that_change_under_a_graph(ihip, Hq, Hkv, lists):  # noqa: F811
+    N, most = max(sum(x) for x in lists), max(max(x) for x in lists)
+    q, k, v = normal(21, N, Hq, D), normal(22, N, Hkv, D), normal(23, N, Hkv, D)
+    cu = offsets(lists[0])
+    out, lse = torch.empty_like(q), torch.empty((N, Hq), device="cuda")
+
+    def step():
+        ihip.prompt_attn(q, k, v, cu, most, out=out, lse=lse)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for new in lists:
+        cu.copy_(offsets(new))
+        out.fill_(5), lse.fill_(5)
+        g.replay()
+        torch.cuda.synchronize()
+        check(q, k, v, new, new, out, lse)
+        n = sum(new)
+        assert bool((out[n:] == 5).all()) and bool((lse[n:] == 5).all())
+
+
+def test_two_calls_at_once(ihip):  # noqa: F811
+    """Two streams, each with calls in shares and by themselves, whose workgroups share the chip."""
+    sets = []
+    for i in range(2):
+        q, k, v = normal(40 + i, 1200, 32, D), normal(50 + i, 21200, 8, D), normal(60 + i, 21200, 8, D)
+        sets.append((q, k, v, [(offsets([1200]), 1200, None, 1200), (offsets([200, 1000]), 1000, offsets([15000, 6200]), 21200)]))
+    want = [[ihip.prompt_attn(q, k[:rows], v[:rows], cu, n, cu_k=cu_k)[0] for cu, n, cu_k, rows in calls] for q, k, v, calls in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(3):
+        got = [[], []]
+        for i, (q, k, v, calls) in enumerate(sets):
+            with torch.cuda.stream(streams[i]):
+                for cu, n, cu_k, rows in calls:
+                    got[i].append(ihip.prompt_attn(q, k[:rows], v[:rows], cu, n, cu_k=cu_k)[0])
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
