@@ -295,6 +295,11 @@ __global__ __launch_bounds__(kD * kMxMergeGroups) void attn_decode_mx4_merge_ker
     if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
 }
 
+// Most slots that a problem has: sink and window are not longer than the sequence, whatever they are given as
+static int64_t mx4_slots(const ihip_shape &s, int n_blocks, int block)
+{
+    return std::min<int64_t>((int64_t)s.n_sink + s.n_stream, s.max_seq_len) + (int64_t)n_blocks * block;
+}
 // Splits of a problem, which the kernel makes equally long.  A workgroup that has a compute unit to itself takes 10.7 ns a slot (it waits
 // for its loads), three that share one 21 ns (they wait for the memory); a round of workgroups 2 us more than its slots, the launch 3, and the
 // merge with its launch 10.  The least of that over one split (no merge), the splits that give every compute unit one, two or three
@@ -303,7 +308,7 @@ __global__ __launch_bounds__(kD * kMxMergeGroups) void attn_decode_mx4_merge_ker
 // (two rounds), 9, 12, 15 and 18 splits 120, 101, 103, 105, 109 and 112.
 static int mx4_splits(const ihip_shape &s, int n_blocks, int block)
 {
-    const int64_t total = (int64_t)s.n_sink + (int64_t)n_blocks * block + s.n_stream, P = std::max(1, s.B * s.Hkv);
+    const int64_t total = std::max<int64_t>(1, mx4_slots(s, n_blocks, block)), P = std::max(1, s.B * s.Hkv);
     const int64_t cu = compute_units(), places = cu * kMxPerCu;
     const int64_t fewest = (total + kMxMaxSplit - 1) / kMxMaxSplit, most = (total + kMxMinSplit - 1) / kMxMinSplit;
     int64_t best = fewest;
@@ -351,7 +356,7 @@ extern "C" int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_t
         return fail(IHIP_ERR_UNSUPPORTED, "%s: strides must be from 0 to 2^32 rows of 64 bytes", who);
     if (n_blocks < 0 || !pow2(block)) return fail(IHIP_ERR_INVALID_ARG, "%s: n_blocks = %d, block = %d", who, n_blocks, block);
     if (n_blocks > 0 && !block_starts) return fail(IHIP_ERR_INVALID_ARG, "%s: block_starts is NULL", who);
-    if ((int64_t)shape->n_sink + (int64_t)n_blocks * block + shape->n_stream > INT32_MAX - kMxMaxSplit)
+    if (mx4_slots(*shape, n_blocks, block) > INT32_MAX - kMxMaxSplit)
         return fail(IHIP_ERR_UNSUPPORTED, "%s: more than 2^31 slots", who);
     if (!out) return fail(IHIP_ERR_INVALID_ARG, "%s: out is NULL", who);
     const size_t need = attn_decode_mx4_workspace(*shape, n_blocks, block);

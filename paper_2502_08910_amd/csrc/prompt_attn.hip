@@ -1,13 +1,13 @@
 // Dense causal attention of packed prompts on v_mfma_f32_32x32x16_bf16.
 //   out_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(c q_i k_j - r_i),   j <= i + (keys - queries),   c = sm_scale log2 e
-// in one pass over the keys, for a reference r_i that is the row's maximum over its first tile (below).  A wave holds the queries (the right
-// operand of the first product, K the left one), so that a lane has 16 of the 32 scores of one query, its exponentials are already
+// in one pass over the keys, for a reference r_i that is the row's maximum over its first tile (below).  A wave holds its rows (queries' heads; the right
+// operand of the first product, K the left one), so that a lane has 16 of the 32 scores of one row, its exponentials are already
 // the right operand of the second product with V^T (whose rows it takes in the order of the scores), and nothing of P goes through LDS.
 // K and V go from memory to LDS by themselves (global_load_lds), 16-byte chunks XORed with the row, so that both the rows of K and the
 // transposed reads of V (ds_read_b64_tr_b16) are without conflicts.
 // Bound by the matrix units (32 cycles an instruction) and the vector units (four instructions a product, 28 cycles, 16 of them for the
 // exponential) of a SIMD's two waves, at the clock that the power limit leaves: one prompt of 32,749 with 32 heads, 8.79 TFLOP, takes
-// 7.1 ms, 1.23 PFLOP/s, where a library product of 16,384^3 reaches 1.31 and one of 8,192^3 1.15.
+// 7.1 ms, 1.24 PFLOP/s, where a library product of 16,384^3 reaches 1.31 and one of 8,192^3 1.15.
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>
@@ -27,7 +27,7 @@ constexpr int kPromptWaves = 4;
 // lane), what is read from LDS serves two matrix instructions, and the keys are read half as often; tiles have 32 keys.
 template <int SETS>
 struct PromptShape {
-    static constexpr int kSetRows = 32 * SETS, kRows = kSetRows * kPromptWaves;          // queries of a wave and of a workgroup
+    static constexpr int kSetRows = 32 * SETS, kRows = kSetRows * kPromptWaves;          // rows of a wave and of a workgroup
     static constexpr int kKeys = 64 / SETS, kEl = kKeys * kD;                            // of a tile
     static constexpr int kPerCu = 3 - SETS;                                              // workgroups of a compute unit
     static constexpr int kStages = SETS == 2 ? 4 : 2;                                    // tiles of K, and of V, in LDS
@@ -54,14 +54,14 @@ struct PromptArgs {
     float *lse;                      // [rows_q, Hq] or null
     // launches whose work is dealt out in equal shares: partial results of parts of blocks, two a workgroup
     float4 *part_o;                  // [part][wave][accumulators of a lane, four at a time: 16 a set][lane]
-    float2 *part_ml;                 // [part][wave][set][32 queries]: reference of the exponentials (log2 units), sum
+    float2 *part_ml;                 // [part][wave][set][32 rows]: reference of the exponentials (log2 units), sum
 };
 
 // ---- shares ------------------------------------------------------------------
 // Where there are too few blocks x heads to keep the compute units busy to the end, the tiles of all blocks are dealt out in equal
 // shares, one to each workgroup that the chip holds at a time, which begin and end inside blocks; a second kernel merges the
-// parts of a block.  The list goes KV head by KV head, sequence by sequence, block by
-// block; a block weighs its tiles and kBlockCost for its beginning and end.
+// parts of a block.  The list goes KV head by KV head, sequence by sequence, block by block; a block weighs its tiles and kBlockCost for
+// its beginning and end.
 
 // A sequence and its blocks of rows.  The G query heads of a KV head go together: row query * G + head.  Fewer keys that only some rows of a
 // block see, fuller last blocks, and keys are read once for all of them.
@@ -864,7 +864,8 @@ static int64_t prompt_blocks(const ihip_packed &p, int rows)
 // longest, or as the rounds of them that the compute units do (blocks of the same length in whole rounds; a whole prompt's blocks, of all
 // lengths up to the longest, fill the rounds), and each begins and ends.  Shares take the mean, and some time for beginnings, ends and the
 // merge.  The longest of several sequences with keys ahead is not known; it is taken for twice the mean, since shares cost a
-// little where all are alike and the others a lot where they are not.  Of 65 calls the estimate takes the faster way on 62, and what is
+// little where all are alike and the others a lot where they are not.  max_q may be a loose bound: no sequence is taken to bring more than
+// 16 times the mean.  Of 65 calls the estimate takes the faster way on 62, and what is
 // 1, 13 and 14 % slower on three.
 // us by themselves / in shares, 32 heads on 8: 1,024 queries 24 / 53, 8,192 469 / 578; 64 on 2,064 keys 36 / 47, 512 on 4,608 66 / 75; 200 on 8,200
 // 109 / 79; 128, 256, 64 and 500 on 3,000 to 12,000 156 / 102; one each of 16 sequences on 8,000 161 / 127; 8 heads, 64 on 60,064 681 /
@@ -875,7 +876,8 @@ static bool prompt_in_shares(const ihip_packed &p, int64_t keys)
 {
     if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return false;
     const double cu = compute_units(), before = std::max<double>(0, (double)(keys - p.rows)) / p.B, mean = (double)p.rows / p.B;
-    const double longest = ((p.B > 1 ? 2 : 1) * before + p.max_q) / 32, tiles = (before + mean / 2) / 32, alike = before / (before + mean / 2);
+    const double most = std::min<double>(p.max_q, std::min<double>(p.rows, 16 * mean));
+    const double longest = ((p.B > 1 ? 2 : 1) * before + most) / 32, tiles = (before + mean / 2) / 32, alike = before / (before + mean / 2);
     auto rounds_of = [&](int rows) {
         return std::min((double)prompt_blocks(p, rows), (double)p.rows * p.Hq / rows + 0.5 * p.B * p.Hkv) / cu;
     };

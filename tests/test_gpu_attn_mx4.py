@@ -148,6 +148,19 @@ def test_scores_that_grow_along_the_keys(ihip):
     check(c, q, out, lse, 0, c.T)
 
 
+@pytest.mark.parametrize("n_sink,n_stream", [(0, 2 ** 31 - 1), (2 ** 31 - 1, 5), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_sinks_and_windows_longer_than_any_sequence(ihip, n_sink, n_stream):
+    """All keys, and scratch for no more than there can be."""
+    lens = [300, 45, 0]
+    c = Cache(ihip, lens, 2, 16, seed=23)
+    q = queries(3, 8, 24)
+    sl = torch.tensor(lens, dtype=torch.int32).cuda()
+    L = ihip.Layer(q, c.store, sl, 1, n_sink, n_stream, max_seq_len=c.T)
+    assert L.workspace(ihip.OP_ATTN_DECODE_MX4, [1], [1]).numel() < 1 << 20
+    out, lse = ihip.sparse_attn_decode_mx4(L, q, c.store, want_lse=True)
+    check(c, q, out, lse, 0, c.T)
+
+
 def test_a_scale_of_zero_gives_the_mean(ihip):
     lens = [300, 45, 1]
     c = Cache(ihip, lens, 2, 16, seed=21)
