@@ -535,7 +535,8 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
  * product, rows are widened to bf16 (exact).  sm_scale is finite and not negative.  The output of an idle place of the
  * batch is 0, its log-sum-exp -INFINITY; so is that of a sequence whose pages all have negative ids
  * (keys on such pages are left out).
- *   ws, ws_bytes device scratch of ihip_workspace_bytes(IHIP_OP_ATTN_DECODE_MX4, ...), 8-byte aligned
+ *   ws, ws_bytes device scratch of ihip_workspace_bytes(IHIP_OP_ATTN_DECODE_MX4, ...), 8-byte aligned; what serves n_blocks serves
+ *                fewer of them, and none
  */
 int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_tensor q, const ihip_kv_store *store,
                                       const int32_t *block_starts, int32_t n_blocks, int32_t block,

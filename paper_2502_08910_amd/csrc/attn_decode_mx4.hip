@@ -306,15 +306,17 @@ static int64_t mx4_slots(const ihip_shape &s, int n_blocks, int block)
 // workgroups, and those that fill two and more rounds.  One split / 768 workgroups or more (us), 8 problems a sequence: 8 sequences of 1,000
 // keys 14.7 / 21.2, 16 of 2,000 25.5 / 20.9, 32 of 1,000 16.9 / 20.2, 32 of 4,000 44.6 / 37.9, 96 of 4,000 88 / 99; 32 of 7,383 to 16,384 in 4, 6
 // (two rounds), 9, 12, 15 and 18 splits 120, 101, 103, 105, 109 and 112.
-static int mx4_splits(const ihip_shape &s, int n_blocks, int block)
+struct MxSplits { int best, most; };                 // most: no less than the best of any shorter list, for the scratch
+static MxSplits mx4_splits(const ihip_shape &s, int n_blocks, int block)
 {
-    const int64_t total = std::max<int64_t>(1, mx4_slots(s, n_blocks, block)), P = std::max(1, s.B * s.Hkv);
+    const int64_t total = mx4_slots(s, n_blocks, block), P = std::max(1, s.B * s.Hkv);
     const int64_t cu = compute_units(), places = cu * kMxPerCu;
-    const int64_t fewest = (total + kMxMaxSplit - 1) / kMxMaxSplit, most = (total + kMxMinSplit - 1) / kMxMinSplit;
+    const int64_t fewest = (total + kMxMaxSplit - 1) / kMxMaxSplit, finest = (total + kMxMinSplit - 1) / kMxMinSplit;
+    const int64_t rounds = (P * fewest + places - 1) / places;
     int64_t best = fewest;
     double least = 1e300;
     auto consider = [&](int64_t n) {
-        n = std::min(std::max(n, fewest), most);
+        n = std::min(std::max(n, fewest), finest);
         const int64_t size = ((total + n - 1) / n + kMxMinSplit - 1) / kMxMinSplit * kMxMinSplit;
         const double share = (double)std::min(P * n, places) / cu, slot = 0.0107 + 0.00515 * std::max(0.0, share - 1);
         const double time = (double)((P * n + places - 1) / places) * ((double)size * slot + 2) + 3 + (n > 1 ? 10 : 0);
@@ -325,14 +327,13 @@ static int mx4_splits(const ihip_shape &s, int n_blocks, int block)
     };
     consider(1);
     for (int k = 1; k <= kMxPerCu; ++k) consider(k * cu / P);
-    const int64_t rounds = (P * fewest + places - 1) / places;
     for (int64_t r = std::max<int64_t>(rounds, 2); r < rounds + 4; ++r) consider(r * places / P);
-    return (int)best;
+    return {(int)best, (int)std::min(std::max((rounds + 3) * places / P, fewest), finest)};
 }
 
 size_t attn_decode_mx4_workspace(const ihip_shape &s, int n_blocks, int block)
 {
-    return (size_t)s.B * s.Hq * mx4_splits(s, n_blocks, block) * (2 + kD) * sizeof(float);
+    return (size_t)s.B * s.Hq * mx4_splits(s, n_blocks, block).most * (2 + kD) * sizeof(float);
 }
 
 }  // namespace ihip
@@ -370,7 +371,7 @@ extern "C" int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_t
     a.block_starts = block_starts;
     a.n_blocks = n_blocks; a.block = block; a.block_log2 = __builtin_ctz(block);
     if ((rc = check_sm_scale(who, sm_scale, &a.scale_log2e)) != IHIP_OK) return rc;
-    a.n_splits = mx4_splits(*shape, n_blocks, block);
+    a.n_splits = mx4_splits(*shape, n_blocks, block).best;
     a.grid = decode_grid(a.ge, a.n_splits, false);
     a.paged = w.paged;
     const int P = shape->B * shape->Hkv;

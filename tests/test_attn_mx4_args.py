@@ -51,3 +51,15 @@ def test_decode_attention_over_4_bit_rows_refuses(b):
     need = L.ihip_workspace_bytes(b.OP_ATTN_DECODE_MX4, ctypes.byref(Shape(2, 8, 2, 128, 1, 1, 4096, 1000, 4, 64, 0)), 1, one(16), one(4))
     assert call(size=need - 1) == -2
     assert call(shape=Shape(0, 8, 2, 128, 1, 1, None, 1000, 4, 64, 0), s=None) == 0
+
+
+def test_scratch_serves_fewer_blocks(b):
+    """With more blocks, or longer ones, no less scratch: what was asked for with one block serves a call without any."""
+    L, one = b.lib(), ctypes.c_int32 * 1
+    for B in (1, 3, 8, 27, 96):
+        for Hkv in (1, 4, 8):
+            for length in (100, 1000, 1921, 4099, 16384, 250007):
+                shape = b.Shape(B, 4 * Hkv, Hkv, 128, 1, 1, 4096, length, 0, length, 0)
+                need = [L.ihip_workspace_bytes(b.OP_ATTN_DECODE_MX4, ctypes.byref(shape), 1, one(block), one(n))
+                        for block, n in ((1, 1), (16, 1), (16, 2), (64, 5), (64, 40), (64, 400))]
+                assert need == sorted(need) and need[0] > 0, (B, Hkv, length, need)

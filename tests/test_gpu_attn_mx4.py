@@ -161,6 +161,21 @@ def test_sinks_and_windows_longer_than_any_sequence(ihip, n_sink, n_stream):
     check(c, q, out, lse, 0, c.T)
 
 
+@pytest.mark.parametrize("B,length", [(1, 500), (4, 1921), (3, 4099), (16, 1000), (27, 700)])
+def test_scratch_asked_for_with_a_block_serves_calls_without(ihip, B, length):
+    lens = [length - 13 * i for i in range(B)]
+    c = Cache(ihip, lens, 8, 16, seed=25)
+    q = queries(B, 32, 26)
+    sl = torch.tensor(lens, dtype=torch.int32).cuda()
+    L = ihip.Layer(q, c.store, sl, 1, 0, length, max_seq_len=length)
+    ws = L.workspace(ihip.OP_ATTN_DECODE_MX4, [16], [1])
+    out, lse = ihip.sparse_attn_decode_mx4(L, q, c.store, want_lse=True, ws=ws)
+    again, lse2 = ihip.sparse_attn_decode_mx4(L, q, c.store, want_lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    if B < 5:
+        check(c, q, out, lse, 0, length)
+
+
 def test_a_scale_of_zero_gives_the_mean(ihip):
     lens = [300, 45, 1]
     c = Cache(ihip, lens, 2, 16, seed=21)
