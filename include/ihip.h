@@ -534,7 +534,8 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
  * exponentials and sums in fp32; the probabilities are rounded to bf16 for the second
  * product, rows are widened to bf16 (exact).  sm_scale is finite and not negative.  The output of an idle place of the
  * batch is 0, its log-sum-exp -INFINITY; so is that of a sequence whose pages all have negative ids
- * (keys on such pages are left out).
+ * (keys on such pages are left out).  A key with a scale of 255 that is attended to makes all results of its KV head's queries NaN, a
+ * value with one the 32 dimensions of the group.
  *   ws, ws_bytes device scratch of ihip_workspace_bytes(IHIP_OP_ATTN_DECODE_MX4, ...), 8-byte aligned; what serves n_blocks serves
  *                fewer of them, and none
  */

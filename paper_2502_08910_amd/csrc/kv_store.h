@@ -16,7 +16,8 @@ struct StoreView {
 int32_t check_store(const char *who, const ihip_kv_store *store, const ihip_shape &for_lengths, StoreView *view);
 
 // ---- MX4 ----------------------------------------------------------------------
-// 2^(s - 127) of a scale byte; what the converters take as their scale (only its exponent counts there).  255 gives infinity.
+// 2^(s - 127) of a scale byte; what the converters take as their scale (only its exponent counts there).  255, which is an infinity here, is
+// NaN to them: all codes widen to NaN, 0 too (checked on the card with codes of 0 and of any kind).
 __device__ inline float mx4_scale(uint32_t s) { return __uint_as_float(s << 23); }
 
 // One byte of codes (in byte SEL of w) -> two bf16, exact: E2M1 times a power of two is a bf16 number
