@@ -531,8 +531,8 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
  * ihip_sparse_attn_decode over a store of 4-bit rows (IHIP_KV_MX4): the same
  * key set, shape, block_starts and outputs.  With n_blocks == 0 (block_starts may
  * then be NULL) and n_stream >= max_seq_len every key is attended to.  Scores,
- * exponentials and sums in fp32; the probabilities are rounded to bf16 for the second
- * product, rows are widened to bf16 (exact).  sm_scale is finite and not negative.  The output of an idle place of the
+ * exponentials and sums in fp32; the probabilities go into the second product with 16 bits or
+ * more, rows are widened to bf16 (exact).  sm_scale is finite and not negative.  The output of an idle place of the
  * batch is 0, its log-sum-exp -INFINITY; so is that of a sequence whose pages all have negative ids
  * (keys on such pages are left out).  A key with a scale of 255 that is attended to makes all results of its KV head's queries NaN, a
  * value with one the 32 dimensions of the group.
