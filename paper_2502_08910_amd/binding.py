@@ -798,8 +798,8 @@ class KVStore:
 
 def _packed_tensor(t: torch.Tensor, name: str, rows: Optional[int] = None, heads: Optional[int] = None) -> Tensor:
     shape, stride = t.shape, t.stride()
-    if t.dtype != torch.bfloat16 or len(shape) != 3 or stride[2] != 1 or not t.is_cuda:
-        raise IhipError(f"{name}: need a 3-d bf16 device tensor [rows, heads, d] with contiguous last dim")
+    if t.dtype != torch.bfloat16 or len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or not t.is_cuda:
+        raise IhipError(f"{name}: need a 3-d bf16 device tensor [rows, heads, 128] with contiguous last dim")
     if rows is not None and (shape[0] != rows or shape[1] != heads):
         raise IhipError(f"{name}: need {rows} rows of {heads} heads, got {tuple(shape[:2])}")
     return Tensor(t.data_ptr(), 0, stride[1], stride[0])
