@@ -521,7 +521,7 @@ typedef struct ihip_packed {
  * elements is the smallest power of two, from 2^-100 to 2^125, with which their largest
  * magnitude is at most 7 (which rounds to 6; above 7 * 2^125 everything does); with a NaN or infinity among them it is 255.
  * A token whose position is outside [0, max_seq_len) is dropped: nothing is written
- * for it.  Two tokens must not share a row of the cache.
+ * for it.  Two tokens must not share a row of the cache; overlapping heads of an output or of the cache are refused.
  */
 int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v,
                        const int32_t *seq_lens, int32_t max_seq_len, const ihip_rope *rope,

@@ -6,6 +6,7 @@
 // (5.0).  One token of each of 32 sequences takes 5.4 us, a chain of latencies: offsets, lengths, page, rows.
 #include "api_checks.h"
 #include "kv_store.h"
+#include <cstdlib>
 #include <type_traits>
 
 namespace ihip {
@@ -220,11 +221,13 @@ int32_t check_packed(const char *who, const ihip_packed *p)
 }
 
 // a bf16 tensor that is written: rows of their own
-int32_t check_output(const ihip_tensor &t, const char *who, const char *name)
+int32_t check_output(const ihip_tensor &t, const char *who, const char *name, int heads)
 {
     const int32_t rc = check_tensor(t, who, name);
     if (rc != IHIP_OK) return rc;
     if (t.stride_t < kD) return fail(IHIP_ERR_INVALID_ARG, "%s: %s.stride_t = %lld < d", who, name, (long long)t.stride_t);
+    if (heads > 1 && t.stride_h < kD && t.stride_h > -kD)
+        return fail(IHIP_ERR_INVALID_ARG, "%s: the heads of %s overlap (stride_h = %lld)", who, name, (long long)t.stride_h);
     return IHIP_OK;
 }
 
@@ -236,7 +239,7 @@ int32_t check_store(const char *who, const ihip_kv_store *store, const ihip_shap
     w.k_scale = w.v_scale = 1.0f;
     int unit = 1;
     if (store->format == IHIP_KV_BF16) {
-        if ((rc = check_output(store->k, who, "k")) != IHIP_OK || (rc = check_output(store->v, who, "v")) != IHIP_OK) return rc;
+        if ((rc = check_output(store->k, who, "k", 1)) != IHIP_OK || (rc = check_output(store->v, who, "v", 1)) != IHIP_OK) return rc;
         unit = 2;
     } else if (store->format == IHIP_KV_E4M3) {
         if ((rc = check_tensor8(store->k, who, "k")) != IHIP_OK || (rc = check_tensor8(store->v, who, "v")) != IHIP_OK) return rc;
@@ -288,8 +291,8 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
     if (packed->B == 0 || packed->rows == 0) return IHIP_OK;
     if ((rc = check_tensor(k, who, "k")) != IHIP_OK || (rc = check_tensor(v, who, "v")) != IHIP_OK) return rc;
     const bool with_q = q_out.ptr != nullptr;
-    if (with_q && ((rc = check_tensor(q, who, "q")) != IHIP_OK || (rc = check_output(q_out, who, "q_out")) != IHIP_OK)) return rc;
-    if (k_out.ptr && (rc = check_output(k_out, who, "k_out")) != IHIP_OK) return rc;
+    if (with_q && ((rc = check_tensor(q, who, "q")) != IHIP_OK || (rc = check_output(q_out, who, "q_out", packed->Hq)) != IHIP_OK)) return rc;
+    if (k_out.ptr && (rc = check_output(k_out, who, "k_out", packed->Hkv)) != IHIP_OK) return rc;
     if (!seq_lens) return fail(IHIP_ERR_INVALID_ARG, "%s: seq_lens is NULL", who);
     if (max_seq_len <= 0) return fail(IHIP_ERR_INVALID_ARG, "%s: max_seq_len = %d", who, max_seq_len);
     if (rope && (!rope->cos || !rope->sin || (((uintptr_t)rope->cos | (uintptr_t)rope->sin) & 15)))
@@ -300,6 +303,9 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
     ihip_shape lengths{};
     lengths.max_seq_len = max_seq_len;
     if ((rc = check_store(who, store, lengths, &a.to)) != IHIP_OK) return rc;
+    const int64_t row = store->format == IHIP_KV_BF16 ? 2 * kD : store->format == IHIP_KV_E4M3 ? kD : kD / 2;
+    if (packed->Hkv > 1 && (std::abs(a.to.k_sh) < row || std::abs(a.to.v_sh) < row))
+        return fail(IHIP_ERR_INVALID_ARG, "%s: the heads of the store overlap", who);
     a.B = packed->B; a.Hq = packed->Hq; a.Hkv = packed->Hkv; a.rows = packed->rows; a.max_len = max_seq_len;
     a.cu = packed->cu_q; a.lens = seq_lens;
     a.q = (const uint16_t *)q.ptr; a.q_sh = q.stride_h; a.q_st = q.stride_t;
@@ -339,8 +345,8 @@ int32_t ihip_kv_gather(const ihip_kv_store *store, int32_t B, int32_t Hkv, int32
     if (max_seq_len < 0) return fail(IHIP_ERR_INVALID_ARG, "%s: max_seq_len = %d", who, max_seq_len);
     if (B == 0 || max_seq_len == 0) return IHIP_OK;
     if (!seq_lens) return fail(IHIP_ERR_INVALID_ARG, "%s: seq_lens is NULL", who);
-    if (k_out.ptr && (rc = check_output(k_out, who, "k_out")) != IHIP_OK) return rc;
-    if (v_out.ptr && (rc = check_output(v_out, who, "v_out")) != IHIP_OK) return rc;
+    if (k_out.ptr && (rc = check_output(k_out, who, "k_out", Hkv)) != IHIP_OK) return rc;
+    if (v_out.ptr && (rc = check_output(v_out, who, "v_out", Hkv)) != IHIP_OK) return rc;
     GatherArgs a{};
     ihip_shape lengths{};
     lengths.max_seq_len = max_seq_len;
