@@ -557,6 +557,7 @@ int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_tensor q, co
  * QK^T and PV run on the matrix cores (bf16 operands, the probabilities rounded to
  * bf16, fp32 accumulation), softmax in fp32.  A query that sees no key (t < n)
  * gets 0, and -INFINITY.  A sequence of more than max_q tokens may be done in part only.
+ * rows * (Hq/Hkv), and the 128 elements of all heads of 256 / (Hq/Hkv) + 2 queries, must be fewer than 2^31.
  * sm_scale is finite and not negative.  A key or a value that is not finite makes only those results NaN or infinite that see it.
  *   ws, ws_bytes device scratch of ihip_prompt_attn_workspace_bytes(packed, rows_k), 16-byte aligned; may be NULL.  A call with few
  *                queries on many keys deals its work out to the whole chip in equal shares and merges the parts there;

@@ -921,6 +921,12 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     // the rows of a tile, and of a wave's queries, are addressed by 32-bit byte offsets from the first
     if ((a.q_st | a.k_st | a.v_st) < 0 || a.q_st >= (1 << 24) || a.k_st >= (1 << 24) || a.v_st >= (1 << 24))
         return fail(IHIP_ERR_UNSUPPORTED, "%s: rows of q, k and v must be less than 2^24 elements apart", who);
+    const int64_t groups = prompt_blocks(*packed, PromptShape<1>::kRows);
+    if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
+    // so are a KV head's rows counted, and the results of a block, which are the heads of up to kRows / G + 2 queries
+    constexpr int most = PromptShape<2>::kRows;
+    if ((int64_t)a.rows_q * a.G > INT32_MAX - most || ((most / a.G + 2) * (int64_t)a.Hq + a.G) * kD > INT32_MAX)
+        return fail(IHIP_ERR_UNSUPPORTED, "%s: %d rows of %d heads (%d KV heads) are too many", who, a.rows_q, a.Hq, a.Hkv);
     if ((rc = check_sm_scale(who, sm_scale, &a.scale_log2e)) != IHIP_OK) return rc;
     a.log2_G = pow2(a.G) ? __builtin_ctz(a.G) : -1;
     a.out = (uint16_t *)out;
@@ -949,11 +955,9 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
     // (A workgroup a block, handed out by the hardware.  512 that stay, each with every 512th block and the first tiles of its next one
     // on their way under the end of the present one: 8 prompts of 640 to 2,048 172 -> 185 us, one of 32,749 7.17 -> 7.52 ms.)
     // The order of the blocks matters where some compute unit has two.  Finding them without it is shorter: 512 queries, 32 heads 18.5 -> 17.6 us
-    const int64_t groups = prompt_blocks(*packed, Shape::kRows);
     a.ordered = packed->B <= kOrderedSeqs && groups > compute_units();
     const int64_t places = ((int64_t)packed->max_q * a.G - 1) / Shape::kRows + 1;
     a.places = groups == places * packed->B * packed->Hkv ? (int)places : 0;
-    if (groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)groups);
     KernelTimer timer("prompt_attn", st);
     hipLaunchKernelGGL(prompt_attn_kernel<1>, dim3((uint32_t)groups), dim3(64 * kPromptWaves), Shape::kLds, st, a);
     return check_launch(who);
