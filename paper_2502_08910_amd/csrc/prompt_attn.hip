@@ -36,8 +36,10 @@ struct PromptShape {
     static constexpr int kBlockCost = 4, kMinPart = 4, kMinShare = 12;
 };
 constexpr int kOrderedSeqs = 64;                     // up to so many sequences, one a lane, blocks go in the order of their keys
-constexpr float kNegBigPrompt = -1.0e30f;            // finite stand-in for -inf in maxima
-constexpr float kPromptMaxSum = 18446744073709551616.0f;      // 2^64: sum of exponentials beyond which a block is done again
+constexpr float kPromptLowest = -3.4028234e38f;      // stand-in for -inf in maxima: no score is below it
+// A block is done again where a sum of exponentials is outside 1/kPromptMaxSum .. kPromptMaxSum or a reference beyond +-kPromptMaxRef (whose
+// rounding the exponentials would show), then with exponentials times 2^-kPromptShift: sums of up to a million of the largest values are finite
+constexpr float kPromptMaxSum = 0x1p64f, kPromptMaxRef = 0x1p22f, kPromptShift = 20.f;
 
 int32_t check_packed(const char *who, const ihip_packed *p);
 
@@ -403,17 +405,17 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sc[s][r] = hide(bits, r, sc[s][r]);
             };
-            auto row_max = [&](const f32x16 &s) {            // scaled; of both halves of the wave
+            auto row_max = [&](const f32x16 &s) {            // of both halves of the wave
                 float mx = s[0];
 #pragma unroll
                 for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-                return half_swap(mx, [](float x, float y) { return fmaxf(x, y); }) * a.scale_log2e;
+                return half_swap(mx, [](float x, float y) { return fmaxf(x, y); });
             };
 
             uint32_t pw[2][8];                               // the probabilities of a turn, in pairs of keys
             float m_ref[SETS], l_run[SETS];
 #pragma unroll
-            for (int s = 0; s < SETS; ++s) m_ref[s] = kNegBigPrompt;
+            for (int s = 0; s < SETS; ++s) m_ref[s] = kPromptLowest;
             // two scores -> two probabilities (exp2(-inf) = 0).  The empty assembly keeps them where they are called: left to themselves all
             // exponentials of a turn would be computed in front of the other's matrix instructions instead of under them.
             auto exponentials = [&](int s, int i, bool masked, uint32_t bits) {
@@ -545,7 +547,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             for (int s = 0; s < 2; ++s) {
                 scores(0, s);
                 mask(0, s);
-                m_ref[qs(s)] = fmaxf(m_ref[qs(s)], row_max(sc[s]));
+                m_ref[qs(s)] = fmaxf(m_ref[qs(s)], row_max(sc[s]) * a.scale_log2e);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) exponentials(0, i, false, 0);
@@ -605,7 +607,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 for (int r = 0; r < 16; ++r)
 #pragma unroll
                     for (int dt = 0; dt < 4; ++dt) zero[dt] = fmaf(o[s][dt][r], 0.f, zero[dt]);
-                fine = fine && l_run[s] <= kPromptMaxSum && zero[0] + zero[1] + zero[2] + zero[3] == 0.f;
+                fine = fine && (last_key[s] < 0 || (l_run[s] >= 1 / kPromptMaxSum && l_run[s] <= kPromptMaxSum && fabsf(m_ref[s]) <= kPromptMaxRef)) &&
+                       zero[0] + zero[1] + zero[2] + zero[3] == 0.f;
             }
             if (__syncthreads_or(!fine) != 0) {              // (all waves have read the stages)
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was requested beyond the last tile)
@@ -619,7 +622,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 k_next = kb;
                 k_tile = 0;
 #pragma unroll
-                for (int s = 0; s < SETS; ++s) m_ref[s] = kNegBigPrompt;
+                for (int s = 0; s < SETS; ++s) m_ref[s] = kPromptLowest;
                 for (t = 0; t < n_tiles; ++t) {
                     tile_here(true, false);
 #pragma unroll
@@ -683,7 +686,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                         scores(0, s);
                         mask(t, s);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) exponentials(s, i, false, 0);
+                        for (int i = 0; i < 8; ++i) {        // against the maximum as it came from the products: scaled, it would be rounded
+                            const float x = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i] - m_ref[qs(s)], a.scale_log2e, -kPromptShift));
+                            const float y = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i + 1] - m_ref[qs(s)], a.scale_log2e, -kPromptShift));
+                            l_run[qs(s)] += x;
+                            l_run[qs(s)] += y;
+                            pw[s][i] = pack_bf16x2(x, y);
+                        }
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             bf16x8 x = v_operand(0, s, i);
@@ -696,6 +705,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 settle();
 #pragma unroll
                 for (int s = 0; s < SETS; ++s) {
+                    m_ref[s] = fmaf(m_ref[s], a.scale_log2e, kPromptShift);
                     l_run[s] = half_swap(l_run[s], [](float x, float y) { return x + y; });
 #pragma unroll
                     for (int dt = 0; dt < 4; ++dt)
@@ -791,7 +801,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
         if (before > 0) return;                      // not the first
     }
     const int n = lane & 31, half = lane >> 5, s = quarter * kPieces / 16;
-    float M = kNegBigPrompt, L = 0.f;
+    float M = kPromptLowest, L = 0.f;
     float4 acc[kPieces];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
