@@ -559,6 +559,7 @@ int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_tensor q, co
  * gets 0, and -INFINITY.  A sequence of more than max_q tokens may be done in part only.
  * rows * (Hq/Hkv), and the 128 elements of all heads of 256 / (Hq/Hkv) + 2 queries, must be fewer than 2^31.
  * sm_scale is finite and not negative.  A key or a value that is not finite makes only those results NaN or infinite that see it.
+ * A value of +INFINITY makes them that, however small its probability, -INFINITY likewise, both or a NaN make them NaN.
  *   ws, ws_bytes device scratch of ihip_prompt_attn_workspace_bytes(packed, rows_k), 16-byte aligned; may be NULL.  A call with few
  *                queries on many keys deals its work out to the whole chip in equal shares and merges the parts there;
  *                with NULL, less or a misaligned pointer it does not (slower; equal up to rounding).  Calls that overlap

@@ -595,9 +595,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             }
             settle();
             // Where a row's sum says that its scores left that range, or a result is not finite, the block is done again, a tile at a time and
-            // against the maxima over all tiles.  What is not finite in V is only for the queries that see it: a probability of 0
-            // times it would be NaN for the others.  So products with the tiles that some queries see in part take 0 in its place, and
-            // the queries that do see some get their NaN at the end; which those are, say the products of "sees it" and "is not finite".
+            // against the maxima over all tiles.  What is not finite in V is for all queries that see it, however small its probability has
+            // become in fp32, and for no others, for whom a probability of 0 times it would be NaN.  So the products take 0 in its place, and
+            // infinity or NaN is added at the end for the queries that see some; which those are, and of what, say the products of "sees it" and a
+            // code for "is +infinity", "-infinity" or "NaN".
             bool fine = true;
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
@@ -612,7 +613,6 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             }
             if (__syncthreads_or(!fine) != 0) {              // (all waves have read the stages)
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was requested beyond the last tile)
-                const int whole = max(seen, 0);
                 auto tile_here = [&](bool k, bool v) {
                     if (k) request_k(0);
                     if (v) request_v(0);
@@ -633,9 +633,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                     }
                     __syncthreads();
                 }
-                // bf16 pairs: 1 where a value is not finite, 0 elsewhere; the values with 0 in their place
-                auto not_finite = [](uint32_t w) {
-                    return ((w & 0x7f80u) == 0x7f80u ? 0x3f80u : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0u);
+                // bf16 pairs: 1, 2^8 and 2^16 for +infinity, -infinity and NaN, 0 elsewhere (sums over a tile are exact); the values with 0 in their place
+                auto code = [](uint32_t w) {
+                    const uint32_t x = w & 0x7fffu, y = w >> 16 & 0x7fffu;
+                    return (x < 0x7f80u ? 0u : x > 0x7f80u ? 0x4780u : (w & 0x8000u) != 0 ? 0x4380u : 0x3f80u) |
+                           (y < 0x7f80u ? 0u : y > 0x7f80u ? 0x4780u : w >> 31 != 0 ? 0x4380u : 0x3f80u) << 16;
                 };
                 auto finite = [](uint32_t w) {
                     return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
@@ -644,38 +646,50 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                     const uint4 w = __builtin_bit_cast(uint4, x);
                     return __builtin_bit_cast(bf16x8, make_uint4(f(w.x), f(w.y), f(w.z), f(w.w)));
                 };
-                clear();
-                v_next = vb + whole * (int64_t)kTileKeys * a.v_st;
-                v_tile = whole;
-                for (t = whole; t < n_tiles; ++t) {
+                uint32_t up[SETS][2], down[SETS][2];         // of the lane's 64 results: which get +infinity, -infinity (both: NaN)
+#pragma unroll
+                for (int s = 0; s < SETS; ++s) up[s][0] = up[s][1] = down[s][0] = down[s][1] = 0;
+                v_next = vb;
+                v_tile = 0;
+                for (t = 0; t < n_tiles; ++t) {
                     tile_here(false, true);
+                    uint32_t any = 0;                        // (all waves see the whole tile)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const uint32_t bits = hidden_keys(t, s);
+                    for (int i = 0; i < 16 / SETS; ++i) {
+                        const uint4 w = __builtin_bit_cast(uint4, of_words(v_operand(0, i >> 3, i & 7), code));
+                        any |= w.x | w.y | w.z | w.w;
+                    }
+                    if (__any(any != 0)) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            pw[s][i] = 0;
+                        for (int s = 0; s < 2; ++s) {
+                            const uint32_t bits = hidden_keys(t, s);
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int r = 2 * i + e;
-                                pw[s][i] |= (bits >> (8 * (r >> 2) + (r & 3)) & 1) != 0 ? 0u : 0x3f80u << (16 * e);
+                            for (int i = 0; i < 8; ++i) {
+                                pw[s][i] = 0;
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const int r = 2 * i + e;
+                                    pw[s][i] |= (bits >> (8 * (r >> 2) + (r & 3)) & 1) != 0 ? 0u : 0x3f80u << (16 * e);
+                                }
                             }
                         }
+                        clear();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) product(s, i, of_words(v_operand(0, s, i), not_finite), probabilities(s, i >> 2));
+                        for (int s = 0; s < 2; ++s)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) product(s, i, of_words(v_operand(0, s, i), code), probabilities(s, i >> 2));
+                        settle();
+#pragma unroll
+                        for (int s = 0; s < SETS; ++s)
+#pragma unroll
+                            for (int r = 0; r < 64; ++r) {
+                                const uint32_t sum = (uint32_t)o[s][r / 16][r % 16];
+                                up[s][r / 32] |= ((sum & 0xffu) != 0 || sum > 0xffffu ? 1u : 0u) << (r % 32);
+                                down[s][r / 32] |= (sum > 0xffu ? 1u : 0u) << (r % 32);
+                            }
                     }
                     __syncthreads();
                 }
-                settle();
-                uint32_t nans[SETS][2];                      // of the lane's 64 results
-#pragma unroll
-                for (int s = 0; s < SETS; ++s)
-#pragma unroll
-                    for (int d = 0; d < 2; ++d) {
-                        nans[s][d] = 0;
-#pragma unroll
-                        for (int r = 0; r < 32; ++r) nans[s][d] |= o[s][2 * d + r / 16][r % 16] != 0.f ? 1u << r : 0u;
-                    }
                 clear();
                 k_next = kb; v_next = vb;
                 k_tile = v_tile = 0;
@@ -694,11 +708,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                             pw[s][i] = pack_bf16x2(x, y);
                         }
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            bf16x8 x = v_operand(0, s, i);
-                            if (t >= whole) x = of_words(x, finite);
-                            product(s, i, x, probabilities(s, i >> 2));
-                        }
+                        for (int i = 0; i < 8; ++i) product(s, i, of_words(v_operand(0, s, i), finite), probabilities(s, i >> 2));
                     }
                     __syncthreads();
                 }
@@ -710,7 +720,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
 #pragma unroll
                     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) o[s][dt][r] = (nans[s][dt / 2] >> (16 * (dt & 1) + r) & 1) != 0 ? NAN : o[s][dt][r];
+                        for (int r = 0; r < 16; ++r) {
+                            if ((up[s][dt / 2] >> (16 * (dt & 1) + r) & 1) != 0) o[s][dt][r] += INFINITY;
+                            if ((down[s][dt / 2] >> (16 * (dt & 1) + r) & 1) != 0) o[s][dt][r] -= INFINITY;
+                        }
                 }
             }
             if (SHARES && n_tiles < all_tiles) {             // a part: its share's first (which does not begin the block) or last one
@@ -803,28 +816,38 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
     const int n = lane & 31, half = lane >> 5, s = quarter * kPieces / 16;
     float M = kPromptLowest, L = 0.f;
     float4 acc[kPieces];
+    auto clear = [&] {
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    // share k's part of the block is [tile_of(k), tile_of(k + 1)), the first one's from 0; a lane finds that of one share.  Up to four parts
-    // are read at a time: 64 queries on 60,064 keys, which are cut into 64 parts, 117 -> 107 us
-    int begun = 0;
-    for (int k0 = j - 1; begun < tiles; k0 += 64) {
-        const int end = tile_of(k0 + lane + 1);
-        int begin = __shfl_up(end, 1, 64);
-        if (lane == 0) begin = begun;
-        begun = __builtin_amdgcn_readlane(end, 63);
-        const int part = 2 * (k0 + lane) + (begin == 0);
-        unsigned long long left = __ballot(begin < end);
+        for (int i = 0; i < kPieces; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    // share k's part of the block is [tile_of(k), tile_of(k + 1)), the first one's from 0; a lane finds that of one share.  f takes the parts
+    // that a wave has found: the lanes that have one, and a lane's
+    auto for_parts = [&](auto f) {
+        int begun = 0;
+        for (int k0 = j - 1; begun < tiles; k0 += 64) {
+            const int end = tile_of(k0 + lane + 1);
+            int begin = __shfl_up(end, 1, 64);
+            if (lane == 0) begin = begun;
+            begun = __builtin_amdgcn_readlane(end, 63);
+            f(__ballot(begin < end), 2 * (k0 + lane) + (begin == 0));
+        }
+    };
+    auto unit_of = [&](unsigned long long left, int part) { return (int64_t)__builtin_amdgcn_readlane(part, __builtin_ctzll(left)) * kPromptWaves + wave; };
+    auto sums_of = [&](int64_t unit) { return a.part_ml[(unit * 2 + s) * 32 + n]; };
+    auto results_of = [&](int64_t unit) { return a.part_o + (unit * 32 + quarter * kPieces) * 64 + lane; };
+    // Up to four parts are read at a time: 64 queries on 60,064 keys, which are cut into 64 parts, 117 -> 107 us
+    clear();
+    for_parts([&](unsigned long long left, int part) {
         auto take = [&](auto count) {
             constexpr int N = decltype(count)::value;
             float2 ml[N];
             float4 x[N][kPieces];
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                const int64_t unit = (int64_t)__builtin_amdgcn_readlane(part, __builtin_ctzll(left)) * kPromptWaves + wave;
+                const int64_t unit = unit_of(left, part);
                 left &= left - 1;
-                ml[c] = a.part_ml[(unit * 2 + s) * 32 + n];
-                const float4 *from = a.part_o + (unit * 32 + quarter * kPieces) * 64 + lane;
+                ml[c] = sums_of(unit);
+                const float4 *from = results_of(unit);
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i) x[c][i] = from[i * 64];
             }
@@ -848,6 +871,26 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
         while (__popcll(left) >= 4) take(std::integral_constant<int, 4>{});
         if (__popcll(left) >= 2) take(std::integral_constant<int, 2>{});
         if (left != 0) take(std::integral_constant<int, 1>{});
+    });
+    // What is infinite, from an infinite value, stays so with any weight, where infinity times 0 would be NaN
+    float zero = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) zero = fmaf(acc[i].x, 0.f, fmaf(acc[i].y, 0.f, fmaf(acc[i].z, 0.f, fmaf(acc[i].w, 0.f, zero))));
+    if (__any(zero != 0.f)) {
+        clear();
+        for_parts([&](unsigned long long left, int part) {
+            for (; left != 0; left &= left - 1) {
+                const int64_t unit = unit_of(left, part);
+                const float w = __builtin_amdgcn_exp2f(sums_of(unit).x - M);
+                const float4 *from = results_of(unit);
+                auto weighted = [&](float x) { return __builtin_isinf(x) ? x : x * w; };
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    const float4 x = from[i * 64];
+                    acc[i] = make_float4(acc[i].x + weighted(x.x), acc[i].y + weighted(x.y), acc[i].z + weighted(x.z), acc[i].w + weighted(x.w));
+                }
+            }
+        });
     }
     const int row = p.m * PromptShape<2>::kRows + wave * PromptShape<2>::kSetRows + s * 32 + n;
     if (row >= seq.rows) return;
