@@ -532,7 +532,7 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
  * key set, shape, block_starts and outputs.  With n_blocks == 0 (block_starts may
  * then be NULL) and n_stream >= max_seq_len every key is attended to.  Scores,
  * exponentials and sums in fp32; the probabilities go into the second product with 16 bits or
- * more, rows are widened to bf16 (exact).  sm_scale is finite and not negative.  The output of an idle place of the
+ * more, rows are widened to bf16 (exact).  sm_scale is not negative and at most 2^127.  The output of an idle place of the
  * batch is 0, its log-sum-exp -INFINITY; so is that of a sequence whose pages all have negative ids
  * (keys on such pages are left out).  A key with a scale of 255 that is attended to makes all results of its KV head's queries NaN, a
  * value with one the 32 dimensions of the group.
@@ -558,7 +558,7 @@ int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_tensor q, co
  * bf16, fp32 accumulation), softmax in fp32.  A query that sees no key (t < n)
  * gets 0, and -INFINITY.  A sequence of more than max_q tokens may be done in part only.
  * rows * (Hq/Hkv), and the 128 elements of all heads of 256 / (Hq/Hkv) + 2 queries, must be fewer than 2^31.
- * sm_scale is finite and not negative.  A key or a value that is not finite makes only those results NaN or infinite that see it.
+ * sm_scale is not negative and at most 2^127.  A key or a value that is not finite makes only those results NaN or infinite that see it.
  * A value of +INFINITY makes them that, however small its probability, -INFINITY likewise, both or a NaN make them NaN.
  *   ws, ws_bytes device scratch of ihip_prompt_attn_workspace_bytes(packed, rows_k), 16-byte aligned; may be NULL.  A call with few
  *                queries on many keys deals its work out to the whole chip in equal shares and merges the parts there;

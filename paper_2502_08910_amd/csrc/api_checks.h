@@ -13,13 +13,13 @@ int32_t check_tensor8(const ihip_tensor &t, const char *who, const char *name); 
 int32_t check_paged(const char *who, const ihip_shape *shape, const ihip_paged_kv *pg, KvFormat *fmt);
 int32_t check_scales(const char *who, float k_scale, float v_scale);
 
-// Not negative and finite (the largest score is then that of the largest product), as a factor for powers of two.  0 becomes the smallest
-// normal number: the scores are 0 as well, and -infinity stays it.
+// Not negative, and finite as a factor for powers of two.  0 becomes the smallest number there is: products times it are close to 0 as well
+// (2^127 * 2^-149), and -infinity stays it.
 inline int32_t check_sm_scale(const char *who, float sm_scale, float *log2_scale)
 {
-    if (!(sm_scale >= 0.0f) || sm_scale > 3.4028234e38f) return fail(IHIP_ERR_INVALID_ARG, "%s: sm_scale = %g", who, sm_scale);
     const float s = sm_scale * 1.44269504088896340736f;
-    *log2_scale = s < 1.17549435e-38f ? 1.17549435e-38f : s;
+    if (!(sm_scale >= 0.0f) || s > 3.4028234e38f) return fail(IHIP_ERR_INVALID_ARG, "%s: sm_scale = %g", who, sm_scale);
+    *log2_scale = s > 0.0f ? s : 0x1p-149f;
     return IHIP_OK;
 }
 
