@@ -613,26 +613,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             }
             if (__syncthreads_or(!fine) != 0) {              // (all waves have read the stages)
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was requested beyond the last tile)
-                auto tile_here = [&](bool k, bool v) {
-                    if (k) request_k(0);
-                    if (v) request_v(0);
+                auto tile_here = [&] {
+                    request_k(0);
+                    request_v(0);
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                     __syncthreads();
                 };
-                k_next = kb;
-                k_tile = 0;
-#pragma unroll
-                for (int s = 0; s < SETS; ++s) m_ref[s] = kPromptLowest;
-                for (t = 0; t < n_tiles; ++t) {
-                    tile_here(true, false);
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        scores(0, s);
-                        mask(t, s);
-                        m_ref[qs(s)] = fmaxf(m_ref[qs(s)], row_max(sc[s]));
-                    }
-                    __syncthreads();
-                }
                 // bf16 pairs: 1, 2^8 and 2^16 for +infinity, -infinity and NaN, 0 elsewhere (sums over a tile are exact); the values with 0 in their place
                 auto code = [](uint32_t w) {
                     const uint32_t x = w & 0x7fffu, y = w >> 16 & 0x7fffu;
@@ -646,20 +632,32 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                     const uint4 w = __builtin_bit_cast(uint4, x);
                     return __builtin_bit_cast(bf16x8, make_uint4(f(w.x), f(w.y), f(w.z), f(w.w)));
                 };
+                bool some = false;                           // values that are not finite
                 uint32_t up[SETS][2], down[SETS][2];         // of the lane's 64 results: which get +infinity, -infinity (both: NaN)
 #pragma unroll
                 for (int s = 0; s < SETS; ++s) up[s][0] = up[s][1] = down[s][0] = down[s][1] = 0;
-                v_next = vb;
-                v_tile = 0;
-                for (t = 0; t < n_tiles; ++t) {
-                    tile_here(false, true);
-                    uint32_t any = 0;                        // (all waves see the whole tile)
 #pragma unroll
-                    for (int i = 0; i < 16 / SETS; ++i) {
-                        const uint4 w = __builtin_bit_cast(uint4, of_words(v_operand(0, i >> 3, i & 7), code));
-                        any |= w.x | w.y | w.z | w.w;
+                for (int s = 0; s < SETS; ++s) m_ref[s] = kPromptLowest;
+                k_next = kb; v_next = vb;
+                k_tile = v_tile = 0;
+                for (t = 0; t < n_tiles; ++t) {
+                    tile_here();
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        scores(0, s);
+                        mask(t, s);
+                        m_ref[qs(s)] = fmaxf(m_ref[qs(s)], row_max(sc[s]));
                     }
-                    if (__any(any != 0)) {
+                    bool found = false;                      // by any of the 256 threads in its share of the tile
+#pragma unroll
+                    for (int i = 0; i < kEl / (8 * 64 * kPromptWaves); ++i) {
+                        const uint4 w = reinterpret_cast<const uint4 *>(smem + kStages * kEl)[i * 64 * kPromptWaves + tid];
+                        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) found |= (x[c] & 0x7f80u) == 0x7f80u || (x[c] & 0x7f800000u) == 0x7f800000u;
+                    }
+                    if (__syncthreads_or(found) != 0) {
+                        some = true;
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
                             const uint32_t bits = hidden_keys(t, s);
@@ -694,7 +692,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 k_next = kb; v_next = vb;
                 k_tile = v_tile = 0;
                 for (t = 0; t < n_tiles; ++t) {
-                    tile_here(true, true);
+                    tile_here();
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         scores(0, s);
@@ -708,7 +706,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                             pw[s][i] = pack_bf16x2(x, y);
                         }
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) product(s, i, of_words(v_operand(0, s, i), finite), probabilities(s, i >> 2));
+                        for (int i = 0; i < 8; ++i) {
+                            bf16x8 x = v_operand(0, s, i);
+                            if (some) x = of_words(x, finite);
+                            product(s, i, x, probabilities(s, i >> 2));
+                        }
                     }
                     __syncthreads();
                 }
