@@ -598,7 +598,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             // against the maxima over all tiles.  What is not finite in V is for all queries that see it, however small its probability has
             // become in fp32, and for no others, for whom a probability of 0 times it would be NaN.  So the products take 0 in its place, and
             // infinity or NaN is added at the end for the queries that see some; which those are, and of what, say the products of "sees it" and a
-            // code for "is +infinity", "-infinity" or "NaN".
+            // code for "is +infinity", "-infinity" or "NaN".  (A sum that is NaN, from a query or a key that is, says all that there is to know of its row.)
             bool fine = true;
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
@@ -608,8 +608,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 for (int r = 0; r < 16; ++r)
 #pragma unroll
                     for (int dt = 0; dt < 4; ++dt) zero[dt] = fmaf(o[s][dt][r], 0.f, zero[dt]);
-                fine = fine && (last_key[s] < 0 || (l_run[s] >= 1 / kPromptMaxSum && l_run[s] <= kPromptMaxSum && fabsf(m_ref[s]) <= kPromptMaxRef)) &&
-                       zero[0] + zero[1] + zero[2] + zero[3] == 0.f;
+                const bool in_range = last_key[s] < 0 || (l_run[s] >= 1 / kPromptMaxSum && l_run[s] <= kPromptMaxSum && fabsf(m_ref[s]) <= kPromptMaxRef);
+                fine = fine && (l_run[s] != l_run[s] || (in_range && zero[0] + zero[1] + zero[2] + zero[3] == 0.f));
             }
             if (__syncthreads_or(!fine) != 0) {              // (all waves have read the stages)
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was requested beyond the last tile)
