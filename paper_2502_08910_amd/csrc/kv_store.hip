@@ -6,6 +6,7 @@
 // (5.0).  One token of each of 32 sequences takes 5.4 us, a chain of latencies: offsets, lengths, page, rows.
 #include "api_checks.h"
 #include "kv_store.h"
+#include <algorithm>
 #include <cstdlib>
 #include <type_traits>
 
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(kStoreThreads) void kv_append_kernel(const AppendAr
 }
 
 struct GatherArgs {
-    int BH, Hkv, max_len;
+    int BH, Hkv, max_len, groups;
     bool past;
     const int32_t *lens;
     StoreView from;
@@ -152,8 +153,10 @@ __global__ __launch_bounds__(kStoreThreads) void kv_gather_kernel(const GatherAr
     constexpr int kRows = kGatherRows;
     using word = typename std::conditional<FORMAT == IHIP_KV_BF16, uint4, typename std::conditional<FORMAT == IHIP_KV_E4M3, uint2, uint32_t>::type>::type;
     const int l16 = threadIdx.x & 15, grp = threadIdx.x >> 4;
-    const int bh = blockIdx.x % a.BH, b = bh / a.Hkv, g = bh % a.Hkv;
-    const int t0 = blockIdx.x / a.BH * (kRows * kStoreGroups);
+    const uint32_t group = blockIdx.y * gridDim.x + blockIdx.x;
+    if (group >= (uint32_t)a.groups) return;
+    const int bh = group % a.BH, b = bh / a.Hkv, g = bh % a.Hkv;
+    const int t0 = group / a.BH * (kRows * kStoreGroups);
     const int len = min(a.lens[b], a.max_len);
     word x[2][kRows];
     uint32_t s[2][kRows];
@@ -355,10 +358,11 @@ int32_t ihip_kv_gather(const ihip_kv_store *store, int32_t B, int32_t Hkv, int32
     const int64_t groups = (int64_t)B * Hkv * ((max_seq_len - 1) / (kGatherRows * kStoreGroups) + 1);
     if ((int64_t)B * Hkv > INT32_MAX || groups > INT32_MAX) return fail(IHIP_ERR_UNSUPPORTED, "%s: B * Hkv * max_seq_len is too large", who);
     a.past = (int64_t)B * Hkv * max_seq_len * kD * 2 * ((k_out.ptr != nullptr) + (v_out.ptr != nullptr)) > kPastBytes;
-    a.BH = B * Hkv; a.Hkv = Hkv; a.max_len = max_seq_len; a.lens = seq_lens;
+    a.groups = (int)groups; a.BH = B * Hkv; a.Hkv = Hkv; a.max_len = max_seq_len; a.lens = seq_lens;
     a.k = (uint16_t *)const_cast<void *>(k_out.ptr); a.k_sb = k_out.stride_b; a.k_sh = k_out.stride_h; a.k_st = k_out.stride_t;
     a.v = (uint16_t *)const_cast<void *>(v_out.ptr); a.v_sb = v_out.stride_b; a.v_sh = v_out.stride_h; a.v_st = v_out.stride_t;
-    const dim3 grid((uint32_t)groups);
+    constexpr uint32_t row = 1u << 23;                       // (a dimension has fewer than 2^32 threads)
+    const dim3 grid(std::min((uint32_t)groups, row), (uint32_t)(groups - 1) / row + 1);
     KernelTimer timer("kv_gather", (hipStream_t)stream);
     if (store->format == IHIP_KV_BF16) hipLaunchKernelGGL((kv_gather_kernel<IHIP_KV_BF16>), grid, dim3(kStoreThreads), 0, (hipStream_t)stream, a);
     else if (store->format == IHIP_KV_E4M3) hipLaunchKernelGGL((kv_gather_kernel<IHIP_KV_E4M3>), grid, dim3(kStoreThreads), 0, (hipStream_t)stream, a);
