@@ -8,13 +8,13 @@
 //            the dims in the order 32 g + 8 j + i for step j, the same for the queries.  Column n, rows 4 g + r: lane (n, g)
 //            gets head n % 8's scores of keys 4 g + r and 16 + 4 g + r.
 //   output   v_mfma_f32_16x16x32_bf16 again, 16 rows x 32 keys x 16 dims, eight times: a lane's eight probabilities are its part of
-//            the left operand as they are (rounded to bf16 in rows 0 .. 7, what that dropped in rows 8 .. 15; the two are added in the
-//            end), key 16 (i / 4) + 4 g + i % 4 for element i; for the right one it brings the
+//            the left operand as they are (rounded to bf16 in rows 0 .. 7, what that dropped in rows 8 .. 15; the two are added in
+//            LDS), key 16 (i / 4) + 4 g + i % 4 for element i; for the right one it brings the
 //            four bytes of dims 8 n .. 8 n + 7 of the same keys, and column n of product j is dim 8 n + j.
-// So a probability is off by at most 2^-16 of it, and a result as good as its last rounding; in one part results were 0.0022 off (root mean
-// square, relative), where the rounding alone is 0.0017, and the largest case took 101.1 us (103.8).  The sum that divides takes them as they were.
-// Bound by memory: 68 bytes a row.  32 sequences of 7,383 to 16,384 tokens, 8 KV heads, 416 MB, take 98 us with the merge, 91 without (4.6
-// TB/s; a copy of 4 GB moves 4.8); one of 4,099 5.4 us and 5.0 for the merge, which is a chain of latencies.
+// So a probability is off by at most 2^-16 of it, and a result as good as its last rounding (0.0017, root mean square and relative; 0.0022 with
+// probabilities of one part).  The sum that divides takes the probabilities as they were.
+// Bound by memory: 68 bytes a row.  32 sequences of 7,383 to 16,384 tokens, 8 KV heads, 416 MB, take 92 us (4.5 TB/s; a copy of 4 GB
+// moves 4.8; also 92 with probabilities of one part) and 5 for the merge; one of 4,099 takes 6.3 (5.8) and 5.1, chains of latencies.
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kMxThreads, kMxPerCu) void attn_decode_mx4_kernel(c
     __shared__ __attribute__((aligned(16))) uint32_t sh_row[kMxMaxSplit];     // row of every slot
     __shared__ uint32_t sh_there[kMxMaxSplit / 32];                           // which slots of a step hold a key
     __shared__ float sh_m[kMxWaves][HEADS], sh_l[kMxWaves][HEADS];
-    __shared__ __attribute__((aligned(16))) float sh_acc[kMxWaves][HEADS][kD];
+    __shared__ __attribute__((aligned(16))) float sh_acc[kMxWaves][2][HEADS][kD];      // of the two parts
 
     bf16x8 qb[4];
     {
@@ -227,22 +227,14 @@ __global__ __launch_bounds__(kMxThreads, kMxPerCu) void attn_decode_mx4_kernel(c
         r = nx;
     }
 
-    // both parts, then the waves through LDS
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const unsigned u = __float_as_uint(acc[j][h]);
-            const auto x = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-            acc[j][h] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
-        }
+    // the waves and both parts are merged through LDS
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (lane < HEADS) { sh_m[wv][lane] = m; sh_l[wv][lane] = l; }
-    if (4 * g < HEADS) {
+    if (4 * (g & 1) < HEADS) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            float *to = &sh_acc[wv][4 * g + h][8 * n];
+            float *to = &sh_acc[wv][g >> 1][4 * (g & 1) + h][8 * n];
             *reinterpret_cast<float4 *>(to) = make_float4(acc[0][h], acc[1][h], acc[2][h], acc[3][h]);
             *reinterpret_cast<float4 *>(to + 4) = make_float4(acc[4][h], acc[5][h], acc[6][h], acc[7][h]);
         }
@@ -258,7 +250,7 @@ __global__ __launch_bounds__(kMxThreads, kMxPerCu) void attn_decode_mx4_kernel(c
         for (int w = 0; w < kMxWaves; ++w) {
             const float x = mx4_weight(sh_m[w][h], M, a.scale_log2e);
             L = fmaf(x, sh_l[w][h], L);
-            A = fmaf(x, sh_acc[w][h][c], A);
+            A = fmaf(x, sh_acc[w][0][h][c] + sh_acc[w][1][h][c], A);
         }
         if (a.n_splits == 1) {                       // nothing to merge
             const int64_t hq = (int64_t)pr.b * a.ge.Hq + pr.g * G + h;
