@@ -555,7 +555,8 @@ int32_t ihip_sparse_attn_decode_mx4kv(const ihip_shape *shape, ihip_tensor q, co
  *   out        bf16 [rows, Hq, d] contiguous
  *   out_lse    fp32 [rows, Hq] natural-log sum-exp of the scaled scores; may be NULL
  * QK^T and PV run on the matrix cores (bf16 operands, the probabilities rounded to
- * bf16, fp32 accumulation), softmax in fp32.  A query that sees no key (t < n)
+ * bf16 as in ihip_sparse_attn_prefill, 8 bits where the decode calls keep 16 and more; fp32
+ * accumulation), softmax in fp32.  A query that sees no key (t < n)
  * gets 0, and -INFINITY.  A sequence of more than max_q tokens may be done in part only.
  * rows * (Hq/Hkv), and the 128 elements of all heads of 256 / (Hq/Hkv) + 2 queries, must be fewer than 2^31.
  * sm_scale is not negative and at most 2^127.  A key or a value that is not finite makes only those results NaN or infinite that see it.

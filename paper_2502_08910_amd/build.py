@@ -22,8 +22,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # compiler drops the canonicalising v_max x,x,x in front of each (a third of the vector
 # instructions of the prefill search loop).  Scores of NaN inputs are then unspecified values.
 EXTRA = {src: ["-fno-honor-nans"] for src in ("prune_stage.hip", "prune_prefill_fp8.hip", "prune_decode_tile.hip", "prune_decode_nest.hip")}
-# One wave of the prompt attention has all 512 registers of a SIMD lane to itself.  Left to itself the compiler then puts every
-# matrix result into the accumulation half and moves scores and accumulators between the halves in every step.
+# The prompt attention's kernel of two sets a wave has all 512 registers of a SIMD lane to itself.  Left to itself the compiler then puts every
+# matrix result into the accumulation half and moves scores and accumulators between the halves in every step.  The kernel of one
+# set, two waves a SIMD, uses ordinary registers alone (219 of 256) with the flag and without.
 EXTRA["prompt_attn.hip"] = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 
 

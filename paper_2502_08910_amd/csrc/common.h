@@ -220,9 +220,8 @@ __device__ inline uint32_t pack_bf16x2(float a, float b)
     return __builtin_bit_cast(uint32_t, v);
 }
 
-// 8 bf16 = 4 (even, odd) dim pairs, each turned by the angle whose cos and sin are given (fp32
-// arithmetic, every product and sum rounded on its own -- no fused multiply-add, so that the value
-// does not depend on the compiler's contraction --, results rounded to bf16, nearest-even):
+// 8 bf16 = 4 (even, odd) dim pairs, each turned by the angle whose cos and sin are given (fp32 arithmetic, in which the compiler makes a
+// product and the sum behind it one fused multiply-add, __fmul_rn and its like notwithstanding; results rounded to bf16, nearest-even):
 // ApplyRope of Sec. 4 on a 16-byte piece of a row
 __device__ inline uint4 rotate_f32x8(const float (&f)[8], const float4 c, const float4 sn)
 {

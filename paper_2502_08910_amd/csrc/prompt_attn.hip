@@ -3,11 +3,13 @@
 // in one pass over the keys, for a reference r_i that is the row's maximum over its first tile (below).  A wave holds its rows (queries' heads; the right
 // operand of the first product, K the left one), so that a lane has 16 of the 32 scores of one row, its exponentials are already
 // the right operand of the second product with V^T (whose rows it takes in the order of the scores), and nothing of P goes through LDS.
+// P is rounded to bf16 for it (2^-8 of each probability at most): what the rounding drops, as second operands, would be half as many matrix
+// instructions again.  The sum that divides takes the probabilities as they were.
 // K and V go from memory to LDS by themselves (global_load_lds), 16-byte chunks XORed with the row, so that both the rows of K and the
 // transposed reads of V (ds_read_b64_tr_b16) are without conflicts.
 // Bound by the matrix units (32 cycles an instruction) and the vector units (four instructions a product, 28 cycles, 16 of them for the
 // exponential) of a SIMD's two waves, at the clock that the power limit leaves: one prompt of 32,749 with 32 heads, 8.79 TFLOP, takes
-// 7.1 ms, 1.24 PFLOP/s, where a library product of 16,384^3 reaches 1.31 and one of 8,192^3 1.15.
+// 7.1 ms, 1.23 PFLOP/s, on a card where a library product of 16,384^3 reaches 1.37 and one of 8,192^3 1.39 (7.8 ms on another).
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>
@@ -925,8 +927,6 @@ static int64_t prompt_blocks(const ihip_packed &p, int rows)
 // us by themselves / in shares, 32 heads on 8: 1,024 queries 24 / 53, 8,192 469 / 578; 64 on 2,064 keys 36 / 47, 512 on 4,608 66 / 75; 200 on 8,200
 // 109 / 79; 128, 256, 64 and 500 on 3,000 to 12,000 156 / 102; one each of 16 sequences on 8,000 161 / 127; 8 heads, 64 on 60,064 681 /
 // 109; 16 heads on 8, 1,500 on 13,500 and 700 on 20,700 326 / 267, 1,000 on 101,000 1,514 / 707.
-// The other pairs were slower nearly everywhere: blocks of two sets by themselves (1,024 queries 37, 20 times 333 90 against 48; 16 heads,
-// 8,192 247 against 253), shares of one set (1,500 and 700 276, 1,000 on 101,000 783; 200 on 8,200 70).
 static bool prompt_in_shares(const ihip_packed &p, int64_t keys)
 {
     if (p.max_q <= 0 || p.rows <= 0 || p.B <= 0) return false;
@@ -1007,8 +1007,6 @@ extern "C" int32_t ihip_prompt_attn(const ihip_packed *packed, ihip_tensor q, ih
         return check_launch(who);
     }
     typedef PromptShape<1> Shape;
-    // (A workgroup a block, handed out by the hardware.  512 that stay, each with every 512th block and the first tiles of its next one
-    // on their way under the end of the present one: 8 prompts of 640 to 2,048 172 -> 185 us, one of 32,749 7.17 -> 7.52 ms.)
     // The order of the blocks matters where some compute unit has two.  Finding them without it is shorter: 512 queries, 32 heads 18.5 -> 17.6 us
     a.ordered = packed->B <= kOrderedSeqs && groups > compute_units();
     const int64_t places = ((int64_t)packed->max_q * a.G - 1) / Shape::kRows + 1;
