@@ -865,7 +865,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
             for (int i = 0; i < kPieces; ++i) acc[i] = make_float4(acc[i].x * old, acc[i].y * old, acc[i].z * old, acc[i].w * old);
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                const float w = __builtin_amdgcn_exp2f(ml[c].x - top);
+                const float w = __builtin_amdgcn_exp2f(ml[c].x - top - kPromptShift);      // (for sums over the parts that are finite)
                 L += ml[c].y * w;
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i)
@@ -885,7 +885,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
         for_parts([&](unsigned long long left, int part) {
             for (; left != 0; left &= left - 1) {
                 const int64_t unit = unit_of(left, part);
-                const float w = __builtin_amdgcn_exp2f(sums_of(unit).x - M);
+                const float w = __builtin_amdgcn_exp2f(sums_of(unit).x - M - kPromptShift);
                 const float4 *from = results_of(unit);
                 auto weighted = [&](float x) { return __builtin_isinf(x) ? x : x * w; };
 #pragma unroll
@@ -907,7 +907,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a, i
         *reinterpret_cast<uint2 *>(a.out + at * kD + piece * 8 + half * 4) =
             L == 0.f ? make_uint2(0, 0) : make_uint2(pack_bf16x2(acc[i].x * inv, acc[i].y * inv), pack_bf16x2(acc[i].z * inv, acc[i].w * inv));
     }
-    if (a.lse != nullptr && half == 0 && quarter * kPieces == 16 * s) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
+    if (a.lse != nullptr && half == 0 && quarter * kPieces == 16 * s) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L * 0x1p20f)) * 0.69314718055994530942f;
 }
 
 // Blocks x KV heads of a call, at most: a part of a block in every sequence beyond the whole ones, and no more than max_q gives each
