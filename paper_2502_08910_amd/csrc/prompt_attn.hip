@@ -415,7 +415,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
             };
 
             uint32_t pw[2][8];                               // the probabilities of a turn, in pairs of keys
-            float m_ref[SETS], l_run[SETS];
+            float m_ref[SETS], l_run[SETS], l_turn;          // (16 probabilities are added up before they go to a sum that may be long)
 #pragma unroll
             for (int s = 0; s < SETS; ++s) m_ref[s] = kPromptLowest;
             // two scores -> two probabilities (exp2(-inf) = 0).  The empty assembly keeps them where they are called: left to themselves all
@@ -429,10 +429,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                 asm volatile("" : "+v"(x), "+v"(y));
                 x = __builtin_amdgcn_exp2f(x);
                 y = __builtin_amdgcn_exp2f(y);
-                l_run[qs(s)] += x;
-                l_run[qs(s)] += y;
+                l_turn = i == 0 ? x + y : l_turn + x + y;
                 pw[s][i] = pack_bf16x2(x, y);
-                asm volatile("" : "+v"(pw[s][i]), "+v"(l_run[qs(s)]));
+                asm volatile("" : "+v"(pw[s][i]), "+v"(l_turn));
+                if (i == 7) {
+                    l_run[qs(s)] += l_turn;
+                    asm volatile("" : "+v"(l_run[qs(s)]));
+                }
             };
             auto probabilities = [&](int s, int kk) {
                 return __builtin_bit_cast(bf16x8, make_uint4(pw[s][4 * kk], pw[s][4 * kk + 1], pw[s][4 * kk + 2], pw[s][4 * kk + 3]));
@@ -703,10 +706,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, PromptShape<SETS>::kPerCu) void 
                         for (int i = 0; i < 8; ++i) {        // against the maximum as it came from the products: scaled, it would be rounded
                             const float x = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i] - m_ref[qs(s)], a.scale_log2e, -kPromptShift));
                             const float y = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i + 1] - m_ref[qs(s)], a.scale_log2e, -kPromptShift));
-                            l_run[qs(s)] += x;
-                            l_run[qs(s)] += y;
+                            l_turn = i == 0 ? x + y : l_turn + x + y;
                             pw[s][i] = pack_bf16x2(x, y);
                         }
+                        l_run[qs(s)] += l_turn;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             bf16x8 x = v_operand(0, s, i);
