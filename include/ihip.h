@@ -584,6 +584,97 @@ int32_t ihip_kv_gather(const ihip_kv_store *store, int32_t B, int32_t Hkv, int32
                        int32_t max_seq_len, ihip_tensor k_out, ihip_tensor v_out, void *stream);
 
 /* ==========================================================================
+ * Caches that keep what was attended to
+ * ========================================================================== */
+
+/*
+ * What stands beside a cache whose rows are evicted by the attention that they got.  Row r of
+ * (sequence b, KV head g) of the cache has element (b*Hkv + g)*rows + r of
+ *   weights    device fp32 [B, Hkv, rows]: the attention weight that it has gathered
+ *   positions  device int32 [B, Hkv, rows]: the position in its sequence of the token in it
+ * and sequence b has had seen[b] tokens (device int32 [B], kept by the caller as seq_lens is, new
+ * tokens counted in both), of which the cache holds seq_lens[b]: a head's rows are its own choice
+ * of them, in any order, which attention over all rows does not mind.
+ */
+typedef struct ihip_kv_track {
+    float *weights;
+    int32_t *positions;
+    int32_t rows;                /* of a head, at least the max_seq_len of the calls */
+    const int32_t *seen;
+} ihip_kv_track;
+
+/*
+ * ihip_kv_append into such a cache: token i of the n that sequence b brings goes to row
+ * seq_lens[b] - n + i, but its position, to which it is rotated, is seen[b] - n + i (rope->n_pos is
+ * held against that, not against max_seq_len).  The row's weights become 0 and its positions
+ * that position, for every KV head.  A token whose row is outside [0, max_seq_len) or whose position is outside
+ * [0, rope->n_pos) is dropped: nothing is written for it; where it has no page, nothing of K, V, weights and positions is.
+ */
+int32_t ihip_kv_append_tracked(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v,
+                               const int32_t *seq_lens, int32_t max_seq_len, const ihip_rope *rope,
+                               const ihip_kv_store *store, const ihip_kv_track *track, ihip_tensor q_out,
+                               ihip_tensor k_out, void *stream);
+
+/*
+ * What the queries of ihip_prompt_attn attend to.  For key j of a sequence of n queries and t keys,
+ *   weights[b][g][j] = decay * before[b][g][j] + sum of exp(sm_scale * q_i k_j - lse_i)
+ * over the last min(window, n) queries i with j <= i + (t - n) and the query heads of KV head g:
+ * key j stands in row j of the cache.  Keys beyond track->rows are left out.
+ *   q, k, cu_k, rows_k, sm_scale   as ihip_prompt_attn had them
+ *   lse        device fp32 [rows, Hq], its out_lse; what is not finite there makes the keys that the query sees NaN, infinite or 0, as the formula has it
+ *   window     at least 1; max_q or more: all queries
+ *   before     device fp32 like track->weights, may be the same; NULL: nothing before
+ *   decay      finite, not negative; not looked at without `before`
+ *   track      only weights and rows are looked at; rows behind a sequence's keys are left as they were
+ *   ws         device scratch of ihip_prompt_key_weights_workspace_bytes(packed, rows_k, window), 16-byte aligned; may be
+ *              NULL.  Few keys under many queries are dealt out to the chip in chunks of queries, whose sums wait there; with NULL, less
+ *              or a misaligned pointer they are not (slower; equal up to rounding).
+ * Scores, exponentials and sums in fp32; the order of the sums is fixed.  A sequence of more than max_q queries may be done in part only.
+ */
+size_t  ihip_prompt_key_weights_workspace_bytes(const ihip_packed *packed, int32_t rows_k, int32_t window);
+int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, const int32_t *cu_k,
+                                int32_t rows_k, float sm_scale, const float *lse, int32_t window,
+                                const float *before, float decay, const ihip_kv_track *track, void *ws,
+                                size_t ws_bytes, void *stream);
+
+/*
+ * Decode attention (Tq == b_q == 1) over all seq_lens[b] rows of a store of any format, which adds to
+ * every row the probabilities that the query heads of its KV head give it:
+ *   weights[b][g][r] = decay * before[b][g][r] + sum over the heads of exp(score - lse).
+ * shape->n_sink and n_stream choose nothing here.  out, out_lse, sm_scale (for E4M3 rows also its product with
+ * k_scale) as in ihip_sparse_attn_decode_mx4kv, and the same arithmetic.  The output of an idle
+ * place of the batch, or of a sequence without pages, is 0, its log-sum-exp -INFINITY; a row on a page with a
+ * negative id is left out, its weight gets nothing but decay * before.  Rows behind a sequence are not
+ * read, and what stands beside them is left as it was.
+ *   before, decay, track   as in ihip_prompt_key_weights
+ *   ws                     device scratch of ihip_attn_decode_tracked_workspace_bytes(shape), 16-byte aligned
+ */
+size_t  ihip_attn_decode_tracked_workspace_bytes(const ihip_shape *shape);
+int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor q, const ihip_kv_store *store,
+                                 float sm_scale, const float *before, float decay, const ihip_kv_track *track,
+                                 void *out, float *out_lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Cuts sequences of more than `keep` rows down to `keep`, for each KV head by itself.  Kept are rows of
+ * positions below n_sink or from seen[b] - n_recent on, and of the others those with most weight (ties: the lower row;
+ * -0.0 == +0.0; NaN behind everything): rows 0 .. keep-1 of the cache, of weights and of positions afterwards.  A kept row
+ * below `keep` stays where it is; the i-th evicted row there is filled with the i-th kept row of those from `keep` on.  Nothing else moves:
+ * rows from `keep` on are left as they were.
+ *   keep       at least 1, at least n_sink + n_recent
+ *   to         weights, positions and rows of the cut cache; may be track or NULL, which is the same.  With arrays of its own all
+ *              kept rows are written there (rows: at least min(keep, max_seq_len)), track's are left as they were
+ *   new_lens   device int32 [B]: min(seq_lens[b], keep); may be seq_lens.  seen does not change
+ *   kept       device int32 [B, Hkv, keep]: the row that each row was, -1 behind a sequence
+ *   ws         device scratch of ihip_kv_evict_workspace_bytes(B, Hkv, max_seq_len, keep), 16-byte aligned
+ * Two rows must not share memory, two sequences no page.  Where one of the two pages of a move has a negative id, K and V do not move.
+ */
+size_t  ihip_kv_evict_workspace_bytes(int32_t B, int32_t Hkv, int32_t max_seq_len, int32_t keep);
+int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track *track, int32_t B, int32_t Hkv, int32_t d,
+                      const int32_t *seq_lens, int32_t max_seq_len, int32_t keep, int32_t n_sink, int32_t n_recent,
+                      const ihip_kv_track *to, int32_t *new_lens, int32_t *kept, void *ws, size_t ws_bytes,
+                      void *stream);
+
+/* ==========================================================================
  * Host-memory KV tier with the on-GPU hot-block cache
  * ========================================================================== */
 

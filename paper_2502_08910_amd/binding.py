@@ -98,6 +98,13 @@ EXPORTS = {
     "ihip_prompt_attn_workspace_bytes": (c_sz, [vp, c_i32]),
     "ihip_prompt_attn": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, c_f, vp, vp, vp, c_sz, vp]),
     "ihip_kv_append": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, vp, vp, Tensor, Tensor, vp]),
+    "ihip_kv_append_tracked": (c_i32, [vp, Tensor, Tensor, Tensor, vp, c_i32, vp, vp, vp, Tensor, Tensor, vp]),
+    "ihip_prompt_key_weights_workspace_bytes": (c_sz, [vp, c_i32, c_i32]),
+    "ihip_prompt_key_weights": (c_i32, [vp, Tensor, Tensor, vp, c_i32, c_f, vp, c_i32, vp, c_f, vp, vp, c_sz, vp]),
+    "ihip_attn_decode_tracked_workspace_bytes": (c_sz, [ctypes.POINTER(Shape)]),
+    "ihip_attn_decode_tracked": (c_i32, [ctypes.POINTER(Shape), Tensor, vp, c_f, vp, c_f, vp, vp, vp, vp, c_sz, vp]),
+    "ihip_kv_evict_workspace_bytes": (c_sz, [c_i32, c_i32, c_i32, c_i32]),
+    "ihip_kv_evict": (c_i32, [vp, vp, c_i32, c_i32, c_i32, vp, c_i32, c_i32, c_i32, c_i32, vp, vp, vp, vp, c_sz, vp]),
     "ihip_kv_gather": (c_i32, [vp, c_i32, c_i32, c_i32, vp, c_i32, Tensor, Tensor, vp]),
     "ihip_cache_device_bytes": (c_sz, [c_i32, c_i32, c_i64, c_i32, c_i32, c_i32]),
     "ihip_cache_device_bytes_fp8": (c_sz, [c_i32, c_i32, c_i64, c_i32, c_i32, c_i32]),
@@ -796,6 +803,52 @@ class KVStore:
         return ctypes.byref(self.c)
 
 
+class TrackStruct(ctypes.Structure):
+    _fields_ = [("weights", vp), ("positions", vp), ("rows", c_i32), ("seen", vp)]
+
+
+class KVTrack:
+    """ihip_kv_track: what stands beside a cache whose rows are evicted.  weights fp32 [B, Hkv, rows], positions int32 of the same
+    shape and seen int32 [B], contiguous device tensors of the caller; positions and seen may be left out where only weights are used."""
+
+    def __init__(self, weights: torch.Tensor, positions: Optional[torch.Tensor] = None, seen: Optional[torch.Tensor] = None):
+        if weights.dtype != torch.float32 or weights.dim() != 3 or not weights.is_cuda or not weights.is_contiguous():
+            raise IhipError("weights: need a contiguous 3-d fp32 device tensor [B, Hkv, rows]")
+        if positions is not None and (positions.dtype != torch.int32 or positions.shape != weights.shape or not positions.is_contiguous() or
+                                      positions.device != weights.device):
+            raise IhipError("positions: need a contiguous int32 tensor of the shape and on the device of the weights")
+        self.weights, self.positions, self.seen, self.device = weights, positions, seen, weights.device
+        self.B, self.Hkv, self.rows = weights.shape
+        self.c = TrackStruct(weights.data_ptr(), _ptr(positions), self.rows, None if seen is None else _lengths(seen, self.B, "seen", self.device))
+
+    @classmethod
+    def empty(cls, B: int, Hkv: int, rows: int, device="cuda:0"):
+        """That of a cache without tokens."""
+        return cls(torch.zeros((B, Hkv, rows), dtype=torch.float32, device=device), torch.zeros((B, Hkv, rows), dtype=torch.int32, device=device),
+                   torch.zeros((B,), dtype=torch.int32, device=device))
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+    def check(self, B: int, Hkv: int, device) -> None:
+        if self.device != device:
+            raise IhipError(f"track is on {self.device}, not on {device}")
+        if B > self.B or Hkv != self.Hkv:
+            raise IhipError(f"track is of {self.B} sequences of {self.Hkv} heads, not of {B} of {Hkv}")
+
+    def before(self, before: Optional[torch.Tensor], fresh: bool) -> Optional[int]:
+        """What weights are added to: None with `fresh`, `before`, or the weights themselves."""
+        if fresh and before is not None:
+            raise IhipError("before: nothing is with fresh")
+        if fresh:
+            return None
+        if before is None:
+            return self.weights.data_ptr()
+        if before.dtype != torch.float32 or before.shape != self.weights.shape or not before.is_contiguous() or before.device != self.device:
+            raise IhipError("before: need a contiguous fp32 tensor of the shape and on the device of the weights")
+        return before.data_ptr()
+
+
 def _packed_tensor(t: torch.Tensor, name: str, rows: Optional[int] = None, heads: Optional[int] = None) -> Tensor:
     shape, stride = t.shape, t.stride()
     if t.dtype != torch.bfloat16 or len(shape) != 3 or shape[2] != 128 or stride[2] != 1 or not t.is_cuda:
@@ -832,11 +885,12 @@ def _enqueue(device, fn, *args) -> None:
 
 def kv_append(store: KVStore, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int,
               q: Optional[torch.Tensor] = None, rope: Optional[Sequence[torch.Tensor]] = None,
-              q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+              q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, track: Optional[KVTrack] = None):
     """ihip_kv_append: packed new tokens k, v [rows, Hkv, d] (bf16) of sequences cu_q int32 [B+1] into the store, at the
     end of sequences that are seq_lens [B] long with them (at most max_seq_len).  rope: (cos, sin) fp32 [n_pos, d/2]:
     keys are rotated to their positions, and the queries q [rows, Hq, d] into q_out (may be q; made if not given).
-    k_out: where the rotated keys go as well.  -> (q_out or None, k_out or None)."""
+    k_out: where the rotated keys go as well.  track (ihip_kv_append_tracked): positions go on from the tokens that the sequences have
+    seen, apart from the rows, whose weights and positions are set.  -> (q_out or None, k_out or None)."""
     rows, Hkv, d = k.shape
     B = cu_q.numel() - 1
     _same_device(store.device, k=k, v=v, q=q, q_out=q_out, k_out=k_out)
@@ -856,9 +910,13 @@ def kv_append(store: KVStore, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tens
     Hq = Hkv if q is None else q.shape[1]
     tq = NO_TENSOR if q is None else _packed_tensor(q, "q", rows, Hq)
     p = PackedStruct(B, Hq, Hkv, d, _lengths(cu_q, B + 1, "cu_q", store.device), rows, rows)
-    _enqueue(store.device, lib().ihip_kv_append, ctypes.byref(p), tq, _packed_tensor(k, "k"), _packed_tensor(v, "v", rows, Hkv),
+    fn, beside = lib().ihip_kv_append, ()
+    if track is not None:
+        track.check(B, Hkv, store.device)
+        fn, beside = lib().ihip_kv_append_tracked, (track.ref(),)
+    _enqueue(store.device, fn, ctypes.byref(p), tq, _packed_tensor(k, "k"), _packed_tensor(v, "v", rows, Hkv),
              _lengths(seq_lens, B, "seq_lens", store.device), max_seq_len, None if cos_sin is None else ctypes.byref(cos_sin),
-             store.ref(), NO_TENSOR if q is None else _packed_tensor(q_out, "q_out", rows, Hq),
+             store.ref(), *beside, NO_TENSOR if q is None else _packed_tensor(q_out, "q_out", rows, Hq),
              NO_TENSOR if k_out is None else _packed_tensor(k_out, "k_out", rows, Hkv))
     return q_out, k_out
 
@@ -940,3 +998,105 @@ def sparse_attn_decode_mx4(layer: "Layer", q: torch.Tensor, store: KVStore, bloc
     _enqueue(layer.device, lib().ihip_sparse_attn_decode_mx4kv, ctypes.byref(layer.shape), _tensor(q, "q"), store.ref(),
              _ptr(block_starts), n_blocks, block, sm_scale, _ptr(out), _ptr(lse), _ptr(ws), ws.numel())
     return out, lse
+
+
+# ---- caches that keep what was attended to ---------------------------------------------
+def prompt_key_weights(q: torch.Tensor, k: torch.Tensor, cu_q: torch.Tensor, max_q: int, lse: torch.Tensor, track: KVTrack,
+                       cu_k: Optional[torch.Tensor] = None, window: Optional[int] = None, sm_scale: Optional[float] = None,
+                       before: Optional[torch.Tensor] = None, decay: float = 1.0, fresh: bool = False, ws: Optional[torch.Tensor] = None):
+    """ihip_prompt_key_weights: track.weights [B, Hkv, rows] = decay * before (track.weights themselves if not given, nothing if
+    fresh) + the probabilities that each key gets from the last `window` queries (None: all) of its sequence.  q, k, cu_q, max_q,
+    cu_k, sm_scale as in prompt_attn, lse [rows, Hq] from it.  ws: device scratch, made if not given and of use (an empty tensor: none)."""
+    rows, Hq, d = q.shape
+    rows_k, Hkv, _ = k.shape
+    B = cu_q.numel() - 1
+    sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
+    window = 2 ** 31 - 1 if window is None else window
+    _same_device(q.device, k=k, lse=lse, ws=ws)
+    track.check(B, Hkv, q.device)
+    if lse.shape != (rows, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise IhipError("lse: need a contiguous fp32 tensor [rows, Hq]")
+    p = PackedStruct(B, Hq, Hkv, d, _lengths(cu_q, B + 1, "cu_q", q.device), rows, max_q)
+    if ws is None:
+        need = lib().ihip_prompt_key_weights_workspace_bytes(ctypes.byref(p), rows_k, window)
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 256 else None
+    _enqueue(q.device, lib().ihip_prompt_key_weights, ctypes.byref(p), _packed_tensor(q, "q"), _packed_tensor(k, "k"),
+             None if cu_k is None else _lengths(cu_k, B + 1, "cu_k", q.device), rows_k, sm_scale, lse.data_ptr(), window,
+             track.before(before, fresh), decay, track.ref(), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+
+
+def _decode_shape(q: torch.Tensor, store: KVStore, seq_lens: Optional[int], max_seq_len: int) -> Shape:
+    if q.dim() != 4 or q.shape[2] != 1:
+        raise IhipError("q: need [B, Hq, 1, d]")
+    if q.shape[0] > store.B or max_seq_len > store.tokens:
+        raise IhipError(f"the store holds {store.B} sequences of {store.tokens} tokens")
+    return Shape(q.shape[0], q.shape[1], store.Hkv, q.shape[3], 1, 1, seq_lens, max_seq_len, 0, 1, 0)
+
+
+def attn_decode_tracked_workspace(q: torch.Tensor, store: KVStore, max_seq_len: int) -> torch.Tensor:
+    """Scratch of attn_decode_tracked for queries like q and sequences of up to max_seq_len rows."""
+    shape = _decode_shape(q, store, 256, max_seq_len)        # (the lengths are not looked at)
+    need = lib().ihip_attn_decode_tracked_workspace_bytes(ctypes.byref(shape))
+    if need == 0:
+        raise IhipError(lib().ihip_last_error().decode())
+    return torch.empty(need, dtype=torch.uint8, device=q.device)
+
+
+def attn_decode_tracked(q: torch.Tensor, store: KVStore, track: KVTrack, seq_lens: torch.Tensor, max_seq_len: int,
+                        sm_scale: Optional[float] = None, before: Optional[torch.Tensor] = None, decay: float = 1.0, fresh: bool = False,
+                        want_lse: bool = False, ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        lse: Optional[torch.Tensor] = None):
+    """ihip_attn_decode_tracked: attention of q [B, Hq, 1, d] over the seq_lens [B] rows of a store of any format, whose probabilities are
+    added to track.weights (before, decay, fresh as in prompt_key_weights).  -> (out bf16 [B, Hq, 1, d], lse fp32 [B, Hq, 1] or None)."""
+    B, Hq, d = q.shape[0], q.shape[1], q.shape[-1]
+    sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
+    shape = _decode_shape(q, store, _lengths(seq_lens, B, "seq_lens", store.device), max_seq_len)
+    track.check(B, store.Hkv, store.device)
+    if out is None:
+        out = torch.empty((B, Hq, 1, d), dtype=torch.bfloat16, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq, 1), dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = attn_decode_tracked_workspace(q, store, max_seq_len)
+    _same_device(store.device, q=q, out=out, lse=lse, ws=ws)
+    for t, name, dt, n in ((out, "out", torch.bfloat16, B * Hq * d), (lse, "lse", torch.float32, B * Hq)):
+        if t is not None and (t.dtype != dt or not t.is_contiguous() or t.numel() != n):
+            raise IhipError(f"{name}: need a contiguous {dt} tensor of {n} elements")
+    _enqueue(store.device, lib().ihip_attn_decode_tracked, ctypes.byref(shape), _tensor(q, "q"), store.ref(), sm_scale, track.before(before, fresh),
+             decay, track.ref(), _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size())
+    return out, lse
+
+
+def kv_evict_workspace(store: KVStore, B: int, max_seq_len: int, keep: int) -> torch.Tensor:
+    """Scratch of kv_evict for B sequences of up to max_seq_len rows."""
+    need = lib().ihip_kv_evict_workspace_bytes(B, store.Hkv, max_seq_len, keep)
+    if need == 0:
+        raise IhipError(lib().ihip_last_error().decode())
+    return torch.empty(need, dtype=torch.uint8, device=store.device)
+
+
+def kv_evict(store: KVStore, track: KVTrack, seq_lens: torch.Tensor, max_seq_len: int, keep: int, n_sink: int = 0, n_recent: int = 0,
+             to: Optional[KVTrack] = None, new_lens: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None,
+             ws: Optional[torch.Tensor] = None):
+    """ihip_kv_evict: sequences of more than `keep` rows are cut down to the first n_sink and last n_recent positions and the rows
+    of most weight between them, for each KV head by itself.  to: a track of its own for the cut cache (None: track itself); new_lens int32
+    [B] (made if not given; may be seq_lens).  -> (new_lens, kept int32 [B, Hkv, keep]: the row that each row was, -1 behind a sequence)."""
+    B = seq_lens.numel()
+    if B > store.B or max_seq_len > store.tokens:
+        raise IhipError(f"the store holds {store.B} sequences of {store.tokens} tokens")
+    for t in (track, to):
+        if t is not None:
+            t.check(B, store.Hkv, store.device)
+    if new_lens is None:
+        new_lens = torch.empty((B,), dtype=torch.int32, device=store.device)
+    if kept is None:
+        kept = torch.empty((B, store.Hkv, max(keep, 0)), dtype=torch.int32, device=store.device)
+    if ws is None:
+        ws = kv_evict_workspace(store, B, max_seq_len, keep)
+    _same_device(store.device, kept=kept, ws=ws)
+    if kept.dtype != torch.int32 or kept.shape != (B, store.Hkv, keep) or not kept.is_contiguous():
+        raise IhipError("kept: need a contiguous int32 tensor [B, Hkv, keep]")
+    _enqueue(store.device, lib().ihip_kv_evict, store.ref(), track.ref(), B, store.Hkv, 128, _lengths(seq_lens, B, "seq_lens", store.device),
+             max_seq_len, keep, n_sink, n_recent, None if to is None else to.ref(), _lengths(new_lens, B, "new_lens", store.device), kept.data_ptr(),
+             _ptr(ws), ws.numel() * ws.element_size())
+    return new_lens, kept

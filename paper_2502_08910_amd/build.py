@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libihip.so")
 SOURCES = ["api.hip", "prune_stage.hip", "prune_prefill_fp8.hip", "prune_decode_tile.hip", "prune_decode_nest.hip", "prune_stage_rope.hip", "select_blocks.hip", "select_chain.hip", "sparse_attn_decode.hip",
-           "sparse_attn_prefill.hip", "sparse_attn_prefill32.hip", "sparse_attn_prefill32_fp8.hip", "cache.hip", "kv_store.hip", "prompt_attn.hip", "attn_decode_mx4.hip", "mfma_rate.hip"]
+           "sparse_attn_prefill.hip", "sparse_attn_prefill32.hip", "sparse_attn_prefill32_fp8.hip", "cache.hip", "kv_store.hip", "prompt_attn.hip", "attn_decode_mx4.hip", "attn_decode_tracked.hip", "prompt_key_weights.hip", "kv_evict.hip", "mfma_rate.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Wno-unknown-warning-option"]

@@ -16,6 +16,7 @@
 // Bound by memory: 68 bytes a row.  32 sequences of 7,383 to 16,384 tokens, 8 KV heads, 416 MB, take 92 us (4.5 TB/s; a copy of 4 GB
 // moves 4.8; also 92 with probabilities of one part) and 5 for the merge; one of 4,099 takes 6.3 (5.8) and 5.1, chains of latencies.
 #include "api_checks.h"
+#include "decode_softmax.h"
 #include "kv_store.h"
 #include <algorithm>
 
@@ -28,19 +29,6 @@ constexpr int kMxThreads = 256, kMxWaves = kMxThreads / kWave;
 constexpr int kMxStep = 32;                          // slots of a wave at a time
 constexpr int kMxMaxSplit = 4096, kMxMinSplit = 128; // slots of a split (multiples of 128: a step of every wave)
 constexpr int kMxPerCu = 3;                          // workgroups that a compute unit holds
-constexpr float kMxLowest = -3.4028234e38f;          // stand-in for -inf in maxima: no score is below it
-// Exponentials are taken against a score (a maximum of some while ago) and times 2^-26, and the reference moves where eight of them add up
-// to more than 2^-20: their products with values, which go up to 6 * 2^125, have finite sums over a million keys, and products with the
-// smallest values that are appended, 2^-101, keep 2^-149 and with it 22 bits.  Scores are not scaled before the reference is taken off: of a
-// large score and a reference that were rounded apart, the difference would be large as well.
-constexpr float kMxShift = 26.f, kMxMaxSum = 0x1p-20f;
-__device__ inline float mx4_exp(float score, float ref, float scale_log2e) { return __builtin_amdgcn_exp2f(fmaf(score - ref, scale_log2e, -kMxShift)); }
-// of what was taken against `from`, where `to` is the reference
-__device__ inline float mx4_weight(float from, float to, float scale_log2e) { return __builtin_amdgcn_exp2f((from - to) * scale_log2e); }
-__device__ inline float mx4_lse(float ref, float sum, float scale_log2e)
-{
-    return sum == 0.f ? -INFINITY : fmaf(ref, scale_log2e, log2f(sum * 0x1p26f)) * 0.69314718055994530942f;
-}
 
 struct AttnMx4Args {
     Geometry ge;
@@ -146,7 +134,7 @@ __global__ __launch_bounds__(kMxThreads, kMxPerCu) void attn_decode_mx4_kernel(c
     f32x4 acc[8];                                    // rows 4 g + r, dim 8 n + j
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = kMxLowest, l = 0.f;                    // of head n (m: the same in the four lanes of a head; l: of this lane's keys)
+    float m = kSoftmaxLowest, l = 0.f;                    // of head n (m: the same in the four lanes of a head; l: of this lane's keys)
     MxRows r, nx;
     if (wv < steps) load(wv, r);
     for (int step = wv; step < steps; step += kMxWaves) {
@@ -173,21 +161,21 @@ __global__ __launch_bounds__(kMxThreads, kMxPerCu) void attn_decode_mx4_kernel(c
         float w[8], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            w[i] = mx4_exp(c[i >> 2][i & 3], m, a.scale_log2e);        // of -inf: 0
+            w[i] = softmax_exp(c[i >> 2][i & 3], m, a.scale_log2e);        // of -inf: 0
             sum += w[i];
         }
-        if (__any(!(sum <= kMxMaxSum))) {            // the reference follows where the scores outgrew it
+        if (__any(!(sum <= kSoftmaxMaxSum))) {            // the reference follows where the scores outgrew it
             float top = c[0][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) top = fmaxf(top, c[i >> 2][i & 3]);
             const float mn = fmaxf(m, max_over_rows(top));
-            const float corr = mx4_weight(m, mn, a.scale_log2e);
+            const float corr = softmax_weight(m, mn, a.scale_log2e);
             m = mn;
             l *= corr;
             sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                w[i] = mx4_exp(c[i >> 2][i & 3], m, a.scale_log2e);
+                w[i] = softmax_exp(c[i >> 2][i & 3], m, a.scale_log2e);
                 sum += w[i];
             }
 #pragma unroll
@@ -242,20 +230,20 @@ __global__ __launch_bounds__(kMxThreads, kMxPerCu) void attn_decode_mx4_kernel(c
     __syncthreads();
     for (int idx = tid; idx < G * kD; idx += kMxThreads) {
         const int h = idx / kD, c = idx % kD;
-        float M = kMxLowest;
+        float M = kSoftmaxLowest;
 #pragma unroll
         for (int w = 0; w < kMxWaves; ++w) M = fmaxf(M, sh_m[w][h]);
         float L = 0.f, A = 0.f;
 #pragma unroll
         for (int w = 0; w < kMxWaves; ++w) {
-            const float x = mx4_weight(sh_m[w][h], M, a.scale_log2e);
+            const float x = softmax_weight(sh_m[w][h], M, a.scale_log2e);
             L = fmaf(x, sh_l[w][h], L);
             A = fmaf(x, sh_acc[w][0][h][c] + sh_acc[w][1][h][c], A);
         }
         if (a.n_splits == 1) {                       // nothing to merge
             const int64_t hq = (int64_t)pr.b * a.ge.Hq + pr.g * G + h;
             a.out[hq * kD + c] = (uint16_t)f32_to_bf16_bits(L == 0.f ? 0.f : A / L);
-            if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = mx4_lse(M, L, a.scale_log2e);
+            if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = softmax_lse(M, L, a.scale_log2e);
             continue;
         }
         a.part_acc[(pbase + h) * kD + c] = A;
@@ -270,7 +258,7 @@ __global__ __launch_bounds__(kD * kMxMergeGroups) void attn_decode_mx4_merge_ker
     const int G = a.ge.G, p = blockIdx.x / G, h = blockIdx.x % G, c = threadIdx.x % kD, grp = threadIdx.x / kD;
     const int64_t pbase = (int64_t)p * a.n_splits * G;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
-    float M = kMxLowest, L = 0.f, A = 0.f;
+    float M = kSoftmaxLowest, L = 0.f, A = 0.f;
     for (int s0 = grp; s0 < a.n_splits; s0 += kMxMergeGroups * kMxMergeAhead) {
         float2 x[kMxMergeAhead];
         float v[kMxMergeAhead], top = M;
@@ -283,14 +271,14 @@ __global__ __launch_bounds__(kD * kMxMergeGroups) void attn_decode_mx4_merge_ker
 #pragma unroll
         for (int i = 0; i < kMxMergeAhead; ++i)
             if (s0 + i * kMxMergeGroups < a.n_splits) top = fmaxf(top, x[i].x);
-        const float corr = mx4_weight(M, top, a.scale_log2e);
+        const float corr = softmax_weight(M, top, a.scale_log2e);
         L *= corr;
         A *= corr;
         M = top;
 #pragma unroll
         for (int i = 0; i < kMxMergeAhead; ++i) {
             if (s0 + i * kMxMergeGroups >= a.n_splits) break;
-            const float w = mx4_weight(x[i].x, M, a.scale_log2e);
+            const float w = softmax_weight(x[i].x, M, a.scale_log2e);
             L = fmaf(w, x[i].y, L);
             A = fmaf(w, v[i], A);
         }
@@ -300,19 +288,19 @@ __global__ __launch_bounds__(kD * kMxMergeGroups) void attn_decode_mx4_merge_ker
     if (c == 0) { sh_m[grp] = M; sh_l[grp] = L; }
     __syncthreads();
     if (grp != 0) return;
-    M = kMxLowest;
+    M = kSoftmaxLowest;
 #pragma unroll
     for (int i = 0; i < kMxMergeGroups; ++i) M = fmaxf(M, sh_m[i]);
     L = A = 0.f;
 #pragma unroll
     for (int i = 0; i < kMxMergeGroups; ++i) {
-        const float w = mx4_weight(sh_m[i], M, a.scale_log2e);
+        const float w = softmax_weight(sh_m[i], M, a.scale_log2e);
         L = fmaf(w, sh_l[i], L);
         A = fmaf(w, sh_a[i][c], A);
     }
     const int64_t hq = (int64_t)(p / a.ge.Hkv) * a.ge.Hq + (p % a.ge.Hkv) * G + h;
     a.out[hq * kD + c] = (uint16_t)f32_to_bf16_bits(L == 0.f ? 0.f : A / L);       // an idle place: 0
-    if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = mx4_lse(M, L, a.scale_log2e);
+    if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = softmax_lse(M, L, a.scale_log2e);
 }
 
 // Most slots that a problem has: sink and window are not longer than the sequence, whatever they are given as

@@ -1,0 +1,423 @@
+// Decode attention over all rows of a cache (bf16, E4M3 or MX FP4) that also says how much attention each row got:
+//   s_hj = q_h k_j,   l_h = sum_j e^(c s_hj),   out_h = sum_j e^(c s_hj) v_j / l_h,   weight_j = decay before_j + sum_h e^(c s_hj) / l_h
+// over the heads h of a KV head.  A weight needs the sum over all rows, so the scores wait for it in scratch.  Two launches: the first cuts a
+// sequence's rows into parts, one workgroup each, and leaves scores and partial results; the second joins the parts, and turns scores into weights.
+//
+// A wave takes 32 rows at a time, the products on v_mfma_f32_16x16x32_bf16 (rows widened to bf16, exact); no value crosses lanes in between:
+//   scores   16 K rows x twice 8 heads (fewer repeat the last).  Lane (n, g) = (l % 16, l / 16) brings 16-byte pieces of row n, and gets head
+//            n % 8's scores of keys 4 g + r and 16 + 4 g + r.  A piece of bf16 is 8 of the dims 32 j + 8 g of step j, of E4M3 16 of 64 j + 16 g
+//            (two steps), of 4 bits the 32 of 32 g, one scale's (four steps); the queries' pieces are the same.
+//   output   16 rows x 32 keys x 16 dims, eight times: a lane's eight probabilities are its part of the left operand as they are (rounded to
+//            bf16 in rows 0 .. 7, what that dropped in rows 8 .. 15; the two are added in LDS), key 16 (i / 4) + 4 g + i % 4 for element i; for the right
+//            one it brings dims 8 n .. 8 n + 7 of the same keys, and column n of product j is dim 8 n + j.
+// So a probability is off by at most 2^-16 of it in the output.  The sums and the weights take the probabilities as they were.
+#include "api_checks.h"
+#include "decode_softmax.h"
+#include "kv_store.h"
+#include <algorithm>
+#include <type_traits>
+
+namespace ihip {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTrThreads = 256, kTrWaves = kTrThreads / kWave;
+constexpr int kTrStep = 32;                          // rows of a wave at a time
+constexpr int kTrMaxSplit = 4096, kTrMinSplit = 128; // rows of a part (multiples of 128: a step of every wave)
+
+struct TrackedArgs {
+    Geometry ge;
+    int max_len;
+    const uint16_t *q; int64_t q_sb, q_sh;
+    StoreView from;
+    int page_log2;                   // a cache without pages is one page a sequence
+    float scale_log2e, v_scale;
+    int n_splits;
+    DecodeGrid grid;
+    float *scores; int64_t score_stride;             // [P, G, score_stride], unscaled
+    float *part_ml, *part_acc;       // [P, n_splits, G, 2] (reference, unscaled, and sum), [P, n_splits, G, 128]
+    uint16_t *out;
+    float *out_lse;
+    const float *before;             // [P, weight_rows] or null
+    float *weights;
+    int weight_rows;
+    float decay;
+};
+
+__device__ inline uint16_t to_bf16(float x) { return (uint16_t)pack_bf16x2(x, x); }        // (NaN stays it)
+__device__ inline int tracked_len(const TrackedArgs &a, int b) { return min(max(a.ge.seq_lens[b], 0), a.max_len); }
+// Rows of each of a sequence's parts
+__device__ inline int tracked_part(const TrackedArgs &a, int len)
+{
+    return min(kTrMaxSplit, max(kTrMinSplit, (int)(((int64_t)len + a.n_splits - 1) / a.n_splits + kTrMinSplit - 1) / kTrMinSplit * kTrMinSplit));
+}
+
+template <int FORMAT>
+struct TrackedRows {
+    typedef typename std::conditional<FORMAT == IHIP_KV_BF16, uint4, typename std::conditional<FORMAT == IHIP_KV_E4M3, uint2, uint32_t>::type>::type word;
+    static constexpr int kPieces = FORMAT == IHIP_KV_BF16 ? 4 : FORMAT == IHIP_KV_E4M3 ? 2 : 1;
+    uint4 k[2][kPieces];             // of rows n and 16 + n
+    word v[8];                       // dims 8 n .. of keys 4 g + r and 16 + 4 g + r
+    uint32_t k_scale[2], v_scale[8]; // 4-bit rows
+    uint32_t there;                  // which of the 32 rows hold a key
+};
+
+template <int FORMAT, int HEADS>
+__global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void attn_decode_tracked_kernel(const TrackedArgs a)
+{
+    typedef TrackedRows<FORMAT> Rows;
+    const int p = a.grid.problem(), split = a.grid.part();
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, g = lane >> 4;
+    const int b = p / a.ge.Hkv, kv_head = p % a.ge.Hkv, G = a.ge.G;
+    const int len = tracked_len(a, b), per = tracked_part(a, len);
+    const int s0 = min(split * per, len), s1 = min(s0 + per, len), steps = (s1 - s0 + kTrStep - 1) / kTrStep;
+    const int64_t pbase = ((int64_t)p * a.n_splits + split) * G;
+
+    __shared__ int32_t sh_page[kTrMaxSplit + 1];     // of the part's rows: page ids, or the sequence
+    __shared__ float sh_m[kTrWaves][HEADS], sh_l[kTrWaves][HEADS];
+    __shared__ __attribute__((aligned(16))) float sh_acc[kTrWaves][2][HEADS][kD];      // of the two parts
+
+    // The operand of step j: 16-byte pieces as above
+    bf16x8 qb[4];
+    {
+        const uint16_t *qp = a.q + b * a.q_sb + (int64_t)(kv_head * G + min(n & 7, G - 1)) * a.q_sh;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            qb[j] = *reinterpret_cast<const bf16x8 *>(qp + (FORMAT == IHIP_KV_BF16 ? 32 * j + 8 * g : FORMAT == IHIP_KV_E4M3 ? 64 * (j >> 1) + 16 * g + 8 * (j & 1) : 32 * g + 8 * j));
+    }
+    const int first_page = s0 >> a.page_log2;
+    const uint32_t in_page = (1u << a.page_log2) - 1;
+    if (s1 > s0) {
+        const int pages = ((s1 - 1) >> a.page_log2) - first_page + 1;
+        const int32_t *table = a.from.paged.block_table ? a.from.paged.block_table + (int64_t)b * a.from.paged.table_stride + first_page : nullptr;
+        for (int i = tid; i < pages; i += kTrThreads) sh_page[i] = table ? table[i] : b;
+    }
+    const uint8_t *kb = a.from.k + kv_head * a.from.k_sh + g * 16, *vb = a.from.v + kv_head * a.from.v_sh + n * (int)sizeof(typename Rows::word);
+    const uint8_t *ksb = a.from.ks + kv_head * (a.from.k_sh / 16) + g, *vsb = a.from.vs + kv_head * (a.from.v_sh / 16) + (n >> 2);
+    __syncthreads();
+
+    // A row behind the part's last key stands for that one, a row on no page for one that can be read
+    auto load = [&](int step, Rows &r) {
+        const int row0 = s0 + step * kTrStep;
+        auto page_of = [&](int row) { return sh_page[(row >> a.page_log2) - first_page]; };
+        {
+            const int row = row0 + (lane & 31);
+            r.there = (uint32_t)__ballot(row < s1 && page_of(min(row, s1 - 1)) >= 0);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int row = min(row0 + 16 * t + n, s1 - 1);
+            const int64_t off = (int64_t)max(page_of(row), 0) * a.from.k_sb + (int64_t)((uint32_t)row & in_page) * a.from.k_st;
+#pragma unroll
+            for (int j = 0; j < Rows::kPieces; ++j) r.k[t][j] = *reinterpret_cast<const uint4 *>(kb + off + 64 * j);
+            if constexpr (FORMAT == IHIP_KV_MX4) r.k_scale[t] = ksb[off / 16];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = min(row0 + 16 * (i >> 2) + 4 * g + (i & 3), s1 - 1);
+            const int64_t off = (int64_t)max(page_of(row), 0) * a.from.v_sb + (int64_t)((uint32_t)row & in_page) * a.from.v_st;
+            r.v[i] = *reinterpret_cast<const typename Rows::word *>(vb + off);
+            if constexpr (FORMAT == IHIP_KV_MX4) r.v_scale[i] = vsb[off / 16];
+        }
+    };
+    // operand of step j of a lane's K row
+    auto k_operand = [&](const Rows &r, int t, int j) {
+        if constexpr (FORMAT == IHIP_KV_BF16) {
+            return __builtin_bit_cast(bf16x8, r.k[t][j]);
+        } else if constexpr (FORMAT == IHIP_KV_E4M3) {
+            const uint4 w = r.k[t][j >> 1];
+            return __builtin_bit_cast(bf16x8, fp8x8_to_bf16x8((j & 1) == 0 ? make_uint2(w.x, w.y) : make_uint2(w.z, w.w)));
+        } else {
+            const uint4 w = r.k[t][0];
+            return __builtin_bit_cast(bf16x8, mx4_to_bf16x8(j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w, mx4_scale(r.k_scale[t])));
+        }
+    };
+    auto v_row = [&](const Rows &r, int i) {
+        if constexpr (FORMAT == IHIP_KV_BF16) return r.v[i];
+        else if constexpr (FORMAT == IHIP_KV_E4M3) return fp8x8_to_bf16x8(r.v[i]);
+        else return mx4_to_bf16x8(r.v[i], mx4_scale(r.v_scale[i]));
+    };
+
+    const uint32_t second = n < 8 ? 0u : ~0u;        // lanes that bring the second parts of the probabilities
+    float *scores = a.scores + ((int64_t)p * G + min(n, G - 1)) * a.score_stride + s0 + 4 * g;
+    f32x4 acc[8];                                    // rows 4 g + r, dim 8 n + j
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = kSoftmaxLowest, l = 0.f;               // of head n (m: the same in the four lanes of a head; l: of this lane's keys)
+    Rows r, nx;
+    if (wv < steps) load(wv, r);
+    for (int step = wv; step < steps; step += kTrWaves) {
+        if (step + kTrWaves < steps) load(step + kTrWaves, nx);
+        f32x4 c[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand(r, t, j), qb[j], c[t], 0, 0, 0);
+        }
+        const uint32_t there = __builtin_amdgcn_readfirstlane(r.there);
+        if (there != ~0u) {                          // (what stands in the rows is not used, but has to be finite)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!((there >> (16 * (i >> 2) + 4 * g + (i & 3))) & 1)) {
+                    c[i >> 2][i & 3] = -INFINITY;
+                    r.v[i] = typename Rows::word{};
+                    r.v_scale[i] = 127;
+                }
+        }
+        if (n < G) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4 *>(scores + step * kTrStep + 16 * t) = c[t];
+        }
+        float w[8], sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w[i] = softmax_exp(c[i >> 2][i & 3], m, a.scale_log2e);    // of -inf: 0
+            sum += w[i];
+        }
+        if (__any(!(sum <= kSoftmaxMaxSum))) {       // the reference follows where the scores outgrew it
+            float top = c[0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, c[i >> 2][i & 3]);
+            const float mn = fmaxf(m, max_over_rows(top));
+            const float corr = softmax_weight(m, mn, a.scale_log2e);
+            m = mn;
+            l *= corr;
+            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = softmax_exp(c[i >> 2][i & 3], m, a.scale_log2e);
+                sum += w[i];
+            }
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const float x = __shfl(corr, 4 * g + h, 64);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j][h] *= x;
+            }
+        }
+        l += sum;
+        uint32_t part[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t first = pack_bf16x2(w[2 * i], w[2 * i + 1]) & second;
+            part[i] = pack_bf16x2(w[2 * i] - __uint_as_float(first << 16), w[2 * i + 1] - __uint_as_float(first & 0xffff0000u));
+        }
+        const bf16x8 pw = __builtin_bit_cast(bf16x8, make_uint4(part[0], part[1], part[2], part[3]));
+        uint4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = v_row(r, i);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {                // dims 8 n + 2 d and 8 n + 2 d + 1
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t even = d == 0 ? x[2 * i].x : d == 1 ? x[2 * i].y : d == 2 ? x[2 * i].z : x[2 * i].w;
+                const uint32_t odd = d == 0 ? x[2 * i + 1].x : d == 1 ? x[2 * i + 1].y : d == 2 ? x[2 * i + 1].z : x[2 * i + 1].w;
+                lo[i] = __builtin_amdgcn_perm(odd, even, 0x05040100u);
+                hi[i] = __builtin_amdgcn_perm(odd, even, 0x07060302u);
+            }
+            acc[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw, __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), acc[2 * d], 0, 0, 0);
+            acc[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw, __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), acc[2 * d + 1], 0, 0, 0);
+        }
+        r = nx;
+    }
+
+    // the waves and both parts are merged through LDS
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (lane < HEADS) { sh_m[wv][lane] = m; sh_l[wv][lane] = l; }
+    if (4 * (g & 1) < HEADS) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            float *to = &sh_acc[wv][g >> 1][4 * (g & 1) + h][8 * n];
+            *reinterpret_cast<float4 *>(to) = make_float4(acc[0][h], acc[1][h], acc[2][h], acc[3][h]);
+            *reinterpret_cast<float4 *>(to + 4) = make_float4(acc[4][h], acc[5][h], acc[6][h], acc[7][h]);
+        }
+    }
+    __syncthreads();
+    for (int idx = tid; idx < G * kD; idx += kTrThreads) {
+        const int h = idx / kD, c = idx % kD;
+        float M = kSoftmaxLowest;
+#pragma unroll
+        for (int w = 0; w < kTrWaves; ++w) M = fmaxf(M, sh_m[w][h]);
+        float L = 0.f, A = 0.f;
+#pragma unroll
+        for (int w = 0; w < kTrWaves; ++w) {
+            const float x = softmax_weight(sh_m[w][h], M, a.scale_log2e);
+            L = fmaf(x, sh_l[w][h], L);
+            A = fmaf(x, sh_acc[w][0][h][c] + sh_acc[w][1][h][c], A);
+        }
+        if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + (pbase + h) * 2) = make_float2(M, L);
+        if (a.n_splits == 1) {                       // nothing to join
+            const int64_t hq = (int64_t)b * a.ge.Hq + kv_head * G + h;
+            a.out[hq * kD + c] = to_bf16(L == 0.f ? 0.f : A / L * a.v_scale);
+            if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = softmax_lse(M, L, a.scale_log2e);
+        } else {
+            a.part_acc[(pbase + h) * kD + c] = A;
+        }
+    }
+}
+
+// The parts joined, and weights: of the workgroups of a problem the first G take a head's output (where there are parts), the others
+// kJoinRows rows each.
+constexpr int kJoinRows = 1024, kJoinAhead = 8;
+__global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(const TrackedArgs a, int out_groups)
+{
+    const int G = a.ge.G, p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int b = p / a.ge.Hkv;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (int64_t)p * a.n_splits * G;
+    __shared__ float sh_m[8], sh_l[8], sh_a[kD];
+    if ((int)blockIdx.y < out_groups) {
+        const int h = blockIdx.y, c = tid % kD, grp = tid / kD;
+        const float *accs = a.part_acc + (int64_t)p * a.n_splits * G * kD;
+        float M = kSoftmaxLowest, L = 0.f, A = 0.f;
+        for (int s0 = grp; s0 < a.n_splits; s0 += 2 * kJoinAhead) {
+            float2 x[kJoinAhead];
+            float v[kJoinAhead], top = M;
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i) {
+                const int64_t at = (int64_t)min(s0 + i * 2, a.n_splits - 1) * G + h;
+                x[i] = ml[at];
+                v[i] = accs[at * kD + c];
+            }
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i)
+                if (s0 + i * 2 < a.n_splits) top = fmaxf(top, x[i].x);
+            const float corr = softmax_weight(M, top, a.scale_log2e);
+            L *= corr;
+            A *= corr;
+            M = top;
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i) {
+                if (s0 + i * 2 >= a.n_splits) break;
+                const float w = softmax_weight(x[i].x, M, a.scale_log2e);
+                L = fmaf(w, x[i].y, L);
+                A = fmaf(w, v[i], A);
+            }
+        }
+        if (grp == 1) {
+            sh_a[c] = A;
+            if (c == 0) { sh_m[0] = M; sh_l[0] = L; }
+        }
+        __syncthreads();
+        if (grp == 1) return;
+        const float top = fmaxf(M, sh_m[0]), mine = softmax_weight(M, top, a.scale_log2e), other = softmax_weight(sh_m[0], top, a.scale_log2e);
+        L = fmaf(other, sh_l[0], mine * L);
+        A = fmaf(other, sh_a[c], mine * A);
+        const int64_t hq = (int64_t)b * a.ge.Hq + (p % a.ge.Hkv) * G + h;
+        a.out[hq * kD + c] = to_bf16(L == 0.f ? 0.f : A / L * a.v_scale);     // an idle place: 0
+        if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = softmax_lse(top, L, a.scale_log2e);
+        return;
+    }
+    const int len = tracked_len(a, b), row0 = ((int)blockIdx.y - out_groups) * kJoinRows;
+    if (row0 >= len) return;
+    for (int h = wv; h < G; h += kTrWaves) {
+        float M = kSoftmaxLowest, L = 0.f;
+        for (int s = lane; s < a.n_splits; s += 64) M = fmaxf(M, ml[(int64_t)s * G + h].x);
+        M = wave_max_f32(M);
+        for (int s = lane; s < a.n_splits; s += 64) {
+            const float2 x = ml[(int64_t)s * G + h];
+            L = fmaf(softmax_weight(x.x, M, a.scale_log2e), x.y, L);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) L += __shfl_xor(L, d, 64);
+        // a row's probability is 2^(c (s - M) - log2 of the sum of those); without a key that is there, 0
+        if (lane == 0) { sh_m[h] = M; sh_l[h] = L == 0.f ? INFINITY : log2f(L) + kSoftmaxShift; }
+    }
+    __syncthreads();
+    const float *scores = a.scores + (int64_t)p * G * a.score_stride;
+#pragma unroll
+    for (int i = 0; i < kJoinRows / kTrThreads; ++i) {
+        const int row = row0 + i * kTrThreads + tid;
+        if (row >= len) break;
+        float w = 0.f;
+        for (int h = 0; h < G; ++h) w += __builtin_amdgcn_exp2f(fmaf(scores[h * a.score_stride + row] - sh_m[h], a.scale_log2e, -sh_l[h]));
+        const int64_t at = (int64_t)p * a.weight_rows + row;
+        a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w;
+    }
+}
+
+struct TrackedPlan { int splits; int64_t score_stride; size_t bytes; };
+static TrackedPlan tracked_plan(const ihip_shape &s)
+{
+    const int64_t total = s.max_seq_len, P = std::max<int64_t>(1, (int64_t)s.B * s.Hkv), places = (int64_t)compute_units() * 2;
+    const int64_t fewest = (total + kTrMaxSplit - 1) / kTrMaxSplit, finest = (total + kTrMinSplit - 1) / kTrMinSplit;
+    TrackedPlan r;
+    r.splits = (int)std::min(std::max((places + P - 1) / P, fewest), finest);
+    r.score_stride = (total + kTrStep - 1) / kTrStep * kTrStep;
+    r.bytes = (size_t)s.B * s.Hq * (r.score_stride + (int64_t)r.splits * (2 + kD)) * sizeof(float);
+    return r;
+}
+
+}  // namespace ihip
+
+using namespace ihip;
+
+extern "C" size_t ihip_attn_decode_tracked_workspace_bytes(const ihip_shape *shape)
+{
+    if (check_shape(shape, "ihip_attn_decode_tracked_workspace_bytes") != IHIP_OK) return 0;
+    return std::max<size_t>(tracked_plan(*shape).bytes, 256);
+}
+
+extern "C" int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor q, const ihip_kv_store *store, float sm_scale,
+                                            const float *before, float decay, const ihip_kv_track *track, void *out,
+                                            float *out_lse, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ihip_attn_decode_tracked";
+    int32_t rc;
+    if ((rc = check_shape(shape, who)) != IHIP_OK) return rc;
+    if (shape->B == 0) return IHIP_OK;
+    if (shape->Tq != 1 || shape->b_q != 1) return fail(IHIP_ERR_INVALID_ARG, "%s: needs Tq == b_q == 1", who);
+    if ((rc = check_tensor(q, who, "q")) != IHIP_OK) return rc;
+    TrackedArgs a{};
+    if ((rc = check_store(who, store, *shape, &a.from)) != IHIP_OK) return rc;
+    if ((rc = check_track(who, track, shape->max_seq_len, false)) != IHIP_OK) return rc;
+    if (!(decay >= 0.f) || decay > 3.4028234e38f) return fail(IHIP_ERR_INVALID_ARG, "%s: decay = %g", who, decay);
+    if (!out) return fail(IHIP_ERR_INVALID_ARG, "%s: out is NULL", who);
+    if ((rc = check_sm_scale(who, sm_scale, &a.scale_log2e)) != IHIP_OK) return rc;
+    if ((rc = check_sm_scale(who, sm_scale * a.from.k_scale, &a.scale_log2e)) != IHIP_OK) return rc;
+    const TrackedPlan plan = tracked_plan(*shape);
+    if (!ws || ((uintptr_t)ws & 15) || ws_bytes < plan.bytes)
+        return fail(IHIP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 16-byte aligned, needed, %zu given", who, plan.bytes, ws_bytes);
+    const int64_t P = (int64_t)shape->B * shape->Hkv;
+    if (P > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld sequences x KV heads are too many", who, (long long)P);
+    const int64_t join_groups = ((int64_t)shape->max_seq_len - 1) / kJoinRows + 1;
+    if (join_groups > 65535 - 8) return fail(IHIP_ERR_UNSUPPORTED, "%s: max_seq_len = %d is too large", who, shape->max_seq_len);
+    a.ge = make_geometry(*shape);
+    a.max_len = shape->max_seq_len;
+    a.q = (const uint16_t *)q.ptr; a.q_sb = q.stride_b; a.q_sh = q.stride_h;
+    a.page_log2 = a.from.paged.block_table ? a.from.paged.page_log2 : 31;
+    a.v_scale = a.from.v_scale;
+    a.n_splits = plan.splits;
+    a.grid = decode_grid(a.ge, a.n_splits, false);
+    a.scores = (float *)ws;
+    a.score_stride = plan.score_stride;
+    a.part_ml = a.scores + P * a.ge.G * plan.score_stride;
+    a.part_acc = a.part_ml + P * a.n_splits * a.ge.G * 2;
+    a.out = (uint16_t *)out;
+    a.out_lse = out_lse;
+    a.before = before;
+    a.weights = track->weights;
+    a.weight_rows = track->rows;
+    a.decay = decay;
+    const hipStream_t st = (hipStream_t)stream;
+    const dim3 grid = a.grid.dims((int)P, a.n_splits);
+    {
+        KernelTimer timer("attn_decode_tracked", st);
+#define IHIP_AT(FMT)                                                                                                              \
+        if (a.ge.G <= 4) hipLaunchKernelGGL((attn_decode_tracked_kernel<FMT, 4>), grid, dim3(kTrThreads), 0, st, a);              \
+        else hipLaunchKernelGGL((attn_decode_tracked_kernel<FMT, 8>), grid, dim3(kTrThreads), 0, st, a)
+        if (store->format == IHIP_KV_BF16) { IHIP_AT(IHIP_KV_BF16); }
+        else if (store->format == IHIP_KV_E4M3) { IHIP_AT(IHIP_KV_E4M3); }
+        else { IHIP_AT(IHIP_KV_MX4); }
+#undef IHIP_AT
+    }
+    if ((rc = check_launch(who)) != IHIP_OK) return rc;
+    const int out_groups = a.n_splits > 1 ? a.ge.G : 0;
+    KernelTimer timer("attn_decode_tracked_join", st);
+    hipLaunchKernelGGL(attn_decode_tracked_join_kernel, dim3((uint32_t)P, (uint32_t)(out_groups + join_groups)), dim3(kTrThreads), 0, st, a, out_groups);
+    return check_launch(who);
+}

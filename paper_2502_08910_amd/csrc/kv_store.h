@@ -14,6 +14,9 @@ struct StoreView {
     PagedView paged;             // block_table == nullptr: stride b goes from sequence to sequence
 };
 int32_t check_store(const char *who, const ihip_kv_store *store, const ihip_shape &for_lengths, StoreView *view);
+// `whole`: with positions and tokens seen; otherwise the weights alone
+int32_t check_track(const char *who, const ihip_kv_track *track, int64_t rows, bool whole);
+int32_t check_packed(const char *who, const ihip_packed *p);
 
 // ---- MX4 ----------------------------------------------------------------------
 // 2^(s - 127) of a scale byte; what the converters take as their scale (only its exponent counts there).  255, which is an infinity here, is

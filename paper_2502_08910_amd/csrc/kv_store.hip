@@ -39,6 +39,11 @@ struct AppendArgs {
     int64_t qo_sh, qo_st, ko_sh, ko_st;
     int first, per_wg;               // first head slot (Hq without queries) and head slots of a workgroup
     bool past;
+    // tracked: what stands beside the rows
+    const int32_t *seen;
+    float *weights;
+    int32_t *positions;
+    int track_rows, n_pos;           // rows of a head; positions that can be rotated to
 };
 
 __device__ inline void append_row(uint8_t *row, uint8_t *scales, const uint4 &raw, const float (&f)[8], bool turned, int l16, int format, float scale, bool past)
@@ -57,14 +62,15 @@ __device__ inline void append_row(uint8_t *row, uint8_t *scales, const uint4 &ra
 }
 
 // A workgroup takes 16 tokens, 16 lanes each, and a.per_wg of the Hq + 2 Hkv rows that each of them has: its queries, keys, values.
-template <int FORMAT, bool ROPE>
+// TRACKED: a token's position is not its row, and both are written down.
+template <int FORMAT, bool ROPE, bool TRACKED>
 __global__ __launch_bounds__(kStoreThreads) void kv_append_kernel(const AppendArgs a)
 {
     constexpr int kBatch = 4;        // rows that a lane asks for at once
     const int tid = threadIdx.x, l16 = tid & 15, grp = tid >> 4;
     const int t0 = blockIdx.x * kStoreGroups, tok = t0 + grp;
     const int s0 = a.first + blockIdx.y * a.per_wg, s1 = min(s0 + a.per_wg, a.Hq + 2 * a.Hkv);
-    __shared__ int sh_b[kStoreGroups], sh_pos[kStoreGroups];
+    __shared__ int sh_b[kStoreGroups], sh_pos[kStoreGroups], sh_at[TRACKED ? kStoreGroups : 1];
 
     uint4 raw[kBatch];
     auto load = [&](int s) {
@@ -88,16 +94,19 @@ __global__ __launch_bounds__(kStoreThreads) void kv_append_kernel(const AppendAr
         for (int t = max(c0, t0); t < min(c1, t0 + kStoreGroups); ++t) {
             sh_b[t - t0] = b;
             sh_pos[t - t0] = len - (c1 - t);
+            if constexpr (TRACKED) sh_at[t - t0] = a.seen[b] - (c1 - t);
         }
     }
     __syncthreads();
     const int b = sh_b[grp], pos = sh_pos[grp];
-    const bool there = b >= 0 && pos >= 0 && pos < a.max_len;
+    int at = pos;                    // position in the sequence (pos: row)
+    if constexpr (TRACKED) at = sh_at[grp];
+    const bool there = b >= 0 && pos >= 0 && pos < a.max_len && (!TRACKED || (at >= 0 && at < a.n_pos));
     if (!there) return;              // (no barrier below)
     float4 c, n;
     if constexpr (ROPE) {
-        c = reinterpret_cast<const float4 *>(a.cos + (int64_t)pos * (kD / 2))[l16];
-        n = reinterpret_cast<const float4 *>(a.sin + (int64_t)pos * (kD / 2))[l16];
+        c = reinterpret_cast<const float4 *>(a.cos + (int64_t)at * (kD / 2))[l16];
+        n = reinterpret_cast<const float4 *>(a.sin + (int64_t)at * (kD / 2))[l16];
     }
     int64_t first = b, in_page = pos;
     if (a.to.paged.block_table) {
@@ -128,6 +137,11 @@ __global__ __launch_bounds__(kStoreThreads) void kv_append_kernel(const AppendAr
                 if (!is_q && kept) {
                     const int64_t o = k_row + (slot - a.Hq) * a.to.k_sh;
                     append_row(a.to.k + o, a.to.ks + o / 16, raw[u], f, ROPE, l16, FORMAT, a.to.k_scale, a.past);
+                    if constexpr (TRACKED) {
+                        const int64_t r = ((int64_t)b * a.Hkv + slot - a.Hq) * a.track_rows + pos;
+                        if (l16 == 0) a.weights[r] = 0.f;
+                        if (l16 == 1) a.positions[r] = at;
+                    }
                 }
             } else if (kept) {
                 const int64_t o = v_row + (slot - a.Hq - a.Hkv) * a.to.v_sh;
@@ -234,6 +248,15 @@ int32_t check_output(const ihip_tensor &t, const char *who, const char *name, in
     return IHIP_OK;
 }
 
+int32_t check_track(const char *who, const ihip_kv_track *track, int64_t rows, bool whole)
+{
+    if (!track) return fail(IHIP_ERR_INVALID_ARG, "%s: track is NULL", who);
+    if (!track->weights || (whole && (!track->positions || !track->seen)))
+        return fail(IHIP_ERR_INVALID_ARG, "%s: an array of track is NULL", who);
+    if (track->rows < 0 || track->rows < rows) return fail(IHIP_ERR_INVALID_ARG, "%s: track has %d rows, %lld are needed", who, track->rows, (long long)rows);
+    return IHIP_OK;
+}
+
 int32_t check_store(const char *who, const ihip_kv_store *store, const ihip_shape &for_lengths, StoreView *view)
 {
     int32_t rc;
@@ -282,13 +305,11 @@ int32_t check_store(const char *who, const ihip_kv_store *store, const ihip_shap
 
 using namespace ihip;
 
-extern "C" {
-
-int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v, const int32_t *seq_lens,
-                       int32_t max_seq_len, const ihip_rope *rope, const ihip_kv_store *store, ihip_tensor q_out,
-                       ihip_tensor k_out, void *stream)
+// track: NULL, or what ihip_kv_append_tracked was given
+static int32_t append_entry(const char *who, const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v, const int32_t *seq_lens,
+                            int32_t max_seq_len, const ihip_rope *rope, const ihip_kv_store *store, const ihip_kv_track *track,
+                            ihip_tensor q_out, ihip_tensor k_out, void *stream)
 {
-    const char *who = "ihip_kv_append";
     int32_t rc;
     if ((rc = check_packed(who, packed)) != IHIP_OK) return rc;
     if (packed->B == 0 || packed->rows == 0) return IHIP_OK;
@@ -300,7 +321,7 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
     if (max_seq_len <= 0) return fail(IHIP_ERR_INVALID_ARG, "%s: max_seq_len = %d", who, max_seq_len);
     if (rope && (!rope->cos || !rope->sin || (((uintptr_t)rope->cos | (uintptr_t)rope->sin) & 15)))
         return fail(IHIP_ERR_INVALID_ARG, "%s: rope tables are NULL or not 16-byte aligned", who);
-    if (rope && rope->n_pos < max_seq_len)
+    if (rope && !track && rope->n_pos < max_seq_len)
         return fail(IHIP_ERR_INVALID_ARG, "%s: rope table has %d positions, max_seq_len is %d", who, rope->n_pos, max_seq_len);
     AppendArgs a{};
     ihip_shape lengths{};
@@ -309,6 +330,10 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
     const int64_t row = store->format == IHIP_KV_BF16 ? 2 * kD : store->format == IHIP_KV_E4M3 ? kD : kD / 2;
     if (packed->Hkv > 1 && (std::abs(a.to.k_sh) < row || std::abs(a.to.v_sh) < row))
         return fail(IHIP_ERR_INVALID_ARG, "%s: the heads of the store overlap", who);
+    if (track) {
+        a.seen = track->seen; a.weights = track->weights; a.positions = track->positions; a.track_rows = track->rows;
+        a.n_pos = rope ? rope->n_pos : INT32_MAX;
+    }
     a.B = packed->B; a.Hq = packed->Hq; a.Hkv = packed->Hkv; a.rows = packed->rows; a.max_len = max_seq_len;
     a.cu = packed->cu_q; a.lens = seq_lens;
     a.q = (const uint16_t *)q.ptr; a.q_sh = q.stride_h; a.q_st = q.stride_t;
@@ -328,14 +353,37 @@ int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, 
     const dim3 grid(groups, (slots + a.per_wg - 1) / a.per_wg);
     if (grid.y > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: %d heads are too many", who, slots);
     KernelTimer timer("kv_append", (hipStream_t)stream);
-#define IHIP_KA(FMT)                                                                                                             \
-    if (rope) hipLaunchKernelGGL((kv_append_kernel<FMT, true>), grid, dim3(kStoreThreads), 0, (hipStream_t)stream, a);           \
-    else hipLaunchKernelGGL((kv_append_kernel<FMT, false>), grid, dim3(kStoreThreads), 0, (hipStream_t)stream, a)
+#define IHIP_KA(FMT)                                                                                                                   \
+    if (rope && track) hipLaunchKernelGGL((kv_append_kernel<FMT, true, true>), grid, dim3(kStoreThreads), 0, (hipStream_t)stream, a);  \
+    else if (rope) hipLaunchKernelGGL((kv_append_kernel<FMT, true, false>), grid, dim3(kStoreThreads), 0, (hipStream_t)stream, a);     \
+    else if (track) hipLaunchKernelGGL((kv_append_kernel<FMT, false, true>), grid, dim3(kStoreThreads), 0, (hipStream_t)stream, a);    \
+    else hipLaunchKernelGGL((kv_append_kernel<FMT, false, false>), grid, dim3(kStoreThreads), 0, (hipStream_t)stream, a)
     if (store->format == IHIP_KV_BF16) { IHIP_KA(IHIP_KV_BF16); }
     else if (store->format == IHIP_KV_E4M3) { IHIP_KA(IHIP_KV_E4M3); }
     else { IHIP_KA(IHIP_KV_MX4); }
 #undef IHIP_KA
     return check_launch(who);
+}
+
+extern "C" {
+
+int32_t ihip_kv_append(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v, const int32_t *seq_lens,
+                       int32_t max_seq_len, const ihip_rope *rope, const ihip_kv_store *store, ihip_tensor q_out,
+                       ihip_tensor k_out, void *stream)
+{
+    return append_entry("ihip_kv_append", packed, q, k, v, seq_lens, max_seq_len, rope, store, nullptr, q_out, k_out, stream);
+}
+
+int32_t ihip_kv_append_tracked(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, ihip_tensor v, const int32_t *seq_lens,
+                               int32_t max_seq_len, const ihip_rope *rope, const ihip_kv_store *store,
+                               const ihip_kv_track *track, ihip_tensor q_out, ihip_tensor k_out, void *stream)
+{
+    const char *who = "ihip_kv_append_tracked";
+    int32_t rc;
+    if ((rc = check_packed(who, packed)) != IHIP_OK) return rc;
+    if (packed->B == 0 || packed->rows == 0) return IHIP_OK;
+    if ((rc = check_track(who, track, max_seq_len, true)) != IHIP_OK) return rc;
+    return append_entry(who, packed, q, k, v, seq_lens, max_seq_len, rope, store, track, q_out, k_out, stream);
 }
 
 int32_t ihip_kv_gather(const ihip_kv_store *store, int32_t B, int32_t Hkv, int32_t d, const int32_t *seq_lens,

@@ -1,0 +1,271 @@
+// What a prompt's queries attend to: for every key the sum of the probabilities that the queries of its KV head give it,
+//   W_j = decay before_j + sum_i 2^(c q_i k_j - r_i),   j <= i + (keys - queries),   c = sm_scale log2 e,   r_i = log2 e times the query's log-sum-exp,
+// over all or the last of the queries and over the query heads of the KV head.  The log-sum-exp is known from the attention itself, so nothing
+// depends on another key: a workgroup owns 256 keys, which stay in registers, and the queries go by.
+// A wave has 64 keys (twice 32, the right operand of v_mfma_f32_32x32x16_bf16), queries' heads are the left operand, so that a lane has 16 scores of
+// one key and adds up their exponentials by itself.  Queries go from memory to LDS in tiles of 64 (query, head) rows, 16-byte chunks
+// XORed with the row against bank conflicts, and serve the four waves.
+// Sums go in order: 16 probabilities, those of a tile, of kSumTiles tiles, of a chunk of tiles, of the chunks; the results do not depend on timing.
+#include "api_checks.h"
+#include "kv_store.h"
+#include <algorithm>
+
+namespace ihip {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kKwThreads = 256, kKwWaves = kKwThreads / kWave;
+constexpr int kKwKeys = 64 * kKwWaves;               // of a workgroup
+constexpr int kKwRows = 64;                          // rows of a tile
+constexpr int kSumTiles = 16;
+
+struct KeyWeightArgs {
+    int B, Hq, Hkv, G, rows_q, rows_k, window;
+    const int32_t *cu_q, *cu_k;
+    const uint16_t *q, *k;
+    int64_t q_sh, q_st, k_sh, k_st;
+    const float *lse;                // [rows_q, Hq]
+    float scale_log2e, decay;
+    const float *before;             // [B, Hkv, weight_rows] or null
+    float *weights;
+    int weight_rows;
+    int chunk_tiles, chunks;         // tiles of a chunk, from the sequence's end; chunks that a sequence can have
+    float *part;                     // [chunk, Hkv, rows_k], or null: one chunk
+};
+
+// A sequence, and the tiles of its rows that count
+struct KeyWeightSeq {
+    int q_first, nq, k_first, nk, ahead, row0, rows;         // rows row0 .. rows - 1 count
+    __device__ KeyWeightSeq(const KeyWeightArgs &a, int b)
+    {
+        q_first = min(max(a.cu_q[b], 0), a.rows_q);
+        nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
+        k_first = min(max(a.cu_k[b], 0), a.rows_k);
+        nk = min(max(a.cu_k[b + 1], k_first), a.rows_k) - k_first;
+        ahead = nk - nq;                             // query i sees keys 0 .. i + ahead
+        row0 = max(0, nq - a.window) * a.G;
+        rows = nq * a.G;
+    }
+    __device__ int tiles() const { return (rows - row0 + kKwRows - 1) / kKwRows; }
+    // the first tile with a query that sees key k
+    __device__ int first_tile(const KeyWeightArgs &a, int k) const { return (int)min(max((int64_t)0, ((int64_t)k - ahead) * a.G - row0) / kKwRows, (int64_t)tiles()); }
+};
+// Blocks of keys are numbered so that sequence b's begin at first key / kKwKeys + b, which leaves room for a part of a block in each
+__device__ inline int key_block_seq(const KeyWeightArgs &a, int id, int lane)
+{
+    int n = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int b = b0 + lane;
+        n += __popcll(__ballot(b < a.B && min(max(a.cu_k[min(b, a.B - 1)], 0), a.rows_k) / kKwKeys + b <= id));
+    }
+    return __builtin_amdgcn_readfirstlane(n - 1);
+}
+
+__global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const KeyWeightArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint16_t sh_q[2][kKwRows * kD];
+    __shared__ __attribute__((aligned(16))) float sh_r[2][kKwRows];          // of a tile's rows: r, and the last key
+    __shared__ __attribute__((aligned(16))) int sh_last[2][kKwRows];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    const int g = blockIdx.x % a.Hkv, id = blockIdx.x / a.Hkv;
+    const int b = key_block_seq(a, id, lane);
+    if (b < 0) return;
+    const KeyWeightSeq seq(a, b);
+    const int block = id - (seq.k_first / kKwKeys + b), k0 = block * kKwKeys;
+    if (block < 0 || k0 >= seq.nk) return;
+    const int tiles = seq.tiles(), begin = seq.first_tile(a, k0);
+    const int end = tiles - (int)min((int64_t)blockIdx.y * a.chunk_tiles, (int64_t)tiles), t0 = max(begin, end - a.chunk_tiles);
+    if (blockIdx.y > 0 && t0 >= end) return;
+    const int kw = k0 + wave * 64;                   // this wave's first key
+
+    bf16x8 kb[2][8];                                 // (behind the last key: that one again)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const uint16_t *kp = a.k + (int64_t)(seq.k_first + min(kw + 32 * s + n, seq.nk - 1)) * a.k_st + g * a.k_sh + half * 8;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) kb[s][ks] = *reinterpret_cast<const bf16x8 *>(kp + ks * 16);
+    }
+
+    auto request = [&](int t, int st) {              // 4-row pieces of a tile, dealt to the waves
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)&sh_q[st][0];
+#pragma unroll
+        for (int i = 0; i < kKwRows / (4 * kKwWaves); ++i) {
+            const int piece = wave + i * kKwWaves, in_tile = 4 * piece + (lane >> 4);
+            const int row = min(seq.row0 + t * kKwRows + in_tile, seq.rows - 1), query = row / a.G;
+            const uint16_t *src = a.q + (int64_t)(seq.q_first + query) * a.q_st + (g * a.G + row - query * a.G) * a.q_sh + (((lane & 15) ^ (in_tile & 15)) << 3);
+            global_to_lds(lds0 + piece * 4 * kD * 2, src);
+        }
+    };
+    auto row_info = [&](int t, float &r, int &last) {        // of row tid of the tile
+        const int row = seq.row0 + t * kKwRows + tid, at = min(row, seq.rows - 1), query = at / a.G;
+        r = a.lse[(int64_t)(seq.q_first + query) * a.Hq + g * a.G + at - query * a.G] * 1.44269504088896340736f;
+        last = row < seq.rows ? query + seq.ahead : -1;
+    };
+
+    float sum[2] = {0.f, 0.f}, near_sum[2] = {0.f, 0.f};
+    if (t0 < end) {
+        request(end - 1, 0);
+        if (tid < kKwRows) row_info(end - 1, sh_r[0][tid], sh_last[0][tid]);
+    }
+    for (int t = end - 1, st = 0; t >= t0; --t, st ^= 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        float r_next;
+        int last_next;
+        if (t > t0) {
+            request(t - 1, st ^ 1);
+            if (tid < kKwRows) row_info(t - 1, r_next, last_next);
+        }
+        const int first_row = seq.row0 + t * kKwRows;
+        const bool whole = first_row / a.G + seq.ahead >= kw + 63 && first_row + kKwRows <= seq.rows;        // all rows see all of the wave's keys
+#pragma unroll
+        for (int h = 0; h < kKwRows / 32; ++h) {
+            f32x16 c[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) {
+                const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&sh_q[st][(32 * h + n) * kD + (((ks * 2 + half) ^ (n & 15)) << 3)]);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) c[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, kb[s][ks], c[s], 0, 0, 0);
+            }
+            // score i is that of row 8 (i / 4) + 4 half + i % 4
+            float tile_sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+                const float4 r4 = *reinterpret_cast<const float4 *>(&sh_r[st][32 * h + 8 * i4 + 4 * half]);
+                const float r[4] = {r4.x, r4.y, r4.z, r4.w};
+                int last[4] = {};
+                if (!whole) {
+                    const int4 l4 = *reinterpret_cast<const int4 *>(&sh_last[st][32 * h + 8 * i4 + 4 * half]);
+                    last[0] = l4.x; last[1] = l4.y; last[2] = l4.z; last[3] = l4.w;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        float w = __builtin_amdgcn_exp2f(fmaf(c[s][4 * i4 + i], a.scale_log2e, -r[i]));
+                        if (!whole) w = kw + 32 * s + n <= last[i] ? w : 0.f;
+                        tile_sum[s] += w;
+                    }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) near_sum[s] += tile_sum[s];
+        }
+        if ((t - t0) % kSumTiles == 0) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                sum[s] += near_sum[s];
+                near_sum[s] = 0.f;
+            }
+        }
+        if (t > t0 && tid < kKwRows) {
+            sh_r[st ^ 1][tid] = r_next;
+            sh_last[st ^ 1][tid] = last_next;
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const float w = sum[s] + __shfl_xor(sum[s], 32, 64);
+        const int key = kw + 32 * s + n;
+        if (half != s || key >= seq.nk) continue;
+        if (a.part) {
+            a.part[((int64_t)blockIdx.y * a.Hkv + g) * a.rows_k + seq.k_first + key] = w;
+        } else if (key < a.weight_rows) {
+            const int64_t at = ((int64_t)b * a.Hkv + g) * a.weight_rows + key;
+            a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w;
+        }
+    }
+}
+
+// The chunks of a block of keys added up, a key a thread
+__global__ __launch_bounds__(kKwKeys) void prompt_key_weights_sum_kernel(const KeyWeightArgs a)
+{
+    const int g = blockIdx.x % a.Hkv, id = blockIdx.x / a.Hkv;
+    const int b = key_block_seq(a, id, threadIdx.x & 63);
+    if (b < 0) return;
+    const KeyWeightSeq seq(a, b);
+    const int k0 = (id - (seq.k_first / kKwKeys + b)) * kKwKeys, key = k0 + threadIdx.x;
+    if (k0 < 0 || key >= seq.nk || key >= a.weight_rows) return;
+    const int chunks = min(a.chunks, max(1, (seq.tiles() - seq.first_tile(a, k0) + a.chunk_tiles - 1) / a.chunk_tiles));
+    float w = 0.f;
+    for (int c = 0; c < chunks; ++c) w += a.part[((int64_t)c * a.Hkv + g) * a.rows_k + seq.k_first + key];
+    const int64_t at = ((int64_t)b * a.Hkv + g) * a.weight_rows + key;
+    a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w;
+}
+
+struct KeyWeightPlan { int64_t blocks; int chunk_tiles, chunks; size_t bytes; };
+static KeyWeightPlan key_weight_plan(const ihip_packed &p, int rows_k, int window)
+{
+    constexpr int kLeast = 8;                        // tiles of a chunk
+    const int64_t G = p.Hq / p.Hkv, most = std::max<int64_t>(1, ((int64_t)std::min({p.max_q, window, p.rows}) * G + kKwRows - 1) / kKwRows);
+    KeyWeightPlan r;
+    r.blocks = rows_k / kKwKeys + p.B;
+    const int64_t places = 4 * 2 * (int64_t)compute_units();
+    const int64_t want = std::max<int64_t>(kLeast, r.blocks * p.Hkv * most / places + 1);
+    r.chunk_tiles = (int)std::min(want, most);
+    r.chunks = (int)((most - 1) / r.chunk_tiles + 1);
+    r.bytes = r.chunks > 1 ? (size_t)r.chunks * p.Hkv * rows_k * sizeof(float) : 0;
+    return r;
+}
+
+}  // namespace ihip
+
+using namespace ihip;
+
+extern "C" size_t ihip_prompt_key_weights_workspace_bytes(const ihip_packed *packed, int32_t rows_k, int32_t window)
+{
+    const char *who = "ihip_prompt_key_weights_workspace_bytes";
+    if (check_packed(who, packed) != IHIP_OK) return 0;
+    if (rows_k < 0 || window < 1) {
+        fail(IHIP_ERR_INVALID_ARG, "%s: rows_k = %d, window = %d", who, rows_k, window);
+        return 0;
+    }
+    return std::max<size_t>(key_weight_plan(*packed, rows_k, window).bytes, 256);
+}
+
+extern "C" int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tensor q, ihip_tensor k, const int32_t *cu_k, int32_t rows_k,
+                                           float sm_scale, const float *lse, int32_t window, const float *before, float decay,
+                                           const ihip_kv_track *track, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *who = "ihip_prompt_key_weights";
+    int32_t rc;
+    if ((rc = check_packed(who, packed)) != IHIP_OK) return rc;
+    if (rows_k < 0 || (!cu_k && rows_k != packed->rows))
+        return fail(IHIP_ERR_INVALID_ARG, "%s: rows_k = %d (without cu_k: the %d rows of q)", who, rows_k, packed->rows);
+    if (window < 1) return fail(IHIP_ERR_INVALID_ARG, "%s: window = %d", who, window);
+    if (packed->B == 0 || rows_k == 0) return IHIP_OK;
+    KeyWeightArgs a{};
+    if ((rc = check_tensor(k, who, "k")) != IHIP_OK) return rc;
+    if (packed->rows > 0 && (rc = check_tensor(q, who, "q")) != IHIP_OK) return rc;
+    if (packed->rows > 0 && !lse) return fail(IHIP_ERR_INVALID_ARG, "%s: lse is NULL", who);
+    if ((rc = check_track(who, track, 0, false)) != IHIP_OK) return rc;
+    if (!(decay >= 0.f) || decay > 3.4028234e38f) return fail(IHIP_ERR_INVALID_ARG, "%s: decay = %g", who, decay);
+    if ((rc = check_sm_scale(who, sm_scale, &a.scale_log2e)) != IHIP_OK) return rc;
+    a.B = packed->B; a.Hq = packed->Hq; a.Hkv = packed->Hkv; a.G = packed->Hq / packed->Hkv;
+    a.rows_q = packed->rows; a.rows_k = rows_k; a.window = window;
+    a.cu_q = packed->cu_q; a.cu_k = cu_k ? cu_k : packed->cu_q;
+    a.q = (const uint16_t *)q.ptr; a.q_sh = q.stride_h; a.q_st = q.stride_t;
+    a.k = (const uint16_t *)k.ptr; a.k_sh = k.stride_h; a.k_st = k.stride_t;
+    a.lse = lse;
+    a.decay = decay;
+    a.before = before; a.weights = track->weights; a.weight_rows = track->rows;
+    if ((int64_t)a.rows_q * a.G > INT32_MAX - kKwRows)
+        return fail(IHIP_ERR_UNSUPPORTED, "%s: %d rows of %d heads (%d KV heads) are too many", who, a.rows_q, a.Hq, a.Hkv);
+    const KeyWeightPlan plan = key_weight_plan(*packed, rows_k, window);
+    if (plan.blocks * a.Hkv > INT32_MAX || plan.chunks > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)plan.blocks * a.Hkv);
+    const bool parts = plan.chunks > 1 && ws && !((uintptr_t)ws & 15) && ws_bytes >= plan.bytes;
+    a.chunk_tiles = parts ? plan.chunk_tiles : INT32_MAX;
+    a.chunks = parts ? plan.chunks : 1;
+    a.part = parts ? (float *)ws : nullptr;
+    const dim3 grid((uint32_t)(plan.blocks * a.Hkv), parts ? plan.chunks : 1);
+    const hipStream_t st = (hipStream_t)stream;
+    {
+        KernelTimer timer("prompt_key_weights", st);
+        hipLaunchKernelGGL(prompt_key_weights_kernel, grid, dim3(kKwThreads), 0, st, a);
+    }
+    if ((rc = check_launch(who)) != IHIP_OK || !parts) return rc;
+    KernelTimer timer("prompt_key_weights_sum", st);
+    hipLaunchKernelGGL(prompt_key_weights_sum_kernel, dim3(grid.x), dim3(kKwKeys), 0, st, a);
+    return check_launch(who);
+}
