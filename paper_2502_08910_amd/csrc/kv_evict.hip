@@ -3,10 +3,12 @@
 // Kept rows stay where they are if that is below `keep`; the i-th evicted row below `keep` is filled with the i-th kept row from behind it.
 // No row is both read and written, so all moves go at once and in any order, and a cache that drops 64 of 1,088 rows moves 64 of them.
 //
-// Two launches.  kv_evict_select_kernel, a workgroup a (sequence, KV head): the threshold is found by its digits, most significant first, in a
-// histogram of all rows and then among the rows of one bin; a row's key is its weight in an order-preserving map over its number from
-// the end, so that no two are the same and ties go to the lower row.  What is kept goes down as one bit a row, and the holes below
-// `keep` are matched to the kept rows above it by their ranks.  kv_evict_move_kernel: 64 places a wave, 16 lanes a row that moves.
+// The threshold is found by its digits, most significant first, in a histogram of all rows and then among the rows of one bin; a row's key is
+// its weight in an order-preserving map over its number from the end, so that no two are the same and ties go to the lower row.  What is
+// kept goes down as one bit a row, and the holes below `keep` are matched to the kept rows above it by their ranks.
+//   up to kHeld rows    kv_evict_select_kernel, a workgroup a (sequence, KV head), keys in LDS.  Few rows move within it.
+//   more                in chunks, one workgroup each: digits, candidates, ranks (a launch each: what all chunks have found is read by the next).
+//   many moves          kv_evict_move_kernel, 16 lanes a row, four rows of each on their way.
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>
@@ -17,8 +19,20 @@ namespace ihip {
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
 constexpr int kEvictBins = 4096, kEvictList = 4096;  // of the first digit; rows of one bin that are looked at on their own
-constexpr int kMoveThreads = 256, kMoveRows = 256;   // places of a workgroup
+constexpr int kAhead = 8;                            // rows of a thread that are on their way together
+constexpr int kHeld = 2 * kAhead * kEvictThreads;    // rows whose keys stay in LDS
+constexpr int kEvictWords = 2048;                    // words of bits in LDS, those of 131,072 rows
+constexpr int kFewMoves = 512;                       // of a (sequence, KV head): within the first kernel
+constexpr int kMoveThreads = 256, kMoveAhead = 4, kMoveRows = kMoveThreads / kRowLanes * kMoveAhead;     // places of a workgroup
+constexpr int kEvictLeast = 4096;                    // rows of a chunk
+constexpr int kEvictMostChunks = 16;                // (all of them look at the histograms of all)
+static_assert(kMoveRows == 64, "a workgroup moves into the rows of one word");
 
+// What is known of a (sequence, KV head) between launches
+struct EvictState {
+    int32_t n;                       // rows
+    uint32_t bin, need, count;       // the first digit, how many rows are kept of those that have it, how many have it
+};
 struct EvictArgs {
     int B, Hkv, max_len, keep, n_sink, n_recent;
     const int32_t *lens, *seen;
@@ -30,11 +44,17 @@ struct EvictArgs {
     int to_rows;
     int32_t *kept;                   // [P, keep]
     int32_t *new_lens;
+    EvictState *state;               // [P]
     uint64_t *bits;                  // [P, words]
+    uint2 *before;                   // [P, words]: holes and movers in front of a word
     int32_t *movers;                 // [P, most]
     int words, most;
+    int chunks;
+    uint2 *listed;                   // [P, kEvictList]: key and row of the rows with the first digit
+    uint32_t *hist;                  // [P, chunks, kEvictBins]
+    uint2 *sure;                     // [P, chunks]: rows above the first digit, below `keep` and from there on
+    bool set_lens;                   // the select kernel writes new_lens
     StoreView store;
-    int row_bytes;                   // 4-bit rows: and 4 of scales
 };
 
 // Larger is kept: protected rows before all weights, NaN behind them; -0 as +0
@@ -46,18 +66,28 @@ __device__ inline uint32_t evict_key(float w, int pos, int n_sink, int recent_fr
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-struct EvictShared {
+struct EvictDigits {
     uint32_t hist[kEvictBins];
-    uint32_t list_key[kEvictList];
-    int32_t list_row[kEvictList];
     uint32_t wave_tot[2][kEvictWaves];
     uint32_t digit, left, count, listed;
+    uint32_t sum[2];
+};
+struct EvictShared : EvictDigits {
+    union {
+        struct { uint32_t key[kEvictList]; int32_t row[kEvictList]; } list;      // while the threshold is looked for
+        struct { int32_t movers[kFewMoves], holes[kFewMoves]; } moves;           // behind that
+    };
+    uint64_t bits[kEvictWords];
+};
+struct EvictHeldShared : EvictShared {
+    uint2 before[kHeld / 64];
+    uint32_t held[kHeld];
 };
 
 // Of `bins` bins, the one from which the `need`-th largest comes: its number, what of `need` is left in it, and its rows
-__device__ inline void evict_find_bin(EvictShared &sh, int bins, uint32_t need, int tid)
+__device__ inline void evict_find_bin(EvictDigits &sh, int bins, uint32_t need)
 {
-    const int lane = tid & 63, wv = tid >> 6, per = max(1, bins / kEvictThreads);
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, per = max(1, bins / kEvictThreads);
     uint32_t h[4] = {0, 0, 0, 0}, mine = 0;          // bins in descending order: thread t has bins - 1 - per t and on
     if (per * tid < bins)
 #pragma unroll
@@ -81,169 +111,472 @@ __device__ inline void evict_find_bin(EvictShared &sh, int bins, uint32_t need, 
     }
     __syncthreads();
 }
-
-__global__ __launch_bounds__(kEvictThreads) void kv_evict_select_kernel(const EvictArgs a)
+__device__ inline void evict_clear(EvictDigits &sh, int bins)
 {
-    __shared__ EvictShared sh;
-    const int p = blockIdx.x, b = p / a.Hkv, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int n = min(max(a.lens[b], 0), a.max_len), keep = a.keep;
-    int32_t *kept = a.kept + (int64_t)p * keep;
-    const int stays = min(n, keep);
-    for (int i = tid; i < keep; i += kEvictThreads) kept[i] = i < stays ? i : -1;
-    if (n <= keep) return;
-    const float *weights = a.weights + (int64_t)p * a.rows;
-    const int32_t *positions = a.positions + (int64_t)p * a.rows;
-    const int recent_from = a.seen[b] - a.n_recent;
-    auto key_at = [&](int i) { return evict_key(weights[i], positions[i], a.n_sink, recent_from); };
-
-    // The threshold as a (key, complement of the row) pair: rows at or above it are kept.  `from` is its digits so far
-    uint32_t need = keep;
-    auto clear = [&](int bins) {
-        for (int i = tid; i < bins; i += kEvictThreads) sh.hist[i] = 0;
-        __syncthreads();
-    };
-    auto composite = [&](uint32_t key, int row) { return (uint64_t)key << 31 | (uint32_t)(0x7fffffff - row); };
-    // adds a wave's digits; the first one's like at once (rows of weight 0 are often many)
-    auto add = [&](uint32_t digit, bool on) {
-        const unsigned long long there = __ballot(on);
-        if (there == 0) return;
-        const uint32_t first = __builtin_amdgcn_readlane(digit, __builtin_ctzll(there));
-        const unsigned long long same = __ballot(on && digit == first);
-        if (on && digit != first) atomicAdd(&sh.hist[digit], 1u);
-        if (lane == __builtin_ctzll(there)) atomicAdd(&sh.hist[first], (uint32_t)__popcll(same));
-    };
-    uint64_t from = 0;
-    int shift = 63 - 12;
-    if (tid == 0) sh.listed = 0;
-    clear(kEvictBins);
-    for (int i0 = wv * 64; i0 < n; i0 += kEvictThreads) {
-        const int i = i0 + lane;
-        add(i < n ? key_at(i) >> 20 : 0, i < n);
-    }
+    for (int i = threadIdx.x; i < bins; i += kEvictThreads) sh.hist[i] = 0;
     __syncthreads();
-    evict_find_bin(sh, kEvictBins, need, tid);
-    from = (uint64_t)sh.digit << shift;
-    need = sh.left;
-    uint32_t count = sh.count;
-    uint32_t in_list = 0;
-    while (need < count && shift > 0) {              // (all of a bin: the threshold is the bin's lowest)
-        if (in_list == 0 && count <= kEvictList) {
-            in_list = count;
-            for (int i = tid; i < n; i += kEvictThreads) {
-                const uint32_t key = key_at(i);
-                if (composite(key, i) >> shift != from >> shift) continue;
-                const uint32_t at = atomicAdd(&sh.listed, 1u);
-                if (at < kEvictList) { sh.list_key[at] = key; sh.list_row[at] = i; }
+}
+// adds a wave's digits; the first one's like at once (rows of weight 0 are often many)
+__device__ inline void evict_count(EvictDigits &sh, uint32_t digit, bool on)
+{
+    const unsigned long long there = __ballot(on);
+    if (there == 0) return;
+    const uint32_t first = __builtin_amdgcn_readlane(digit, __builtin_ctzll(there));
+    const unsigned long long same = __ballot(on && digit == first);
+    if (on && digit != first) atomicAdd(&sh.hist[digit], 1u);
+    if ((threadIdx.x & 63) == __builtin_ctzll(there)) atomicAdd(&sh.hist[first], (uint32_t)__popcll(same));
+}
+// A row's key over its number from the end: 63 bits, the first digit the upper 12
+__device__ inline uint64_t evict_composite(uint32_t key, int row) { return (uint64_t)key << 31 | (uint32_t)(0x7fffffff - row); }
+constexpr int kEvictShift = 63 - 12;
+
+// The threshold: rows whose composite is at least that are kept, `need` of the `count` rows that have the digits in `from` down to bit `shift`.
+// in_list: they are all listed; otherwise for_rows(f) goes over all rows with f(key, row, there)
+template <class ForRows>
+__device__ inline uint64_t evict_threshold(EvictShared &sh, uint64_t from, uint32_t need, uint32_t count, int in_list, ForRows for_rows)
+{
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    for (int shift = kEvictShift; need < count && shift > 0;) {      // (all of a bin: the threshold is the bin's lowest)
+        const int width = min(shift, 10), low = shift - width;
+        evict_clear(sh, 1 << width);                 // (with a barrier, behind which the list is there as well)
+        auto look = [&](uint64_t c, bool on) { evict_count(sh, (uint32_t)(c >> low) & ((1u << width) - 1), on && c >> shift == from >> shift); };
+        if (in_list != 0) {
+            for (int i0 = wv * 64; i0 < in_list; i0 += kEvictThreads) {
+                const int i = min(i0 + lane, in_list - 1);
+                look(evict_composite(sh.list.key[i], sh.list.row[i]), i0 + lane < in_list);
             }
-        }
-        const int width = min(shift, 10), low = shift - width, m = in_list != 0 ? in_list : n;
-        clear(1 << width);                           // (with a barrier, behind which the list is there as well)
-        for (int i0 = wv * 64; i0 < m; i0 += kEvictThreads) {
-            const int i = i0 + lane;
-            uint64_t c = 0;
-            if (i < m) c = in_list != 0 ? composite(sh.list_key[i], sh.list_row[i]) : composite(key_at(i), i);
-            add((uint32_t)(c >> low) & ((1u << width) - 1), i < m && c >> shift == from >> shift);
+        } else {
+            for_rows([&](uint32_t key, int row, bool there) { look(evict_composite(key, row), there); });
         }
         __syncthreads();
-        evict_find_bin(sh, 1 << width, need, tid);
+        evict_find_bin(sh, 1 << width, need);
         from |= (uint64_t)sh.digit << low;
         need = sh.left;
         count = sh.count;
         shift = low;
         __syncthreads();
     }
+    return from;
+}
 
-    // one bit a row
-    uint64_t *bits = a.bits + (int64_t)p * a.words;
-    for (int i0 = wv * 64; i0 < n; i0 += kEvictThreads) {
-        const int i = i0 + lane;
-        const uint64_t word = __ballot(i < n && composite(key_at(i), i) >= from);
-        if (lane == 0) bits[i0 >> 6] = word;
-    }
-    __syncthreads();
-    // holes below `keep`, kept rows from there on, counted by their words in order
-    const int words = (n + 63) / 64, per = (words + kEvictThreads - 1) / kEvictThreads, w0 = min(tid * per, words), w1 = min(w0 + per, words);
-    auto below = [&](int w) { return keep >= 64 * w + 64 ? ~0ull : keep <= 64 * w ? 0ull : (1ull << (keep - 64 * w)) - 1; };
+// Of word w of the bits: which rows are below `keep`
+__device__ inline uint64_t evict_below(int keep, int w) { return keep - 64 * w >= 64 ? ~0ull : keep <= 64 * w ? 0ull : (1ull << (keep - 64 * w)) - 1; }
+// Ranks of words [w0, w1), bits[w - w0], of holes and movers that follow hole_at and mover_at
+__device__ inline void evict_ranks(EvictDigits &sh, const uint64_t *bits, uint2 *before, int w0, int w1, int keep, uint32_t hole_at, uint32_t mover_at)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, per = (w1 - w0 + kEvictThreads - 1) / kEvictThreads;
+    const int first = min(w0 + tid * per, w1), end = min(first + per, w1);
     uint32_t holes = 0, movers = 0;
-    for (int w = w0; w < w1; ++w) {
-        const uint64_t x = bits[w], mask = below(w);
+    for (int w = first; w < end; ++w) {
+        const uint64_t x = bits[w - w0], mask = evict_below(keep, w);
         holes += __popcll(~x & mask);
         movers += __popcll(x & ~mask);
     }
     const uint32_t holes_incl = wave_scan_u32(holes, lane), movers_incl = wave_scan_u32(movers, lane);
     if (lane == 63) { sh.wave_tot[0][wv] = holes_incl; sh.wave_tot[1][wv] = movers_incl; }
     __syncthreads();
-    uint32_t hole_at = holes_incl - holes, mover_at = movers_incl - movers;
+    hole_at += holes_incl - holes;
+    mover_at += movers_incl - movers;
     for (int w = 0; w < wv; ++w) { hole_at += sh.wave_tot[0][w]; mover_at += sh.wave_tot[1][w]; }
-    int32_t *list = a.movers + (int64_t)p * a.most;
-    for (int w = w0; w < w1; ++w)
-        for (uint64_t x = bits[w] & ~below(w); x != 0; x &= x - 1, ++mover_at)
-            if (mover_at < (uint32_t)a.most) list[mover_at] = 64 * w + __builtin_ctzll(x);
+    for (int w = first; w < end; ++w) {
+        const uint64_t x = bits[w - w0], mask = evict_below(keep, w);
+        before[w - w0] = make_uint2(hole_at, mover_at);
+        hole_at += __popcll(~x & mask);
+        mover_at += __popcll(x & ~mask);
+    }
     __syncthreads();
-    for (int w = w0; w < w1; ++w)
-        for (uint64_t x = ~bits[w] & below(w); x != 0; x &= x - 1, ++hole_at)
-            if (hole_at < (uint32_t)a.most) kept[64 * w + __builtin_ctzll(x)] = list[hole_at];
+}
+// The movers of words [w0, w1) in their places of the list
+__device__ inline void evict_movers(const uint64_t *bits, const uint2 *before, int w0, int w1, int keep, int32_t *movers, int most)
+{
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    for (int w = max(w0, keep / 64) + wv; w < w1; w += kEvictWaves) {
+        const uint64_t x = bits[w - w0] & ~evict_below(keep, w);
+        const uint32_t at = before[w - w0].y + __popcll(x & ((1ull << lane) - 1));
+        if (((x >> lane) & 1) && at < (uint32_t)most) movers[at] = 64 * w + lane;
+    }
 }
 
+// Keys of a (sequence, KV head)
+struct EvictKeys {
+    const float *weights;
+    const int32_t *positions;
+    int n_sink, recent_from;
+    __device__ EvictKeys(const EvictArgs &a, int p)
+        : weights(a.weights + (int64_t)p * a.rows), positions(a.positions + (int64_t)p * a.rows), n_sink(a.n_sink), recent_from(a.seen[p / a.Hkv] - a.n_recent) {}
+    // f(key, row, there) for rows [r0, r1): a thread has every 1024th, a wave 64 neighbours, kAhead of a thread are on their way together
+    template <class F>
+    __device__ void for_rows(int r0, int r1, F f) const
+    {
+        for (int at = r0; at < r1; at += kAhead * kEvictThreads) {
+            float w[kAhead];
+            int pos[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int row = min(at + i * kEvictThreads + (int)threadIdx.x, r1 - 1);
+                w[i] = weights[row];
+                pos[i] = positions[row];
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int row = at + i * kEvictThreads + (int)threadIdx.x;
+                if (at + i * kEvictThreads >= r1) break;
+                f(evict_key(w[i], pos[i], n_sink, recent_from), row, row < r1);
+            }
+        }
+    }
+};
+
+// Rows of a store that are copied
 template <int FORMAT>
-__global__ __launch_bounds__(kMoveThreads) void kv_evict_move_kernel(const EvictArgs a)
-{
+struct EvictRow {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     typedef typename std::conditional<FORMAT == IHIP_KV_BF16, u32x4, typename std::conditional<FORMAT == IHIP_KV_E4M3, u32x2, uint32_t>::type>::type word;
-    const int p = blockIdx.x, b = p / a.Hkv, g = p % a.Hkv, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    if (g == 0 && blockIdx.y == 0 && tid == 0) a.new_lens[b] = min(min(max(a.lens[b], 0), a.max_len), a.keep);
-    const int at = blockIdx.y * kMoveRows + wv * 64 + lane;          // (the lengths are not looked at: they may be written above)
-    const int source = at < a.keep ? a.kept[(int64_t)p * a.keep + at] : -1;
-    if (source >= 0) {
-        const int64_t from = (int64_t)p * a.rows + source, to = (int64_t)p * a.to_rows + at;
-        const float w = a.weights[from];
-        const int32_t pos = a.positions[from];
-        if (source != at || a.to_weights != a.weights) a.to_weights[to] = w;
-        if (source != at || a.to_positions != a.positions) a.to_positions[to] = pos;
+    int64_t k_to, v_to;
+    word k, v;
+    uint32_t scales;
+    bool on;
+    // one of 16 lanes of row src on its way to row dst
+    __device__ void load(const EvictArgs &a, int b, int g, int src, int dst, int l16)
+    {
+        const StoreView &s = a.store;
+        int64_t from = b, to = b, from_in = src, to_in = dst;
+        if (s.paged.block_table) {
+            const int32_t *table = s.paged.block_table + (int64_t)b * s.paged.table_stride;
+            const int in_page = (1 << s.paged.page_log2) - 1;
+            from = table[src >> s.paged.page_log2];
+            to = table[dst >> s.paged.page_log2];
+            from_in = src & in_page;
+            to_in = dst & in_page;
+        }
+        on = from >= 0 && to >= 0;
+        if (!on) return;
+        const int64_t k_from = from * s.k_sb + g * s.k_sh + from_in * s.k_st, v_from = from * s.v_sb + g * s.v_sh + from_in * s.v_st;
+        k_to = to * s.k_sb + g * s.k_sh + to_in * s.k_st;
+        v_to = to * s.v_sb + g * s.v_sh + to_in * s.v_st;
+        k = reinterpret_cast<const word *>(s.k + k_from)[l16];
+        v = reinterpret_cast<const word *>(s.v + v_from)[l16];
+        if (FORMAT == IHIP_KV_MX4 && l16 < 2) scales = *reinterpret_cast<const uint32_t *>(l16 == 0 ? s.ks + k_from / 16 : s.vs + v_from / 16);
     }
-    // rows, four at a time
-    const int32_t *table = a.store.paged.block_table ? a.store.paged.block_table + (int64_t)b * a.store.paged.table_stride : nullptr;
-    auto row_of = [&](int row, int64_t sb, int64_t sh, int64_t st) {
-        int64_t first = b, in_page = row;
-        if (table) {
-            first = table[row >> a.store.paged.page_log2];
-            in_page = row & ((1 << a.store.paged.page_log2) - 1);
-        }
-        return first < 0 ? (int64_t)-1 : first * sb + g * sh + in_page * st;
-    };
-    const int l16 = lane & 15, quarter = lane >> 4;
-    for (unsigned long long left = __ballot(source >= 0 && source != at); left != 0;) {
-        unsigned long long mine = left;
-        for (int i = 0; i < quarter; ++i) mine &= mine - 1;
-        const bool on = mine != 0;
-        const int which = on ? __builtin_ctzll(mine) : 0;
-        const int src = __shfl(source, which, 64), dst = __shfl(at, which, 64);
-        if (on) {
-            const int64_t ks = row_of(src, a.store.k_sb, a.store.k_sh, a.store.k_st), kd = row_of(dst, a.store.k_sb, a.store.k_sh, a.store.k_st);
-            const int64_t vs = row_of(src, a.store.v_sb, a.store.v_sh, a.store.v_st), vd = row_of(dst, a.store.v_sb, a.store.v_sh, a.store.v_st);
-            if (ks != -1 && kd != -1) {
-                const word x = reinterpret_cast<const word *>(a.store.k + ks)[l16], y = reinterpret_cast<const word *>(a.store.v + vs)[l16];
-                reinterpret_cast<word *>(a.store.k + kd)[l16] = x;
-                reinterpret_cast<word *>(a.store.v + vd)[l16] = y;
-                if (FORMAT == IHIP_KV_MX4 && l16 < 2) {
-                    if (l16 == 0) *reinterpret_cast<uint32_t *>(a.store.ks + kd / 16) = *reinterpret_cast<const uint32_t *>(a.store.ks + ks / 16);
-                    else *reinterpret_cast<uint32_t *>(a.store.vs + vd / 16) = *reinterpret_cast<const uint32_t *>(a.store.vs + vs / 16);
-                }
+    __device__ void store(const EvictArgs &a, int l16) const
+    {
+        if (!on) return;
+        reinterpret_cast<word *>(a.store.k + k_to)[l16] = k;
+        reinterpret_cast<word *>(a.store.v + v_to)[l16] = v;
+        if (FORMAT == IHIP_KV_MX4 && l16 < 2) *reinterpret_cast<uint32_t *>(l16 == 0 ? a.store.ks + k_to / 16 : a.store.vs + v_to / 16) = scales;
+    }
+};
+__device__ inline void evict_beside(const EvictArgs &a, int p, int source, int at)       // weight and position of a place
+{
+    const int64_t from = (int64_t)p * a.rows + source, to = (int64_t)p * a.to_rows + at;
+    if (source != at || a.to_weights != a.weights) a.to_weights[to] = a.weights[from];
+    if (source != at || a.to_positions != a.positions) a.to_positions[to] = a.positions[from];
+}
+__device__ inline int evict_len(const EvictArgs &a, int b) { return min(max(a.lens[b], 0), a.max_len); }
+
+// FORMAT: that of the rows that are moved here, -1: none are
+template <int FORMAT>
+__global__ __launch_bounds__(kEvictThreads) void kv_evict_select_kernel(const EvictArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    EvictHeldShared &sh = *reinterpret_cast<EvictHeldShared *>(smem);
+    const int p = blockIdx.x, b = p / a.Hkv, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int n = evict_len(a, b), keep = a.keep;
+    if (a.set_lens && p % a.Hkv == 0 && tid == 0) a.new_lens[b] = min(n, keep);
+    if (FORMAT < 0 && tid == 0) a.state[p].n = n;
+    int32_t *kept = a.kept + (int64_t)p * keep;
+    if (n <= keep) {
+        if (FORMAT >= 0)
+            for (int i = tid; i < keep; i += kEvictThreads) {
+                kept[i] = i < n ? i : -1;
+                if (i < n) evict_beside(a, p, i, i);
             }
+        return;
+    }
+    if (tid == 0) sh.listed = 0;
+    evict_clear(sh, kEvictBins);
+    EvictKeys(a, p).for_rows(0, n, [&](uint32_t key, int row, bool there) {
+        evict_count(sh, key >> 20, there);
+        sh.held[row] = key;
+    });
+    __syncthreads();
+    evict_find_bin(sh, kEvictBins, keep);
+    const uint32_t bin = sh.digit, need = sh.left, count = sh.count;
+    auto for_rows = [&](auto f) {
+        for (int row0 = wv * 64; row0 < n; row0 += kEvictThreads) f(sh.held[row0 + lane], row0 + lane, row0 + lane < n);
+    };
+    const int words = (n + 63) / 64, in_list = need < count && count <= kEvictList ? count : 0;
+    for_rows([&](uint32_t key, int row, bool there) {        // those above the bin are kept, the bin's listed
+        const uint64_t word = __ballot(there && key >> 20 > bin);
+        if (lane == 0) sh.bits[row >> 6] = word;
+        if (in_list != 0 && there && key >> 20 == bin) {
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            sh.list.key[at] = key;
+            sh.list.row[at] = row;
         }
-        for (int i = 0; i < 4; ++i) left &= left - 1;
+    });
+    const uint64_t from = evict_threshold(sh, (uint64_t)bin << kEvictShift, need, count, in_list, for_rows);
+    __syncthreads();
+    if (in_list != 0) {
+        for (int i = tid; i < in_list; i += kEvictThreads) {
+            const int row = sh.list.row[i];
+            if (evict_composite(sh.list.key[i], row) >= from) atomicOr(reinterpret_cast<uint32_t *>(sh.bits) + (row >> 5), 1u << (row & 31));
+        }
+    } else {
+        for_rows([&](uint32_t key, int row, bool there) {
+            const uint64_t word = __ballot(there && evict_composite(key, row) >= from);
+            if (lane == 0) sh.bits[row >> 6] = word;
+        });
+    }
+    __syncthreads();
+    evict_ranks(sh, sh.bits, sh.before, 0, words, keep, 0, 0);
+    if constexpr (FORMAT < 0) {
+        for (int w = tid; w < words; w += kEvictThreads) {
+            a.bits[(int64_t)p * a.words + w] = sh.bits[w];
+            a.before[(int64_t)p * a.words + w] = sh.before[w];
+        }
+        evict_movers(sh.bits, sh.before, 0, words, keep, a.movers + (int64_t)p * a.most, a.most);
+    } else {
+        evict_movers(sh.bits, sh.before, 0, words, keep, sh.moves.movers, kFewMoves);
+        __syncthreads();
+        for (int w = wv; 64 * w < keep; w += kEvictWaves) {
+            const uint64_t x = ~sh.bits[w];
+            const int row = 64 * w + lane;
+            if (row >= keep) continue;
+            const uint32_t at = sh.before[w].x + __popcll(x & ((1ull << lane) - 1));
+            const bool hole = ((x >> lane) & 1) && at < (uint32_t)kFewMoves;
+            const int source = hole ? sh.moves.movers[at] : row;
+            kept[row] = source;
+            evict_beside(a, p, source, row);
+            if (hole) sh.moves.holes[at] = row;
+        }
+        __syncthreads();
+        const int last = (keep - 1) / 64, l16 = tid & 15, grp = tid >> 4;
+        const int moves = min((int)(sh.before[last].x + __popcll(~sh.bits[last] & evict_below(keep, last))), kFewMoves);
+        for (int i0 = grp; i0 < moves; i0 += kEvictThreads / kRowLanes * kMoveAhead) {
+            EvictRow<FORMAT> row[kMoveAhead];
+#pragma unroll
+            for (int i = 0; i < kMoveAhead; ++i) {
+                const int at = i0 + i * (kEvictThreads / kRowLanes);
+                row[i].on = false;
+                if (at < moves) row[i].load(a, b, p % a.Hkv, sh.moves.movers[at], sh.moves.holes[at], l16);
+            }
+#pragma unroll
+            for (int i = 0; i < kMoveAhead; ++i) row[i].store(a, l16);
+        }
     }
 }
 
-struct EvictPlan { int64_t words, most; size_t bytes; };
+// ---- in chunks -----------------------------------------------------------------
+// Rows of chunk c of n rows: whole words
+__device__ inline int evict_chunk(const EvictArgs &a, int n, int c)
+{
+    const int64_t size = (((int64_t)n + a.chunks - 1) / a.chunks + 63) & ~63ll;
+    return (int)min(c * size, (int64_t)n);
+}
+
+// How many of a chunk's rows have which first digit
+__global__ __launch_bounds__(kEvictThreads) void kv_evict_digits_kernel(const EvictArgs a)
+{
+    __shared__ __attribute__((aligned(16))) EvictDigits sh;
+    const int p = blockIdx.x, c = blockIdx.y, tid = threadIdx.x, n = evict_len(a, p / a.Hkv);
+    if (c == 0 && tid == 0) a.state[p].n = n;
+    if (n <= a.keep) return;
+    evict_clear(sh, kEvictBins);
+    EvictKeys(a, p).for_rows(evict_chunk(a, n, c), evict_chunk(a, n, c + 1), [&](uint32_t key, int, bool there) { evict_count(sh, key >> 20, there); });
+    __syncthreads();
+    reinterpret_cast<uint4 *>(a.hist + ((int64_t)p * a.chunks + c) * kEvictBins)[tid] = reinterpret_cast<const uint4 *>(sh.hist)[tid];
+}
+static_assert(kEvictBins == 4 * kEvictThreads, "");
+
+// The threshold's first digit; rows above it are kept, those that have it are listed, each chunk's in its place
+__global__ __launch_bounds__(kEvictThreads) void kv_evict_candidates_kernel(const EvictArgs a)
+{
+    __shared__ __attribute__((aligned(16))) EvictDigits sh;
+    const int p = blockIdx.x, c = blockIdx.y, tid = threadIdx.x, lane = tid & 63, n = a.state[p].n, keep = a.keep;
+    if (n <= keep) return;
+    const uint32_t *hist = a.hist + (int64_t)p * a.chunks * kEvictBins;
+    uint4 all = make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < a.chunks; ++i) {
+        const uint4 x = reinterpret_cast<const uint4 *>(hist + (int64_t)i * kEvictBins)[tid];
+        all = make_uint4(all.x + x.x, all.y + x.y, all.z + x.z, all.w + x.w);
+    }
+    reinterpret_cast<uint4 *>(sh.hist)[tid] = all;
+    if (tid == 0) sh.listed = sh.sum[0] = sh.sum[1] = 0;
+    __syncthreads();
+    evict_find_bin(sh, kEvictBins, keep);
+    const uint32_t bin = sh.digit, need = sh.left, count = sh.count;
+    if (c == 0 && tid == 0) {
+        a.state[p].bin = bin;
+        a.state[p].need = need;
+        a.state[p].count = count;
+    }
+    const bool list = need < count && count <= kEvictList;
+    uint32_t at0 = 0;
+    if (list)
+        for (int i = lane; i < c; i += 64) at0 += hist[(int64_t)i * kEvictBins + bin];
+    at0 = wave_sum_u32(at0);
+    uint64_t *bits = a.bits + (int64_t)p * a.words;
+    uint2 *listed = a.listed + (int64_t)p * kEvictList;
+    uint32_t below = 0, beyond = 0;                  // of this wave
+    EvictKeys(a, p).for_rows(evict_chunk(a, n, c), evict_chunk(a, n, c + 1), [&](uint32_t key, int row, bool there) {
+        // (a bin that is kept whole goes with those above it)
+        const uint64_t word = __ballot(there && (key >> 20 > bin || (need == count && key >> 20 == bin)));
+        if (lane == 0 && there) {
+            bits[row >> 6] = word;
+            const uint64_t mask = evict_below(keep, row >> 6);
+            below += __popcll(word & mask);
+            beyond += __popcll(word & ~mask);
+        }
+        if (list && there && key >> 20 == bin) {
+            const uint32_t at = at0 + atomicAdd(&sh.listed, 1u);
+            if (at < kEvictList) listed[at] = make_uint2(key, row);
+        }
+    });
+    if (lane == 0) {
+        atomicAdd(&sh.sum[0], below);
+        atomicAdd(&sh.sum[1], beyond);
+    }
+    __syncthreads();
+    if (tid == 0) a.sure[(int64_t)p * a.chunks + c] = make_uint2(sh.sum[0], sh.sum[1]);
+}
+
+// The whole threshold; a chunk's bits, the ranks of its holes and movers, and its movers in their places
+__global__ __launch_bounds__(kEvictThreads) void kv_evict_ranks_kernel(const EvictArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    EvictShared &sh = *reinterpret_cast<EvictShared *>(smem);
+    const int p = blockIdx.x, c = blockIdx.y, tid = threadIdx.x, lane = tid & 63, keep = a.keep;
+    const EvictState state = a.state[p];
+    const int n = state.n;
+    if (n <= keep) return;
+    const int r0 = evict_chunk(a, n, c), r1 = evict_chunk(a, n, c + 1), w0 = r0 / 64, w1 = (r1 + 63) / 64;
+    if (r0 >= r1) return;
+    const int in_list = state.need < state.count && state.count <= kEvictList ? state.count : 0;
+    const uint2 *listed = a.listed + (int64_t)p * kEvictList;
+    for (int i = tid; i < in_list; i += kEvictThreads) {
+        const uint2 x = listed[i];
+        sh.list.key[i] = x.x;
+        sh.list.row[i] = x.y;
+    }
+    uint64_t *bits = a.bits + (int64_t)p * a.words;
+    for (int w = w0 + tid; w < w1; w += kEvictThreads) sh.bits[w - w0] = bits[w];
+    // kept rows in front of the chunk, below `keep` and from there on
+    uint32_t below = 0, beyond = 0;
+    for (int i = tid; i < c; i += kEvictThreads) {
+        const uint2 x = a.sure[(int64_t)p * a.chunks + i];
+        below += x.x;
+        beyond += x.y;
+    }
+    if (tid == 0) sh.sum[0] = sh.sum[1] = 0;
+    const EvictKeys keys(a, p);
+    const uint64_t from = evict_threshold(sh, (uint64_t)state.bin << kEvictShift, state.need, state.count, in_list, [&](auto f) { keys.for_rows(0, n, f); });
+    __syncthreads();
+    if (in_list != 0) {
+        for (int i = tid; i < in_list; i += kEvictThreads) {
+            const int row = sh.list.row[i];
+            if (evict_composite(sh.list.key[i], row) < from) continue;
+            if (row < r0) (row < keep ? below : beyond) += 1;
+            else if (row < r1) atomicOr(reinterpret_cast<uint32_t *>(sh.bits) + ((row - r0) >> 5), 1u << (row & 31));
+        }
+    } else if (state.need < state.count) {           // more rows than are listed: all are looked at again
+        below = beyond = 0;
+        keys.for_rows(0, r1, [&](uint32_t key, int row, bool there) {
+            const bool on = there && evict_composite(key, row) >= from;
+            if (on && row < r0) (row < keep ? below : beyond) += 1;
+            const uint64_t word = __ballot(on);
+            if (lane == 0 && row >= r0 && row < r1) sh.bits[(row - r0) >> 6] = word;
+        });
+    }
+    below = wave_sum_u32(below);
+    beyond = wave_sum_u32(beyond);
+    if (lane == 0) {
+        atomicAdd(&sh.sum[0], below);
+        atomicAdd(&sh.sum[1], beyond);
+    }
+    __syncthreads();
+    for (int w = w0 + tid; w < w1; w += kEvictThreads) bits[w] = sh.bits[w - w0];
+    uint2 *before = a.before + (int64_t)p * a.words + w0;
+    evict_ranks(sh, sh.bits, before, w0, w1, keep, min(r0, keep) - sh.sum[0], sh.sum[1]);
+    evict_movers(sh.bits, before, w0, w1, keep, a.movers + (int64_t)p * a.most, a.most);
+}
+
+// The 64 rows of a word of bits
+template <int FORMAT>
+__global__ __launch_bounds__(kMoveThreads) void kv_evict_move_kernel(const EvictArgs a)
+{
+    __shared__ int sh_source[kMoveRows];
+    const int p = blockIdx.x, b = p / a.Hkv, g = p % a.Hkv, w = blockIdx.y, tid = threadIdx.x, l16 = tid & 15, grp = tid >> 4;
+    if (g == 0 && w == 0 && tid == 0) a.new_lens[b] = min(evict_len(a, b), a.keep);
+    const int n = a.state[p].n;                      // (the lengths are not looked at: they may be written above)
+    if (tid < kMoveRows) {
+        const int at = w * kMoveRows + tid;
+        int source = at < n && at < a.keep ? at : -1;
+        if (n > a.keep && source >= 0) {
+            const uint64_t x = ~a.bits[(int64_t)p * a.words + w];
+            const uint32_t rank = a.before[(int64_t)p * a.words + w].x + __popcll(x & ((1ull << tid) - 1));
+            if (((x >> tid) & 1) && rank < (uint32_t)a.most) source = a.movers[(int64_t)p * a.most + rank];
+        }
+        sh_source[tid] = source;
+        if (at < a.keep) a.kept[(int64_t)p * a.keep + at] = source;
+        if (source >= 0) evict_beside(a, p, source, at);
+    }
+    __syncthreads();
+    EvictRow<FORMAT> row[kMoveAhead];
+#pragma unroll
+    for (int i = 0; i < kMoveAhead; ++i) {
+        const int in_word = grp * kMoveAhead + i, at = w * kMoveRows + in_word, source = sh_source[in_word];
+        row[i].on = false;
+        if (source >= 0 && source != at) row[i].load(a, b, g, source, at, l16);
+    }
+#pragma unroll
+    for (int i = 0; i < kMoveAhead; ++i) row[i].store(a, l16);
+}
+
+__global__ __launch_bounds__(kMoveThreads) void kv_evict_lens_kernel(const EvictArgs a)
+{
+    const int b = blockIdx.x * kMoveThreads + threadIdx.x;
+    if (b < a.B) a.new_lens[b] = min(evict_len(a, b), a.keep);
+}
+
+struct EvictPlan {
+    bool few, chunked;
+    int64_t words, most, chunks;
+    size_t bytes, listed, hist, sure, state, bits, before, movers;   // all of scratch, and where in it
+};
 static EvictPlan evict_plan(int64_t B, int64_t Hkv, int64_t max_len, int64_t keep)
 {
-    EvictPlan r;
+    const int64_t P = B * Hkv;
+    EvictPlan r{};
     r.words = (max_len + 63) / 64;
     r.most = std::max<int64_t>(0, std::min(keep, max_len - keep));
-    r.bytes = (size_t)(B * Hkv) * (r.words * sizeof(uint64_t) + r.most * sizeof(int32_t));
+    r.chunked = r.most > 0 && max_len > kHeld;
+    r.few = !r.chunked && r.most <= kFewMoves;
+    // as many workgroups as there are compute units, of kEvictLeast rows or more; a chunk's bits are in LDS
+    r.chunks = std::max<int64_t>({std::min<int64_t>({kEvictMostChunks, max_len / kEvictLeast, compute_units() / std::max<int64_t>(P, 1)}), r.words / (kEvictWords - 1) + 1, 2});
+    auto take = [&](size_t bytes) {
+        const size_t at = r.bytes;
+        r.bytes += (bytes + 15) / 16 * 16;
+        return at;
+    };
+    if (r.few) return r;
+    r.state = take(P * sizeof(EvictState));
+    r.bits = take(P * r.words * sizeof(uint64_t));
+    r.before = take(P * r.words * sizeof(uint2));
+    r.movers = take(P * r.most * sizeof(int32_t));
+    if (!r.chunked) return r;
+    r.listed = take(P * kEvictList * sizeof(uint2));
+    r.sure = take(P * r.chunks * sizeof(uint2));
+    r.hist = take(P * r.chunks * kEvictBins * sizeof(uint32_t));
     return r;
+}
+// (dynamic LDS beyond the 64 KiB that need no leave)
+template <class Kernel>
+static void launch_evict(Kernel *kernel, dim3 grid, size_t lds, hipStream_t st, const EvictArgs &a)
+{
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    hipLaunchKernelGGL(kernel, grid, dim3(kEvictThreads), lds, st, a);
 }
 static int32_t check_evict(const char *who, int32_t B, int32_t Hkv, int32_t d, int32_t max_seq_len, int32_t keep)
 {
@@ -288,7 +621,7 @@ extern "C" int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track
     if (Hkv > 1 && (std::abs(a.store.k_sh) < row || std::abs(a.store.v_sh) < row))
         return fail(IHIP_ERR_INVALID_ARG, "%s: the heads of the store overlap", who);
     const EvictPlan plan = evict_plan(B, Hkv, max_seq_len, keep);
-    if (!ws || ((uintptr_t)ws & 15) || ws_bytes < plan.bytes)
+    if (plan.bytes > 0 && (!ws || ((uintptr_t)ws & 15) || ws_bytes < plan.bytes))
         return fail(IHIP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 16-byte aligned, needed, %zu given", who, plan.bytes, ws_bytes);
     const int64_t P = (int64_t)B * Hkv, moves = ((int64_t)keep - 1) / kMoveRows + 1;
     if (P > INT32_MAX / kEvictThreads || moves > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: B * Hkv = %lld, keep = %d are too large", who, (long long)P, keep);
@@ -297,14 +630,47 @@ extern "C" int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track
     a.weights = track->weights; a.positions = track->positions; a.rows = track->rows;
     a.to_weights = to->weights; a.to_positions = to->positions; a.to_rows = to->rows;
     a.kept = kept; a.new_lens = new_lens;
-    a.bits = (uint64_t *)ws; a.words = (int)plan.words; a.most = (int)plan.most;
-    a.movers = (int32_t *)(a.bits + P * plan.words);
+    uint8_t *const scratch = (uint8_t *)ws;
+    a.words = (int)plan.words; a.most = (int)plan.most; a.chunks = (int)plan.chunks;
+    a.state = (EvictState *)(scratch + plan.state);
+    a.bits = (uint64_t *)(scratch + plan.bits);
+    a.before = (uint2 *)(scratch + plan.before);
+    a.movers = (int32_t *)(scratch + plan.movers);
+    a.listed = (uint2 *)(scratch + plan.listed);
+    a.sure = (uint2 *)(scratch + plan.sure);
+    a.hist = (uint32_t *)(scratch + plan.hist);
     const hipStream_t st = (hipStream_t)stream;
-    {
+    // lengths that are read by one workgroup are not written by another of the same launch
+    const uintptr_t lens_at = (uintptr_t)seq_lens, new_at = (uintptr_t)new_lens, lens_bytes = B * sizeof(int32_t);
+    a.set_lens = plan.few && (new_at + lens_bytes <= lens_at || lens_at + lens_bytes <= new_at);
+    if (!plan.chunked) {
         KernelTimer timer("kv_evict_select", st);
-        hipLaunchKernelGGL(kv_evict_select_kernel, dim3((uint32_t)P), dim3(kEvictThreads), 0, st, a);
+        const dim3 grid((uint32_t)P);
+        if (!plan.few) launch_evict(kv_evict_select_kernel<-1>, grid, sizeof(EvictHeldShared), st, a);
+        else if (store->format == IHIP_KV_BF16) launch_evict(kv_evict_select_kernel<IHIP_KV_BF16>, grid, sizeof(EvictHeldShared), st, a);
+        else if (store->format == IHIP_KV_E4M3) launch_evict(kv_evict_select_kernel<IHIP_KV_E4M3>, grid, sizeof(EvictHeldShared), st, a);
+        else launch_evict(kv_evict_select_kernel<IHIP_KV_MX4>, grid, sizeof(EvictHeldShared), st, a);
+    } else {
+        const dim3 grid((uint32_t)P, (uint32_t)plan.chunks);
+        {
+            KernelTimer timer("kv_evict_digits", st);
+            hipLaunchKernelGGL(kv_evict_digits_kernel, grid, dim3(kEvictThreads), 0, st, a);
+        }
+        if ((rc = check_launch(who)) != IHIP_OK) return rc;
+        {
+            KernelTimer timer("kv_evict_candidates", st);
+            hipLaunchKernelGGL(kv_evict_candidates_kernel, grid, dim3(kEvictThreads), 0, st, a);
+        }
+        if ((rc = check_launch(who)) != IHIP_OK) return rc;
+        KernelTimer timer("kv_evict_ranks", st);
+        launch_evict(kv_evict_ranks_kernel, grid, sizeof(EvictShared), st, a);
     }
-    if ((rc = check_launch(who)) != IHIP_OK) return rc;
+    if ((rc = check_launch(who)) != IHIP_OK || a.set_lens) return rc;
+    if (plan.few) {
+        KernelTimer timer("kv_evict_lens", st);
+        hipLaunchKernelGGL(kv_evict_lens_kernel, dim3((B - 1) / kMoveThreads + 1), dim3(kMoveThreads), 0, st, a);
+        return check_launch(who);
+    }
     KernelTimer timer("kv_evict_move", st);
     const dim3 grid((uint32_t)P, (uint32_t)moves);
     if (store->format == IHIP_KV_BF16) hipLaunchKernelGGL(kv_evict_move_kernel<IHIP_KV_BF16>, grid, dim3(kMoveThreads), 0, st, a);

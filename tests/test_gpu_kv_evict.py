@@ -91,7 +91,7 @@ def test_evict(ihip, fmt, page, Hkv, lens, keep, n_sink, n_recent, token_major):
 
 
 @pytest.mark.parametrize("kind", ["few", "zero", "close", "odd"])
-@pytest.mark.parametrize("n,keep", [(90, 20), (4500, 1100), (4500, 4400), (9000, 17), (12345, 5000)])
+@pytest.mark.parametrize("n,keep", [(90, 20), (4500, 1100), (4500, 4400), (9000, 17), (12345, 5000), (20001, 7000), (33000, 100), (33000, 32990)])
 def test_weights_that_tie(ihip, kind, n, keep):
     """Equal weights, all in one bin of the histogram (more than are listed at once too), not finite, negative, tiny."""
     c = Cache(ihip, "mx4", [n, n - 1], 1, 0, seed=n)

@@ -133,9 +133,11 @@ def test_evict_refuses(b):  # noqa: F811
     t = b.Tensor(4096, 8192, 64, 128)
     assert evict(b, store=store_of(b, 0, k=t, v=t)) == BAD and b"heads of the store overlap" in L.ihip_last_error()
     assert evict(b, store=store_of(b, 2, k_scales=None)) == BAD
-    need = L.ihip_kv_evict_workspace_bytes(2, 2, 64, 16)
-    assert need == 2 * 2 * (8 + 16 * 4) and evict(b, ws_bytes=need - 1) == WORKSPACE
-    assert evict(b, ws=None) == WORKSPACE and evict(b, ws=4104) == WORKSPACE and evict(b, ws_bytes=0) == WORKSPACE
+    for rows in (4096, 50000):                        # many rows that move; rows in chunks
+        need = L.ihip_kv_evict_workspace_bytes(2, 2, rows, 1024)
+        big = dict(max_len=rows, keep=1024, track=track_of(b, rows=rows))
+        assert need > 256 and evict(b, ws_bytes=need - 1, **big) == WORKSPACE
+        assert evict(b, ws=None, **big) == WORKSPACE and evict(b, ws=4104, **big) == WORKSPACE and evict(b, ws_bytes=0, **big) == WORKSPACE
     assert evict(b, keep=1 << 30, max_len=64, B=1) == UNSUPPORTED
     assert L.ihip_kv_evict_workspace_bytes(2, 2, 64, 0) == 0 and L.ihip_kv_evict_workspace_bytes(2, 0, 64, 1) == 0
     assert evict(b, B=0, track=None, lens=None, kept=None) == 0
