@@ -9,6 +9,7 @@
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace ihip {
 
@@ -32,6 +33,7 @@ struct KeyWeightArgs {
     int weight_rows;
     int chunk_tiles, chunks;         // tiles of a chunk, from the sequence's end; chunks that a sequence can have
     float *part;                     // [chunk, Hkv, rows_k], or null: one chunk
+    bool near;                       // G divides a tile's rows, whose queries are less than 2^31 bytes apart
 };
 
 // A sequence, and the tiles of its rows that count
@@ -62,11 +64,18 @@ __device__ inline int key_block_seq(const KeyWeightArgs &a, int id, int lane)
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
+// 16 bytes a lane from a scalar base and the lane's byte offset to the LDS byte address dst + 16 l (counts on vmcnt).  M0 is left as it is:
+// nothing else in this kernel reads it, and it is not the compiler's to keep values in.
+__device__ inline void key_weights_to_lds(uint32_t dst, const uint16_t *base, uint32_t byte_off)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(byte_off), "s"(base) : "memory");
+}
+
 __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const KeyWeightArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint16_t sh_q[2][kKwRows * kD];
-    __shared__ __attribute__((aligned(16))) float sh_r[2][kKwRows];          // of a tile's rows: r, and the last key
-    __shared__ __attribute__((aligned(16))) int sh_last[2][kKwRows];
+    __shared__ __attribute__((aligned(16))) float sh_r[3][kKwRows];          // of a tile's rows: r, and the last key
+    __shared__ __attribute__((aligned(16))) int sh_last[3][kKwRows];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int g = blockIdx.x % a.Hkv, id = blockIdx.x / a.Hkv;
@@ -88,81 +97,163 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const
         for (int ks = 0; ks < 8; ++ks) kb[s][ks] = *reinterpret_cast<const bf16x8 *>(kp + ks * 16);
     }
 
-    auto request = [&](int t, int st) {              // 4-row pieces of a tile, dealt to the waves
-        const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)&sh_q[st][0];
+    // A thread's rows of a tile, of which it brings 16-byte pieces, and another one, whose r it brings.  The next tile's are 64 rows less: addresses go on
+    // by differences (multiplications take four times as long as additions)
+    constexpr int kPieces = kKwRows / (4 * kKwWaves);
+    const int per_tile = kKwRows / a.G, heads_left = kKwRows % a.G, last_row = seq.row0 + (end - 1) * kKwRows;       // of the first tile, its first
+    const int64_t q_step = per_tile * a.q_st + heads_left * a.q_sh, q_wrap = a.G * a.q_sh - a.q_st;
+    const int r_step = per_tile * a.Hq + heads_left, r_wrap = a.G - a.Hq;
+    const uint16_t *const qb = a.q + (int64_t)seq.q_first * a.q_st + (int64_t)g * a.G * a.q_sh;
+    const float *const lse = a.lse + (int64_t)seq.q_first * a.Hq + g * a.G;
+    auto in_tile = [&](int i) { return 4 * (wave + i * kKwWaves) + (lane >> 4); };
+    auto q_of = [&](int query, int head, int i) { return qb + query * a.q_st + head * a.q_sh + (((lane & 15) ^ (in_tile(i) & 15)) << 3); };
+    const uint16_t *q_at[kPieces];
+    int q_head[kPieces];
 #pragma unroll
-        for (int i = 0; i < kKwRows / (4 * kKwWaves); ++i) {
-            const int piece = wave + i * kKwWaves, in_tile = 4 * piece + (lane >> 4);
-            const int row = min(seq.row0 + t * kKwRows + in_tile, seq.rows - 1), query = row / a.G;
-            const uint16_t *src = a.q + (int64_t)(seq.q_first + query) * a.q_st + (g * a.G + row - query * a.G) * a.q_sh + (((lane & 15) ^ (in_tile & 15)) << 3);
-            global_to_lds(lds0 + piece * 4 * kD * 2, src);
+    for (int i = 0; i < kPieces; ++i) {
+        const int row = last_row + in_tile(i), query = row / a.G;
+        q_head[i] = row - query * a.G;
+        q_at[i] = q_of(query, q_head[i], i);
+    }
+    int r_query = (last_row + (tid & (kKwRows - 1))) / a.G, r_head = last_row + (tid & (kKwRows - 1)) - r_query * a.G;
+    const float *r_at = lse + (int64_t)r_query * a.Hq + r_head;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)&sh_q[0][0] + wave * 4 * kD * 2;
+    auto stage_of = [&](int st, int i) { return lds0 + (st * kKwRows + i * 4 * kKwWaves) * kD * 2; };
+    auto send = [&](int st, int i, const uint16_t *from) { global_to_lds(stage_of(st, i), from); };
+    // where the heads of a query share tiles alike and are not far apart, addresses are a scalar and a lane's offset that stays
+    const uint16_t *q_base = qb + (int64_t)(last_row / a.G) * a.q_st;
+    uint32_t q_off[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) q_off[i] = (uint32_t)((const uint8_t *)q_at[i] - (const uint8_t *)q_base);
+    auto request = [&](int st) {                     // the next tile
+        if (a.near) {
+            q_base -= q_step;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) key_weights_to_lds(stage_of(st, i), q_base, q_off[i]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            q_at[i] -= q_step;
+            q_head[i] -= heads_left;
+            if (q_head[i] < 0) { q_head[i] += a.G; q_at[i] += q_wrap; }
+            send(st, i, q_at[i]);
         }
     };
-    auto row_info = [&](int t, float &r, int &last) {        // of row tid of the tile
-        const int row = seq.row0 + t * kKwRows + tid, at = min(row, seq.rows - 1), query = at / a.G;
-        r = a.lse[(int64_t)(seq.q_first + query) * a.Hq + g * a.G + at - query * a.G] * 1.44269504088896340736f;
-        last = row < seq.rows ? query + seq.ahead : -1;
+    auto row_info = [&](float &r, int &last) {
+        r_at -= r_step;
+        r_query -= per_tile;
+        r_head -= heads_left;
+        if (r_head < 0) { r_head += a.G; --r_query; r_at += r_wrap; }
+        r = *r_at;
+        last = r_query + seq.ahead;
     };
 
+    // the keys are waited for here: in the loop the compiler, which does not know what has been waited for in assembly, would wait for all loads at their use
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(kb[s][ks]));
+
     float sum[2] = {0.f, 0.f}, near_sum[2] = {0.f, 0.f};
-    if (t0 < end) {
-        request(end - 1, 0);
-        if (tid < kKwRows) row_info(end - 1, sh_r[0][tid], sh_last[0][tid]);
+    if (t0 < end) {                                  // the first tile: rows behind the last one stand for that one
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) send(0, i, last_row + in_tile(i) < seq.rows ? q_at[i] : q_of(seq.nq - 1, a.G - 1, i));
+        if (tid < kKwRows) {
+            const bool there = last_row + tid < seq.rows;
+            sh_r[0][tid] = (there ? *r_at : lse[(int64_t)(seq.nq - 1) * a.Hq + a.G - 1]) * 1.44269504088896340736f;
+            sh_last[0][tid] = there ? r_query + seq.ahead : -1;
+        }
     }
+    // Half a tile at a time: the products of 32 rows with the wave's keys, and between them, two scores after each, the exponentials of the half
+    // before.  Score i is that of row 8 (i / 4) + 4 half + i % 4.
+    f32x16 c[2][2];                                  // of the present and the previous half
+    auto operand = [&](int st, int h, int ks) { return *reinterpret_cast<const bf16x8 *>(&sh_q[st][(32 * h + n) * kD + (((ks * 2 + half) ^ (n & 15)) << 3)]); };
+    float part_sum[2];
+    auto exponentials = [&](int h, int st3, int i, auto masked, const float4 &r4) {
+        const float r = i % 4 == 0 ? r4.x : i % 4 == 1 ? r4.y : i % 4 == 2 ? r4.z : r4.w;
+        int last = 0;
+        if constexpr (decltype(masked)::value) last = sh_last[st3][32 * h + 8 * (i / 4) + 4 * half + i % 4];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            float w = __builtin_amdgcn_exp2f(fmaf(c[h][s][i], a.scale_log2e, -r));
+            if constexpr (decltype(masked)::value) w = kw + 32 * s + n <= last ? w : 0.f;
+            part_sum[s] = i == 0 ? w : part_sum[s] + w;
+            if (i == 15) near_sum[s] += part_sum[s];
+        }
+    };
+    auto rows_r = [&](int h, int st3, int i4) { return *reinterpret_cast<const float4 *>(&sh_r[st3][32 * h + 8 * i4 + 4 * half]); };
+    // products of half h of the tile in stage st, exponentials of the other half (`other`: stage of its r), if there are any.  The first operands
+    // have been asked for; those of half 1 are at the end of half 0
+    constexpr int kOps = 3;                          // operands that are read ahead of their use
+    bf16x8 x[kOps + 1];
+    float4 r4[2];
+    auto first_operands = [&](int st, int h, int other, auto any) {
+#pragma unroll
+        for (int ks = 0; ks < kOps; ++ks) x[ks] = operand(st, h, ks);
+        if constexpr (decltype(any)::value) r4[0] = rows_r(1 - h, other, 0);
+    };
+    auto half_tile = [&](int h, int st, int other, auto masked, auto any) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int ks = i / 2, s = i % 2;
+            if (s == 0 && ks + kOps < 8) x[(ks + kOps) % (kOps + 1)] = operand(st, h, ks + kOps);
+            if (decltype(any)::value && i % 4 == 0 && i < 12) r4[(i / 4 + 1) % 2] = rows_r(1 - h, other, i / 4 + 1);
+            c[h][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[ks % (kOps + 1)], kb[s][ks], ks == 0 ? f32x16{} : c[h][s], 0, 0, 0);
+            if constexpr (decltype(any)::value) exponentials(1 - h, other, i, masked, r4[(i / 4) % 2]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto last_half = [&](int st3, auto masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) exponentials(1, st3, i, masked, rows_r(1, st3, i / 4));
+    };
+    int first_query = (seq.row0 + (end - 1) * kKwRows) / a.G;        // that of a tile's first row
+    int first_head = seq.row0 + (end - 1) * kKwRows - first_query * a.G;
+    bool whole_before = true;
+    int st3 = 0, before3 = 2;                        // stages of r
     for (int t = end - 1, st = 0; t >= t0; --t, st ^= 1) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
+        if (t == end - 1) first_operands(st, 0, before3, std::false_type{});
+        else first_operands(st, 0, before3, std::true_type{});
         float r_next;
         int last_next;
         if (t > t0) {
-            request(t - 1, st ^ 1);
-            if (tid < kKwRows) row_info(t - 1, r_next, last_next);
+            request(st ^ 1);
+            if (tid < kKwRows) row_info(r_next, last_next);
         }
-        const int first_row = seq.row0 + t * kKwRows;
-        const bool whole = first_row / a.G + seq.ahead >= kw + 63 && first_row + kKwRows <= seq.rows;        // all rows see all of the wave's keys
-#pragma unroll
-        for (int h = 0; h < kKwRows / 32; ++h) {
-            f32x16 c[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-                const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&sh_q[st][(32 * h + n) * kD + (((ks * 2 + half) ^ (n & 15)) << 3)]);
-#pragma unroll
-                for (int s = 0; s < 2; ++s) c[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, kb[s][ks], c[s], 0, 0, 0);
-            }
-            // score i is that of row 8 (i / 4) + 4 half + i % 4
-            float tile_sum[2] = {0.f, 0.f};
-#pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-                const float4 r4 = *reinterpret_cast<const float4 *>(&sh_r[st][32 * h + 8 * i4 + 4 * half]);
-                const float r[4] = {r4.x, r4.y, r4.z, r4.w};
-                int last[4] = {};
-                if (!whole) {
-                    const int4 l4 = *reinterpret_cast<const int4 *>(&sh_last[st][32 * h + 8 * i4 + 4 * half]);
-                    last[0] = l4.x; last[1] = l4.y; last[2] = l4.z; last[3] = l4.w;
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        float w = __builtin_amdgcn_exp2f(fmaf(c[s][4 * i4 + i], a.scale_log2e, -r[i]));
-                        if (!whole) w = kw + 32 * s + n <= last[i] ? w : 0.f;
-                        tile_sum[s] += w;
-                    }
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) near_sum[s] += tile_sum[s];
-        }
-        if ((t - t0) % kSumTiles == 0) {
+        // all rows see all of the wave's keys (and the last tile's last rows are there)
+        const bool whole = first_query + seq.ahead >= kw + 63 && seq.row0 + (t + 1) * kKwRows <= seq.rows;
+        if (t == end - 1) half_tile(0, st, before3, std::true_type{}, std::false_type{});
+        else if (whole_before) half_tile(0, st, before3, std::false_type{}, std::true_type{});
+        else half_tile(0, st, before3, std::true_type{}, std::true_type{});
+        if ((end - t) % kSumTiles == 0) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 sum[s] += near_sum[s];
                 near_sum[s] = 0.f;
             }
         }
+        first_operands(st, 1, st3, std::true_type{});
+        if (whole) half_tile(1, st, st3, std::false_type{}, std::true_type{});
+        else half_tile(1, st, st3, std::true_type{}, std::true_type{});
+        whole_before = whole;
+        before3 = st3;
+        st3 = st3 == 2 ? 0 : st3 + 1;
+        first_query -= per_tile;
+        first_head -= heads_left;
+        if (first_head < 0) { first_head += a.G; --first_query; }
         if (t > t0 && tid < kKwRows) {
-            sh_r[st ^ 1][tid] = r_next;
-            sh_last[st ^ 1][tid] = last_next;
+            sh_r[st3][tid] = r_next * 1.44269504088896340736f;      // (not before: the load would be waited for there)
+            sh_last[st3][tid] = last_next;
         }
+    }
+    if (t0 < end) {
+        if (whole_before) last_half(before3, std::false_type{});
+        else last_half(before3, std::true_type{});
+#pragma unroll
+        for (int s = 0; s < 2; ++s) sum[s] += near_sum[s];
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -201,7 +292,7 @@ static KeyWeightPlan key_weight_plan(const ihip_packed &p, int rows_k, int windo
     const int64_t G = p.Hq / p.Hkv, most = std::max<int64_t>(1, ((int64_t)std::min({p.max_q, window, p.rows}) * G + kKwRows - 1) / kKwRows);
     KeyWeightPlan r;
     r.blocks = rows_k / kKwKeys + p.B;
-    const int64_t places = 4 * 2 * (int64_t)compute_units();
+    const int64_t places = 24 * 2 * (int64_t)compute_units();
     const int64_t want = std::max<int64_t>(kLeast, r.blocks * p.Hkv * most / places + 1);
     r.chunk_tiles = (int)std::min(want, most);
     r.chunks = (int)((most - 1) / r.chunk_tiles + 1);
@@ -256,6 +347,7 @@ extern "C" int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tenso
     if (plan.blocks * a.Hkv > INT32_MAX || plan.chunks > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)plan.blocks * a.Hkv);
     const bool parts = plan.chunks > 1 && ws && !((uintptr_t)ws & 15) && ws_bytes >= plan.bytes;
     a.chunk_tiles = parts ? plan.chunk_tiles : INT32_MAX;
+    a.near = kKwRows % a.G == 0 && a.q_st >= 0 && a.q_sh >= 0 && a.q_st < (1 << 22) && (int64_t)(a.G - 1) * a.q_sh < (1 << 28);
     a.chunks = parts ? plan.chunks : 1;
     a.part = parts ? (float *)ws : nullptr;
     const dim3 grid((uint32_t)(plan.blocks * a.Hkv), parts ? plan.chunks : 1);
