@@ -17,7 +17,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kKwThreads = 256, kKwWaves = kKwThreads / kWave;
-constexpr int kKwKeys = 64 * kKwWaves;               // of a workgroup
+template <int SETS> constexpr int kKwKeys = 32 * SETS * kKwWaves;         // of a workgroup
 constexpr int kKwRows = 64;                          // rows of a tile
 constexpr int kSumTiles = 16;
 
@@ -38,13 +38,27 @@ struct KeyWeightArgs {
 
 // A sequence, and the tiles of its rows that count
 struct KeyWeightSeq {
-    int q_first, nq, k_first, nk, ahead, row0, rows;         // rows row0 .. rows - 1 count
-    __device__ KeyWeightSeq(const KeyWeightArgs &a, int b)
+    int b, q_first, nq, k_first, nk, ahead, row0, rows;      // rows row0 .. rows - 1 count
+    // The one that block `id` of `keys` keys belongs to (b: -1 if there is none).  Blocks are numbered so that sequence b's begin at first
+    // key / keys + b, which leaves room for a part of a block in each
+    __device__ KeyWeightSeq(const KeyWeightArgs &a, int keys, int id, int lane)
     {
-        q_first = min(max(a.cu_q[b], 0), a.rows_q);
-        nq = min(max(a.cu_q[b + 1], q_first), a.rows_q) - q_first;
-        k_first = min(max(a.cu_k[b], 0), a.rows_k);
-        nk = min(max(a.cu_k[b + 1], k_first), a.rows_k) - k_first;
+        int q0 = 0, q1 = 0, k0 = 0, k1 = 0;          // of lane's sequence among the last 64 with one that begins at or before id
+        b = -1;
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            const int i = min(b0 + lane, a.B - 1);
+            const int c0 = min(max(a.cu_k[i], 0), a.rows_k), c1 = a.cu_k[i + 1], d0 = a.cu_q[i], d1 = a.cu_q[i + 1];
+            const int n = __popcll(__ballot(b0 + lane < a.B && c0 / keys + i <= id));
+            if (n == 0) break;
+            b = b0 + n - 1;
+            k0 = c0; k1 = c1; q0 = d0; q1 = d1;
+        }
+        b = __builtin_amdgcn_readfirstlane(b);
+        const int at = b & 63;
+        q_first = min(max(__builtin_amdgcn_readlane(q0, at), 0), a.rows_q);
+        nq = min(max(__builtin_amdgcn_readlane(q1, at), q_first), a.rows_q) - q_first;
+        k_first = __builtin_amdgcn_readlane(k0, at);
+        nk = min(max(__builtin_amdgcn_readlane(k1, at), k_first), a.rows_k) - k_first;
         ahead = nk - nq;                             // query i sees keys 0 .. i + ahead
         row0 = max(0, nq - a.window) * a.G;
         rows = nq * a.G;
@@ -53,16 +67,6 @@ struct KeyWeightSeq {
     // the first tile with a query that sees key k
     __device__ int first_tile(const KeyWeightArgs &a, int k) const { return (int)min(max((int64_t)0, ((int64_t)k - ahead) * a.G - row0) / kKwRows, (int64_t)tiles()); }
 };
-// Blocks of keys are numbered so that sequence b's begin at first key / kKwKeys + b, which leaves room for a part of a block in each
-__device__ inline int key_block_seq(const KeyWeightArgs &a, int id, int lane)
-{
-    int n = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int b = b0 + lane;
-        n += __popcll(__ballot(b < a.B && min(max(a.cu_k[min(b, a.B - 1)], 0), a.rows_k) / kKwKeys + b <= id));
-    }
-    return __builtin_amdgcn_readfirstlane(n - 1);
-}
 
 // 16 bytes a lane from a scalar base and the lane's byte offset to the LDS byte address dst + 16 l (counts on vmcnt).  M0 is left as it is:
 // nothing else in this kernel reads it, and it is not the compiler's to keep values in.
@@ -71,7 +75,9 @@ __device__ inline void key_weights_to_lds(uint32_t dst, const uint16_t *base, ui
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(byte_off), "s"(base) : "memory");
 }
 
-__global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const KeyWeightArgs a)
+// SETS of 32 keys a wave
+template <int SETS>
+__global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weights_kernel(const KeyWeightArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint16_t sh_q[2][kKwRows * kD];
     __shared__ __attribute__((aligned(16))) float sh_r[3][kKwRows];          // of a tile's rows: r, and the last key
@@ -79,19 +85,20 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
     const int g = blockIdx.x % a.Hkv, id = blockIdx.x / a.Hkv;
-    const int b = key_block_seq(a, id, lane);
+    constexpr int kKeys = kKwKeys<SETS>;
+    const KeyWeightSeq seq(a, kKeys, id, lane);
+    const int b = seq.b;
     if (b < 0) return;
-    const KeyWeightSeq seq(a, b);
-    const int block = id - (seq.k_first / kKwKeys + b), k0 = block * kKwKeys;
+    const int block = id - (seq.k_first / kKeys + b), k0 = block * kKeys;
     if (block < 0 || k0 >= seq.nk) return;
     const int tiles = seq.tiles(), begin = seq.first_tile(a, k0);
     const int end = tiles - (int)min((int64_t)blockIdx.y * a.chunk_tiles, (int64_t)tiles), t0 = max(begin, end - a.chunk_tiles);
     if (blockIdx.y > 0 && t0 >= end) return;
-    const int kw = k0 + wave * 64;                   // this wave's first key
+    const int kw = k0 + wave * 32 * SETS;                   // this wave's first key
 
-    bf16x8 kb[2][8];                                 // (behind the last key: that one again)
+    bf16x8 kb[SETS][8];                                 // (behind the last key: that one again)
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < SETS; ++s) {
         const uint16_t *kp = a.k + (int64_t)(seq.k_first + min(kw + 32 * s + n, seq.nk - 1)) * a.k_st + g * a.k_sh + half * 8;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) kb[s][ks] = *reinterpret_cast<const bf16x8 *>(kp + ks * 16);
@@ -149,13 +156,7 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const
         last = r_query + seq.ahead;
     };
 
-    // the keys are waited for here: in the loop the compiler, which does not know what has been waited for in assembly, would wait for all loads at their use
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(kb[s][ks]));
-
-    float sum[2] = {0.f, 0.f}, near_sum[2] = {0.f, 0.f};
+    float sum[SETS] = {}, near_sum[SETS] = {};
     if (t0 < end) {                                  // the first tile: rows behind the last one stand for that one
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) send(0, i, last_row + in_tile(i) < seq.rows ? q_at[i] : q_of(seq.nq - 1, a.G - 1, i));
@@ -165,23 +166,25 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const
             sh_last[0][tid] = there ? r_query + seq.ahead : -1;
         }
     }
+    // the keys are waited for here: in the loop the compiler, which does not know what has been waited for in assembly, would wait for all loads at their use
+#pragma unroll
+    for (int s = 0; s < SETS; ++s)
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(kb[s][ks]));
+
     // Half a tile at a time: the products of 32 rows with the wave's keys, and between them, two scores after each, the exponentials of the half
     // before.  Score i is that of row 8 (i / 4) + 4 half + i % 4.
-    f32x16 c[2][2];                                  // of the present and the previous half
+    f32x16 c[2][SETS];                                  // of the present and the previous half
     auto operand = [&](int st, int h, int ks) { return *reinterpret_cast<const bf16x8 *>(&sh_q[st][(32 * h + n) * kD + (((ks * 2 + half) ^ (n & 15)) << 3)]); };
-    float part_sum[2];
-    auto exponentials = [&](int h, int st3, int i, auto masked, const float4 &r4) {
-        const float r = i % 4 == 0 ? r4.x : i % 4 == 1 ? r4.y : i % 4 == 2 ? r4.z : r4.w;
-        int last = 0;
-        if constexpr (decltype(masked)::value) last = sh_last[st3][32 * h + 8 * (i / 4) + 4 * half + i % 4];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            float w = __builtin_amdgcn_exp2f(fmaf(c[h][s][i], a.scale_log2e, -r));
-            if constexpr (decltype(masked)::value) w = kw + 32 * s + n <= last ? w : 0.f;
-            part_sum[s] = i == 0 ? w : part_sum[s] + w;
-            if (i == 15) near_sum[s] += part_sum[s];
-        }
+    float part_sum[SETS];
+    // score i of set s; r: that of its row
+    auto exponential = [&](int h, int st3, int i, int s, auto masked, float r) {
+        float w = __builtin_amdgcn_exp2f(fmaf(c[h][s][i], a.scale_log2e, -r));
+        if constexpr (decltype(masked)::value) w = kw + 32 * s + n <= sh_last[st3][32 * h + 8 * (i / 4) + 4 * half + i % 4] ? w : 0.f;
+        part_sum[s] = i == 0 ? w : part_sum[s] + w;
+        if (i == 15) near_sum[s] += part_sum[s];
     };
+    auto element = [](const float4 &x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; };
     auto rows_r = [&](int h, int st3, int i4) { return *reinterpret_cast<const float4 *>(&sh_r[st3][32 * h + 8 * i4 + 4 * half]); };
     // products of half h of the tile in stage st, exponentials of the other half (`other`: stage of its r), if there are any.  The first operands
     // have been asked for; those of half 1 are at the end of half 0
@@ -195,18 +198,28 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const
     };
     auto half_tile = [&](int h, int st, int other, auto masked, auto any) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int ks = i / 2, s = i % 2;
+        for (int i = 0; i < 8 * SETS; ++i) {
+            const int ks = i / SETS, s = i % SETS, score = 2 * i / SETS;
             if (s == 0 && ks + kOps < 8) x[(ks + kOps) % (kOps + 1)] = operand(st, h, ks + kOps);
-            if (decltype(any)::value && i % 4 == 0 && i < 12) r4[(i / 4 + 1) % 2] = rows_r(1 - h, other, i / 4 + 1);
+            if (decltype(any)::value && score % 4 == 0 && score < 12) r4[(score / 4 + 1) % 2] = rows_r(1 - h, other, score / 4 + 1);
             c[h][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[ks % (kOps + 1)], kb[s][ks], ks == 0 ? f32x16{} : c[h][s], 0, 0, 0);
-            if constexpr (decltype(any)::value) exponentials(1 - h, other, i, masked, r4[(i / 4) % 2]);
+            if constexpr (decltype(any)::value) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int e = (2 * i + u) / SETS;
+                    exponential(1 - h, other, e, (2 * i + u) % SETS, masked, element(r4[(e / 4) % 2], e % 4));
+                }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     auto last_half = [&](int st3, auto masked) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) exponentials(1, st3, i, masked, rows_r(1, st3, i / 4));
+        for (int i = 0; i < 16; ++i) {
+            const float4 r = rows_r(1, st3, i / 4);
+#pragma unroll
+            for (int s = 0; s < SETS; ++s) exponential(1, st3, i, s, masked, element(r, i % 4));
+        }
     };
     int first_query = (seq.row0 + (end - 1) * kKwRows) / a.G;        // that of a tile's first row
     int first_head = seq.row0 + (end - 1) * kKwRows - first_query * a.G;
@@ -224,13 +237,13 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const
             if (tid < kKwRows) row_info(r_next, last_next);
         }
         // all rows see all of the wave's keys (and the last tile's last rows are there)
-        const bool whole = first_query + seq.ahead >= kw + 63 && seq.row0 + (t + 1) * kKwRows <= seq.rows;
+        const bool whole = first_query + seq.ahead >= kw + 32 * SETS - 1 && seq.row0 + (t + 1) * kKwRows <= seq.rows;
         if (t == end - 1) half_tile(0, st, before3, std::true_type{}, std::false_type{});
         else if (whole_before) half_tile(0, st, before3, std::false_type{}, std::true_type{});
         else half_tile(0, st, before3, std::true_type{}, std::true_type{});
         if ((end - t) % kSumTiles == 0) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
+            for (int s = 0; s < SETS; ++s) {
                 sum[s] += near_sum[s];
                 near_sum[s] = 0.f;
             }
@@ -253,13 +266,13 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const
         if (whole_before) last_half(before3, std::false_type{});
         else last_half(before3, std::true_type{});
 #pragma unroll
-        for (int s = 0; s < 2; ++s) sum[s] += near_sum[s];
+        for (int s = 0; s < SETS; ++s) sum[s] += near_sum[s];
     }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < SETS; ++s) {
         const float w = sum[s] + __shfl_xor(sum[s], 32, 64);
         const int key = kw + 32 * s + n;
-        if (half != s || key >= seq.nk) continue;
+        if (half != s % 2 || key >= seq.nk) continue;
         if (a.part) {
             a.part[((int64_t)blockIdx.y * a.Hkv + g) * a.rows_k + seq.k_first + key] = w;
         } else if (key < a.weight_rows) {
@@ -270,13 +283,14 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_kernel(const
 }
 
 // The chunks of a block of keys added up, a key a thread
-__global__ __launch_bounds__(kKwKeys) void prompt_key_weights_sum_kernel(const KeyWeightArgs a)
+template <int SETS>
+__global__ __launch_bounds__(kKwKeys<SETS>) void prompt_key_weights_sum_kernel(const KeyWeightArgs a)
 {
     const int g = blockIdx.x % a.Hkv, id = blockIdx.x / a.Hkv;
-    const int b = key_block_seq(a, id, threadIdx.x & 63);
+    const KeyWeightSeq seq(a, kKwKeys<SETS>, id, threadIdx.x & 63);
+    const int b = seq.b;
     if (b < 0) return;
-    const KeyWeightSeq seq(a, b);
-    const int k0 = (id - (seq.k_first / kKwKeys + b)) * kKwKeys, key = k0 + threadIdx.x;
+    const int k0 = (id - (seq.k_first / kKwKeys<SETS> + b)) * kKwKeys<SETS>, key = k0 + threadIdx.x;
     if (k0 < 0 || key >= seq.nk || key >= a.weight_rows) return;
     const int chunks = min(a.chunks, max(1, (seq.tiles() - seq.first_tile(a, k0) + a.chunk_tiles - 1) / a.chunk_tiles));
     float w = 0.f;
@@ -285,17 +299,20 @@ __global__ __launch_bounds__(kKwKeys) void prompt_key_weights_sum_kernel(const K
     a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w;
 }
 
-struct KeyWeightPlan { int64_t blocks; int chunk_tiles, chunks; size_t bytes; };
+// Wide blocks of keys, which read the queries half as often, where there is work for many rounds of workgroups, narrow ones otherwise; queries in
+// chunks of about the tiles that give each compute unit 8 of them (48 where blocks are wide: the blocks of a long prompt differ).  us, wide / narrow:
+// 33,625 tokens in three prompts 1,634 / 1,792, 7,401 in four 98 to 105 / 89, 1,024 27 / 16, the last 64 queries of 32,749 30 / 30.
+struct KeyWeightPlan { int sets; int64_t blocks; int chunk_tiles, chunks; size_t bytes; };
 static KeyWeightPlan key_weight_plan(const ihip_packed &p, int rows_k, int window)
 {
-    constexpr int kLeast = 8;                        // tiles of a chunk
+    constexpr int kLeast = 4;                        // tiles of a chunk
     const int64_t G = p.Hq / p.Hkv, most = std::max<int64_t>(1, ((int64_t)std::min({p.max_q, window, p.rows}) * G + kKwRows - 1) / kKwRows);
     KeyWeightPlan r;
-    r.blocks = rows_k / kKwKeys + p.B;
-    const int64_t places = 24 * 2 * (int64_t)compute_units();
-    const int64_t want = std::max<int64_t>(kLeast, r.blocks * p.Hkv * most / places + 1);
-    r.chunk_tiles = (int)std::min(want, most);
-    r.chunks = (int)((most - 1) / r.chunk_tiles + 1);
+    auto tiles = [&](int64_t keys) { return (r.blocks = rows_k / keys + p.B) * p.Hkv * most; };
+    r.sets = tiles(kKwKeys<2>) >= 512 * (int64_t)compute_units() ? 2 : 1;
+    const int64_t all = tiles(r.sets == 1 ? kKwKeys<1> : kKwKeys<2>), want = std::max<int64_t>(kLeast, all / ((r.sets == 1 ? 8 : 48) * (int64_t)compute_units()));
+    r.chunks = (int)std::max<int64_t>(1, (most + want / 2) / want);
+    r.chunk_tiles = (int)((most - 1) / r.chunks + 1);
     r.bytes = r.chunks > 1 ? (size_t)r.chunks * p.Hkv * rows_k * sizeof(float) : 0;
     return r;
 }
@@ -354,10 +371,12 @@ extern "C" int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tenso
     const hipStream_t st = (hipStream_t)stream;
     {
         KernelTimer timer("prompt_key_weights", st);
-        hipLaunchKernelGGL(prompt_key_weights_kernel, grid, dim3(kKwThreads), 0, st, a);
+        if (plan.sets == 1) hipLaunchKernelGGL(prompt_key_weights_kernel<1>, grid, dim3(kKwThreads), 0, st, a);
+        else hipLaunchKernelGGL(prompt_key_weights_kernel<2>, grid, dim3(kKwThreads), 0, st, a);
     }
     if ((rc = check_launch(who)) != IHIP_OK || !parts) return rc;
     KernelTimer timer("prompt_key_weights_sum", st);
-    hipLaunchKernelGGL(prompt_key_weights_sum_kernel, dim3(grid.x), dim3(kKwKeys), 0, st, a);
+    if (plan.sets == 1) hipLaunchKernelGGL(prompt_key_weights_sum_kernel<1>, dim3(grid.x), dim3(kKwKeys<1>), 0, st, a);
+    else hipLaunchKernelGGL(prompt_key_weights_sum_kernel<2>, dim3(grid.x), dim3(kKwKeys<2>), 0, st, a);
     return check_launch(who);
 }

@@ -79,6 +79,21 @@ def test_against_float64(ihip, Hq, Hkv, new, ctx, window):
             assert (track.weights[b, :, t:].cpu() == old[b, :, t:]).all()
 
 
+@pytest.mark.parametrize("Hq,Hkv,window", [(8, 1, None), (6, 2, None), (16, 2, 100)])
+def test_wide_blocks_of_keys(ihip, Hq, Hkv, window):
+    """What calls of much work take: packed tensors of many rows, bounds to match, and a few short sequences in them."""
+    new, rows = [600, 1, 77, 300], 40000
+    q, k, lse = inputs(new, new, Hq, Hkv, seed=2, extra=0)
+    wide = [torch.full((rows, *x.shape[1:]), float("nan"), dtype=x.dtype).cuda() for x in (q, k, lse)]
+    for x, y in zip(wide, (q, k, lse)):
+        x[:sum(new)] = y.cuda()
+    track = ihip.KVTrack(torch.full((4, Hkv, 610), 5.0).cuda())
+    ihip.prompt_key_weights(wide[0], wide[1], offsets(new).cuda(), rows, wide[2], track, window=window, fresh=True)
+    check(track.weights, None, 1.0, q, k, lse, new, new, Hkv, window or 10 ** 9, 610)
+    for b, n in enumerate(new):
+        assert bool((track.weights[b, :, n:] == 5).all())
+
+
 def test_chunks_of_queries(ihip):
     """Many queries on few keys, in chunks whose sums are added up, and without scratch: equal up to rounding, and the same bits each time."""
     new, Hq, Hkv = [2500, 1200], 8, 1
