@@ -24,16 +24,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTrThreads = 256, kTrWaves = kTrThreads / kWave;
 constexpr int kTrStep = 32;                          // rows of a wave at a time
-constexpr int kTrMaxSplit = 4096, kTrMinSplit = 128; // rows of a part (multiples of 128: a step of every wave)
+constexpr int kTrMaxSplit = 768, kTrMinSplit = 128;  // rows of a part (multiples of 128: a step of every wave)
 
 struct TrackedArgs {
     Geometry ge;
     int max_len;
     const uint16_t *q; int64_t q_sb, q_sh;
     StoreView from;
-    int page_log2;                   // a cache without pages is one page a sequence
     float scale_log2e, v_scale;
-    int n_splits;
+    int n_splits, per;               // parts of a problem, rows of one
     DecodeGrid grid;
     float *scores; int64_t score_stride;             // [P, G, score_stride], unscaled
     float *part_ml, *part_acc;       // [P, n_splits, G, 2] (reference, unscaled, and sum), [P, n_splits, G, 128]
@@ -47,12 +46,6 @@ struct TrackedArgs {
 
 __device__ inline uint16_t to_bf16(float x) { return (uint16_t)pack_bf16x2(x, x); }        // (NaN stays it)
 __device__ inline int tracked_len(const TrackedArgs &a, int b) { return min(max(a.ge.seq_lens[b], 0), a.max_len); }
-// Rows of each of a sequence's parts
-__device__ inline int tracked_part(const TrackedArgs &a, int len)
-{
-    return min(kTrMaxSplit, max(kTrMinSplit, (int)(((int64_t)len + a.n_splits - 1) / a.n_splits + kTrMinSplit - 1) / kTrMinSplit * kTrMinSplit));
-}
-
 template <int FORMAT>
 struct TrackedRows {
     typedef typename std::conditional<FORMAT == IHIP_KV_BF16, uint4, typename std::conditional<FORMAT == IHIP_KV_E4M3, uint2, uint32_t>::type>::type word;
@@ -60,24 +53,28 @@ struct TrackedRows {
     uint4 k[2][kPieces];             // of rows n and 16 + n
     word v[8];                       // dims 8 n .. of keys 4 g + r and 16 + 4 g + r
     uint32_t k_scale[2], v_scale[8]; // 4-bit rows
-    uint32_t there;                  // which of the 32 rows hold a key
 };
 
 template <int FORMAT, int HEADS>
-__global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void attn_decode_tracked_kernel(const TrackedArgs a)
+__global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void attn_decode_tracked_kernel(const TrackedArgs a)
 {
     typedef TrackedRows<FORMAT> Rows;
     const int p = a.grid.problem(), split = a.grid.part();
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
     const int b = p / a.ge.Hkv, kv_head = p % a.ge.Hkv, G = a.ge.G;
-    const int len = tracked_len(a, b), per = tracked_part(a, len);
-    const int s0 = min(split * per, len), s1 = min(s0 + per, len), steps = (s1 - s0 + kTrStep - 1) / kTrStep;
+    const int len = tracked_len(a, b);
+    const int s0 = (int)min((int64_t)split * a.per, (int64_t)len), s1 = min(s0 + a.per, len), steps = (s1 - s0 + kTrStep - 1) / kTrStep;
+    if (split > 0 && steps == 0) return;             // (part 0 of an idle place has its output to write)
     const int64_t pbase = ((int64_t)p * a.n_splits + split) * G;
 
-    __shared__ int32_t sh_page[kTrMaxSplit + 1];     // of the part's rows: page ids, or the sequence
+    // where the part's rows are, in bytes from row 0; behind the last step: the waves' results, of the two parts of the probabilities
+    __shared__ __attribute__((aligned(16))) union {
+        struct { int64_t k[kTrMaxSplit], v[kTrMaxSplit]; } row;
+        float acc[kTrWaves][2][HEADS][kD];
+    } sh;
+    __shared__ uint32_t sh_there[kTrMaxSplit / kTrStep];     // which of a step's rows hold a key
     __shared__ float sh_m[kTrWaves][HEADS], sh_l[kTrWaves][HEADS];
-    __shared__ __attribute__((aligned(16))) float sh_acc[kTrWaves][2][HEADS][kD];      // of the two parts
 
     // The operand of step j: 16-byte pieces as above
     bf16x8 qb[4];
@@ -87,39 +84,38 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void at
         for (int j = 0; j < 4; ++j)
             qb[j] = *reinterpret_cast<const bf16x8 *>(qp + (FORMAT == IHIP_KV_BF16 ? 32 * j + 8 * g : FORMAT == IHIP_KV_E4M3 ? 64 * (j >> 1) + 16 * g + 8 * (j & 1) : 32 * g + 8 * j));
     }
-    const int first_page = s0 >> a.page_log2;
-    const uint32_t in_page = (1u << a.page_log2) - 1;
-    if (s1 > s0) {
-        const int pages = ((s1 - 1) >> a.page_log2) - first_page + 1;
-        const int32_t *table = a.from.paged.block_table ? a.from.paged.block_table + (int64_t)b * a.from.paged.table_stride + first_page : nullptr;
-        for (int i = tid; i < pages; i += kTrThreads) sh_page[i] = table ? table[i] : b;
+    // A row behind the part's last key stands for that one, a row on no page for one that can be read
+    const int32_t *table = a.from.paged.block_table ? a.from.paged.block_table + (int64_t)b * a.from.paged.table_stride : nullptr;
+    for (int i = tid; i < steps * kTrStep; i += kTrThreads) {
+        const int row = min(s0 + i, s1 - 1);
+        int first = b, in_page = row;
+        if (table) {
+            first = table[row >> a.from.paged.page_log2];
+            in_page = row & ((1 << a.from.paged.page_log2) - 1);
+        }
+        const unsigned long long there = __ballot(s0 + i < s1 && first >= 0);
+        if ((lane & 31) == 0) sh_there[i >> 5] = (uint32_t)(there >> (lane & 32));
+        first = max(first, 0);
+        sh.row.k[i] = first * a.from.k_sb + in_page * a.from.k_st;
+        sh.row.v[i] = first * a.from.v_sb + in_page * a.from.v_st;
     }
     const uint8_t *kb = a.from.k + kv_head * a.from.k_sh + g * 16, *vb = a.from.v + kv_head * a.from.v_sh + n * (int)sizeof(typename Rows::word);
     const uint8_t *ksb = a.from.ks + kv_head * (a.from.k_sh / 16) + g, *vsb = a.from.vs + kv_head * (a.from.v_sh / 16) + (n >> 2);
     __syncthreads();
 
-    // A row behind the part's last key stands for that one, a row on no page for one that can be read
     auto load = [&](int step, Rows &r) {
-        const int row0 = s0 + step * kTrStep;
-        auto page_of = [&](int row) { return sh_page[(row >> a.page_log2) - first_page]; };
-        {
-            const int row = row0 + (lane & 31);
-            r.there = (uint32_t)__ballot(row < s1 && page_of(min(row, s1 - 1)) >= 0);
-        }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int row = min(row0 + 16 * t + n, s1 - 1);
-            const int64_t off = (int64_t)max(page_of(row), 0) * a.from.k_sb + (int64_t)((uint32_t)row & in_page) * a.from.k_st;
+            const int64_t off = sh.row.k[step * kTrStep + 16 * t + n];
 #pragma unroll
             for (int j = 0; j < Rows::kPieces; ++j) r.k[t][j] = *reinterpret_cast<const uint4 *>(kb + off + 64 * j);
             if constexpr (FORMAT == IHIP_KV_MX4) r.k_scale[t] = ksb[off / 16];
-        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = min(row0 + 16 * (i >> 2) + 4 * g + (i & 3), s1 - 1);
-            const int64_t off = (int64_t)max(page_of(row), 0) * a.from.v_sb + (int64_t)((uint32_t)row & in_page) * a.from.v_st;
-            r.v[i] = *reinterpret_cast<const typename Rows::word *>(vb + off);
-            if constexpr (FORMAT == IHIP_KV_MX4) r.v_scale[i] = vsb[off / 16];
+            for (int i = 0; i < 4; ++i) {
+                const int64_t v_off = sh.row.v[step * kTrStep + 16 * t + 4 * g + i];
+                r.v[4 * t + i] = *reinterpret_cast<const typename Rows::word *>(vb + v_off);
+                if constexpr (FORMAT == IHIP_KV_MX4) r.v_scale[4 * t + i] = vsb[v_off / 16];
+            }
         }
     };
     // operand of step j of a lane's K row
@@ -134,22 +130,28 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void at
             return __builtin_bit_cast(bf16x8, mx4_to_bf16x8(j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w, mx4_scale(r.k_scale[t])));
         }
     };
-    auto v_row = [&](const Rows &r, int i) {
-        if constexpr (FORMAT == IHIP_KV_BF16) return r.v[i];
-        else if constexpr (FORMAT == IHIP_KV_E4M3) return fp8x8_to_bf16x8(r.v[i]);
-        else return mx4_to_bf16x8(r.v[i], mx4_scale(r.v_scale[i]));
+    // two dims of a V row, as bf16
+    auto v_pair = [&](const Rows &r, int i, auto d) -> uint32_t {
+        constexpr int D = decltype(d)::value;
+        if constexpr (FORMAT == IHIP_KV_BF16) return D == 0 ? r.v[i].x : D == 1 ? r.v[i].y : D == 2 ? r.v[i].z : r.v[i].w;
+        else if constexpr (FORMAT == IHIP_KV_E4M3) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(D < 2 ? r.v[i].x : r.v[i].y, 1.0f, D % 2 == 1));
+        else return mx4_pair<D>(r.v[i], mx4_scale(r.v_scale[i]));
     };
 
     const uint32_t second = n < 8 ? 0u : ~0u;        // lanes that bring the second parts of the probabilities
-    float *scores = a.scores + ((int64_t)p * G + min(n, G - 1)) * a.score_stride + s0 + 4 * g;
+    float *scores = a.scores + ((int64_t)p * G + min(n & 7, G - 1)) * a.score_stride + s0 + 4 * g;
     f32x4 acc[8];                                    // rows 4 g + r, dim 8 n + j
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = kSoftmaxLowest, l = 0.f;               // of head n (m: the same in the four lanes of a head; l: of this lane's keys)
     Rows r, nx;
-    if (wv < steps) load(wv, r);
+    // Wide rows are asked for a step ahead, two waves a SIMD; of narrow ones four waves have as many bytes on their way, and one step's registers
+    // (E4M3, MX FP4 with three waves and a step ahead: 187 and 75 us where this takes 186 and 70)
+    constexpr bool kAheadLoads = FORMAT == IHIP_KV_BF16;
+    if (kAheadLoads && wv < steps) load(wv, r);
     for (int step = wv; step < steps; step += kTrWaves) {
-        if (step + kTrWaves < steps) load(step + kTrWaves, nx);
+        if (!kAheadLoads) load(step, r);
+        else if (step + kTrWaves < steps) load(step + kTrWaves, nx);
         f32x4 c[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -157,7 +159,7 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void at
 #pragma unroll
             for (int j = 0; j < 4; ++j) c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand(r, t, j), qb[j], c[t], 0, 0, 0);
         }
-        const uint32_t there = __builtin_amdgcn_readfirstlane(r.there);
+        const uint32_t there = __builtin_amdgcn_readfirstlane(sh_there[step]);
         if (there != ~0u) {                          // (what stands in the rows is not used, but has to be finite)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -167,10 +169,9 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void at
                     r.v_scale[i] = 127;
                 }
         }
-        if (n < G) {
+        // (lanes of the same head write the same: under a branch the compiler would not know how many requests are on their way, and wait for all)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4 *>(scores + step * kTrStep + 16 * t) = c[t];
-        }
+        for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4 *>(scores + step * kTrStep + 16 * t) = c[t];
         float w[8], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -206,33 +207,35 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void at
             part[i] = pack_bf16x2(w[2 * i] - __uint_as_float(first << 16), w[2 * i + 1] - __uint_as_float(first & 0xffff0000u));
         }
         const bf16x8 pw = __builtin_bit_cast(bf16x8, make_uint4(part[0], part[1], part[2], part[3]));
-        uint4 x[8];
+        auto dims = [&](auto d) {                    // 8 n + 2 d and 8 n + 2 d + 1
+            uint32_t x[8], lo[4], hi[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = v_row(r, i);
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {                // dims 8 n + 2 d and 8 n + 2 d + 1
-            uint32_t lo[4], hi[4];
+            for (int i = 0; i < 8; ++i) x[i] = v_pair(r, i, d);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t even = d == 0 ? x[2 * i].x : d == 1 ? x[2 * i].y : d == 2 ? x[2 * i].z : x[2 * i].w;
-                const uint32_t odd = d == 0 ? x[2 * i + 1].x : d == 1 ? x[2 * i + 1].y : d == 2 ? x[2 * i + 1].z : x[2 * i + 1].w;
-                lo[i] = __builtin_amdgcn_perm(odd, even, 0x05040100u);
-                hi[i] = __builtin_amdgcn_perm(odd, even, 0x07060302u);
+                lo[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
+                hi[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
             }
-            acc[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw, __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), acc[2 * d], 0, 0, 0);
-            acc[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw, __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), acc[2 * d + 1], 0, 0, 0);
-        }
-        r = nx;
+            f32x4 &even = acc[2 * decltype(d)::value], &odd = acc[2 * decltype(d)::value + 1];
+            even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw, __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), even, 0, 0, 0);
+            odd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw, __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), odd, 0, 0, 0);
+        };
+        dims(std::integral_constant<int, 0>{});
+        dims(std::integral_constant<int, 1>{});
+        dims(std::integral_constant<int, 2>{});
+        dims(std::integral_constant<int, 3>{});
+        if (kAheadLoads) r = nx;
     }
 
     // the waves and both parts are merged through LDS
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (lane < HEADS) { sh_m[wv][lane] = m; sh_l[wv][lane] = l; }
+    __syncthreads();
     if (4 * (g & 1) < HEADS) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            float *to = &sh_acc[wv][g >> 1][4 * (g & 1) + h][8 * n];
+            float *to = &sh.acc[wv][g >> 1][4 * (g & 1) + h][8 * n];
             *reinterpret_cast<float4 *>(to) = make_float4(acc[0][h], acc[1][h], acc[2][h], acc[3][h]);
             *reinterpret_cast<float4 *>(to + 4) = make_float4(acc[4][h], acc[5][h], acc[6][h], acc[7][h]);
         }
@@ -248,7 +251,7 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void at
         for (int w = 0; w < kTrWaves; ++w) {
             const float x = softmax_weight(sh_m[w][h], M, a.scale_log2e);
             L = fmaf(x, sh_l[w][h], L);
-            A = fmaf(x, sh_acc[w][0][h][c] + sh_acc[w][1][h][c], A);
+            A = fmaf(x, sh.acc[w][0][h][c] + sh.acc[w][1][h][c], A);
         }
         if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + (pbase + h) * 2) = make_float2(M, L);
         if (a.n_splits == 1) {                       // nothing to join
@@ -263,90 +266,119 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 3) void at
 
 // The parts joined, and weights: of the workgroups of a problem the first G take a head's output (where there are parts), the others
 // kJoinRows rows each.
-constexpr int kJoinRows = 1024, kJoinAhead = 8;
+constexpr int kJoinRows = 1024, kJoinAhead = 8, kJoinGroups = kTrThreads / 32;
+template <int G>
 __global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(const TrackedArgs a, int out_groups)
 {
-    const int G = a.ge.G, p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int b = p / a.ge.Hkv;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (int64_t)p * a.n_splits * G;
-    __shared__ float sh_m[8], sh_l[8], sh_a[kD];
+    __shared__ float sh_m[kJoinGroups], sh_l[kJoinGroups];
+    __shared__ __attribute__((aligned(16))) float sh_a[kJoinGroups][kD];
+    static_assert(G <= kJoinGroups, "");
     if ((int)blockIdx.y < out_groups) {
-        const int h = blockIdx.y, c = tid % kD, grp = tid / kD;
-        const float *accs = a.part_acc + (int64_t)p * a.n_splits * G * kD;
-        float M = kSoftmaxLowest, L = 0.f, A = 0.f;
-        for (int s0 = grp; s0 < a.n_splits; s0 += 2 * kJoinAhead) {
+        // a head's parts: 32 lanes a part, 4 dims each
+        const int h = blockIdx.y, l32 = tid & 31, grp = tid >> 5, parts = (tracked_len(a, b) + a.per - 1) / a.per;
+        const float4 *accs = reinterpret_cast<const float4 *>(a.part_acc + (int64_t)p * a.n_splits * G * kD) + l32;
+        float M = kSoftmaxLowest, L = 0.f;
+        float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s0 = grp; s0 < parts; s0 += kJoinGroups * kJoinAhead) {
             float2 x[kJoinAhead];
-            float v[kJoinAhead], top = M;
+            float4 v[kJoinAhead];
+            float top = M;
 #pragma unroll
             for (int i = 0; i < kJoinAhead; ++i) {
-                const int64_t at = (int64_t)min(s0 + i * 2, a.n_splits - 1) * G + h;
+                const int64_t at = (int64_t)min(s0 + i * kJoinGroups, parts - 1) * G + h;
                 x[i] = ml[at];
-                v[i] = accs[at * kD + c];
+                v[i] = accs[at * (kD / 4)];
             }
 #pragma unroll
             for (int i = 0; i < kJoinAhead; ++i)
-                if (s0 + i * 2 < a.n_splits) top = fmaxf(top, x[i].x);
+                if (s0 + i * kJoinGroups < parts) top = fmaxf(top, x[i].x);
             const float corr = softmax_weight(M, top, a.scale_log2e);
             L *= corr;
-            A *= corr;
+            A = make_float4(A.x * corr, A.y * corr, A.z * corr, A.w * corr);
             M = top;
 #pragma unroll
             for (int i = 0; i < kJoinAhead; ++i) {
-                if (s0 + i * 2 >= a.n_splits) break;
+                if (s0 + i * kJoinGroups >= parts) break;
                 const float w = softmax_weight(x[i].x, M, a.scale_log2e);
                 L = fmaf(w, x[i].y, L);
-                A = fmaf(w, v[i], A);
+                A = make_float4(fmaf(w, v[i].x, A.x), fmaf(w, v[i].y, A.y), fmaf(w, v[i].z, A.z), fmaf(w, v[i].w, A.w));
             }
         }
-        if (grp == 1) {
-            sh_a[c] = A;
-            if (c == 0) { sh_m[0] = M; sh_l[0] = L; }
-        }
+        *reinterpret_cast<float4 *>(&sh_a[grp][4 * l32]) = A;
+        if (l32 == 0) { sh_m[grp] = M; sh_l[grp] = L; }
         __syncthreads();
-        if (grp == 1) return;
-        const float top = fmaxf(M, sh_m[0]), mine = softmax_weight(M, top, a.scale_log2e), other = softmax_weight(sh_m[0], top, a.scale_log2e);
-        L = fmaf(other, sh_l[0], mine * L);
-        A = fmaf(other, sh_a[c], mine * A);
+        if (tid >= kD) return;
+        M = kSoftmaxLowest;
+#pragma unroll
+        for (int i = 0; i < kJoinGroups; ++i) M = fmaxf(M, sh_m[i]);
+        float sum = 0.f, out = 0.f;
+#pragma unroll
+        for (int i = 0; i < kJoinGroups; ++i) {
+            const float w = softmax_weight(sh_m[i], M, a.scale_log2e);
+            sum = fmaf(w, sh_l[i], sum);
+            out = fmaf(w, sh_a[i][tid], out);
+        }
         const int64_t hq = (int64_t)b * a.ge.Hq + (p % a.ge.Hkv) * G + h;
-        a.out[hq * kD + c] = to_bf16(L == 0.f ? 0.f : A / L * a.v_scale);     // an idle place: 0
-        if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = softmax_lse(top, L, a.scale_log2e);
+        a.out[hq * kD + tid] = to_bf16(sum == 0.f ? 0.f : out / sum * a.v_scale);         // an idle place: 0
+        if (a.out_lse != nullptr && tid == 0) a.out_lse[hq] = softmax_lse(M, sum, a.scale_log2e);
         return;
     }
     const int len = tracked_len(a, b), row0 = ((int)blockIdx.y - out_groups) * kJoinRows;
     if (row0 >= len) return;
+    // (what the weights are made of is on its way while the sums are joined)
+    constexpr int kRows = kJoinRows / kTrThreads;
+    const float *scores = a.scores + (int64_t)p * G * a.score_stride;
+    float x[kRows][G], old[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int row = min(row0 + i * kTrThreads + tid, len - 1);
+#pragma unroll
+        for (int h = 0; h < G; ++h) x[i][h] = scores[h * a.score_stride + row];
+        old[i] = a.before ? a.before[(int64_t)p * a.weight_rows + row] : 0.f;
+    }
+    const int parts = (len - 1) / a.per + 1;
     for (int h = wv; h < G; h += kTrWaves) {
         float M = kSoftmaxLowest, L = 0.f;
-        for (int s = lane; s < a.n_splits; s += 64) M = fmaxf(M, ml[(int64_t)s * G + h].x);
-        M = wave_max_f32(M);
-        for (int s = lane; s < a.n_splits; s += 64) {
-            const float2 x = ml[(int64_t)s * G + h];
-            L = fmaf(softmax_weight(x.x, M, a.scale_log2e), x.y, L);
+        for (int s = lane; s < parts; s += 64) {
+            const float2 y = ml[(int64_t)s * G + h];
+            const float top = fmaxf(M, y.x);
+            L = fmaf(softmax_weight(y.x, top, a.scale_log2e), y.y, softmax_weight(M, top, a.scale_log2e) * L);
+            M = top;
         }
+        const float top = wave_max_f32(M);
+        L *= softmax_weight(M, top, a.scale_log2e);
+        M = top;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) L += __shfl_xor(L, d, 64);
         // a row's probability is 2^(c (s - M) - log2 of the sum of those); without a key that is there, 0
         if (lane == 0) { sh_m[h] = M; sh_l[h] = L == 0.f ? INFINITY : log2f(L) + kSoftmaxShift; }
     }
     __syncthreads();
-    const float *scores = a.scores + (int64_t)p * G * a.score_stride;
 #pragma unroll
-    for (int i = 0; i < kJoinRows / kTrThreads; ++i) {
+    for (int i = 0; i < kRows; ++i) {
         const int row = row0 + i * kTrThreads + tid;
         if (row >= len) break;
         float w = 0.f;
-        for (int h = 0; h < G; ++h) w += __builtin_amdgcn_exp2f(fmaf(scores[h * a.score_stride + row] - sh_m[h], a.scale_log2e, -sh_l[h]));
-        const int64_t at = (int64_t)p * a.weight_rows + row;
-        a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w;
+#pragma unroll
+        for (int h = 0; h < G; ++h) w += __builtin_amdgcn_exp2f(fmaf(x[i][h] - sh_m[h], a.scale_log2e, -sh_l[h]));
+        a.weights[(int64_t)p * a.weight_rows + row] = a.before ? fmaf(a.decay, old[i], w) : w;
     }
 }
 
-struct TrackedPlan { int splits; int64_t score_stride; size_t bytes; };
+// All parts have as many rows, so that workgroups take as long as each other where sequences do not: kTrMaxSplit, or fewer where that would leave
+// compute units with less than two.  us for 768 / 512 / 1,024 / 2,048 rows: 8 sequences of 20,637 to 32,768 in MX FP4 74 / 77 / 78 / 83, 32 of
+// 7,383 to 16,384 in E4M3 200 / 201 / 201 / 207, one of 200,001 in MX FP4 77 / 82 / 77 / 82; one of 30,001 in bf16, with 128 / 256 / 512 rows
+// 39 / 32 / 29.
+struct TrackedPlan { int splits, per; int64_t score_stride; size_t bytes; };
 static TrackedPlan tracked_plan(const ihip_shape &s)
 {
-    const int64_t total = s.max_seq_len, P = std::max<int64_t>(1, (int64_t)s.B * s.Hkv), places = (int64_t)compute_units() * 2;
-    const int64_t fewest = (total + kTrMaxSplit - 1) / kTrMaxSplit, finest = (total + kTrMinSplit - 1) / kTrMinSplit;
+    const int64_t total = s.max_seq_len, P = std::max<int64_t>(1, (int64_t)s.B * s.Hkv);
     TrackedPlan r;
-    r.splits = (int)std::min(std::max((places + P - 1) / P, fewest), finest);
+    r.per = (int)std::min<int64_t>(kTrMaxSplit, (total * P / (2 * compute_units()) + kTrMinSplit) / kTrMinSplit * kTrMinSplit);
+    r.splits = (int)((total - 1) / r.per + 1);
     r.score_stride = (total + kTrStep - 1) / kTrStep * kTrStep;
     r.bytes = (size_t)s.B * s.Hq * (r.score_stride + (int64_t)r.splits * (2 + kD)) * sizeof(float);
     return r;
@@ -389,9 +421,9 @@ extern "C" int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor
     a.ge = make_geometry(*shape);
     a.max_len = shape->max_seq_len;
     a.q = (const uint16_t *)q.ptr; a.q_sb = q.stride_b; a.q_sh = q.stride_h;
-    a.page_log2 = a.from.paged.block_table ? a.from.paged.page_log2 : 31;
     a.v_scale = a.from.v_scale;
     a.n_splits = plan.splits;
+    a.per = plan.per;
     a.grid = decode_grid(a.ge, a.n_splits, false);
     a.scores = (float *)ws;
     a.score_stride = plan.score_stride;
@@ -418,6 +450,10 @@ extern "C" int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor
     if ((rc = check_launch(who)) != IHIP_OK) return rc;
     const int out_groups = a.n_splits > 1 ? a.ge.G : 0;
     KernelTimer timer("attn_decode_tracked_join", st);
-    hipLaunchKernelGGL(attn_decode_tracked_join_kernel, dim3((uint32_t)P, (uint32_t)(out_groups + join_groups)), dim3(kTrThreads), 0, st, a, out_groups);
+    const dim3 join((uint32_t)P, (uint32_t)(out_groups + join_groups));
+    if (a.ge.G == 1) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<1>, join, dim3(kTrThreads), 0, st, a, out_groups);
+    else if (a.ge.G == 2) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<2>, join, dim3(kTrThreads), 0, st, a, out_groups);
+    else if (a.ge.G == 4) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<4>, join, dim3(kTrThreads), 0, st, a, out_groups);
+    else hipLaunchKernelGGL(attn_decode_tracked_join_kernel<8>, join, dim3(kTrThreads), 0, st, a, out_groups);
     return check_launch(who);
 }
