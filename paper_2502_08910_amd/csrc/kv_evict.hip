@@ -7,7 +7,8 @@
 // its weight in an order-preserving map over its number from the end, so that no two are the same and ties go to the lower row.  What is
 // kept goes down as one bit a row, and the holes below `keep` are matched to the kept rows above it by their ranks.
 //   up to kHeld rows    kv_evict_select_kernel, a workgroup a (sequence, KV head), keys in LDS.  Few rows move within it.
-//   more                in chunks, one workgroup each: digits, candidates, ranks (a launch each: what all chunks have found is read by the next).
+//   more                in chunks, one workgroup each: digits, candidates, ranks (a launch each: what all chunks have found is read by the next);
+//                       of very many rows two digits.  Only where more than kEvictList rows have them does each workgroup look at all rows for the rest.
 //   many moves          kv_evict_move_kernel, 16 lanes a row, four rows of each on their way.
 #include "api_checks.h"
 #include "kv_store.h"
@@ -25,13 +26,14 @@ constexpr int kEvictWords = 2048;                    // words of bits in LDS, th
 constexpr int kFewMoves = 512;                       // of a (sequence, KV head): within the first kernel
 constexpr int kMoveThreads = 256, kMoveAhead = 4, kMoveRows = kMoveThreads / kRowLanes * kMoveAhead;     // places of a workgroup
 constexpr int kEvictLeast = 4096;                    // rows of a chunk
+constexpr int64_t kEvictOneDigit = 131072;           // rows up to which one digit usually leaves no more than kEvictList of them
 constexpr int kEvictMostChunks = 16;                // (all of them look at the histograms of all)
 static_assert(kMoveRows == 64, "a workgroup moves into the rows of one word");
 
 // What is known of a (sequence, KV head) between launches
 struct EvictState {
     int32_t n;                       // rows
-    uint32_t bin, need, count;       // the first digit, how many rows are kept of those that have it, how many have it
+    uint32_t bin, need, count;       // the threshold's first digits, how many rows are kept of those that have them, how many have them
 };
 struct EvictArgs {
     int B, Hkv, max_len, keep, n_sink, n_recent;
@@ -51,7 +53,8 @@ struct EvictArgs {
     int words, most;
     int chunks;
     uint2 *listed;                   // [P, kEvictList]: key and row of the rows with the first digit
-    uint32_t *hist;                  // [P, chunks, kEvictBins]
+    uint32_t *hist;                  // [digits, P, chunks, kEvictBins]
+    int digits;                      // of 12 bits each that histograms of all rows find: 1 or 2
     uint2 *sure;                     // [P, chunks]: rows above the first digit, below `keep` and from there on
     bool set_lens;                   // the select kernel writes new_lens
     StoreView store;
@@ -133,10 +136,10 @@ constexpr int kEvictShift = 63 - 12;
 // The threshold: rows whose composite is at least that are kept, `need` of the `count` rows that have the digits in `from` down to bit `shift`.
 // in_list: they are all listed; otherwise for_rows(f) goes over all rows with f(key, row, there)
 template <class ForRows>
-__device__ inline uint64_t evict_threshold(EvictShared &sh, uint64_t from, uint32_t need, uint32_t count, int in_list, ForRows for_rows)
+__device__ inline uint64_t evict_threshold(EvictShared &sh, uint64_t from, int shift, uint32_t need, uint32_t count, int in_list, ForRows for_rows)
 {
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    for (int shift = kEvictShift; need < count && shift > 0;) {      // (all of a bin: the threshold is the bin's lowest)
+    while (need < count && shift > 0) {              // (all of a bin: the threshold is the bin's lowest)
         const int width = min(shift, 10), low = shift - width;
         evict_clear(sh, 1 << width);                 // (with a barrier, behind which the list is there as well)
         auto look = [&](uint64_t c, bool on) { evict_count(sh, (uint32_t)(c >> low) & ((1u << width) - 1), on && c >> shift == from >> shift); };
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(kEvictThreads) void kv_evict_select_kernel(const Ev
             sh.list.row[at] = row;
         }
     });
-    const uint64_t from = evict_threshold(sh, (uint64_t)bin << kEvictShift, need, count, in_list, for_rows);
+    const uint64_t from = evict_threshold(sh, (uint64_t)bin << kEvictShift, kEvictShift, need, count, in_list, for_rows);
     __syncthreads();
     if (in_list != 0) {
         for (int i = tid; i < in_list; i += kEvictThreads) {
@@ -376,37 +379,65 @@ __device__ inline int evict_chunk(const EvictArgs &a, int n, int c)
     return (int)min(c * size, (int64_t)n);
 }
 
-// How many of a chunk's rows have which first digit
-__global__ __launch_bounds__(kEvictThreads) void kv_evict_digits_kernel(const EvictArgs a)
+// The histograms of all chunks added up, and the bin in which the `need`-th largest is
+__device__ inline void evict_find_in_chunks(EvictDigits &sh, const EvictArgs &a, int p, int digit, uint32_t need)
 {
-    __shared__ __attribute__((aligned(16))) EvictDigits sh;
-    const int p = blockIdx.x, c = blockIdx.y, tid = threadIdx.x, n = evict_len(a, p / a.Hkv);
-    if (c == 0 && tid == 0) a.state[p].n = n;
-    if (n <= a.keep) return;
-    evict_clear(sh, kEvictBins);
-    EvictKeys(a, p).for_rows(evict_chunk(a, n, c), evict_chunk(a, n, c + 1), [&](uint32_t key, int, bool there) { evict_count(sh, key >> 20, there); });
+    const int tid = threadIdx.x;
+    const uint4 *hist = reinterpret_cast<const uint4 *>(a.hist + ((int64_t)digit * gridDim.x + p) * a.chunks * kEvictBins) + tid;
+    uint4 all = make_uint4(0, 0, 0, 0);
+    for (int i0 = 0; i0 < a.chunks; i0 += kAhead) {
+        uint4 x[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) x[i] = hist[(int64_t)min(i0 + i, a.chunks - 1) * (kEvictBins / 4)];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (i0 + i < a.chunks) all = make_uint4(all.x + x[i].x, all.y + x[i].y, all.z + x[i].z, all.w + x[i].w);
+    }
     __syncthreads();
-    reinterpret_cast<uint4 *>(a.hist + ((int64_t)p * a.chunks + c) * kEvictBins)[tid] = reinterpret_cast<const uint4 *>(sh.hist)[tid];
+    reinterpret_cast<uint4 *>(sh.hist)[tid] = all;
+    __syncthreads();
+    evict_find_bin(sh, kEvictBins, need);
 }
 static_assert(kEvictBins == 4 * kEvictThreads, "");
 
-// The threshold's first digit; rows above it are kept, those that have it are listed, each chunk's in its place
+// How many of a chunk's rows have which first digit, or which second one of those that have the threshold's first
+template <int DIGIT>
+__global__ __launch_bounds__(kEvictThreads) void kv_evict_digits_kernel(const EvictArgs a)
+{
+    __shared__ __attribute__((aligned(16))) EvictDigits sh;
+    const int p = blockIdx.x, c = blockIdx.y, tid = threadIdx.x, n = DIGIT == 0 ? evict_len(a, p / a.Hkv) : a.state[p].n;
+    if (DIGIT == 0 && c == 0 && tid == 0) a.state[p].n = n;
+    if (n <= a.keep) return;
+    uint32_t bin = 0;
+    if (DIGIT == 1) {
+        evict_find_in_chunks(sh, a, p, 0, a.keep);
+        bin = sh.digit;
+    }
+    evict_clear(sh, kEvictBins);
+    EvictKeys(a, p).for_rows(evict_chunk(a, n, c), evict_chunk(a, n, c + 1), [&](uint32_t key, int, bool there) {
+        if constexpr (DIGIT == 0) evict_count(sh, key >> 20, there);
+        else evict_count(sh, key >> 8 & (kEvictBins - 1), there && key >> 20 == bin);
+    });
+    __syncthreads();
+    reinterpret_cast<uint4 *>(a.hist + (((int64_t)DIGIT * gridDim.x + p) * a.chunks + c) * kEvictBins)[tid] = reinterpret_cast<const uint4 *>(sh.hist)[tid];
+}
+
+// The threshold's first digits; rows above them are kept, those that have them are listed, each chunk's in its place
 __global__ __launch_bounds__(kEvictThreads) void kv_evict_candidates_kernel(const EvictArgs a)
 {
     __shared__ __attribute__((aligned(16))) EvictDigits sh;
     const int p = blockIdx.x, c = blockIdx.y, tid = threadIdx.x, lane = tid & 63, n = a.state[p].n, keep = a.keep;
     if (n <= keep) return;
-    const uint32_t *hist = a.hist + (int64_t)p * a.chunks * kEvictBins;
-    uint4 all = make_uint4(0, 0, 0, 0);
-    for (int i = 0; i < a.chunks; ++i) {
-        const uint4 x = reinterpret_cast<const uint4 *>(hist + (int64_t)i * kEvictBins)[tid];
-        all = make_uint4(all.x + x.x, all.y + x.y, all.z + x.z, all.w + x.w);
-    }
-    reinterpret_cast<uint4 *>(sh.hist)[tid] = all;
     if (tid == 0) sh.listed = sh.sum[0] = sh.sum[1] = 0;
-    __syncthreads();
-    evict_find_bin(sh, kEvictBins, keep);
-    const uint32_t bin = sh.digit, need = sh.left, count = sh.count;
+    evict_find_in_chunks(sh, a, p, 0, keep);
+    uint32_t bin = sh.digit, need = sh.left, count = sh.count;
+    if (a.digits == 2) {
+        evict_find_in_chunks(sh, a, p, 1, need);
+        bin = bin << 12 | sh.digit;
+        need = sh.left;
+        count = sh.count;
+    }
+    const int shift = 32 - 12 * a.digits;
     if (c == 0 && tid == 0) {
         a.state[p].bin = bin;
         a.state[p].need = need;
@@ -414,22 +445,25 @@ __global__ __launch_bounds__(kEvictThreads) void kv_evict_candidates_kernel(cons
     }
     const bool list = need < count && count <= kEvictList;
     uint32_t at0 = 0;
-    if (list)
-        for (int i = lane; i < c; i += 64) at0 += hist[(int64_t)i * kEvictBins + bin];
+    if (list) {
+        const uint32_t *hist = a.hist + ((int64_t)(a.digits - 1) * gridDim.x + p) * a.chunks * kEvictBins + (bin & (kEvictBins - 1));
+        for (int i = lane; i < c; i += 64) at0 += hist[(int64_t)i * kEvictBins];
+    }
     at0 = wave_sum_u32(at0);
     uint64_t *bits = a.bits + (int64_t)p * a.words;
     uint2 *listed = a.listed + (int64_t)p * kEvictList;
     uint32_t below = 0, beyond = 0;                  // of this wave
     EvictKeys(a, p).for_rows(evict_chunk(a, n, c), evict_chunk(a, n, c + 1), [&](uint32_t key, int row, bool there) {
         // (a bin that is kept whole goes with those above it)
-        const uint64_t word = __ballot(there && (key >> 20 > bin || (need == count && key >> 20 == bin)));
+        const bool has = key >> shift == bin;
+        const uint64_t word = __ballot(there && (key >> shift > bin || (need == count && has)));
         if (lane == 0 && there) {
             bits[row >> 6] = word;
             const uint64_t mask = evict_below(keep, row >> 6);
             below += __popcll(word & mask);
             beyond += __popcll(word & ~mask);
         }
-        if (list && there && key >> 20 == bin) {
+        if (list && there && has) {
             const uint32_t at = at0 + atomicAdd(&sh.listed, 1u);
             if (at < kEvictList) listed[at] = make_uint2(key, row);
         }
@@ -471,7 +505,8 @@ __global__ __launch_bounds__(kEvictThreads) void kv_evict_ranks_kernel(const Evi
     }
     if (tid == 0) sh.sum[0] = sh.sum[1] = 0;
     const EvictKeys keys(a, p);
-    const uint64_t from = evict_threshold(sh, (uint64_t)state.bin << kEvictShift, state.need, state.count, in_list, [&](auto f) { keys.for_rows(0, n, f); });
+    const int shift = 63 - 12 * a.digits;
+    const uint64_t from = evict_threshold(sh, (uint64_t)state.bin << shift, shift, state.need, state.count, in_list, [&](auto f) { keys.for_rows(0, n, f); });
     __syncthreads();
     if (in_list != 0) {
         for (int i = tid; i < in_list; i += kEvictThreads) {
@@ -543,6 +578,7 @@ __global__ __launch_bounds__(kMoveThreads) void kv_evict_lens_kernel(const Evict
 struct EvictPlan {
     bool few, chunked;
     int64_t words, most, chunks;
+    int digits;
     size_t bytes, listed, hist, sure, state, bits, before, movers;   // all of scratch, and where in it
 };
 static EvictPlan evict_plan(int64_t B, int64_t Hkv, int64_t max_len, int64_t keep)
@@ -568,7 +604,8 @@ static EvictPlan evict_plan(int64_t B, int64_t Hkv, int64_t max_len, int64_t kee
     if (!r.chunked) return r;
     r.listed = take(P * kEvictList * sizeof(uint2));
     r.sure = take(P * r.chunks * sizeof(uint2));
-    r.hist = take(P * r.chunks * kEvictBins * sizeof(uint32_t));
+    r.digits = max_len > kEvictOneDigit ? 2 : 1;
+    r.hist = take(r.digits * P * r.chunks * kEvictBins * sizeof(uint32_t));
     return r;
 }
 // (dynamic LDS beyond the 64 KiB that need no leave)
@@ -631,7 +668,7 @@ extern "C" int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track
     a.to_weights = to->weights; a.to_positions = to->positions; a.to_rows = to->rows;
     a.kept = kept; a.new_lens = new_lens;
     uint8_t *const scratch = (uint8_t *)ws;
-    a.words = (int)plan.words; a.most = (int)plan.most; a.chunks = (int)plan.chunks;
+    a.words = (int)plan.words; a.most = (int)plan.most; a.chunks = (int)plan.chunks; a.digits = plan.digits;
     a.state = (EvictState *)(scratch + plan.state);
     a.bits = (uint64_t *)(scratch + plan.bits);
     a.before = (uint2 *)(scratch + plan.before);
@@ -654,7 +691,8 @@ extern "C" int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track
         const dim3 grid((uint32_t)P, (uint32_t)plan.chunks);
         {
             KernelTimer timer("kv_evict_digits", st);
-            hipLaunchKernelGGL(kv_evict_digits_kernel, grid, dim3(kEvictThreads), 0, st, a);
+            hipLaunchKernelGGL(kv_evict_digits_kernel<0>, grid, dim3(kEvictThreads), 0, st, a);
+            if (a.digits == 2) hipLaunchKernelGGL(kv_evict_digits_kernel<1>, grid, dim3(kEvictThreads), 0, st, a);
         }
         if ((rc = check_launch(who)) != IHIP_OK) return rc;
         {

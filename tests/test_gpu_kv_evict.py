@@ -139,11 +139,14 @@ def test_lengths_beyond_the_bound(ihip):
     assert (kept[0, 0].cpu().numpy() == m).all() and (kept[1] == -1).all()
 
 
-@pytest.mark.parametrize("Hkv,lens,keep", [(2, [70001, 66000], 20000), (1, [262144 + 77], 1000)])
-def test_long(ihip, Hkv, lens, keep):
+@pytest.mark.parametrize("Hkv,lens,keep,equal", [(2, [70001, 66000], 20000, False), (1, [262144 + 77], 1000, False), (1, [200003, 4], 50000, True), (1, [140000], 139000, False)])
+def test_long(ihip, Hkv, lens, keep, equal):
+    """equal: a tenth of the rows has the weight at which the kept ones end."""
     c = Cache(ihip, "mx4", lens, Hkv, 64, seed=5)
     g = torch.Generator().manual_seed(9)
     w = torch.randn((len(lens), Hkv, c.T), generator=g).mul(2).exp()
+    if equal:
+        w[torch.rand(w.shape, generator=g) < 0.1] = float(w[0, 0].sort(descending=True).values[keep])
     pos = torch.arange(c.T, dtype=torch.int32).repeat(len(lens), Hkv, 1)
     check(ihip, c, ihip.KVTrack(w.cuda(), pos.cuda(), c.seq_lens.clone()), keep, 4, 64, in_place=False)
 
