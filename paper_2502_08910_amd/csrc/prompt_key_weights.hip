@@ -33,6 +33,7 @@ struct KeyWeightArgs {
     int weight_rows;
     int chunk_tiles, chunks;         // tiles of a chunk, from the sequence's end; chunks that a sequence can have
     float *part;                     // [chunk, Hkv, rows_k], or null: one chunk
+    int window_rows, wg_keys, log2_G;        // rows in LDS, keys of a workgroup of the window's kernel; -1: G is not a power of two
     bool near;                       // G divides a tile's rows, whose queries are less than 2^31 bytes apart
 };
 
@@ -75,6 +76,123 @@ __device__ inline void key_weights_to_lds(uint32_t dst, const uint16_t *base, ui
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(byte_off), "s"(base) : "memory");
 }
 
+// A wave's SETS times 32 keys and what has been added up for them.  Rows come half a tile at a time: the products of 32 rows with the keys, and between
+// them, two scores after each, the exponentials of the half before.  Score i is that of row 8 (i / 4) + 4 half + i % 4.
+struct KeyWeightTile { const uint16_t *q; const float *r; const int *last; };        // 64 rows in LDS: chunks XORed with the row; r; the last key
+template <int SETS>
+struct KeyWeightWave {
+    static constexpr int kOps = 3;                   // operands that are read ahead of their use
+    int n, half, kw;                                 // lane's key and half, first key
+    float scale_log2e;
+    bf16x8 kb[SETS][8];                              // (behind the last key: that one again)
+    f32x16 c[2][SETS];                               // of the present and the previous half
+    float part_sum[SETS], near_sum[SETS];
+    bf16x8 x[kOps + 1];
+    float4 r4[2];
+
+    __device__ KeyWeightWave(int lane, float scale) : n(lane & 31), half(lane >> 5), scale_log2e(scale) {}
+    __device__ void load_keys(const KeyWeightArgs &a, const KeyWeightSeq &seq, int g, int first, bf16x8 (&to)[SETS][8]) const
+    {
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) {
+            const uint16_t *kp = a.k + (int64_t)(seq.k_first + min(first + 32 * s + n, seq.nk - 1)) * a.k_st + g * a.k_sh + half * 8;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) to[s][ks] = *reinterpret_cast<const bf16x8 *>(kp + ks * 16);
+        }
+    }
+    __device__ void begin(int first)
+    {
+        kw = first;
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) near_sum[s] = 0.f;
+    }
+    // The keys are waited for here: in the loop the compiler, which does not know what has been waited for in assembly, would wait for all loads at
+    // their use
+    __device__ void keys_are_there()
+    {
+#pragma unroll
+        for (int s = 0; s < SETS; ++s)
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(kb[s][ks]));
+    }
+    __device__ bf16x8 operand(const KeyWeightTile &t, int h, int ks) const { return *reinterpret_cast<const bf16x8 *>(t.q + (32 * h + n) * kD + (((ks * 2 + half) ^ (n & 15)) << 3)); }
+    __device__ float4 rows_r(const KeyWeightTile &t, int h, int i4) const { return *reinterpret_cast<const float4 *>(t.r + 32 * h + 8 * i4 + 4 * half); }
+    static __device__ float element(const float4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+    // score i of set s; r: that of its row
+    template <bool MASKED>
+    __device__ void exponential(const KeyWeightTile &t, int h, int i, int s, float r)
+    {
+        float w = __builtin_amdgcn_exp2f(fmaf(c[h][s][i], scale_log2e, -r));
+        if constexpr (MASKED) w = kw + 32 * s + n <= t.last[32 * h + 8 * (i / 4) + 4 * half + i % 4] ? w : 0.f;
+        part_sum[s] = i == 0 ? w : part_sum[s] + w;
+        if (i == 15) near_sum[s] += part_sum[s];
+    }
+    // Of half h, and of the r of the half before, if there is one
+    template <bool BEFORE>
+    __device__ void first_operands(const KeyWeightTile &t, int h, const KeyWeightTile &before)
+    {
+#pragma unroll
+        for (int ks = 0; ks < kOps; ++ks) x[ks] = operand(t, h, ks);
+        if constexpr (BEFORE) r4[0] = rows_r(before, 1 - h, 0);
+    }
+    // products of half h, whose first operands have been asked for; exponentials of the half before, MASKED if not all of its rows see all keys
+    template <bool MASKED, bool BEFORE>
+    __device__ void half_tile(const KeyWeightTile &t, int h, const KeyWeightTile &before)
+    {
+#pragma unroll
+        for (int i = 0; i < 8 * SETS; ++i) {
+            const int ks = i / SETS, s = i % SETS, score = 2 * i / SETS;
+            if (s == 0 && ks + kOps < 8) x[(ks + kOps) % (kOps + 1)] = operand(t, h, ks + kOps);
+            if (BEFORE && score % 4 == 0 && score < 12) r4[(score / 4 + 1) % 2] = rows_r(before, 1 - h, score / 4 + 1);
+            c[h][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[ks % (kOps + 1)], kb[s][ks], ks == 0 ? f32x16{} : c[h][s], 0, 0, 0);
+            if constexpr (BEFORE) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int e = (2 * i + u) / SETS;
+                    exponential<MASKED>(before, 1 - h, e, (2 * i + u) % SETS, element(r4[(e / 4) % 2], e % 4));
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __device__ void half_tile(const KeyWeightTile &t, int h, const KeyWeightTile &before, bool masked)
+    {
+        if (masked) half_tile<true, true>(t, h, before);
+        else half_tile<false, true>(t, h, before);
+    }
+    template <bool MASKED>
+    __device__ void last_half(const KeyWeightTile &t)
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float4 r = rows_r(t, 1, i / 4);
+#pragma unroll
+            for (int s = 0; s < SETS; ++s) exponential<MASKED>(t, 1, i, s, element(r, i % 4));
+        }
+    }
+    __device__ void last_half(const KeyWeightTile &t, bool masked)
+    {
+        if (masked) last_half<true>(t);
+        else last_half<false>(t);
+    }
+    // f(key, sum), a lane a key
+    template <class F>
+    __device__ void for_keys(const float (&sum)[SETS], F f) const
+    {
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) {
+            const float w = sum[s] + __shfl_xor(sum[s], 32, 64);
+            if (half == s % 2) f(kw + 32 * s + n, w);
+        }
+    }
+};
+__device__ inline void store_key_weight(const KeyWeightArgs &a, int b, int g, int key, float w)
+{
+    if (key >= a.weight_rows) return;
+    const int64_t at = ((int64_t)b * a.Hkv + g) * a.weight_rows + key;
+    a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w;
+}
+
 // SETS of 32 keys a wave
 template <int SETS>
 __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weights_kernel(const KeyWeightArgs a)
@@ -83,7 +201,6 @@ __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weig
     __shared__ __attribute__((aligned(16))) float sh_r[3][kKwRows];          // of a tile's rows: r, and the last key
     __shared__ __attribute__((aligned(16))) int sh_last[3][kKwRows];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 31, half = lane >> 5;
     const int g = blockIdx.x % a.Hkv, id = blockIdx.x / a.Hkv;
     constexpr int kKeys = kKwKeys<SETS>;
     const KeyWeightSeq seq(a, kKeys, id, lane);
@@ -94,15 +211,9 @@ __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weig
     const int tiles = seq.tiles(), begin = seq.first_tile(a, k0);
     const int end = tiles - (int)min((int64_t)blockIdx.y * a.chunk_tiles, (int64_t)tiles), t0 = max(begin, end - a.chunk_tiles);
     if (blockIdx.y > 0 && t0 >= end) return;
-    const int kw = k0 + wave * 32 * SETS;                   // this wave's first key
-
-    bf16x8 kb[SETS][8];                                 // (behind the last key: that one again)
-#pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-        const uint16_t *kp = a.k + (int64_t)(seq.k_first + min(kw + 32 * s + n, seq.nk - 1)) * a.k_st + g * a.k_sh + half * 8;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) kb[s][ks] = *reinterpret_cast<const bf16x8 *>(kp + ks * 16);
-    }
+    KeyWeightWave<SETS> keys(lane, a.scale_log2e);
+    keys.begin(k0 + wave * 32 * SETS);
+    keys.load_keys(a, seq, g, keys.kw, keys.kb);
 
     // A thread's rows of a tile, of which it brings 16-byte pieces, and another one, whose r it brings.  The next tile's are 64 rows less: addresses go on
     // by differences (multiplications take four times as long as additions)
@@ -156,7 +267,7 @@ __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weig
         last = r_query + seq.ahead;
     };
 
-    float sum[SETS] = {}, near_sum[SETS] = {};
+    float sum[SETS] = {};
     if (t0 < end) {                                  // the first tile: rows behind the last one stand for that one
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) send(0, i, last_row + in_tile(i) < seq.rows ? q_at[i] : q_of(seq.nq - 1, a.G - 1, i));
@@ -166,93 +277,40 @@ __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weig
             sh_last[0][tid] = there ? r_query + seq.ahead : -1;
         }
     }
-    // the keys are waited for here: in the loop the compiler, which does not know what has been waited for in assembly, would wait for all loads at their use
-#pragma unroll
-    for (int s = 0; s < SETS; ++s)
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(kb[s][ks]));
+    keys.keys_are_there();
 
-    // Half a tile at a time: the products of 32 rows with the wave's keys, and between them, two scores after each, the exponentials of the half
-    // before.  Score i is that of row 8 (i / 4) + 4 half + i % 4.
-    f32x16 c[2][SETS];                                  // of the present and the previous half
-    auto operand = [&](int st, int h, int ks) { return *reinterpret_cast<const bf16x8 *>(&sh_q[st][(32 * h + n) * kD + (((ks * 2 + half) ^ (n & 15)) << 3)]); };
-    float part_sum[SETS];
-    // score i of set s; r: that of its row
-    auto exponential = [&](int h, int st3, int i, int s, auto masked, float r) {
-        float w = __builtin_amdgcn_exp2f(fmaf(c[h][s][i], a.scale_log2e, -r));
-        if constexpr (decltype(masked)::value) w = kw + 32 * s + n <= sh_last[st3][32 * h + 8 * (i / 4) + 4 * half + i % 4] ? w : 0.f;
-        part_sum[s] = i == 0 ? w : part_sum[s] + w;
-        if (i == 15) near_sum[s] += part_sum[s];
-    };
-    auto element = [](const float4 &x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; };
-    auto rows_r = [&](int h, int st3, int i4) { return *reinterpret_cast<const float4 *>(&sh_r[st3][32 * h + 8 * i4 + 4 * half]); };
-    // products of half h of the tile in stage st, exponentials of the other half (`other`: stage of its r), if there are any.  The first operands
-    // have been asked for; those of half 1 are at the end of half 0
-    constexpr int kOps = 3;                          // operands that are read ahead of their use
-    bf16x8 x[kOps + 1];
-    float4 r4[2];
-    auto first_operands = [&](int st, int h, int other, auto any) {
-#pragma unroll
-        for (int ks = 0; ks < kOps; ++ks) x[ks] = operand(st, h, ks);
-        if constexpr (decltype(any)::value) r4[0] = rows_r(1 - h, other, 0);
-    };
-    auto half_tile = [&](int h, int st, int other, auto masked, auto any) {
-#pragma unroll
-        for (int i = 0; i < 8 * SETS; ++i) {
-            const int ks = i / SETS, s = i % SETS, score = 2 * i / SETS;
-            if (s == 0 && ks + kOps < 8) x[(ks + kOps) % (kOps + 1)] = operand(st, h, ks + kOps);
-            if (decltype(any)::value && score % 4 == 0 && score < 12) r4[(score / 4 + 1) % 2] = rows_r(1 - h, other, score / 4 + 1);
-            c[h][s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[ks % (kOps + 1)], kb[s][ks], ks == 0 ? f32x16{} : c[h][s], 0, 0, 0);
-            if constexpr (decltype(any)::value) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int e = (2 * i + u) / SETS;
-                    exponential(1 - h, other, e, (2 * i + u) % SETS, masked, element(r4[(e / 4) % 2], e % 4));
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    auto last_half = [&](int st3, auto masked) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float4 r = rows_r(1, st3, i / 4);
-#pragma unroll
-            for (int s = 0; s < SETS; ++s) exponential(1, st3, i, s, masked, element(r, i % 4));
-        }
-    };
     int first_query = (seq.row0 + (end - 1) * kKwRows) / a.G;        // that of a tile's first row
     int first_head = seq.row0 + (end - 1) * kKwRows - first_query * a.G;
-    bool whole_before = true;
-    int st3 = 0, before3 = 2;                        // stages of r
+    bool masked_before = false;
+    int st3 = 0;                                     // stage of r
+    KeyWeightTile before{};
     for (int t = end - 1, st = 0; t >= t0; --t, st ^= 1) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (t == end - 1) first_operands(st, 0, before3, std::false_type{});
-        else first_operands(st, 0, before3, std::true_type{});
+        const KeyWeightTile tile{sh_q[st], sh_r[st3], sh_last[st3]};
+        if (t == end - 1) keys.template first_operands<false>(tile, 0, before);
+        else keys.template first_operands<true>(tile, 0, before);
         float r_next;
         int last_next;
         if (t > t0) {
             request(st ^ 1);
             if (tid < kKwRows) row_info(r_next, last_next);
         }
-        // all rows see all of the wave's keys (and the last tile's last rows are there)
-        const bool whole = first_query + seq.ahead >= kw + 32 * SETS - 1 && seq.row0 + (t + 1) * kKwRows <= seq.rows;
-        if (t == end - 1) half_tile(0, st, before3, std::true_type{}, std::false_type{});
-        else if (whole_before) half_tile(0, st, before3, std::false_type{}, std::true_type{});
-        else half_tile(0, st, before3, std::true_type{}, std::true_type{});
+        // not all rows see all of the wave's keys, or the last tile's last rows are not there
+        const bool masked = first_query + seq.ahead < keys.kw + 32 * SETS - 1 || seq.row0 + (t + 1) * kKwRows > seq.rows;
+        if (t == end - 1) keys.template half_tile<true, false>(tile, 0, before);
+        else keys.half_tile(tile, 0, before, masked_before);
         if ((end - t) % kSumTiles == 0) {
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
-                sum[s] += near_sum[s];
-                near_sum[s] = 0.f;
+                sum[s] += keys.near_sum[s];
+                keys.near_sum[s] = 0.f;
             }
         }
-        first_operands(st, 1, st3, std::true_type{});
-        if (whole) half_tile(1, st, st3, std::false_type{}, std::true_type{});
-        else half_tile(1, st, st3, std::true_type{}, std::true_type{});
-        whole_before = whole;
-        before3 = st3;
+        keys.template first_operands<true>(tile, 1, tile);
+        keys.half_tile(tile, 1, tile, masked);
+        masked_before = masked;
+        before = tile;
         st3 = st3 == 2 ? 0 : st3 + 1;
         first_query -= per_tile;
         first_head -= heads_left;
@@ -262,23 +320,82 @@ __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weig
             sh_last[st3][tid] = last_next;
         }
     }
-    if (t0 < end) {
-        if (whole_before) last_half(before3, std::false_type{});
-        else last_half(before3, std::true_type{});
+    if (t0 < end) keys.last_half(before, masked_before);
 #pragma unroll
-        for (int s = 0; s < SETS; ++s) sum[s] += near_sum[s];
+    for (int s = 0; s < SETS; ++s) sum[s] += keys.near_sum[s];
+    keys.for_keys(sum, [&](int key, float w) {
+        if (key >= seq.nk) return;
+        if (a.part) a.part[((int64_t)blockIdx.y * a.Hkv + g) * a.rows_k + seq.k_first + key] = w;
+        else store_key_weight(a, b, g, key, w);
+    });
+}
+
+// Few rows, as of a window: they stay in LDS, and each wave goes through keys by itself, the next 32 on their way under the products of the present ones
+// (so many that a compute unit has room for two workgroups: 512 rows, one of them, 49 us where the other kernel takes 47)
+constexpr int kWindowRows = 256;
+__global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_window_kernel(const KeyWeightArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = blockIdx.x % a.Hkv, id = blockIdx.x / a.Hkv;
+    const KeyWeightSeq seq(a, a.wg_keys, id, lane);
+    const int b = seq.b;
+    if (b < 0) return;
+    const int block = id - (seq.k_first / a.wg_keys + b), k0 = block * a.wg_keys, k1 = min(k0 + a.wg_keys, seq.nk);
+    if (block < 0 || k0 >= k1) return;
+    constexpr int kStep = 32 * kKwWaves;
+    KeyWeightWave<1> keys(lane, a.scale_log2e);
+    int first = k0 + wave * 32;
+    keys.load_keys(a, seq, g, first, keys.kb);
+    // (of more rows than there is room for, which is what max_q says, the last)
+    const int row0 = max(seq.row0, seq.rows - a.window_rows), rows = seq.rows - row0, tiles = (rows + kKwRows - 1) / kKwRows;
+    float *const sh_r = reinterpret_cast<float *>(smem + a.window_rows * kD);
+    int *const sh_last = reinterpret_cast<int *>(sh_r + a.window_rows);
+    auto query_of = [&](int row) { return a.log2_G >= 0 ? row >> a.log2_G : row / a.G; };
+    const uint16_t *const qb = a.q + (int64_t)seq.q_first * a.q_st + (int64_t)g * a.G * a.q_sh;
+    const float *const lse = a.lse + (int64_t)seq.q_first * a.Hq + g * a.G;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
+    for (int i = wave; i < tiles * (kKwRows / 4); i += kKwWaves) {         // four rows; those behind the last one stand for that one
+        const int in_tile = 4 * i + (lane >> 4), row = row0 + min(in_tile, rows - 1), query = query_of(row);
+        global_to_lds(lds0 + i * 4 * kD * 2, qb + query * a.q_st + (row - query * a.G) * a.q_sh + (((lane & 15) ^ (in_tile & 15)) << 3));
     }
-#pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-        const float w = sum[s] + __shfl_xor(sum[s], 32, 64);
-        const int key = kw + 32 * s + n;
-        if (half != s % 2 || key >= seq.nk) continue;
-        if (a.part) {
-            a.part[((int64_t)blockIdx.y * a.Hkv + g) * a.rows_k + seq.k_first + key] = w;
-        } else if (key < a.weight_rows) {
-            const int64_t at = ((int64_t)b * a.Hkv + g) * a.weight_rows + key;
-            a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w;
+    for (int i = tid; i < tiles * kKwRows; i += kKwThreads) {
+        const int row = row0 + min(i, rows - 1), query = query_of(row);
+        sh_r[i] = lse[(int64_t)query * a.Hq + row - query * a.G] * 1.44269504088896340736f;
+        sh_last[i] = i < rows ? query + seq.ahead : -1;
+    }
+    keys.keys_are_there();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    auto tile_of = [&](int t) { return KeyWeightTile{smem + t * kKwRows * kD, sh_r + t * kKwRows, sh_last + t * kKwRows}; };
+    for (; first < k1; first += kStep) {
+        keys.begin(first);
+        bf16x8 next[1][8];
+        keys.load_keys(a, seq, g, first + kStep, next);      // (behind the last key: that one again)
+        bool masked_before = false;
+        const int t0 = min((int)(max((int64_t)0, ((int64_t)first - seq.ahead) * a.G - row0) / kKwRows), tiles);
+        for (int t = t0; t < tiles; ++t) {
+            const KeyWeightTile tile = tile_of(t), before = tile_of(max(t - 1, 0));
+            const bool masked = __builtin_amdgcn_readfirstlane(tile.last[0]) < first + 31 || (t + 1) * kKwRows > rows;
+            if (t == t0) {
+                keys.first_operands<false>(tile, 0, before);
+                keys.half_tile<true, false>(tile, 0, before);
+            } else {
+                keys.first_operands<true>(tile, 0, before);
+                keys.half_tile(tile, 0, before, masked_before);
+            }
+            keys.first_operands<true>(tile, 1, tile);
+            keys.half_tile(tile, 1, tile, masked);
+            masked_before = masked;
         }
+        if (t0 < tiles) keys.last_half(tile_of(tiles - 1), masked_before);
+        const float sum[1] = {keys.near_sum[0]};
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) keys.kb[0][ks] = next[0][ks];
+        keys.keys_are_there();                       // (in front of the store, which would be waited for as well)
+        keys.for_keys(sum, [&](int key, float w) {
+            if (key < k1) store_key_weight(a, b, g, key, w);
+        });
     }
 }
 
@@ -295,19 +412,27 @@ __global__ __launch_bounds__(kKwKeys<SETS>) void prompt_key_weights_sum_kernel(c
     const int chunks = min(a.chunks, max(1, (seq.tiles() - seq.first_tile(a, k0) + a.chunk_tiles - 1) / a.chunk_tiles));
     float w = 0.f;
     for (int c = 0; c < chunks; ++c) w += a.part[((int64_t)c * a.Hkv + g) * a.rows_k + seq.k_first + key];
-    const int64_t at = ((int64_t)b * a.Hkv + g) * a.weight_rows + key;
-    a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w;
+    store_key_weight(a, b, g, key, w);
 }
 
 // Wide blocks of keys, which read the queries half as often, where there is work for many rounds of workgroups, narrow ones otherwise; queries in
 // chunks of about the tiles that give each compute unit 8 of them (48 where blocks are wide: the blocks of a long prompt differ).  us, wide / narrow:
-// 33,625 tokens in three prompts 1,634 / 1,792, 7,401 in four 98 to 105 / 89, 1,024 27 / 16, the last 64 queries of 32,749 30 / 30.
-struct KeyWeightPlan { int sets; int64_t blocks; int chunk_tiles, chunks; size_t bytes; };
+// 33,625 tokens in three prompts 1,634 / 1,792, 7,401 in four 98 to 105 / 89, 1,024 27 / 16.  Rows that fit LDS: the window's kernel (the last 16,
+// 32 and 64 queries of 32,749, 32 heads on 8, 15.3, 19.2 and 25.7 where narrow blocks take 18.4, 22.3 and 30.3), with two workgroups a compute unit.
+struct KeyWeightPlan { int sets; int64_t blocks; int chunk_tiles, chunks; size_t bytes; int window_rows, wg_keys; };       // window_rows: 0, or the window's kernel
 static KeyWeightPlan key_weight_plan(const ihip_packed &p, int rows_k, int window)
 {
     constexpr int kLeast = 4;                        // tiles of a chunk
     const int64_t G = p.Hq / p.Hkv, most = std::max<int64_t>(1, ((int64_t)std::min({p.max_q, window, p.rows}) * G + kKwRows - 1) / kKwRows);
-    KeyWeightPlan r;
+    KeyWeightPlan r{};
+    if (most * kKwRows <= kWindowRows) {
+        r.window_rows = (int)most * kKwRows;
+        const int64_t each = 32 * kKwWaves, all = (rows_k / each + p.B) * p.Hkv;
+        r.wg_keys = (int)(each * std::min<int64_t>(std::max<int64_t>(all / (2 * (int64_t)compute_units()), 1), 64));
+        r.blocks = rows_k / r.wg_keys + p.B;
+        r.chunks = 1;
+        return r;
+    }
     auto tiles = [&](int64_t keys) { return (r.blocks = rows_k / keys + p.B) * p.Hkv * most; };
     r.sets = tiles(kKwKeys<2>) >= 512 * (int64_t)compute_units() ? 2 : 1;
     const int64_t all = tiles(r.sets == 1 ? kKwKeys<1> : kKwKeys<2>), want = std::max<int64_t>(kLeast, all / ((r.sets == 1 ? 8 : 48) * (int64_t)compute_units()));
@@ -368,7 +493,17 @@ extern "C" int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tenso
     a.chunks = parts ? plan.chunks : 1;
     a.part = parts ? (float *)ws : nullptr;
     const dim3 grid((uint32_t)(plan.blocks * a.Hkv), parts ? plan.chunks : 1);
+    a.window_rows = plan.window_rows;
+    a.wg_keys = plan.wg_keys;
+    a.log2_G = pow2(a.G) ? __builtin_ctz(a.G) : -1;
     const hipStream_t st = (hipStream_t)stream;
+    if (plan.window_rows > 0) {
+        const int lds = plan.window_rows * (kD * (int)sizeof(uint16_t) + 8);
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_key_weights_window_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        KernelTimer timer("prompt_key_weights_window", st);
+        hipLaunchKernelGGL(prompt_key_weights_window_kernel, grid, dim3(kKwThreads), lds, st, a);
+        return check_launch(who);
+    }
     {
         KernelTimer timer("prompt_key_weights", st);
         if (plan.sets == 1) hipLaunchKernelGGL(prompt_key_weights_kernel<1>, grid, dim3(kKwThreads), 0, st, a);
