@@ -87,6 +87,16 @@ struct EvictHeldShared : EvictShared {
     uint32_t held[kHeld];
 };
 
+// Sum of what the waves before this one have left
+__device__ inline uint32_t evict_waves_before(const uint32_t (&tot)[kEvictWaves], int lane, int wv)
+{
+    static_assert(kEvictWaves == 16, "a row of 16 lanes");
+    uint32_t v = (lane & 15) < wv ? tot[lane & 15] : 0u;
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true);       // quad_perm [1,0,3,2]
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true);       // quad_perm [2,3,0,1]
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true);      // row_half_mirror
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, true);        // row_mirror
+}
 // Of `bins` bins, the one from which the `need`-th largest comes: its number, what of `need` is left in it, and its rows
 __device__ inline void evict_find_bin(EvictDigits &sh, int bins, uint32_t need)
 {
@@ -99,7 +109,7 @@ __device__ inline void evict_find_bin(EvictDigits &sh, int bins, uint32_t need)
     uint32_t incl = wave_scan_u32(mine, lane);
     if (lane == 63) sh.wave_tot[0][wv] = incl;
     __syncthreads();
-    for (int w = 0; w < wv; ++w) incl += sh.wave_tot[0][w];
+    incl += evict_waves_before(sh.wave_tot[0], lane, wv);
     uint32_t above = incl - mine;
     if (above < need && incl >= need) {
 #pragma unroll
@@ -180,7 +190,8 @@ __device__ inline void evict_ranks(EvictDigits &sh, const uint64_t *bits, uint2 
     __syncthreads();
     hole_at += holes_incl - holes;
     mover_at += movers_incl - movers;
-    for (int w = 0; w < wv; ++w) { hole_at += sh.wave_tot[0][w]; mover_at += sh.wave_tot[1][w]; }
+    hole_at += evict_waves_before(sh.wave_tot[0], lane, wv);
+    mover_at += evict_waves_before(sh.wave_tot[1], lane, wv);
     for (int w = first; w < end; ++w) {
         const uint64_t x = bits[w - w0], mask = evict_below(keep, w);
         before[w - w0] = make_uint2(hole_at, mover_at);
@@ -657,6 +668,9 @@ extern "C" int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track
     const int64_t row = store->format == IHIP_KV_BF16 ? 2 * kD : store->format == IHIP_KV_E4M3 ? kD : kD / 2;
     if (Hkv > 1 && (std::abs(a.store.k_sh) < row || std::abs(a.store.v_sh) < row))
         return fail(IHIP_ERR_INVALID_ARG, "%s: the heads of the store overlap", who);
+    const uintptr_t lens_at = (uintptr_t)seq_lens, new_at = (uintptr_t)new_lens, lens_bytes = B * sizeof(int32_t);
+    const bool apart = new_at + lens_bytes <= lens_at || lens_at + lens_bytes <= new_at;
+    if (!apart && new_at != lens_at) return fail(IHIP_ERR_INVALID_ARG, "%s: new_lens overlaps seq_lens in part", who);
     const EvictPlan plan = evict_plan(B, Hkv, max_seq_len, keep);
     if (plan.bytes > 0 && (!ws || ((uintptr_t)ws & 15) || ws_bytes < plan.bytes))
         return fail(IHIP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 16-byte aligned, needed, %zu given", who, plan.bytes, ws_bytes);
@@ -678,8 +692,7 @@ extern "C" int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track
     a.hist = (uint32_t *)(scratch + plan.hist);
     const hipStream_t st = (hipStream_t)stream;
     // lengths that are read by one workgroup are not written by another of the same launch
-    const uintptr_t lens_at = (uintptr_t)seq_lens, new_at = (uintptr_t)new_lens, lens_bytes = B * sizeof(int32_t);
-    a.set_lens = plan.few && (new_at + lens_bytes <= lens_at || lens_at + lens_bytes <= new_at);
+    a.set_lens = plan.few && apart;
     if (!plan.chunked) {
         KernelTimer timer("kv_evict_select", st);
         const dim3 grid((uint32_t)P);

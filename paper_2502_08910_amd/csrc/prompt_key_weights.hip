@@ -486,7 +486,7 @@ extern "C" int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tenso
     if ((int64_t)a.rows_q * a.G > INT32_MAX - kKwRows)
         return fail(IHIP_ERR_UNSUPPORTED, "%s: %d rows of %d heads (%d KV heads) are too many", who, a.rows_q, a.Hq, a.Hkv);
     const KeyWeightPlan plan = key_weight_plan(*packed, rows_k, window);
-    if (plan.blocks * a.Hkv > INT32_MAX || plan.chunks > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)plan.blocks * a.Hkv);
+    if (plan.blocks * a.Hkv > UINT32_MAX / kKwThreads || plan.chunks > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld workgroups are too many", who, (long long)plan.blocks * a.Hkv);
     const bool parts = plan.chunks > 1 && ws && !((uintptr_t)ws & 15) && ws_bytes >= plan.bytes;
     a.chunk_tiles = parts ? plan.chunk_tiles : INT32_MAX;
     a.near = kKwRows % a.G == 0 && a.q_st >= 0 && a.q_sh >= 0 && a.q_st < (1 << 22) && (int64_t)(a.G - 1) * a.q_sh < (1 << 28);

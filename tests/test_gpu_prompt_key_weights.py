@@ -94,6 +94,35 @@ def test_wide_blocks_of_keys(ihip, Hq, Hkv, window):
         assert bool((track.weights[b, :, n:] == 5).all())
 
 
+def test_windows_of_many_keys(ihip):
+    """Workgroups that go through several blocks of keys: a call of many rows, with a few short sequences in them."""
+    new, rows, Hq = [700, 1, 260], 200000, 8
+    q, k, lse = inputs(new, new, Hq, 1, seed=3, extra=0)
+    wide = [torch.full((rows, *x.shape[1:]), float("nan"), dtype=x.dtype).cuda() for x in (q, k, lse)]
+    for x, y in zip(wide, (q, k, lse)):
+        x[:sum(new)] = y.cuda()
+    track = ihip.KVTrack(torch.full((3, 1, 710), 5.0).cuda())
+    ihip.prompt_key_weights(wide[0], wide[1], offsets(new).cuda(), rows, wide[2], track, window=30, fresh=True)
+    check(track.weights, None, 1.0, q, k, lse, new, new, 1, 30, 710)
+    for b, n in enumerate(new):
+        assert bool((track.weights[b, :, n:] == 5).all())
+
+
+@pytest.mark.parametrize("window", [None, 40])
+def test_sequences_longer_than_max_q(ihip, window):
+    """They may be done in part; the others are not."""
+    new, Hq, Hkv = [30, 500, 40], 8, 2
+    q, k, lse = inputs(new, new, Hq, Hkv, seed=9)
+    k = k[:q.shape[0]]
+    track = ihip.KVTrack(torch.full((3, Hkv, 510), 5.0).cuda())
+    ihip.prompt_key_weights(q.cuda(), k.cuda(), offsets(new).cuda(), 40, lse.cuda(), track, window=window, fresh=True)
+    whole = ihip.KVTrack(torch.full((3, Hkv, 510), 5.0).cuda())
+    ihip.prompt_key_weights(q.cuda(), k.cuda(), offsets(new).cuda(), 500, lse.cuda(), whole, window=window, fresh=True)
+    for b in (0, 2):
+        assert (track.weights[b] - whole.weights[b]).abs().max() <= 2.0 ** -12          # (sums in another order)
+    assert bool((track.weights[1, :, :500] <= whole.weights[1, :, :500] + 2.0 ** -12).all()) and bool((track.weights[1, :, 500:] == 5).all())
+
+
 def test_chunks_of_queries(ihip):
     """Many queries on few keys, in chunks whose sums are added up, and without scratch: equal up to rounding, and the same bits each time."""
     new, Hq, Hkv = [2500, 1200], 8, 1

@@ -124,6 +124,7 @@ def test_evict_refuses(b):  # noqa: F811
     assert evict(b, n_sink=10, n_recent=7) == BAD and b"keep = 16" in L.ihip_last_error()
     assert evict(b, keep=2 ** 31 - 1, n_sink=2 ** 31 - 1, n_recent=1) == BAD
     assert evict(b, lens=None) == BAD and evict(b, new=None) == BAD and evict(b, kept=None) == BAD
+    assert evict(b, new=4100) == BAD and evict(b, new=4092) == BAD and b"overlaps" in L.ihip_last_error()
     assert evict(b, track=None) == BAD and evict(b, track=track_of(b, rows=63)) == BAD
     for name in ("weights", "positions", "seen"):
         assert evict(b, track=track_of(b, **{name: None})) == BAD
