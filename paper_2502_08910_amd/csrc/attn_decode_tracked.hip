@@ -2,6 +2,7 @@
 //   s_hj = q_h k_j,   l_h = sum_j e^(c s_hj),   out_h = sum_j e^(c s_hj) v_j / l_h,   weight_j = decay before_j + sum_h e^(c s_hj) / l_h
 // over the heads h of a KV head.  A weight needs the sum over all rows, so the scores wait for it in scratch.  Two launches: the first cuts a
 // sequence's rows into parts, one workgroup each, and leaves scores and partial results; the second joins the parts, and turns scores into weights.
+// (Where sequences are one part each, the first does it all.)
 //
 // A wave takes 32 rows at a time, the products on v_mfma_f32_16x16x32_bf16 (rows widened to bf16, exact); no value crosses lanes in between:
 //   scores   16 K rows x twice 8 heads (fewer repeat the last).  Lane (n, g) = (l % 16, l / 16) brings 16-byte pieces of row n, and gets head
@@ -11,6 +12,9 @@
 //            bf16 in rows 0 .. 7, what that dropped in rows 8 .. 15; the two are added in LDS), key 16 (i / 4) + 4 g + i % 4 for element i; for the right
 //            one it brings dims 8 n .. 8 n + 7 of the same keys, and column n of product j is dim 8 n + j.
 // So a probability is off by at most 2^-16 of it in the output.  The sums and the weights take the probabilities as they were.
+// Bound by memory: 4 sequences of 57,654 to 100,003 rows in bf16, 32 heads on 8, 1.39 GB, take 306 us (4.5 TB/s, a copy of 2 GB moves 5.0; the
+// scores are 43 MB more) and 17 for the join; 32 of 7,383 to 16,384 in E4M3, 768 MB, 186 (4.1; scores 48 MB) and 16; 8 of 20,637 to 32,768 in
+// MX FP4, 199 MB, 66 (3.0; scores 23 MB, and 20 requests for 32 rows) and 9.  One of 2,051 takes 6 and 4, chains of latencies.
 #include "api_checks.h"
 #include "decode_softmax.h"
 #include "kv_store.h"
@@ -25,6 +29,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kTrThreads = 256, kTrWaves = kTrThreads / kWave;
 constexpr int kTrStep = 32;                          // rows of a wave at a time
 constexpr int kTrMaxSplit = 768, kTrMinSplit = 128;  // rows of a part (multiples of 128: a step of every wave)
+constexpr int kTrOnePart = 1024;                     // rows of sequences that are one part each, if there are few of them
 
 struct TrackedArgs {
     Geometry ge;
@@ -46,6 +51,11 @@ struct TrackedArgs {
 
 __device__ inline uint16_t to_bf16(float x) { return (uint16_t)pack_bf16x2(x, x); }        // (NaN stays it)
 __device__ inline int tracked_len(const TrackedArgs &a, int b) { return min(max(a.ge.seq_lens[b], 0), a.max_len); }
+// A row's probability is 2^(c (s - reference) - log2 of the sum of those); without a key that is there, 0.  sum: as it was added up, times 2^-kSoftmaxShift
+__device__ inline float tracked_log2_sum(float sum) { return sum == 0.f ? INFINITY : log2f(sum) + kSoftmaxShift; }
+__device__ inline float tracked_probability(float score, float2 all, float scale_log2e) { return __builtin_amdgcn_exp2f(fmaf(score - all.x, scale_log2e, -all.y)); }
+__device__ inline void store_tracked_weight(const TrackedArgs &a, int64_t at, float w) { a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w; }
+
 template <int FORMAT>
 struct TrackedRows {
     typedef typename std::conditional<FORMAT == IHIP_KV_BF16, uint4, typename std::conditional<FORMAT == IHIP_KV_E4M3, uint2, uint32_t>::type>::type word;
@@ -70,11 +80,12 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
 
     // where the part's rows are, in bytes from row 0; behind the last step: the waves' results, of the two parts of the probabilities
     __shared__ __attribute__((aligned(16))) union {
-        struct { int64_t k[kTrMaxSplit], v[kTrMaxSplit]; } row;
+        struct { int64_t k[kTrOnePart], v[kTrOnePart]; } row;
         float acc[kTrWaves][2][HEADS][kD];
     } sh;
-    __shared__ uint32_t sh_there[kTrMaxSplit / kTrStep];     // which of a step's rows hold a key
+    __shared__ uint32_t sh_there[kTrOnePart / kTrStep];     // which of a step's rows hold a key
     __shared__ float sh_m[kTrWaves][HEADS], sh_l[kTrWaves][HEADS];
+    __shared__ float2 sh_all[HEADS];
 
     // The operand of step j: 16-byte pieces as above
     bf16x8 qb[4];
@@ -253,30 +264,41 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
             L = fmaf(x, sh_l[w][h], L);
             A = fmaf(x, sh.acc[w][0][h][c] + sh.acc[w][1][h][c], A);
         }
-        if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + (pbase + h) * 2) = make_float2(M, L);
         if (a.n_splits == 1) {                       // nothing to join
             const int64_t hq = (int64_t)b * a.ge.Hq + kv_head * G + h;
             a.out[hq * kD + c] = to_bf16(L == 0.f ? 0.f : A / L * a.v_scale);
-            if (a.out_lse != nullptr && c == 0) a.out_lse[hq] = softmax_lse(M, L, a.scale_log2e);
+            if (c == 0) {
+                if (a.out_lse != nullptr) a.out_lse[hq] = softmax_lse(M, L, a.scale_log2e);
+                sh_all[h] = make_float2(M, tracked_log2_sum(L));
+            }
         } else {
             a.part_acc[(pbase + h) * kD + c] = A;
+            if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + (pbase + h) * 2) = make_float2(M, L);
         }
+    }
+    if (a.n_splits > 1) return;
+    __syncthreads();                                 // (the scores are this workgroup's own)
+    const float *all = a.scores + (int64_t)p * G * a.score_stride;
+    for (int row = tid; row < len; row += kTrThreads) {
+        float w = 0.f;
+        for (int h = 0; h < G; ++h) w += tracked_probability(all[h * a.score_stride + row], sh_all[h], a.scale_log2e);
+        store_tracked_weight(a, (int64_t)p * a.weight_rows + row, w);
     }
 }
 
-// The parts joined, and weights: of the workgroups of a problem the first G take a head's output (where there are parts), the others
-// kJoinRows rows each.
+// The parts joined, and weights: of the workgroups of a problem the first G take a head's output, the others kJoinRows rows each.
 constexpr int kJoinRows = 1024, kJoinAhead = 8, kJoinGroups = kTrThreads / 32;
 template <int G>
-__global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(const TrackedArgs a, int out_groups)
+__global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(const TrackedArgs a)
 {
     const int p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int b = p / a.ge.Hkv;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (int64_t)p * a.n_splits * G;
     __shared__ float sh_m[kJoinGroups], sh_l[kJoinGroups];
+    __shared__ float2 sh_all[G];
     __shared__ __attribute__((aligned(16))) float sh_a[kJoinGroups][kD];
     static_assert(G <= kJoinGroups, "");
-    if ((int)blockIdx.y < out_groups) {
+    if ((int)blockIdx.y < G) {
         // a head's parts: 32 lanes a part, 4 dims each
         const int h = blockIdx.y, l32 = tid & 31, grp = tid >> 5, parts = (tracked_len(a, b) + a.per - 1) / a.per;
         const float4 *accs = reinterpret_cast<const float4 *>(a.part_acc + (int64_t)p * a.n_splits * G * kD) + l32;
@@ -326,7 +348,7 @@ __global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(co
         if (a.out_lse != nullptr && tid == 0) a.out_lse[hq] = softmax_lse(M, sum, a.scale_log2e);
         return;
     }
-    const int len = tracked_len(a, b), row0 = ((int)blockIdx.y - out_groups) * kJoinRows;
+    const int len = tracked_len(a, b), row0 = ((int)blockIdx.y - G) * kJoinRows;
     if (row0 >= len) return;
     // (what the weights are made of is on its way while the sums are joined)
     constexpr int kRows = kJoinRows / kTrThreads;
@@ -353,8 +375,7 @@ __global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(co
         M = top;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) L += __shfl_xor(L, d, 64);
-        // a row's probability is 2^(c (s - M) - log2 of the sum of those); without a key that is there, 0
-        if (lane == 0) { sh_m[h] = M; sh_l[h] = L == 0.f ? INFINITY : log2f(L) + kSoftmaxShift; }
+        if (lane == 0) sh_all[h] = make_float2(M, tracked_log2_sum(L));
     }
     __syncthreads();
 #pragma unroll
@@ -363,7 +384,7 @@ __global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(co
         if (row >= len) break;
         float w = 0.f;
 #pragma unroll
-        for (int h = 0; h < G; ++h) w += __builtin_amdgcn_exp2f(fmaf(x[i][h] - sh_m[h], a.scale_log2e, -sh_l[h]));
+        for (int h = 0; h < G; ++h) w += tracked_probability(x[i][h], sh_all[h], a.scale_log2e);
         a.weights[(int64_t)p * a.weight_rows + row] = a.before ? fmaf(a.decay, old[i], w) : w;
     }
 }
@@ -371,13 +392,15 @@ __global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(co
 // All parts have as many rows, so that workgroups take as long as each other where sequences do not: kTrMaxSplit, or fewer where that would leave
 // compute units with less than two.  us for 768 / 512 / 1,024 / 2,048 rows: 8 sequences of 20,637 to 32,768 in MX FP4 74 / 77 / 78 / 83, 32 of
 // 7,383 to 16,384 in E4M3 200 / 201 / 201 / 207, one of 200,001 in MX FP4 77 / 82 / 77 / 82; one of 30,001 in bf16, with 128 / 256 / 512 rows
-// 39 / 32 / 29.
+// 39 / 32 / 29.  Short sequences in one part each need no join: 4 of 1,000 14.7 where parts take 17.8, 16 of 1,000 16.7 / 17.7, 32 of 1,024 to 1,055
+// 20.3 / 19.6.
 struct TrackedPlan { int splits, per; int64_t score_stride; size_t bytes; };
 static TrackedPlan tracked_plan(const ihip_shape &s)
 {
     const int64_t total = s.max_seq_len, P = std::max<int64_t>(1, (int64_t)s.B * s.Hkv);
     TrackedPlan r;
     r.per = (int)std::min<int64_t>(kTrMaxSplit, (total * P / (2 * compute_units()) + kTrMinSplit) / kTrMinSplit * kTrMinSplit);
+    if (total <= (P < compute_units() ? kTrOnePart : kTrOnePart / 2)) r.per = (int)((total + kTrMinSplit - 1) / kTrMinSplit * kTrMinSplit);
     r.splits = (int)((total - 1) / r.per + 1);
     r.score_stride = (total + kTrStep - 1) / kTrStep * kTrStep;
     r.bytes = (size_t)s.B * s.Hq * (r.score_stride + (int64_t)r.splits * (2 + kD)) * sizeof(float);
@@ -447,13 +470,12 @@ extern "C" int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor
         else { IHIP_AT(IHIP_KV_MX4); }
 #undef IHIP_AT
     }
-    if ((rc = check_launch(who)) != IHIP_OK) return rc;
-    const int out_groups = a.n_splits > 1 ? a.ge.G : 0;
+    if ((rc = check_launch(who)) != IHIP_OK || a.n_splits == 1) return rc;
     KernelTimer timer("attn_decode_tracked_join", st);
-    const dim3 join((uint32_t)P, (uint32_t)(out_groups + join_groups));
-    if (a.ge.G == 1) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<1>, join, dim3(kTrThreads), 0, st, a, out_groups);
-    else if (a.ge.G == 2) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<2>, join, dim3(kTrThreads), 0, st, a, out_groups);
-    else if (a.ge.G == 4) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<4>, join, dim3(kTrThreads), 0, st, a, out_groups);
-    else hipLaunchKernelGGL(attn_decode_tracked_join_kernel<8>, join, dim3(kTrThreads), 0, st, a, out_groups);
+    const dim3 join((uint32_t)P, (uint32_t)(a.ge.G + join_groups));
+    if (a.ge.G == 1) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<1>, join, dim3(kTrThreads), 0, st, a);
+    else if (a.ge.G == 2) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<2>, join, dim3(kTrThreads), 0, st, a);
+    else if (a.ge.G == 4) hipLaunchKernelGGL(attn_decode_tracked_join_kernel<4>, join, dim3(kTrThreads), 0, st, a);
+    else hipLaunchKernelGGL(attn_decode_tracked_join_kernel<8>, join, dim3(kTrThreads), 0, st, a);
     return check_launch(who);
 }
