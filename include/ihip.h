@@ -621,7 +621,8 @@ int32_t ihip_kv_append_tracked(const ihip_packed *packed, ihip_tensor q, ihip_te
  * over the last min(window, n) queries i with j <= i + (t - n) and the query heads of KV head g:
  * key j stands in row j of the cache.  Keys beyond track->rows are left out.
  *   q, k, cu_k, rows_k, sm_scale   as ihip_prompt_attn had them
- *   lse        device fp32 [rows, Hq], its out_lse; what is not finite there makes the keys that the query sees NaN, infinite or 0, as the formula has it
+ *   lse        device fp32 [rows, Hq], its out_lse; what is not finite there makes the keys that the query sees NaN, infinite or 0, as the formula has
+ *              it.  A probability is off by what lse and the score were rounded to, 2^-24 of each
  *   window     at least 1; max_q or more: all queries
  *   before     device fp32 like track->weights, may be the same; NULL: nothing before
  *   decay      finite, not negative; not looked at without `before`
@@ -645,7 +646,8 @@ int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tensor q, ihip_t
  * k_scale) as in ihip_sparse_attn_decode_mx4kv, and the same arithmetic.  The output of an idle
  * place of the batch, or of a sequence without pages, is 0, its log-sum-exp -INFINITY; a row on a page with a
  * negative id is left out, its weight gets nothing but decay * before.  Rows behind a sequence are not
- * read, and what stands beside them is left as it was.
+ * read, and what stands beside them is left as it was.  What is not finite in an attended K or V row makes the results NaN or infinite that it goes
+ * into: of a K row all outputs and weights of its KV head's queries.
  *   before, decay, track   as in ihip_prompt_key_weights
  *   ws                     device scratch of ihip_attn_decode_tracked_workspace_bytes(shape), 16-byte aligned
  */

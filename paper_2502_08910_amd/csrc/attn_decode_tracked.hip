@@ -438,7 +438,6 @@ extern "C" int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor
     if (!ws || ((uintptr_t)ws & 15) || ws_bytes < plan.bytes)
         return fail(IHIP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 16-byte aligned, needed, %zu given", who, plan.bytes, ws_bytes);
     const int64_t P = (int64_t)shape->B * shape->Hkv;
-    if (P > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld sequences x KV heads are too many", who, (long long)P);
     const int64_t join_groups = ((int64_t)shape->max_seq_len - 1) / kJoinRows + 1;
     if (join_groups > 65535 - 8) return fail(IHIP_ERR_UNSUPPORTED, "%s: max_seq_len = %d is too large", who, shape->max_seq_len);
     a.ge = make_geometry(*shape);
@@ -448,6 +447,8 @@ extern "C" int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor
     a.n_splits = plan.splits;
     a.per = plan.per;
     a.grid = decode_grid(a.ge, a.n_splits, false);
+    if (P > (a.grid.problems_first ? (int64_t)UINT32_MAX / kTrThreads : 65535))
+        return fail(IHIP_ERR_UNSUPPORTED, "%s: %lld sequences x KV heads are too many", who, (long long)P);
     a.scores = (float *)ws;
     a.score_stride = plan.score_stride;
     a.part_ml = a.scores + P * a.ge.G * plan.score_stride;

@@ -151,9 +151,12 @@ def test_long(ihip, Hkv, lens, keep, equal):
     check(ihip, c, ihip.KVTrack(w.cuda(), pos.cuda(), c.seq_lens.clone()), keep, 4, 64, in_place=False)
 
 
-def test_captured_and_replayed(ihip):
-    """A captured call, replayed on lengths and weights that change under it, on a stream of its own; two graphs with scratch of their own."""
-    caches = [Cache(ihip, "bf16", [120, 80], 2, 16, seed=s) for s in (1, 2)]
+@pytest.mark.parametrize("most,keep,steps", [([120, 80], 40, ([120, 80], [41, 40], [0, 77])), ([2000, 1500], 700, ([2000, 1500], [699, 1001])),
+                                             ([20000, 17000], 3000, ([20000, 17000], [2999, 16500], [20000, 1]))])
+def test_captured_and_replayed(ihip, most, keep, steps):
+    """A captured call, replayed on lengths and weights that change under it, on a stream of its own; two graphs with scratch of their own.  Few moves,
+    many, and rows in chunks."""
+    caches = [Cache(ihip, "bf16", most, 2, 16, seed=s) for s in (1, 2)]
     tracks = [make_track(ihip, c, c.T, seed=3) for c in caches]
     fresh = [[x.clone() for x in (c.k, c.v, t.weights, t.positions)] for c, t in zip(caches, tracks)]
     out, graphs = [], []
@@ -161,13 +164,13 @@ def test_captured_and_replayed(ihip):
     stream.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(stream):
         for c, t in zip(caches, tracks):
-            ws, new, kept = ihip.kv_evict_workspace(c.store, 2, c.T, 40), torch.zeros(2, dtype=torch.int32).cuda(), torch.zeros((2, 2, 40), dtype=torch.int32).cuda()
+            ws, new, kept = ihip.kv_evict_workspace(c.store, 2, c.T, keep), torch.zeros(2, dtype=torch.int32).cuda(), torch.zeros((2, 2, keep), dtype=torch.int32).cuda()
             graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(graph, stream=stream):
-                ihip.kv_evict(c.store, t, c.seq_lens, c.T, 40, n_sink=2, n_recent=8, new_lens=new, kept=kept, ws=ws)
+                ihip.kv_evict(c.store, t, c.seq_lens, c.T, keep, n_sink=2, n_recent=8, new_lens=new, kept=kept, ws=ws)
             graphs.append(graph)
             out.append((new, kept))
-        for lens in ([120, 80], [41, 40], [0, 77]):
+        for lens in steps:
             for i in (0, 1, 0):
                 c, t = caches[i], tracks[i]
                 for x, y in zip((c.k, c.v, t.weights, t.positions), fresh[i]):
@@ -177,8 +180,8 @@ def test_captured_and_replayed(ihip):
                 graphs[i].replay()
                 torch.cuda.synchronize()
                 new, kept = out[i]
-                assert new.cpu().tolist() == [min(x, 40) for x in lens]
+                assert new.cpu().tolist() == [min(x, keep) for x in lens]
                 for b, n in enumerate(lens):
                     for g in range(2):
-                        m = evicted(fresh[i][2][b, g].cpu().numpy(), fresh[i][3][b, g].cpu().numpy(), n, 40, 2, int(t.seen[b]) - 8)
+                        m = evicted(fresh[i][2][b, g].cpu().numpy(), fresh[i][3][b, g].cpu().numpy(), n, keep, 2, int(t.seen[b]) - 8)
                         assert (kept[b, g].cpu().numpy() == m).all()

@@ -182,6 +182,19 @@ def test_queries_without_keys(ihip):
     check(track.weights, None, 1.0, q, k, lse, new, total, Hkv, 10 ** 9, 12)
 
 
+def test_no_queries_at_all(ihip):
+    """Keys, and no new tokens in any sequence: what was there fades."""
+    k = torch.randn((50, 2, D), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    old = torch.rand((2, 2, 40), generator=torch.Generator().manual_seed(2))
+    track = ihip.KVTrack(old.clone().cuda())
+    ihip.prompt_key_weights(torch.zeros((0, 8, D), dtype=torch.bfloat16).cuda(), k, offsets([0, 0]).cuda(), 0, torch.zeros((0, 8)).cuda(), track,
+                            cu_k=offsets([30, 20]).cuda(), decay=0.5)
+    want = old.clone()
+    want[0, :, :30] *= 0.5
+    want[1, :, :20] *= 0.5
+    assert torch.equal(track.weights.cpu(), want)
+
+
 def test_strides_and_fewer_rows_than_keys(ihip):
     """Queries and keys inside wider tensors; a track of fewer rows than a sequence has keys."""
     new, Hq, Hkv = [130, 70], 8, 2

@@ -184,3 +184,31 @@ def test_prompts_then_steps_with_evictions(ihip):
             cut()
     assert track.seen.cpu().tolist() == [p + steps for p in prompts]
     assert lens.cpu().tolist() == [keep + steps % slack] * B
+
+
+def test_two_streams_at_once(ihip):
+    """Two caches in the hands of two streams, step by step without a wait between them, and the same one after the other: the same bits."""
+    B, Hq, Hkv, T, keep = 2, 8, 2, 400, 300
+    lens0, results = [400, 333], []
+    for streams in (1, 2):
+        runs = []
+        pool = [torch.cuda.Stream() for _ in range(streams)]
+        for i in range(2):
+            store, mem = junk_store(ihip, "e4m3", B, Hkv, T, 16, seed=i)
+            g = torch.Generator().manual_seed(20 + i)
+            track = ihip.KVTrack(torch.rand((B, Hkv, T), generator=g).cuda(), torch.arange(T, dtype=torch.int32).repeat(B, Hkv, 1).cuda(),
+                                 torch.tensor(lens0, dtype=torch.int32).cuda())
+            runs.append([store, mem, track, torch.tensor(lens0, dtype=torch.int32).cuda(), None])
+        qs = [normal(30 + s, B, Hq, 1, D).cuda() for s in range(4)]
+        torch.cuda.synchronize()
+        for q in qs:
+            for i, run in enumerate(runs):
+                store, mem, track, lens, _ = run
+                with torch.cuda.stream(pool[i % streams]):
+                    run[4] = ihip.attn_decode_tracked(q, store, track, lens, T, want_lse=True)
+                    ihip.kv_evict(store, track, lens, T, keep, n_sink=2, n_recent=20, new_lens=lens)
+        torch.cuda.synchronize()
+        results.append([[x.cpu() for x in (*run[1], run[2].weights, run[2].positions, run[3], *run[4])] for run in runs])
+    for a, b in zip(*results):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
