@@ -1033,6 +1033,11 @@ def _decode_shape(q: torch.Tensor, store: KVStore, seq_lens: Optional[int], max_
     return Shape(q.shape[0], q.shape[1], store.Hkv, q.shape[3], 1, 1, seq_lens, max_seq_len, 0, 1, 0)
 
 
+def _result(t: torch.Tensor, name: str, dtype, n: int, device) -> None:
+    if t.dtype != dtype or t.numel() != n or t.device != device or not t.is_contiguous():
+        raise IhipError(f"{name}: need a contiguous {dtype} tensor of {n} elements on {device}")
+
+
 def attn_decode_tracked_workspace(q: torch.Tensor, store: KVStore, max_seq_len: int) -> torch.Tensor:
     """Scratch of attn_decode_tracked for queries like q and sequences of up to max_seq_len rows."""
     shape = _decode_shape(q, store, 256, max_seq_len)        # (the lengths are not looked at)
@@ -1049,21 +1054,24 @@ def attn_decode_tracked(q: torch.Tensor, store: KVStore, track: KVTrack, seq_len
     """ihip_attn_decode_tracked: attention of q [B, Hq, 1, d] over the seq_lens [B] rows of a store of any format, whose probabilities are
     added to track.weights (before, decay, fresh as in prompt_key_weights).  -> (out bf16 [B, Hq, 1, d], lse fp32 [B, Hq, 1] or None)."""
     B, Hq, d = q.shape[0], q.shape[1], q.shape[-1]
-    sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    shape = _decode_shape(q, store, _lengths(seq_lens, B, "seq_lens", store.device), max_seq_len)
-    track.check(B, store.Hkv, store.device)
+    device = store.device
+    shape = _decode_shape(q, store, _lengths(seq_lens, B, "seq_lens", device), max_seq_len)
+    track.check(B, store.Hkv, device)
+    _same_device(device, q=q)
     if out is None:
-        out = torch.empty((B, Hq, 1, d), dtype=torch.bfloat16, device=q.device)
-    if lse is None and want_lse:
-        lse = torch.empty((B, Hq, 1), dtype=torch.float32, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    else:
+        _result(out, "out", torch.bfloat16, B * Hq * d, device)
+    if lse is not None:
+        _result(lse, "lse", torch.float32, B * Hq, device)
+    elif want_lse:
+        lse = torch.empty((B, Hq, 1), dtype=torch.float32, device=device)
     if ws is None:
         ws = attn_decode_tracked_workspace(q, store, max_seq_len)
-    _same_device(store.device, q=q, out=out, lse=lse, ws=ws)
-    for t, name, dt, n in ((out, "out", torch.bfloat16, B * Hq * d), (lse, "lse", torch.float32, B * Hq)):
-        if t is not None and (t.dtype != dt or not t.is_contiguous() or t.numel() != n):
-            raise IhipError(f"{name}: need a contiguous {dt} tensor of {n} elements")
-    _enqueue(store.device, lib().ihip_attn_decode_tracked, ctypes.byref(shape), _tensor(q, "q"), store.ref(), sm_scale, track.before(before, fresh),
-             decay, track.ref(), _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size())
+    elif ws.device != device:
+        raise IhipError(f"ws is on {ws.device}, not on {device}")
+    _enqueue(device, lib().ihip_attn_decode_tracked, ctypes.byref(shape), _tensor(q, "q"), store.ref(), 1.0 / math.sqrt(d) if sm_scale is None else sm_scale,
+             track.before(before, fresh), decay, track.ref(), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size())
     return out, lse
 
 
@@ -1091,11 +1099,12 @@ def kv_evict(store: KVStore, track: KVTrack, seq_lens: torch.Tensor, max_seq_len
         new_lens = torch.empty((B,), dtype=torch.int32, device=store.device)
     if kept is None:
         kept = torch.empty((B, store.Hkv, max(keep, 0)), dtype=torch.int32, device=store.device)
+    else:
+        _result(kept, "kept", torch.int32, B * store.Hkv * keep, store.device)
     if ws is None:
         ws = kv_evict_workspace(store, B, max_seq_len, keep)
-    _same_device(store.device, kept=kept, ws=ws)
-    if kept.dtype != torch.int32 or kept.shape != (B, store.Hkv, keep) or not kept.is_contiguous():
-        raise IhipError("kept: need a contiguous int32 tensor [B, Hkv, keep]")
+    elif ws.device != store.device:
+        raise IhipError(f"ws is on {ws.device}, not on {store.device}")
     _enqueue(store.device, lib().ihip_kv_evict, store.ref(), track.ref(), B, store.Hkv, 128, _lengths(seq_lens, B, "seq_lens", store.device),
              max_seq_len, keep, n_sink, n_recent, None if to is None else to.ref(), _lengths(new_lens, B, "new_lens", store.device), kept.data_ptr(),
              _ptr(ws), ws.numel() * ws.element_size())
