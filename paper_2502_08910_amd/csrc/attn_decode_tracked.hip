@@ -13,8 +13,8 @@
 //            one it brings dims 8 n .. 8 n + 7 of the same keys, and column n of product j is dim 8 n + j.
 // So a probability is off by at most 2^-16 of it in the output.  The sums and the weights take the probabilities as they were.
 // Bound by memory: 4 sequences of 57,654 to 100,003 rows in bf16, 32 heads on 8, 1.39 GB, take 306 us (4.5 TB/s, a copy of 2 GB moves 5.0; the
-// scores are 43 MB more) and 17 for the join; 32 of 7,383 to 16,384 in E4M3, 768 MB, 186 (4.1; scores 48 MB) and 16; 8 of 20,637 to 32,768 in
-// MX FP4, 199 MB, 66 (3.0; scores 23 MB, and 20 requests for 32 rows) and 9.  One of 2,051 takes 6 and 4, chains of latencies.
+// scores are 43 MB more) and 17 for the join; 32 of 7,383 to 16,384 in E4M3, 782 MB, 186 (4.2; scores 49 MB) and 17; 8 of 20,637 to 32,768 in
+// MX FP4, 232 MB, 64 (3.6; scores 27 MB, and 20 requests for 32 rows) and 9.  One of 2,051 takes 6 and 4, chains of latencies.
 #include "api_checks.h"
 #include "decode_softmax.h"
 #include "kv_store.h"
