@@ -624,8 +624,8 @@ int32_t ihip_kv_append_tracked(const ihip_packed *packed, ihip_tensor q, ihip_te
  *   lse        device fp32 [rows, Hq], its out_lse; what is not finite there makes the keys that the query sees NaN, infinite or 0, as the formula has
  *              it.  A probability is off by what lse and the score were rounded to, 2^-24 of each
  *   window     at least 1; max_q or more: all queries
- *   before     device fp32 like track->weights, may be the same; NULL: nothing before
- *   decay      finite, not negative; not looked at without `before`
+ *   before     device fp32 like track->weights, the same array or one apart from it; NULL: nothing before
+ *   decay      finite, not negative; without `before` it changes nothing
  *   track      only weights and rows are looked at; rows behind a sequence's keys are left as they were
  *   ws         device scratch of ihip_prompt_key_weights_workspace_bytes(packed, rows_k, window), 16-byte aligned; may be
  *              NULL.  Few keys under many queries are dealt out to the chip in chunks of queries, whose sums wait there; with NULL, less
@@ -663,9 +663,9 @@ int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor q, const i
  * below `keep` stays where it is; the i-th evicted row there is filled with the i-th kept row of those from `keep` on.  Nothing else moves:
  * rows from `keep` on are left as they were.
  *   keep       at least 1, at least n_sink + n_recent
- *   to         weights, positions and rows of the cut cache; may be track or NULL, which is the same.  With arrays of its own all
+ *   to         weights, positions and rows of the cut cache; may be track or NULL, which is the same.  With arrays of its own, apart from track's, all
  *              kept rows are written there (rows: at least min(keep, max_seq_len)), track's are left as they were
- *   new_lens   device int32 [B]: min(seq_lens[b], keep); may be seq_lens.  seen does not change
+ *   new_lens   device int32 [B]: min(seq_lens[b], keep); may be seq_lens, not a part of it.  seen does not change
  *   kept       device int32 [B, Hkv, keep]: the row that each row was, -1 behind a sequence
  *   ws         device scratch of ihip_kv_evict_workspace_bytes(B, Hkv, max_seq_len, keep), 16-byte aligned
  * Two rows must not share memory, two sequences no page.  Where one of the two pages of a move has a negative id, K and V do not move.

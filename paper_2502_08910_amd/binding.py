@@ -1011,7 +1011,7 @@ def prompt_key_weights(q: torch.Tensor, k: torch.Tensor, cu_q: torch.Tensor, max
     rows_k, Hkv, _ = k.shape
     B = cu_q.numel() - 1
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    window = 2 ** 31 - 1 if window is None else window
+    window = 2 ** 31 - 1 if window is None else min(window, 2 ** 31 - 1)
     _same_device(q.device, k=k, lse=lse, ws=ws)
     track.check(B, Hkv, q.device)
     if lse.shape != (rows, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous():

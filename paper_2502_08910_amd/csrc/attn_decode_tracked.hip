@@ -430,7 +430,7 @@ extern "C" int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor
     TrackedArgs a{};
     if ((rc = check_store(who, store, *shape, &a.from)) != IHIP_OK) return rc;
     if ((rc = check_track(who, track, shape->max_seq_len, false)) != IHIP_OK) return rc;
-    if (!(decay >= 0.f) || decay > 3.4028234e38f) return fail(IHIP_ERR_INVALID_ARG, "%s: decay = %g", who, decay);
+    if ((rc = check_before(who, before, decay, track, (int64_t)shape->B * shape->Hkv)) != IHIP_OK) return rc;
     if (!out) return fail(IHIP_ERR_INVALID_ARG, "%s: out is NULL", who);
     if ((rc = check_sm_scale(who, sm_scale, &a.scale_log2e)) != IHIP_OK) return rc;
     if ((rc = check_sm_scale(who, sm_scale * a.from.k_scale, &a.scale_log2e)) != IHIP_OK) return rc;

@@ -668,12 +668,15 @@ extern "C" int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track
     if (!to->positions) return fail(IHIP_ERR_INVALID_ARG, "%s: an array of to is NULL", who);
     if ((to->weights == track->weights || to->positions == track->positions) && to->rows != track->rows)
         return fail(IHIP_ERR_INVALID_ARG, "%s: to and track share arrays of %d and %d rows", who, to->rows, track->rows);
+    const int64_t here = (int64_t)B * Hkv * track->rows * 4, there = (int64_t)B * Hkv * to->rows * 4;
+    if (overlap_in_part(to->weights, there, track->weights, here) || overlap_in_part(to->positions, there, track->positions, here))
+        return fail(IHIP_ERR_INVALID_ARG, "%s: to and track overlap in part", who);
     const int64_t row = store->format == IHIP_KV_BF16 ? 2 * kD : store->format == IHIP_KV_E4M3 ? kD : kD / 2;
     if (Hkv > 1 && (std::abs(a.store.k_sh) < row || std::abs(a.store.v_sh) < row))
         return fail(IHIP_ERR_INVALID_ARG, "%s: the heads of the store overlap", who);
-    const uintptr_t lens_at = (uintptr_t)seq_lens, new_at = (uintptr_t)new_lens, lens_bytes = B * sizeof(int32_t);
-    const bool apart = new_at + lens_bytes <= lens_at || lens_at + lens_bytes <= new_at;
-    if (!apart && new_at != lens_at) return fail(IHIP_ERR_INVALID_ARG, "%s: new_lens overlaps seq_lens in part", who);
+    const int64_t lens_bytes = B * (int64_t)sizeof(int32_t);
+    const bool apart = new_lens != seq_lens;
+    if (overlap_in_part(new_lens, lens_bytes, seq_lens, lens_bytes)) return fail(IHIP_ERR_INVALID_ARG, "%s: new_lens overlaps seq_lens in part", who);
     const EvictPlan plan = evict_plan(B, Hkv, max_seq_len, keep);
     if (plan.bytes > 0 && (!ws || ((uintptr_t)ws & 15) || ws_bytes < plan.bytes))
         return fail(IHIP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 16-byte aligned, needed, %zu given", who, plan.bytes, ws_bytes);

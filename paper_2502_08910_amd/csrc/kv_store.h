@@ -17,6 +17,14 @@ int32_t check_store(const char *who, const ihip_kv_store *store, const ihip_shap
 // `whole`: with positions and tokens seen; otherwise the weights alone
 int32_t check_track(const char *who, const ihip_kv_track *track, int64_t rows, bool whole);
 int32_t check_packed(const char *who, const ihip_packed *p);
+// `before`, decay and the weights [heads, rows] that they go into: arrays that are the same or apart
+int32_t check_before(const char *who, const float *before, float decay, const ihip_kv_track *track, int64_t heads);
+// Arrays that have bytes in common and do not begin together
+inline bool overlap_in_part(const void *x, int64_t x_bytes, const void *y, int64_t y_bytes)
+{
+    const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y;
+    return a != b && a < b + (uintptr_t)y_bytes && b < a + (uintptr_t)x_bytes;
+}
 
 // ---- MX4 ----------------------------------------------------------------------
 // 2^(s - 127) of a scale byte; what the converters take as their scale (only its exponent counts there).  255, which is an infinity here, is

@@ -258,6 +258,14 @@ int32_t check_track(const char *who, const ihip_kv_track *track, int64_t rows, b
     return IHIP_OK;
 }
 
+int32_t check_before(const char *who, const float *before, float decay, const ihip_kv_track *track, int64_t heads)
+{
+    if (!(decay >= 0.f) || decay > 3.4028234e38f) return fail(IHIP_ERR_INVALID_ARG, "%s: decay = %g", who, decay);
+    const int64_t bytes = heads * track->rows * (int64_t)sizeof(float);
+    if (before && overlap_in_part(before, bytes, track->weights, bytes)) return fail(IHIP_ERR_INVALID_ARG, "%s: before overlaps the weights in part", who);
+    return IHIP_OK;
+}
+
 int32_t check_store(const char *who, const ihip_kv_store *store, const ihip_shape &for_lengths, StoreView *view)
 {
     int32_t rc;

@@ -476,7 +476,7 @@ extern "C" int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tenso
     if (packed->rows > 0 && (rc = check_tensor(q, who, "q")) != IHIP_OK) return rc;
     if (packed->rows > 0 && !lse) return fail(IHIP_ERR_INVALID_ARG, "%s: lse is NULL", who);
     if ((rc = check_track(who, track, 0, false)) != IHIP_OK) return rc;
-    if (!(decay >= 0.f) || decay > 3.4028234e38f) return fail(IHIP_ERR_INVALID_ARG, "%s: decay = %g", who, decay);
+    if ((rc = check_before(who, before, decay, track, (int64_t)packed->B * packed->Hkv)) != IHIP_OK) return rc;
     if ((rc = check_sm_scale(who, sm_scale, &a.scale_log2e)) != IHIP_OK) return rc;
     a.B = packed->B; a.Hq = packed->Hq; a.Hkv = packed->Hkv; a.G = packed->Hq / packed->Hkv;
     a.rows_q = packed->rows; a.rows_k = rows_k; a.window = window;

@@ -78,9 +78,9 @@ def test_key_weights_scratch(b):  # noqa: F811
     assert need(many, 4000, 16) == 256
 
 
-def decode(b, shape=None, q=None, store=None, scale=0.1, decay=1.0, track=0, out=4096, ws=4096, ws_bytes=1 << 30):  # noqa: F811
+def decode(b, shape=None, q=None, store=None, scale=0.1, before=None, decay=1.0, track=0, out=4096, ws=4096, ws_bytes=1 << 30):  # noqa: F811
     s = b.Shape(2, 8, 2, 128, 1, 1, 4096, 64, 0, 1, 0) if shape is None else shape
-    return b.lib().ihip_attn_decode_tracked(by(s), q or b.Tensor(4096, 1024, 128, 128), by(store or store_of(b, 0)), scale, None, decay,
+    return b.lib().ihip_attn_decode_tracked(by(s), q or b.Tensor(4096, 1024, 128, 128), by(store or store_of(b, 0)), scale, before, decay,
                                             by(track_of(b, positions=None, seen=None) if track == 0 else track), out, None, ws, ws_bytes, None)
 
 
@@ -142,6 +142,25 @@ def test_evict_refuses(b):  # noqa: F811
     assert evict(b, keep=1 << 30, max_len=64, B=1) == UNSUPPORTED
     assert L.ihip_kv_evict_workspace_bytes(2, 2, 64, 0) == 0 and L.ihip_kv_evict_workspace_bytes(2, 0, 64, 1) == 0
     assert evict(b, B=0, track=None, lens=None, kept=None) == 0
+
+
+def test_arrays_that_overlap_in_part(b):  # noqa: F811
+    """The same array or one apart is taken, a shifted one is not: rows of it would be read behind their change."""
+    L, at = b.lib(), 1 << 20
+    bytes_ = 2 * 2 * 64 * 4
+    track = track_of(b, weights=at, positions=at + 8 * bytes_)
+    for shift in (4, -4, bytes_ - 4, 4 - bytes_):
+        assert weights(b, before=at + shift, track=track) == BAD and b"before" in L.ihip_last_error()
+        assert decode(b, before=at + shift, track=track) == BAD and b"before" in L.ihip_last_error()
+        assert evict(b, track=track, to=track_of(b, weights=at + shift, positions=4096)) == BAD and b"overlap" in L.ihip_last_error()
+        assert evict(b, track=track, to=track_of(b, weights=4096, positions=at + 8 * bytes_ + shift)) == BAD and b"overlap" in L.ihip_last_error()
+    for shift in (0, bytes_, -bytes_):                # (refused for what is looked at later)
+        assert decode(b, before=at + shift, track=track, ws=None) == WORKSPACE
+    big = dict(max_len=4096, keep=1024)
+    at, rows = 1 << 30, 2 * 2 * 4096 * 4
+    track = track_of(b, rows=4096, weights=at, positions=at)
+    for shift in (0, rows, -rows):
+        assert evict(b, track=track, to=track_of(b, rows=4096, weights=at + shift, positions=at), ws=None, **big) == WORKSPACE
 
 
 def test_tensors_that_are_refused(b):  # noqa: F811
