@@ -100,6 +100,39 @@ def test_many_sequences(ihip):
     check(c, q, out, lse, w, old)
 
 
+def test_more_problems_than_a_grid_has_rows(ihip):
+    """8,200 sequences of 8 KV heads: the same bits as in calls of fewer of them."""
+    B, Hkv, Hq, T = 8200, 8, 16, 4
+    g = torch.Generator().manual_seed(31)
+    k, v = (torch.randn((B, Hkv, T, D), generator=g).bfloat16().cuda() for _ in range(2))
+    lens = torch.randint(0, T + 1, (B,), generator=g).to(torch.int32).cuda()
+    q = queries(B, Hq, 32)
+    old = torch.rand((B, Hkv, T), generator=g).cuda()
+    track = ihip.KVTrack(old.clone())
+    out, lse = ihip.attn_decode_tracked(q, ihip.KVStore.bf16(k, v), track, lens, T, want_lse=True)
+    for b0 in range(0, B, 2050):
+        b1 = b0 + 2050
+        part = ihip.KVTrack(old[b0:b1].clone())
+        o, l = ihip.attn_decode_tracked(q[b0:b1], ihip.KVStore.bf16(k[b0:b1], v[b0:b1]), part, lens[b0:b1].clone(), T, want_lse=True)
+        assert torch.equal(o, out[b0:b1]) and torch.equal(l, lse[b0:b1]) and torch.equal(part.weights, track.weights[b0:b1])
+
+
+def test_heads_that_are_one_in_memory(ihip):
+    """K and V heads that stand for all of them, a query that is that of all sequences: what copies of them give."""
+    lens = torch.tensor([777, 64], dtype=torch.int32).cuda()
+    k, v = (queries(2, 800, s).view(2, 1, 800, D) for s in (33, 34))
+    q = queries(1, 8, 35)
+    got = []
+    for copies in (False, True):
+        a, b, x = k.expand(-1, 4, -1, -1), v.expand(-1, 4, -1, -1), q.expand(2, -1, -1, -1)
+        if copies:
+            a, b, x = a.contiguous(), b.contiguous(), x.contiguous()
+        track = ihip.KVTrack(torch.zeros((2, 4, 800)).cuda())
+        got.append((*ihip.attn_decode_tracked(x, ihip.KVStore.bf16(a, b), track, lens, 800, want_lse=True), track.weights))
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_rows_on_no_page(ihip, fmt):
     c = Cache(ihip, fmt, [100, 40, 33], 2, 16, seed=6, missing=[(0, 2), (1, 0), (1, 1), (1, 2), (2, 2)])

@@ -113,6 +113,25 @@ def test_first_and_last_positions_are_kept(ihip):
         assert len(left) == 32 and set(range(8)) | set(range(290, 300)) <= left
 
 
+@pytest.mark.parametrize("n,keep", [(300, 250), (2000, 700), (20000, 900)])
+@pytest.mark.parametrize("shared", ["weights", "positions"])
+def test_a_cut_track_that_shares_an_array(ihip, n, keep, shared):
+    """One of the two arrays of `to` is that of the track itself, the other one apart."""
+    c = Cache(ihip, "e4m3", [n, n // 2], 2, 16, seed=21)
+    track = make_track(ihip, c, c.T, seed=22)
+    w, p, seen = (x.clone() for x in (track.weights, track.positions, track.seen))
+    other = torch.full(w.shape, 7.0 if shared == "positions" else 7, dtype=torch.float32 if shared == "positions" else torch.int32).cuda()
+    to = ihip.KVTrack(other, track.positions) if shared == "positions" else ihip.KVTrack(track.weights, other)
+    ihip.kv_evict(c.store, track, c.seq_lens, c.T, keep, n_sink=2, n_recent=9, to=to)
+    for b, t in enumerate(c.lens):
+        for g in range(2):
+            m = evicted(w[b, g].cpu().numpy(), p[b, g].cpu().numpy(), t, keep, 2, int(seen[b]) - 9)
+            m = torch.from_numpy(m[:min(t, keep)]).long().cuda()
+            assert torch.equal(to.weights[b, g, :len(m)], w[b, g, m]) and torch.equal(to.positions[b, g, :len(m)], p[b, g, m])
+            assert bool((other[b, g, len(m):] == 7).all())
+    assert torch.equal(track.positions if shared == "weights" else track.weights, p if shared == "weights" else w)
+
+
 def test_more_protected_rows_than_are_kept(ihip):
     """Positions that are not distinct: no more than `keep` rows, the lower ones."""
     c = Cache(ihip, "bf16", [200], 1, 0, seed=1)

@@ -108,6 +108,30 @@ def test_windows_of_many_keys(ihip):
         assert bool((track.weights[b, :, n:] == 5).all())
 
 
+@pytest.mark.parametrize("max_q,window", [(9, None), (100, None), (9, 2)])
+def test_many_sequences(ihip, max_q, window):
+    """More sequences than a wave has lanes, empty ones among them; a bound that is loose by much."""
+    new, total = [i * 7 % 10 for i in range(150)], [i * 7 % 10 + i * i % 23 for i in range(150)]
+    q, k, lse = inputs(new, total, 8, 1, seed=11)
+    track = ihip.KVTrack(torch.full((150, 1, 40), 5.0).cuda())
+    ihip.prompt_key_weights(q.cuda(), k.cuda(), offsets(new).cuda(), max_q, lse.cuda(), track, cu_k=offsets(total).cuda(), window=window, fresh=True)
+    check(track.weights, None, 1.0, q, k, lse, new, total, 1, window or 10 ** 9, 40)
+    for b, t in enumerate(total):
+        assert bool((track.weights[b, :, t:] == 5).all())
+
+
+@pytest.mark.parametrize("window", [None, 16])
+def test_heads_that_are_one_in_memory(ihip, window):
+    """A key head that stands for all of them, a query's heads that are the same."""
+    new, Hq, Hkv = [140, 33], 8, 4
+    q, k, lse = inputs(new, new, 1, 1, seed=12, extra=0)
+    q, k, lse = q.expand(-1, Hq, -1), k.expand(-1, Hkv, -1), lse.expand(-1, Hq).contiguous()
+    track = ihip.KVTrack(torch.zeros((2, Hkv, 140)).cuda())
+    ihip.prompt_key_weights(q[:, :1].cuda().expand(-1, Hq, -1), k[:, :1].cuda().expand(-1, Hkv, -1), offsets(new).cuda(), 140, lse.cuda(), track, window=window,
+                            fresh=True)
+    check(track.weights, None, 1.0, q, k, lse, new, new, Hkv, window or 10 ** 9, 140)
+
+
 @pytest.mark.parametrize("window", [None, 40])
 def test_sequences_longer_than_max_q(ihip, window):
     """They may be done in part; the others are not."""
