@@ -643,7 +643,7 @@ int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tensor q, ihip_t
  * every row the probabilities that the query heads of its KV head give it:
  *   weights[b][g][r] = decay * before[b][g][r] + sum over the heads of exp(score - lse).
  * shape->n_sink and n_stream choose nothing here.  out, out_lse, sm_scale (for E4M3 rows also its product with
- * k_scale) as in ihip_sparse_attn_decode_mx4kv, and the same arithmetic.  The output of an idle
+ * k_scale) as in ihip_sparse_attn_decode_mx4kv; probabilities keep 24 bits in the output.  The output of an idle
  * place of the batch, or of a sequence without pages, is 0, its log-sum-exp -INFINITY; a row on a page with a
  * negative id is left out, its weight gets nothing but decay * before.  Rows behind a sequence are not
  * read, and what stands beside them is left as it was.  What is not finite in an attended K or V row makes the results NaN or infinite that it goes

@@ -5,13 +5,14 @@
 // (Where sequences are one part each, the first does it all.)
 //
 // A wave takes 32 rows at a time, the products on v_mfma_f32_16x16x32_bf16 (rows widened to bf16, exact); no value crosses lanes in between:
-//   scores   16 K rows x twice 8 heads (fewer repeat the last).  Lane (n, g) = (l % 16, l / 16) brings 16-byte pieces of row n, and gets head
-//            n % 8's scores of keys 4 g + r and 16 + 4 g + r.  A piece of bf16 is 8 of the dims 32 j + 8 g of step j, of E4M3 16 of 64 j + 16 g
+//   scores   16 K rows x twice 8 heads, or four times 4 (fewer repeat the last).  Lane (n, g) = (l % 16, l / 16) brings 16-byte pieces of row n, and gets
+//            head n % 8's (n % 4's) scores of keys 4 g + r and 16 + 4 g + r.  A piece of bf16 is 8 of the dims 32 j + 8 g of step j, of E4M3 16 of 64 j + 16 g
 //            (two steps), of 4 bits the 32 of 32 g, one scale's (four steps); the queries' pieces are the same.
-//   output   16 rows x 32 keys x 16 dims, eight times: a lane's eight probabilities are its part of the left operand as they are (rounded to
-//            bf16 in rows 0 .. 7, what that dropped in rows 8 .. 15; the two are added in LDS), key 16 (i / 4) + 4 g + i % 4 for element i; for the right
-//            one it brings dims 8 n .. 8 n + 7 of the same keys, and column n of product j is dim 8 n + j.
-// So a probability is off by at most 2^-16 of it in the output.  The sums and the weights take the probabilities as they were.
+//   output   16 rows x 32 keys x 16 dims, eight times: a lane's eight probabilities are its part of the left operand as they are, key
+//            16 (i / 4) + 4 g + i % 4 for element i; for the right one it brings dims 8 n .. 8 n + 7 of the same keys, and column n of product j is dim 8 n + j.
+// A probability goes into the products as three bf16 numbers, what one dropped in the next, which are its 24 bits.  Up to four heads have them in rows
+// 0 .. 3, 8 .. 11 and 4 .. 7 (12 .. 15: 0); eight have two in rows 0 .. 7 and 8 .. 15, and the third in rows 0 .. 7 of eight products more.  The rows are
+// added in LDS.  (Two parts alone: one output in 400 is another bf16 number than that of fp32 probabilities, with three one in 2,000.)
 // Bound by memory: 4 sequences of 57,654 to 100,003 rows in bf16, 32 heads on 8, 1.39 GB, take 306 us (4.5 TB/s, a copy of 2 GB moves 5.0; the
 // scores are 43 MB more) and 17 for the join; 32 of 7,383 to 16,384 in E4M3, 782 MB, 186 (4.2; scores 49 MB) and 17; 8 of 20,637 to 32,768 in
 // MX FP4, 232 MB, 64 (3.6; scores 27 MB, and 20 requests for 32 rows) and 9.  One of 2,051 takes 6 and 4, chains of latencies.
@@ -51,6 +52,8 @@ struct TrackedArgs {
 
 __device__ inline uint16_t to_bf16(float x) { return (uint16_t)pack_bf16x2(x, x); }        // (NaN stays it)
 __device__ inline int tracked_len(const TrackedArgs &a, int b) { return min(max(a.ge.seq_lens[b], 0), a.max_len); }
+// softmax_exp with the exponent rounded by itself: against the 26 of kSoftmaxShift its last five bits would go
+__device__ inline float tracked_exp(float score, float ref, float scale_log2e) { return __builtin_amdgcn_exp2f((score - ref) * scale_log2e) * 0x1p-26f; }
 // A row's probability is 2^(c (s - reference) - log2 of the sum of those); without a key that is there, 0.  sum: as it was added up, times 2^-kSoftmaxShift
 __device__ inline float tracked_log2_sum(float sum) { return sum == 0.f ? INFINITY : log2f(sum) + kSoftmaxShift; }
 __device__ inline float tracked_probability(float score, float2 all, float scale_log2e) { return __builtin_amdgcn_exp2f(fmaf(score - all.x, scale_log2e, -all.y)); }
@@ -78,10 +81,11 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
     if (split > 0 && steps == 0) return;             // (part 0 of an idle place has its output to write)
     const int64_t pbase = ((int64_t)p * a.n_splits + split) * G;
 
-    // where the part's rows are, in bytes from row 0; behind the last step: the waves' results, of the two parts of the probabilities
+    // where the part's rows are, in bytes from row 0; behind the last step: the waves' results, of four rows of the products at a time
+    constexpr int kParts = HEADS == 4 ? 3 : 2;
     __shared__ __attribute__((aligned(16))) union {
         struct { int64_t k[kTrOnePart], v[kTrOnePart]; } row;
-        float acc[kTrWaves][2][HEADS][kD];
+        float acc[kTrWaves][kParts][HEADS][kD];
     } sh;
     __shared__ uint32_t sh_there[kTrOnePart / kTrStep];     // which of a step's rows hold a key
     __shared__ float sh_m[kTrWaves][HEADS], sh_l[kTrWaves][HEADS];
@@ -90,7 +94,7 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
     // The operand of step j: 16-byte pieces as above
     bf16x8 qb[4];
     {
-        const uint16_t *qp = a.q + b * a.q_sb + (int64_t)(kv_head * G + min(n & 7, G - 1)) * a.q_sh;
+        const uint16_t *qp = a.q + b * a.q_sb + (int64_t)(kv_head * G + min(n & (HEADS - 1), G - 1)) * a.q_sh;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             qb[j] = *reinterpret_cast<const bf16x8 *>(qp + (FORMAT == IHIP_KV_BF16 ? 32 * j + 8 * g : FORMAT == IHIP_KV_E4M3 ? 64 * (j >> 1) + 16 * g + 8 * (j & 1) : 32 * g + 8 * j));
@@ -149,8 +153,9 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
         else return mx4_pair<D>(r.v[i], mx4_scale(r.v_scale[i]));
     };
 
-    const uint32_t second = n < 8 ? 0u : ~0u;        // lanes that bring the second parts of the probabilities
-    float *scores = a.scores + ((int64_t)p * G + min(n & 7, G - 1)) * a.score_stride + s0 + 4 * g;
+    // lanes whose first, and first and second parts of the probabilities other lanes bring; lanes that bring none
+    const uint32_t not_first = (HEADS == 4 ? n < 4 : n < 8) ? 0u : ~0u, not_second = n >= 4 && n < 8 ? ~0u : 0u, none = n >= 12 ? 0u : ~0u;
+    float *scores = a.scores + ((int64_t)p * G + min(n & (HEADS - 1), G - 1)) * a.score_stride + s0 + 4 * g;
     f32x4 acc[8];                                    // rows 4 g + r, dim 8 n + j
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -186,7 +191,7 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
         float w[8], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            w[i] = softmax_exp(c[i >> 2][i & 3], m, a.scale_log2e);    // of -inf: 0
+            w[i] = tracked_exp(c[i >> 2][i & 3], m, a.scale_log2e);    // of -inf: 0
             sum += w[i];
         }
         if (__any(!(sum <= kSoftmaxMaxSum))) {       // the reference follows where the scores outgrew it
@@ -200,7 +205,7 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
             sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                w[i] = softmax_exp(c[i >> 2][i & 3], m, a.scale_log2e);
+                w[i] = tracked_exp(c[i >> 2][i & 3], m, a.scale_log2e);
                 sum += w[i];
             }
 #pragma unroll
@@ -211,11 +216,20 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
             }
         }
         l += sum;
-        uint32_t part[4];
+        uint32_t part[4], third[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t first = pack_bf16x2(w[2 * i], w[2 * i + 1]) & second;
-            part[i] = pack_bf16x2(w[2 * i] - __uint_as_float(first << 16), w[2 * i + 1] - __uint_as_float(first & 0xffff0000u));
+            auto dropped = [](float x, uint32_t p, int j) { return x - __uint_as_float(j == 0 ? p << 16 : p & 0xffff0000u); };
+            const uint32_t first = pack_bf16x2(w[2 * i], w[2 * i + 1]), from_w = first & not_first;
+            const float x = dropped(w[2 * i], HEADS == 4 ? from_w : first, 0), y = dropped(w[2 * i + 1], HEADS == 4 ? from_w : first, 1);
+            const uint32_t next = pack_bf16x2(x, y);
+            if constexpr (HEADS == 4) {              // (nothing is taken off in the lanes of the first parts, once in those of the second, twice of the third)
+                const uint32_t from_x = next & not_second;
+                part[i] = pack_bf16x2(dropped(x, from_x, 0), dropped(y, from_x, 1)) & none;
+            } else {
+                part[i] = not_first ? next : first;
+                third[i] = pack_bf16x2(dropped(x, next, 0), dropped(y, next, 1)) & ~not_first;
+            }
         }
         const bf16x8 pw = __builtin_bit_cast(bf16x8, make_uint4(part[0], part[1], part[2], part[3]));
         auto dims = [&](auto d) {                    // 8 n + 2 d and 8 n + 2 d + 1
@@ -228,8 +242,12 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
                 hi[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
             }
             f32x4 &even = acc[2 * decltype(d)::value], &odd = acc[2 * decltype(d)::value + 1];
-            even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw, __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), even, 0, 0, 0);
-            odd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw, __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), odd, 0, 0, 0);
+            auto add = [&](const bf16x8 &p) {
+                even = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), even, 0, 0, 0);
+                odd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), odd, 0, 0, 0);
+            };
+            add(pw);
+            if constexpr (HEADS == 8) add(__builtin_bit_cast(bf16x8, make_uint4(third[0], third[1], third[2], third[3])));
         };
         dims(std::integral_constant<int, 0>{});
         dims(std::integral_constant<int, 1>{});
@@ -238,15 +256,15 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
         if (kAheadLoads) r = nx;
     }
 
-    // the waves and both parts are merged through LDS
+    // the waves and the parts are merged through LDS
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (lane < HEADS) { sh_m[wv][lane] = m; sh_l[wv][lane] = l; }
     __syncthreads();
-    if (4 * (g & 1) < HEADS) {
+    if (HEADS == 8 || g < kParts) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-            float *to = &sh.acc[wv][g >> 1][4 * (g & 1) + h][8 * n];
+            float *to = HEADS == 8 ? &sh.acc[wv][g >> 1][4 * (g & 1) + h][8 * n] : &sh.acc[wv][g][h][8 * n];
             *reinterpret_cast<float4 *>(to) = make_float4(acc[0][h], acc[1][h], acc[2][h], acc[3][h]);
             *reinterpret_cast<float4 *>(to + 4) = make_float4(acc[4][h], acc[5][h], acc[6][h], acc[7][h]);
         }
@@ -262,7 +280,7 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
         for (int w = 0; w < kTrWaves; ++w) {
             const float x = softmax_weight(sh_m[w][h], M, a.scale_log2e);
             L = fmaf(x, sh_l[w][h], L);
-            A = fmaf(x, sh.acc[w][0][h][c] + sh.acc[w][1][h][c], A);
+            A = fmaf(x, sh.acc[w][0][h][c] + (kParts == 3 ? sh.acc[w][1][h][c] + sh.acc[w][kParts - 1][h][c] : sh.acc[w][1][h][c]), A);
         }
         if (a.n_splits == 1) {                       // nothing to join
             const int64_t hq = (int64_t)b * a.ge.Hq + kv_head * G + h;
