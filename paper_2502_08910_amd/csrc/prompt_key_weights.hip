@@ -40,6 +40,13 @@ struct KeyWeightArgs {
     bool near;                       // G divides a tile's rows, whose queries are less than 2^31 bytes apart
 };
 
+// A log-sum-exp to base 2 with one rounding: that of log2 e would be a factor of all of a query's probabilities (1.4e-7 for one of 10)
+__device__ inline float key_weight_r(float lse)
+{
+    constexpr float kLog2e = 1.44269504088896340736f, kRest = (float)(1.44269504088896340736 - (double)kLog2e);
+    return fmaf(lse, kLog2e, lse * kRest);
+}
+
 // A sequence, and the tiles of its rows that count
 struct KeyWeightSeq {
     int b, q_first, nq, k_first, nk, ahead, row0, rows;      // rows row0 .. rows - 1 count
@@ -276,7 +283,7 @@ __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weig
         for (int i = 0; i < kPieces; ++i) send(0, i, last_row + in_tile(i) < seq.rows ? q_at[i] : q_of(seq.nq - 1, a.G - 1, i));
         if (tid < kKwRows) {
             const bool there = last_row + tid < seq.rows;
-            sh_r[0][tid] = (there ? *r_at : lse[(int64_t)(seq.nq - 1) * a.Hq + a.G - 1]) * 1.44269504088896340736f;
+            sh_r[0][tid] = key_weight_r(there ? *r_at : lse[(int64_t)(seq.nq - 1) * a.Hq + a.G - 1]);
             sh_last[0][tid] = there ? r_query + seq.ahead : -1;
         }
     }
@@ -319,7 +326,7 @@ __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weig
         first_head -= heads_left;
         if (first_head < 0) { first_head += a.G; --first_query; }
         if (t > t0 && tid < kKwRows) {
-            sh_r[st3][tid] = r_next * 1.44269504088896340736f;      // (not before: the load would be waited for there)
+            sh_r[st3][tid] = key_weight_r(r_next);      // (not before: the load would be waited for there)
             sh_last[st3][tid] = last_next;
         }
     }
@@ -364,7 +371,7 @@ __global__ __launch_bounds__(kKwThreads, 2) void prompt_key_weights_window_kerne
     }
     for (int i = tid; i < tiles * kKwRows; i += kKwThreads) {
         const int row = row0 + min(i, rows - 1), query = query_of(row);
-        sh_r[i] = lse[(int64_t)query * a.Hq + row - query * a.G] * 1.44269504088896340736f;
+        sh_r[i] = key_weight_r(lse[(int64_t)query * a.Hq + row - query * a.G]);
         sh_last[i] = i < rows ? query + seq.ahead : -1;
     }
     keys.keys_are_there();
