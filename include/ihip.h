@@ -646,8 +646,9 @@ int32_t ihip_prompt_key_weights(const ihip_packed *packed, ihip_tensor q, ihip_t
  * k_scale) as in ihip_sparse_attn_decode_mx4kv; probabilities keep 24 bits in the output.  The output of an idle
  * place of the batch, or of a sequence without pages, is 0, its log-sum-exp -INFINITY; a row on a page with a
  * negative id is left out, its weight gets nothing but decay * before.  Rows behind a sequence are not
- * read, and what stands beside them is left as it was.  What is not finite in an attended K or V row makes the results NaN or infinite that it goes
- * into: of a K row all outputs and weights of its KV head's queries.
+ * read, and what stands beside them is left as it was.  What is not finite in an attended V row makes the results NaN or infinite that it goes
+ * into.  A score of NaN or +INFINITY makes output, log-sum-exp and probabilities of its query head NaN, a score of -INFINITY is a probability of 0
+ * (a sequence of such scores alone: as one without pages).
  *   before, decay, track   as in ihip_prompt_key_weights
  *   ws                     device scratch of ihip_attn_decode_tracked_workspace_bytes(shape), 16-byte aligned
  */

@@ -56,7 +56,12 @@ __device__ inline int tracked_len(const TrackedArgs &a, int b) { return min(max(
 __device__ inline float tracked_exp(float score, float ref, float scale_log2e) { return __builtin_amdgcn_exp2f((score - ref) * scale_log2e) * 0x1p-26f; }
 // A row's probability is 2^(c (s - reference) - log2 of the sum of those); without a key that is there, 0.  sum: as it was added up, times 2^-kSoftmaxShift
 __device__ inline float tracked_log2_sum(float sum) { return sum == 0.f ? INFINITY : log2f(sum) + kSoftmaxShift; }
-__device__ inline float tracked_probability(float score, float2 all, float scale_log2e) { return __builtin_amdgcn_exp2f(fmaf(score - all.x, scale_log2e, -all.y)); }
+// (a score of -inf, as of a row that is not there, is 0 beside any other scores, NaN among them)
+__device__ inline float tracked_probability(float score, float2 all, float scale_log2e)
+{
+    const float p = __builtin_amdgcn_exp2f(fmaf(score - all.x, scale_log2e, -all.y));
+    return score == -INFINITY ? 0.f : p;
+}
 __device__ inline void store_tracked_weight(const TrackedArgs &a, int64_t at, float w) { a.weights[at] = a.before ? fmaf(a.decay, a.before[at], w) : w; }
 
 template <int FORMAT>
