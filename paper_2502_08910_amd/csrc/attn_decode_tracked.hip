@@ -417,7 +417,7 @@ __global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(co
 // 7,383 to 16,384 in E4M3 200 / 201 / 201 / 207, one of 200,001 in MX FP4 77 / 82 / 77 / 82; one of 30,001 in bf16, with 128 / 256 / 512 rows
 // 39 / 32 / 29.  Short sequences in one part each need no join: 4 of 1,000 14.7 where parts take 17.8, 16 of 1,000 16.7 / 17.7, 32 of 1,024 to 1,055
 // 20.3 / 19.6.
-struct TrackedPlan { int splits, per; int64_t score_stride; size_t bytes; };
+struct TrackedPlan { int splits, per; int64_t score_stride, ml; size_t bytes; };         // ml: floats of part_ml, in whole 16 bytes (part_acc is behind it)
 static TrackedPlan tracked_plan(const ihip_shape &s)
 {
     const int64_t total = s.max_seq_len, P = std::max<int64_t>(1, (int64_t)s.B * s.Hkv);
@@ -426,7 +426,9 @@ static TrackedPlan tracked_plan(const ihip_shape &s)
     if (total <= (P < compute_units() ? kTrOnePart : kTrOnePart / 2)) r.per = (int)((total + kTrMinSplit - 1) / kTrMinSplit * kTrMinSplit);
     r.splits = (int)((total - 1) / r.per + 1);
     r.score_stride = (total + kTrStep - 1) / kTrStep * kTrStep;
-    r.bytes = (size_t)s.B * s.Hq * (r.score_stride + (int64_t)r.splits * (2 + kD)) * sizeof(float);
+    const int64_t heads = (int64_t)s.B * s.Hq;
+    r.ml = (heads * r.splits * 2 + 3) / 4 * 4;
+    r.bytes = (size_t)(heads * (r.score_stride + (int64_t)r.splits * kD) + r.ml) * sizeof(float);
     return r;
 }
 
@@ -475,7 +477,7 @@ extern "C" int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor
     a.scores = (float *)ws;
     a.score_stride = plan.score_stride;
     a.part_ml = a.scores + P * a.ge.G * plan.score_stride;
-    a.part_acc = a.part_ml + P * a.n_splits * a.ge.G * 2;
+    a.part_acc = a.part_ml + plan.ml;
     a.out = (uint16_t *)out;
     a.out_lse = out_lse;
     a.before = before;
