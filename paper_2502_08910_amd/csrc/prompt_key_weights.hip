@@ -79,13 +79,6 @@ struct KeyWeightSeq {
     __device__ int first_tile(const KeyWeightArgs &a, int k) const { return (int)min(max((int64_t)0, ((int64_t)k - ahead) * a.G - row0) / kKwRows, (int64_t)tiles()); }
 };
 
-// 16 bytes a lane from a scalar base and the lane's byte offset to the LDS byte address dst + 16 l (counts on vmcnt).  M0 is left as it is:
-// nothing else in this kernel reads it, and it is not the compiler's to keep values in.
-__device__ inline void key_weights_to_lds(uint32_t dst, const uint16_t *base, uint32_t byte_off)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(byte_off), "s"(base) : "memory");
-}
-
 // A wave's SETS times 32 keys and what has been added up for them.  Rows come half a tile at a time: the products of 32 rows with the keys, and between
 // them, two scores after each, the exponentials of the half before.  Score i is that of row 8 (i / 4) + 4 half + i % 4.
 struct KeyWeightTile { const uint16_t *q; const float *r; const int *last; };        // 64 rows in LDS: chunks XORed with the row; r; the last key
@@ -257,7 +250,7 @@ __global__ __launch_bounds__(kKwThreads, SETS == 2 ? 2 : 3) void prompt_key_weig
         if (a.near) {
             q_base -= q_step;
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) key_weights_to_lds(stage_of(st, i), q_base, q_off[i]);
+            for (int i = 0; i < kPieces; ++i) global_to_lds(stage_of(st, i), q_base, q_off[i]);
             return;
         }
 #pragma unroll
