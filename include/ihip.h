@@ -666,7 +666,7 @@ int32_t ihip_attn_decode_tracked(const ihip_shape *shape, ihip_tensor q, const i
  *   keep       at least 1, at least n_sink + n_recent
  *   to         weights, positions and rows of the cut cache; may be track or NULL, which is the same.  With arrays of its own, apart from track's, all
  *              kept rows are written there (rows: at least min(keep, max_seq_len)), track's are left as they were
- *   new_lens   device int32 [B]: min(seq_lens[b], keep); may be seq_lens, not a part of it.  seen does not change
+ *   new_lens   device int32 [B]: min(seq_lens[b], keep); may be seq_lens, not a part of it, and nothing of seen, which does not change
  *   kept       device int32 [B, Hkv, keep]: the row that each row was, -1 behind a sequence
  *   ws         device scratch of ihip_kv_evict_workspace_bytes(B, Hkv, max_seq_len, keep), 16-byte aligned
  * Two rows must not share memory, two sequences no page.  Where one of the two pages of a move has a negative id, K and V do not move.

@@ -682,6 +682,9 @@ extern "C" int32_t ihip_kv_evict(const ihip_kv_store *store, const ihip_kv_track
         return fail(IHIP_ERR_WORKSPACE, "%s: workspace of %zu bytes, 16-byte aligned, needed, %zu given", who, plan.bytes, ws_bytes);
     const int64_t P = (int64_t)B * Hkv, moves = ((int64_t)keep - 1) / kMoveRows + 1;
     if (P > INT32_MAX / kEvictThreads || moves > 65535) return fail(IHIP_ERR_UNSUPPORTED, "%s: B * Hkv = %lld, keep = %d are too large", who, (long long)P, keep);
+    // (the tokens seen are read while lengths are written, and would be the cut ones afterwards)
+    if (new_lens == track->seen || overlap_in_part(new_lens, lens_bytes, track->seen, lens_bytes))
+        return fail(IHIP_ERR_INVALID_ARG, "%s: new_lens overlaps the tokens seen", who);
     a.B = B; a.Hkv = Hkv; a.max_len = max_seq_len; a.keep = keep; a.n_sink = n_sink; a.n_recent = n_recent;
     a.lens = seq_lens; a.seen = track->seen;
     a.weights = track->weights; a.positions = track->positions; a.rows = track->rows;
