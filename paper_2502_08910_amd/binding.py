@@ -1011,7 +1011,8 @@ def prompt_key_weights(q: torch.Tensor, k: torch.Tensor, cu_q: torch.Tensor, max
     rows_k, Hkv, _ = k.shape
     B = cu_q.numel() - 1
     sm_scale = 1.0 / math.sqrt(d) if sm_scale is None else sm_scale
-    window = 2 ** 31 - 1 if window is None else min(window, 2 ** 31 - 1)
+    window = 2 ** 31 - 1 if window is None else max(-1, min(window, 2 ** 31 - 1))
+    max_q = max(-1, min(max_q, 2 ** 31 - 1))
     _same_device(q.device, k=k, lse=lse, ws=ws)
     track.check(B, Hkv, q.device)
     if lse.shape != (rows, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous():
@@ -1090,6 +1091,8 @@ def kv_evict(store: KVStore, track: KVTrack, seq_lens: torch.Tensor, max_seq_len
     of most weight between them, for each KV head by itself.  to: a track of its own for the cut cache (None: track itself); new_lens int32
     [B] (made if not given; may be seq_lens).  -> (new_lens, kept int32 [B, Hkv, keep]: the row that each row was, -1 behind a sequence)."""
     B = seq_lens.numel()
+    if max(keep, n_sink, n_recent) >= 2 ** 31 or min(keep, n_sink, n_recent) < 0:        # (32 bits of them would go on)
+        raise IhipError(f"keep = {keep}, n_sink = {n_sink}, n_recent = {n_recent}: need numbers from 0 to 2^31 - 1")
     if B > store.B or max_seq_len > store.tokens:
         raise IhipError(f"the store holds {store.B} sequences of {store.tokens} tokens")
     for t in (track, to):
