@@ -12,10 +12,11 @@
 //            16 (i / 4) + 4 g + i % 4 for element i; for the right one it brings dims 8 n .. 8 n + 7 of the same keys, and column n of product j is dim 8 n + j.
 // A probability goes into the products as three bf16 numbers, what one dropped in the next, which are its 24 bits.  Up to four heads have them in rows
 // 0 .. 3, 8 .. 11 and 4 .. 7 (12 .. 15: 0); eight have two in rows 0 .. 7 and 8 .. 15, and the third in rows 0 .. 7 of eight products more.  The rows are
-// added in LDS.  (Two parts alone: one output in 400 is another bf16 number than that of fp32 probabilities, with three one in 2,000.)
-// Bound by memory: 4 sequences of 57,654 to 100,003 rows in bf16, 32 heads on 8, 1.39 GB, take 306 us (4.5 TB/s, a copy of 2 GB moves 5.0; the
-// scores are 43 MB more) and 17 for the join; 32 of 7,383 to 16,384 in E4M3, 782 MB, 186 (4.2; scores 49 MB) and 17; 8 of 20,637 to 32,768 in
-// MX FP4, 232 MB, 64 (3.6; scores 27 MB, and 20 requests for 32 rows) and 9.  One of 2,051 takes 6 and 4, chains of latencies.
+// added in LDS.  (Of 32 sequences in E4M3 0.02 % of the outputs are another bf16 number than float64's, with two parts 0.24 %.)
+// Bound by memory: 4 sequences of 57,654 to 100,003 rows in bf16, 32 heads on 8, 1.39 GB, take 314 us (4.4 TB/s, a copy of 2 GB moves 5.0; the
+// scores are 43 MB more) and 18 for the join; 32 of 7,383 to 16,384 in E4M3, 782 MB, 193 (4.1; scores 49 MB) and 18; 8 of 20,637 to 32,768 in
+// MX FP4, 232 MB, 66 (3.5; scores 27 MB, and 20 requests for 32 rows) and 10.  One of 2,051 takes 7 and 4, chains of latencies.  (The two kernels
+// by themselves, medians under the profiler.)
 #include "api_checks.h"
 #include "decode_softmax.h"
 #include "kv_store.h"
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(kTrThreads, FORMAT == IHIP_KV_BF16 ? 2 : 4) void at
     float m = kSoftmaxLowest, l = 0.f;               // of head n (m: the same in the four lanes of a head; l: of this lane's keys)
     Rows r, nx;
     // Wide rows are asked for a step ahead, two waves a SIMD; of narrow ones four waves have as many bytes on their way, and one step's registers
-    // (E4M3, MX FP4 with three waves and a step ahead: 187 and 75 us where this takes 186 and 70)
+    // (three waves and a step ahead: as long in E4M3, 7 % longer in MX FP4)
     constexpr bool kAheadLoads = FORMAT == IHIP_KV_BF16;
     if (kAheadLoads && wv < steps) load(wv, r);
     for (int step = wv; step < steps; step += kTrWaves) {
@@ -413,7 +414,7 @@ __global__ __launch_bounds__(kTrThreads) void attn_decode_tracked_join_kernel(co
 }
 
 // All parts have as many rows, so that workgroups take as long as each other where sequences do not: kTrMaxSplit, or fewer where that would leave
-// compute units with less than two.  us for 768 / 512 / 1,024 / 2,048 rows: 8 sequences of 20,637 to 32,768 in MX FP4 74 / 77 / 78 / 83, 32 of
+// compute units with less than two.  us a call, with probabilities of two bf16 numbers (three: 2 more in MX FP4, 1 in E4M3), for 768 / 512 / 1,024 / 2,048 rows: 8 sequences of 20,637 to 32,768 in MX FP4 74 / 77 / 78 / 83, 32 of
 // 7,383 to 16,384 in E4M3 200 / 201 / 201 / 207, one of 200,001 in MX FP4 77 / 82 / 77 / 82; one of 30,001 in bf16, with 128 / 256 / 512 rows
 // 39 / 32 / 29.  Short sequences in one part each need no join: 4 of 1,000 14.7 where parts take 17.8, 16 of 1,000 16.7 / 17.7, 32 of 1,024 to 1,055
 // 20.3 / 19.6.

@@ -10,9 +10,10 @@
 //   more                in chunks, one workgroup each: digits, candidates, ranks (a launch each: what all chunks have found is read by the next);
 //                       of very many rows two digits.  Only where more than kEvictList rows have them does each workgroup look at all rows for the rest.
 //   many moves          kv_evict_move_kernel, 16 lanes a row, four rows of each on their way.
-// 1,088 rows to 1,024, 32 sequences of 8 KV heads, take 9 us, phases between barriers; 32,749 to 4,096 bf16 rows 27, four launches of 5 to 9;
-// 77,777 to 131,072 E4M3 rows of four sequences to 16,384 each 100, of which 62 move 450,000 rows of K and of V (4.1 TB/s) and 37 are three passes
-// over 34 MB of weights and positions.
+// 1,088 rows to 1,024, 32 sequences of 8 KV heads, take 9 us, phases between barriers; 32,749 to 4,096 bf16 rows 27, four launches of 5 to 8;
+// 77,777 to 131,072 E4M3 rows of four sequences to 16,384 each 100, of which 63 move 450,000 rows of K and of V (4.0 TB/s) and 38 are three passes
+// over 28 MB of weights and positions.  That is where weights spread over octaves.  A first digit is an eighth of an octave: of the sums that 64 queries of
+// random vectors leave, 11,500 of 32,749 rows have the threshold's, 45,400 of 131,072, and the two calls take 61 and 224.
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>
@@ -29,7 +30,7 @@ constexpr int kEvictWords = 2048;                    // words of bits in LDS, th
 constexpr int kFewMoves = 512;                       // of a (sequence, KV head): within the first kernel
 constexpr int kMoveThreads = 256, kMoveAhead = 4, kMoveRows = kMoveThreads / kRowLanes * kMoveAhead;     // places of a workgroup
 constexpr int kEvictLeast = 4096;                    // rows of a chunk
-constexpr int64_t kEvictOneDigit = 131072;           // rows up to which one digit usually leaves no more than kEvictList of them
+constexpr int64_t kEvictOneDigit = 131072;           // rows up to which one digit leaves no more than kEvictList of them if weights spread over octaves
 constexpr int kEvictMostChunks = 16;                // (all of them look at the histograms of all)
 static_assert(kMoveRows == 64, "a workgroup moves into the rows of one word");
 

@@ -7,8 +7,9 @@
 // XORed with the row against bank conflicts, and serve the four waves.
 // Sums go in order: 16 probabilities, those of a tile, of kSumTiles tiles, of a chunk of tiles, of the chunks; the results do not depend on timing.
 // Bound by the vector units (an exponential, a product and a sum a score, 16 cycles for 64, and about 4 more) beside the matrix units (16
-// cycles), at the clock that the power limit leaves: 33,625 tokens in three prompts, 32 heads on 8, 1.73 TFLOP of products, take 1.69 ms, 1.02
-// PFLOP/s, where a library product of 16,384^3 reaches 1.39.  The last 64 queries of 32,749 tokens take 25.7 us (their keys, 67 MB, alone 14).
+// cycles), at the clock that the power limit leaves: 33,625 tokens in three prompts, 32 heads on 8, 1.73 TFLOP of products, take 1.70 ms, 1.02
+// PFLOP/s, where a library product of 16,384^3 reaches 1.39 (1.65 ms on another card).  The last 64 queries of 32,749 tokens take 27 us under the
+// profiler, 25.5 a call one behind the other (their keys, 67 MB, alone 14).
 #include "api_checks.h"
 #include "kv_store.h"
 #include <algorithm>
